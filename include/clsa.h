@@ -100,7 +100,8 @@ typedef enum {
 /* Bits reported by clsa_get_device_error(). */
 enum {
     CLSA_DEVERR_SEQ_LEN = 1, /* a seq_lens[b] outside [0, max_len] was clamped        */
-    CLSA_DEVERR_N_SEL = 2    /* an n_sel[r] outside [0, top_k] was clamped            */
+    CLSA_DEVERR_N_SEL = 2,   /* an n_sel[r] outside [0, top_k] was clamped            */
+    CLSA_DEVERR_APPEND = 4   /* start / count of appended tokens that do not fit      */
 };
 
 typedef enum {
@@ -110,7 +111,10 @@ typedef enum {
     CLSA_OP_DECODE = 3, /* clsa_decode_step and clsa_decode_step_grouped */
     CLSA_OP_DENSE = 4,  /* clsa_dense_attn */
     CLSA_OP_KD_TARGET = 5, /* clsa_kd_target (size grows with n_layers) */
-    CLSA_OP_KD_LOSS = 6    /* clsa_kd_loss */
+    CLSA_OP_KD_LOSS = 6,   /* clsa_kd_loss */
+    CLSA_OP_ATTN8 = 7,     /* clsa_sparse_attn8 */
+    CLSA_OP_DENSE8 = 8,    /* clsa_dense_attn8 */
+    CLSA_OP_BLOCK_TOPK = 9 /* clsa_block_topk (n_layers: the block)  */
 } clsa_op;
 
 typedef struct clsa_shape {
@@ -131,7 +135,8 @@ typedef struct clsa_shape {
 } clsa_shape;
 
 /* Bytes of workspace `op` needs for `shape` (n_layers matters for
- * CLSA_OP_KD_TARGET only, whose statistics buffer grows with the layer count;
+ * CLSA_OP_KD_TARGET, whose statistics buffer grows with the layer count, and for
+ * CLSA_OP_BLOCK_TOPK, where it holds the tokens per block;
  * for CLSA_OP_DECODE it never changes the size: layers reuse the same buffers).
  * Returns 0 for CLSA_OP_INDEX, and also 0 when the shape is invalid or
  * unsupported (the entry point then reports the reason). */
@@ -284,6 +289,83 @@ clsa_status clsa_kd_loss(const clsa_shape *shape, const float *abar, const void 
                          const void *k_idx, const int32_t *page_table, const int32_t *seq_lens,
                          const int32_t *q_pos, float *loss, float *dq_idx, float *dk_idx,
                          void *ws, size_t ws_bytes, void *stream);
+
+/* ---- The shared cache in 8 bits ----
+ *
+ * K and V as e4m3 bytes (1 sign, 4 exponent, 3 mantissa bits, no infinity) with
+ * one fp32 scale, a power of two, for each block of `block` consecutive tokens
+ * (16, 32, 64 or 128; in a paged cache at most page_size) and KV head:
+ *   k8, v8            bytes, in the layout of k_cache / v_cache
+ *   k_scale, v_scale  fp32 [batch, ceil(max_len / block), kv_heads]      contiguous
+ *                     fp32 [num_pages, page_size / block, kv_heads]      paged
+ * A cached value is its byte times its block's scale.  Half the bytes of a bf16
+ * cache, each value off by at most 2^-4 of itself (or 2^-18 of the largest of its
+ * block).  The index keys and the routing stay as they are. */
+
+/* Appends new tokens' rows.  k, v: bf16 [batch, n_q, kv_heads, head_dim]; of
+ * sequence b, rows 0 .. count[b]-1 go to positions start[b] .. start[b]+count[b]-1,
+ * and the rows behind them are not read.  A block's scale is the least 2^e (e >= -100)
+ * that holds the largest new magnitude within 448 * 2^e, or the scale that it has if
+ * that is larger and the block keeps tokens before start[b]: those keep their
+ * scale's values, or are rounded to the new scale where it grew.  A block that the
+ * new tokens begin starts afresh.  Bytes of positions from start[b]+count[b] on are
+ * left as they are.  NaN and infinities are held as NaN and do not enter the scale;
+ * magnitudes above 240 * 2^120 are held as that.  count[b] outside [0, n_q], start[b]
+ * outside [0, max_len] (nothing is appended) and positions past max_len (dropped)
+ * raise CLSA_DEVERR_APPEND.  Two sequences must not append to the same block.
+ * Scales of a fresh cache need no initialisation.  q_heads, top_k, causal and
+ * softmax_scale are not used (they must still be valid).  Needs no workspace. */
+clsa_status clsa_cache_append8(const clsa_shape *shape, int32_t block, const void *k, const void *v,
+                               const int32_t *start, const int32_t *count,
+                               const int32_t *page_table, void *k8, void *v8, float *k_scale,
+                               float *v_scale, void *stream);
+
+/* clsa_sparse_attn over the 8-bit cache: the same index lists (of clsa_topk or
+ * clsa_block_topk), outputs, conventions and errors.  Logits, softmax and sums in
+ * fp32; each weight times its value's scale is rounded to bf16 for the product with
+ * the values.  A NaN in the cache reaches the rows that select its token, and no
+ * others.  Workspace: CLSA_OP_ATTN8. */
+clsa_status clsa_sparse_attn8(const clsa_shape *shape, int32_t block, const void *q, const void *k8,
+                              const void *v8, const float *k_scale, const float *v_scale,
+                              const int32_t *page_table, const int32_t *idx, const int32_t *n_sel,
+                              void *out, float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/* clsa_dense_attn over the 8-bit cache.  Workspace: CLSA_OP_DENSE8. */
+clsa_status clsa_dense_attn8(const clsa_shape *shape, int32_t block, const void *q, const void *k8,
+                             const void *v8, const float *k_scale, const float *v_scale,
+                             const int32_t *page_table, const int32_t *seq_lens,
+                             const int32_t *q_pos, void *out, float *lse, void *ws,
+                             size_t ws_bytes, void *stream);
+
+/* ---- Block routing ----
+ *
+ * In place of one score for every cached token, one for every block of `block`
+ * consecutive tokens (16, 32, 64 or 128; paged: at most page_size): 1 / block of
+ * the index keys' bytes.  The result is an index list like clsa_topk's, for any of
+ * the attention calls, shared by the layers in the same way.
+ *   means  bf16 [batch, ceil(max_len / block), 256]        contiguous
+ *          bf16 [num_pages, page_size / block, 256]        paged */
+
+/* The mean index key of every block whose last token is among the tokens
+ * start[b] .. start[b]+count[b]-1 of sequence b just written to k_idx (n_q bounds
+ * count; errors as clsa_cache_append8), rounded once to fp32 and once to bf16.
+ * Other blocks' means are left as they are: a block has none until it is complete,
+ * and none is read before.  Needs no workspace. */
+clsa_status clsa_block_means(const clsa_shape *shape, int32_t block, const void *k_idx,
+                             const int32_t *start, const int32_t *count,
+                             const int32_t *page_table, void *means, void *stream);
+
+/* For every row (b,t) with n valid keys: the row's own block (that of key n-1, up to
+ * it), and of the blocks before it the top_k / block - 1 with the largest
+ * q_idx[b,t,:] . means (ties to the lowest), or all of them if there are no more; their
+ * tokens in ascending order to idx[b,t,:], padded with -1, and their count to
+ * n_sel[b,t].  The set is the one that exact scores give (64-bit ones where fp32 does
+ * not decide).  NaN scores are not supported.  top_k must be a multiple of block.
+ * Workspace: CLSA_OP_BLOCK_TOPK, whose size asks for the block in n_layers. */
+clsa_status clsa_block_topk(const clsa_shape *shape, int32_t block, const void *q_idx,
+                            const void *means, const int32_t *page_table, const int32_t *seq_lens,
+                            const int32_t *q_pos, int32_t *idx, int32_t *n_sel, void *ws,
+                            size_t ws_bytes, void *stream);
 
 /* Static, human-readable name of a status code. */
 const char *clsa_status_string(clsa_status status);

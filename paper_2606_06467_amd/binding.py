@@ -33,6 +33,9 @@ CLSA_OP_DECODE = 3
 CLSA_OP_DENSE = 4
 CLSA_OP_KD_TARGET = 5
 CLSA_OP_KD_LOSS = 6
+CLSA_OP_ATTN8 = 7
+CLSA_OP_DENSE8 = 8
+CLSA_OP_BLOCK_TOPK = 9
 
 
 class ClsaError(RuntimeError):
@@ -89,6 +92,11 @@ def lib() -> ctypes.CDLL:
         "clsa_project_append": (i32, [SP, i32, P, P, P, P, P, P, P, P, P]),
         "clsa_kd_target": (i32, [SP, i32, P, P, P, P, P, P, P, P, sz, P]),
         "clsa_kd_loss": (i32, [SP, P, P, P, P, P, P, P, P, P, P, sz, P]),
+        "clsa_cache_append8": (i32, [SP, i32, P, P, P, P, P, P, P, P, P, P]),
+        "clsa_sparse_attn8": (i32, [SP, i32, P, P, P, P, P, P, P, P, P, P, P, sz, P]),
+        "clsa_dense_attn8": (i32, [SP, i32, P, P, P, P, P, P, P, P, P, P, P, sz, P]),
+        "clsa_block_means": (i32, [SP, i32, P, P, P, P, P, P]),
+        "clsa_block_topk": (i32, [SP, i32, P, P, P, P, P, P, P, P, sz, P]),
         "clsa_status_string": (ctypes.c_char_p, [i32]),
         "clsa_set_phase_events": (i32, [ctypes.POINTER(P), i32]),
         "clsa_get_device_error": (i32, [ctypes.POINTER(ctypes.c_uint32)]),
@@ -234,8 +242,57 @@ def clsa_kd_loss(shape, abar, q_idx, k_idx, page_table, seq_lens, q_pos, loss, d
                               _ptr(ws, "ws"), wsb, _stream(stream)), "clsa_kd_loss")
 
 
+def clsa_cache_append8(shape, block, k, v, start, count, page_table, k8, v8, k_scale, v_scale,
+                       stream=None):
+    _check(lib().clsa_cache_append8(ctypes.byref(shape), int(block), _ptr(k, "k"), _ptr(v, "v"),
+                                    _ptr(start, "start"), _ptr(count, "count"),
+                                    _ptr(page_table, "page_table"), _ptr(k8, "k8"), _ptr(v8, "v8"),
+                                    _ptr(k_scale, "k_scale"), _ptr(v_scale, "v_scale"),
+                                    _stream(stream)), "clsa_cache_append8")
+
+
+def clsa_sparse_attn8(shape, block, q, k8, v8, k_scale, v_scale, page_table, idx, n_sel, out,
+                      lse=None, ws=None, stream=None):
+    wsb = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(lib().clsa_sparse_attn8(ctypes.byref(shape), int(block), _ptr(q, "q"), _ptr(k8, "k8"),
+                                   _ptr(v8, "v8"), _ptr(k_scale, "k_scale"),
+                                   _ptr(v_scale, "v_scale"), _ptr(page_table, "page_table"),
+                                   _ptr(idx, "idx"), _ptr(n_sel, "n_sel"), _ptr(out, "out"),
+                                   _ptr(lse, "lse"), _ptr(ws, "ws"), wsb, _stream(stream)),
+           "clsa_sparse_attn8")
+
+
+def clsa_dense_attn8(shape, block, q, k8, v8, k_scale, v_scale, page_table, seq_lens, q_pos, out,
+                     lse=None, ws=None, stream=None):
+    wsb = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(lib().clsa_dense_attn8(ctypes.byref(shape), int(block), _ptr(q, "q"), _ptr(k8, "k8"),
+                                  _ptr(v8, "v8"), _ptr(k_scale, "k_scale"),
+                                  _ptr(v_scale, "v_scale"), _ptr(page_table, "page_table"),
+                                  _ptr(seq_lens, "seq_lens"), _ptr(q_pos, "q_pos"),
+                                  _ptr(out, "out"), _ptr(lse, "lse"), _ptr(ws, "ws"), wsb,
+                                  _stream(stream)), "clsa_dense_attn8")
+
+
+def clsa_block_means(shape, block, k_idx, start, count, page_table, means, stream=None):
+    _check(lib().clsa_block_means(ctypes.byref(shape), int(block), _ptr(k_idx, "k_idx"),
+                                  _ptr(start, "start"), _ptr(count, "count"),
+                                  _ptr(page_table, "page_table"), _ptr(means, "means"),
+                                  _stream(stream)), "clsa_block_means")
+
+
+def clsa_block_topk(shape, block, q_idx, means, page_table, seq_lens, q_pos, idx, n_sel, ws,
+                    stream=None):
+    wsb = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(lib().clsa_block_topk(ctypes.byref(shape), int(block), _ptr(q_idx, "q_idx"),
+                                 _ptr(means, "means"), _ptr(page_table, "page_table"),
+                                 _ptr(seq_lens, "seq_lens"), _ptr(q_pos, "q_pos"),
+                                 _ptr(idx, "idx"), _ptr(n_sel, "n_sel"), _ptr(ws, "ws"), wsb,
+                                 _stream(stream)), "clsa_block_topk")
+
+
 CLSA_DEVERR_SEQ_LEN = 1
 CLSA_DEVERR_N_SEL = 2
+CLSA_DEVERR_APPEND = 4
 
 
 def clsa_get_device_error() -> int:
@@ -258,7 +315,8 @@ def clsa_set_phase_events(events: Optional[Sequence[int]]) -> None:
 
 
 def workspace(shape: ClsaShape, op: int, n_layers: int = 0, device="cuda") -> Optional[torch.Tensor]:
-    """A device byte tensor large enough for ``op`` (None if none is needed)."""
+    """A device byte tensor large enough for ``op`` (None if none is needed); for
+    CLSA_OP_BLOCK_TOPK ``n_layers`` is the tokens per block."""
     n = clsa_workspace_bytes(shape, op, n_layers)
     if n == 0:
         return None

@@ -85,6 +85,14 @@ clsa_status check_shape(const clsa_shape *s, unsigned needs, Geometry *g) {
     return CLSA_OK;
 }
 
+// The 8-bit cache's and block routing's tokens per block.
+clsa_status check_block(const clsa_shape *s, int32_t block) {
+    if (block < 1) return CLSA_ERR_INVALID_ARG;
+    if (block != 16 && block != 32 && block != 64 && block != 128) return CLSA_ERR_UNSUPPORTED;
+    if (s->page_size && block > s->page_size) return CLSA_ERR_UNSUPPORTED;  // a block lies in one page
+    return CLSA_OK;
+}
+
 clsa_status check_ptr(const void *p, uintptr_t align) {
     if (!p || !aligned(p, align)) return CLSA_ERR_INVALID_ARG;
     return CLSA_OK;
@@ -224,6 +232,21 @@ size_t attn_ws_bytes(const Geometry &g, bool dense = false) {
     return c.off;
 }
 
+size_t floats_ws_bytes(size_t floats) { return align_up(sizeof(float) * floats); }
+
+clsa_status check_cache8(const void *k8, const void *v8, const float *k_scale, const float *v_scale) {
+    CLSA_TRY(check_ptr(k8, 16));
+    CLSA_TRY(check_ptr(v8, 16));
+    CLSA_TRY(check_ptr(k_scale, 4));
+    CLSA_TRY(check_ptr(v_scale, 4));
+    return CLSA_OK;
+}
+
+clsa::Cache8 cache8(const void *k8, const void *v8, const float *k_scale, const float *v_scale,
+                    const int32_t *page_table, int32_t block) {
+    return {k8, v8, k_scale, v_scale, page_table, log2i(block)};
+}
+
 clsa_status from_hip(hipError_t e) { return e == hipSuccess ? CLSA_OK : CLSA_ERR_HIP; }
 
 }  // namespace
@@ -253,6 +276,17 @@ size_t clsa_workspace_bytes(const clsa_shape *shape, int32_t op, int32_t n_layer
             if (check_shape(shape, kIndex | kDense, &g) != CLSA_OK || !clsa::kd_loss_supported(g))
                 return 0;
             return align_up(sizeof(float) * clsa::kd_loss_ws_floats(g));
+        case CLSA_OP_ATTN8:
+            if (check_shape(shape, kAttn, &g) != CLSA_OK) return 0;
+            return floats_ws_bytes(clsa::sparse_attn8_floats(g));
+        case CLSA_OP_DENSE8:
+            if (check_shape(shape, kAttn | kDense, &g) != CLSA_OK) return 0;
+            return floats_ws_bytes(clsa::dense_attn8_floats(g));
+        case CLSA_OP_BLOCK_TOPK:  // n_layers: the block
+            if (check_shape(shape, kIndex | kTopk, &g) != CLSA_OK ||
+                check_block(shape, n_layers) != CLSA_OK || g.top_k % n_layers != 0)
+                return 0;
+            return clsa::block_topk_ws_bytes(g, n_layers);
         case CLSA_OP_DECODE: {
             // layers run one after another and reuse the same buffers
             if (check_shape(shape, kIndex | kTopk | kAttn, &g) != CLSA_OK || n_layers < 0)
@@ -593,6 +627,100 @@ clsa_status clsa_kd_loss(const clsa_shape *shape, const float *abar, const void 
     return CLSA_OK;
 }
 
+clsa_status clsa_cache_append8(const clsa_shape *shape, int32_t block, const void *k, const void *v,
+                               const int32_t *start, const int32_t *count,
+                               const int32_t *page_table, void *k8, void *v8, float *k_scale,
+                               float *v_scale, void *stream) {
+    Geometry g;
+    CLSA_TRY(check_shape(shape, kAttn, &g));
+    CLSA_TRY(check_block(shape, block));
+    CLSA_TRY(check_ptr(k, 16));
+    CLSA_TRY(check_ptr(v, 16));
+    CLSA_TRY(check_ptr(start, 4));
+    CLSA_TRY(check_ptr(count, 4));
+    CLSA_TRY(check_cache8(k8, v8, k_scale, v_scale));
+    CLSA_TRY(check_common(shape, page_table, nullptr, false, true));
+    return from_hip(clsa::launch_append8(g, block, k, v, start, count, page_table, k8, v8, k_scale,
+                                         v_scale, static_cast<hipStream_t>(stream)));
+}
+
+clsa_status clsa_sparse_attn8(const clsa_shape *shape, int32_t block, const void *q, const void *k8,
+                              const void *v8, const float *k_scale, const float *v_scale,
+                              const int32_t *page_table, const int32_t *idx, const int32_t *n_sel,
+                              void *out, float *lse, void *ws, size_t ws_bytes, void *stream) {
+    Geometry g;
+    CLSA_TRY(check_shape(shape, kAttn, &g));
+    CLSA_TRY(check_block(shape, block));
+    CLSA_TRY(check_ptr(q, 16));
+    CLSA_TRY(check_cache8(k8, v8, k_scale, v_scale));
+    CLSA_TRY(check_ptr(idx, 4));
+    CLSA_TRY(check_ptr(n_sel, 4));
+    CLSA_TRY(check_ptr(out, 16));
+    if (lse) CLSA_TRY(check_ptr(lse, 4));
+    CLSA_TRY(check_common(shape, page_table, nullptr, false, true));
+    const size_t need = floats_ws_bytes(clsa::sparse_attn8_floats(g));
+    if (need && (!ws || ws_bytes < need || !aligned(ws, kAlign))) return CLSA_ERR_WORKSPACE;
+    return from_hip(clsa::launch_sparse_attn8(
+        g, cache8(k8, v8, k_scale, v_scale, page_table, block), q, idx, n_sel, out, lse,
+        static_cast<float *>(ws), static_cast<hipStream_t>(stream)));
+}
+
+clsa_status clsa_dense_attn8(const clsa_shape *shape, int32_t block, const void *q, const void *k8,
+                             const void *v8, const float *k_scale, const float *v_scale,
+                             const int32_t *page_table, const int32_t *seq_lens,
+                             const int32_t *q_pos, void *out, float *lse, void *ws,
+                             size_t ws_bytes, void *stream) {
+    Geometry g;
+    CLSA_TRY(check_shape(shape, kAttn | kDense, &g));
+    CLSA_TRY(check_block(shape, block));
+    CLSA_TRY(check_ptr(q, 16));
+    CLSA_TRY(check_cache8(k8, v8, k_scale, v_scale));
+    CLSA_TRY(check_ptr(seq_lens, 4));
+    CLSA_TRY(check_ptr(out, 16));
+    if (lse) CLSA_TRY(check_ptr(lse, 4));
+    CLSA_TRY(check_common(shape, page_table, q_pos, true, true));
+    const size_t need = floats_ws_bytes(clsa::dense_attn8_floats(g));
+    if (need && (!ws || ws_bytes < need || !aligned(ws, kAlign))) return CLSA_ERR_WORKSPACE;
+    return from_hip(clsa::launch_dense_attn8(
+        g, cache8(k8, v8, k_scale, v_scale, page_table, block), q, seq_lens, q_pos, out, lse,
+        static_cast<float *>(ws), static_cast<hipStream_t>(stream)));
+}
+
+clsa_status clsa_block_means(const clsa_shape *shape, int32_t block, const void *k_idx,
+                             const int32_t *start, const int32_t *count,
+                             const int32_t *page_table, void *means, void *stream) {
+    Geometry g;
+    CLSA_TRY(check_shape(shape, kIndex, &g));
+    CLSA_TRY(check_block(shape, block));
+    CLSA_TRY(check_ptr(k_idx, 16));
+    CLSA_TRY(check_ptr(start, 4));
+    CLSA_TRY(check_ptr(count, 4));
+    CLSA_TRY(check_ptr(means, 16));
+    CLSA_TRY(check_common(shape, page_table, nullptr, false, true));
+    return from_hip(clsa::launch_block_means(g, block, k_idx, start, count, page_table, means,
+                                             static_cast<hipStream_t>(stream)));
+}
+
+clsa_status clsa_block_topk(const clsa_shape *shape, int32_t block, const void *q_idx,
+                            const void *means, const int32_t *page_table, const int32_t *seq_lens,
+                            const int32_t *q_pos, int32_t *idx, int32_t *n_sel, void *ws,
+                            size_t ws_bytes, void *stream) {
+    Geometry g;
+    CLSA_TRY(check_shape(shape, kIndex | kTopk, &g));
+    CLSA_TRY(check_block(shape, block));
+    if (g.top_k % block != 0) return CLSA_ERR_INVALID_ARG;
+    CLSA_TRY(check_ptr(q_idx, 16));
+    CLSA_TRY(check_ptr(means, 16));
+    CLSA_TRY(check_ptr(seq_lens, 4));
+    CLSA_TRY(check_ptr(idx, 4));
+    CLSA_TRY(check_ptr(n_sel, 4));
+    CLSA_TRY(check_common(shape, page_table, q_pos, true, true));
+    const size_t need = clsa::block_topk_ws_bytes(g, block);
+    if (!ws || ws_bytes < need || !aligned(ws, kAlign)) return CLSA_ERR_WORKSPACE;
+    return from_hip(clsa::launch_block_topk(g, block, q_idx, means, page_table, seq_lens, q_pos, idx,
+                                            n_sel, ws, static_cast<hipStream_t>(stream)));
+}
+
 const char *clsa_status_string(clsa_status status) {
     switch (status) {
         case CLSA_OK: return "CLSA_OK";
@@ -617,6 +745,10 @@ clsa_status clsa_get_device_error(uint32_t *bits) {
     CLSA_TRY(from_hip(clsa::take_device_error_tile_attn(&v)));
     CLSA_TRY(from_hip(clsa::take_device_error_kd(&v)));
     CLSA_TRY(from_hip(clsa::take_device_error_kd_loss(&v)));
+    CLSA_TRY(from_hip(clsa::take_device_error_cache8(&v)));
+    CLSA_TRY(from_hip(clsa::take_device_error_sparse_attn8(&v)));
+    CLSA_TRY(from_hip(clsa::take_device_error_tile_attn8(&v)));
+    CLSA_TRY(from_hip(clsa::take_device_error_block_route(&v)));
     *bits = v;
     return CLSA_OK;
 }

@@ -204,6 +204,60 @@ hipError_t launch_masked_attn(const Geometry &g, const void *q, const void *k_ca
                               void *out, float *lse, hipStream_t stream);
 hipError_t take_device_error_tile_attn(uint32_t *bits);
 
+// ---- 8-bit shared cache (cache8.hip, sparse_attn8.hip, tile_attn8.hip) ----
+// e4m3 bytes [..., kv_heads, 128] in the layout of the bf16 caches, and a power-of-two
+// scale per (block of tokens, KV head): [batch, ceil(max_len / block), kv_heads], or
+// [pages, page_size / block, kv_heads].
+struct Cache8 {
+    const void *k, *v;
+    const float *k_scale, *v_scale;
+    const int32_t *page_table;
+    int block_shift;
+};
+// Blocks that n_q tokens can reach, whatever the first one's position in its block.
+inline int append_slots(const Geometry &g, int block) { return (int)(((long)g.n_q + block - 2) / block + 1); }
+hipError_t launch_append8(const Geometry &g, int block, const void *k, const void *v,
+                          const int32_t *start, const int32_t *count, const int32_t *page_table,
+                          void *k8, void *v8, float *k_scale, float *v_scale, hipStream_t stream);
+// Mean index key (bf16) of every block that the appended tokens complete.
+hipError_t launch_block_means(const Geometry &g, int block, const void *k_idx,
+                              const int32_t *start, const int32_t *count,
+                              const int32_t *page_table, void *means, hipStream_t stream);
+// Partial buffer floats of the two attention calls below (0 with one split).
+size_t sparse_attn8_floats(const Geometry &g);
+size_t dense_attn8_floats(const Geometry &g);
+bool dense8_in_tiles(const Geometry &g);  // whether the second one runs over key tiles
+hipError_t launch_sparse_attn8(const Geometry &g, const Cache8 &c, const void *q,
+                               const int32_t *idx, const int32_t *n_sel, void *out, float *lse,
+                               float *partials, hipStream_t stream);
+hipError_t launch_dense_attn8(const Geometry &g, const Cache8 &c, const void *q,
+                              const int32_t *seq_lens, const int32_t *q_pos, void *out, float *lse,
+                              float *partials, hipStream_t stream);
+hipError_t launch_tile_attn8(const Geometry &g, const Cache8 &c, const void *q,
+                             const int32_t *seq_lens, const int32_t *q_pos, int splits, int span,
+                             void *out, float *lse, float *part_o, float *part_ml,
+                             hipStream_t stream);
+// Combines the key ranges of every (row, query head) (sparse_attn.hip): partials
+// [rows, q_heads, splits, 128] and (m, l) [rows, q_heads, splits, 2], range s holding
+// keys s * span .. of the row; ranges without keys are not read into the result.
+// span: a multiple of 64.
+hipError_t launch_split_merge(const Geometry &g, bool dense, const int32_t *n_sel,
+                              const int32_t *seq_lens, const int32_t *q_pos, int splits, int span,
+                              const float *part_o, const float *part_ml, void *out, float *lse,
+                              hipStream_t stream);
+hipError_t take_device_error_cache8(uint32_t *bits);
+hipError_t take_device_error_sparse_attn8(uint32_t *bits);
+hipError_t take_device_error_tile_attn8(uint32_t *bits);
+
+// ---- block_route.hip ----
+// Block routing: workspace bytes, and the token lists of every row.
+size_t block_topk_ws_bytes(const Geometry &g, int block);
+hipError_t launch_block_topk(const Geometry &g, int block, const void *q_idx, const void *means,
+                             const int32_t *page_table, const int32_t *seq_lens,
+                             const int32_t *q_pos, int32_t *idx, int32_t *n_sel, void *ws,
+                             hipStream_t stream);
+hipError_t take_device_error_block_route(uint32_t *bits);
+
 // ---- project.hip ----
 // d_model values the projection kernels support (multiples of 512 up to 8192).
 bool project_supported(int d_model);

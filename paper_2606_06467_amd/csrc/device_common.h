@@ -104,6 +104,7 @@ __device__ __forceinline__ uint32_t score_key(float s) {
 // value the host cannot check lies outside its documented range and is clamped.
 constexpr uint32_t kDevErrSeqLen = 1u;  // seq_lens[b] outside [0, max_len]
 constexpr uint32_t kDevErrNSel = 2u;    // n_sel[r] outside [0, top_k]
+constexpr uint32_t kDevErrAppend = 4u;  // appended tokens that do not fit
 static __device__ uint32_t g_device_error;
 
 // One atomic per wave that meets the condition (called inside the branch that

@@ -700,6 +700,29 @@ static hipError_t launch_merge(const AttnArgs &a, int units, hipStream_t stream)
     return hipGetLastError();
 }
 
+hipError_t launch_split_merge(const Geometry &g, bool dense, const int32_t *n_sel,
+                              const int32_t *seq_lens, const int32_t *q_pos, int splits, int span,
+                              const float *part_o, const float *part_ml, void *out, float *lse,
+                              hipStream_t stream) {
+    AttnArgs a{};
+    a.n_sel = n_sel;
+    a.seq_lens = seq_lens;
+    a.q_pos = q_pos;
+    a.out = static_cast<uint16_t *>(out);
+    a.lse = lse;
+    a.part_o = const_cast<float *>(part_o);
+    a.part_ml = const_cast<float *>(part_ml);
+    a.n_q = g.n_q;
+    a.max_len = g.max_len;
+    a.top_k = g.top_k;
+    a.q_heads = g.q_heads;
+    a.causal = g.causal;
+    a.splits = splits;
+    a.chunks_per_split = span / 64;
+    const int units = g.rows * g.q_heads;
+    return dense ? launch_merge<true>(a, units, stream) : launch_merge<false>(a, units, stream);
+}
+
 template <int G, bool DENSE>
 static hipError_t launch_attn_g(const AttnArgs &a, bool paged, dim3 grid, int units,
                                 hipStream_t stream, hipEvent_t split_done) {

@@ -1,0 +1,372 @@
+"""GPU parity of the 8-bit cache: appending, and sparse and dense attention from it, against
+plain 64-bit references (tests/cache8_util.py)."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from paper_2606_06467_amd import inputs
+from tests import cache8_util as C
+from tests import gpu_util as U
+
+pytestmark = pytest.mark.gpu
+SCALE = 1 / np.sqrt(128)
+
+
+def _dev(a):
+    import torch
+    return None if a is None else torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def _bf16(bits):
+    from paper_2606_06467_amd import binding as B
+    return B.bf16_from_bits(bits)
+
+
+def _shape(batch, n_q, max_len, heads, page=0, top_k=64, group=1, causal=False, **kw):
+    from paper_2606_06467_amd import binding as B
+    return B.make_shape(batch, n_q, max_len, top_k, q_heads=heads * group, kv_heads=heads,
+                        page_size=page, max_pages=max_len // page if page else 0, causal=causal, **kw)
+
+
+class Pair:
+    """K and V caches on both sides."""
+
+    def __init__(self, k, v):
+        self.k, self.v = k, v
+        self.push()
+
+    def push(self):
+        self.k8, self.v8 = _dev(self.k.bytes), _dev(self.v.bytes)
+        self.ks, self.vs = _dev(self.k.scale), _dev(self.v.scale)
+        self.pt = _dev(self.k.pt)
+
+    def append(self, sh, block, x, start, count):
+        """x: (K, V) values [B, n_q, H, D] that bf16 holds; on the GPU and in the references."""
+        from paper_2606_06467_amd import binding as B
+        bits = [C.bf16(a)[1] for a in x]
+        B.clsa_cache_append8(sh, block, _bf16(bits[0]), _bf16(bits[1]), _dev(np.int32(start)),
+                             _dev(np.int32(count)), self.pt, self.k8, self.v8, self.ks, self.vs)
+        for c, a in ((self.k, x[0]), (self.v, x[1])):
+            for b, (s, n) in enumerate(zip(start, count)):
+                n = min(max(n, 0), a.shape[1])
+                if 0 <= s <= c.max_len and n:
+                    n = min(n, c.max_len - s)
+                    if n:
+                        c.append(b, s, a[b, :n].copy())
+
+    def check(self):
+        for c, b8, s in ((self.k, self.k8, self.ks), (self.v, self.v8, self.vs)):
+            assert np.array_equal(s.cpu().numpy(), c.scale), "scales"
+            assert C.same_bytes(b8.cpu().numpy(), c.bytes), "bytes"
+
+
+def _random(g, batch, n_q, heads, spread=2.0):
+    x = g.standard_normal((2, batch, n_q, heads, 128))
+    x *= 2.0 ** (spread * g.standard_normal((2, batch, n_q, heads, 1)))
+    return [C.bf16(a)[0] for a in x]
+
+
+@pytest.mark.parametrize("block,page,heads,n_q", [
+    (16, 0, 4, 40), (32, 64, 2, 100), (64, 64, 8, 130), (64, 0, 1, 200), (128, 128, 4, 300),
+    (16, 4096, 3, 33), (128, 0, 5, 129), (64, 128, 8, 1)])
+def test_append_ragged(block, page, heads, n_q):
+    """Several chunks behind one another: starts inside blocks, counts from 0 to n_q."""
+    g = np.random.default_rng(block + page + heads + n_q)
+    batch, max_len = 5, 1000 if not page else -(-1000 // page) * page
+    pt = C.page_table(3, [max_len] * batch, page, max_len) if page else None
+    p = Pair(*(C.Cache(batch, max_len, heads, block, page, pt) for _ in "kv"))
+    sh = _shape(batch, n_q, max_len, heads, page)
+    at = np.array([0, block - 1, 5 * block, 7, max_len - n_q if not page else 2])
+    for _ in range(3):
+        count = g.integers(0, n_q + 1, size=batch)
+        count[0] = n_q
+        count = np.minimum(count, max_len - at)
+        p.append(sh, block, _random(g, batch, n_q, heads), at, count)
+        at = at + count
+        p.check()
+
+
+@pytest.mark.parametrize("block", [16, 64])
+def test_append_token_by_token(block):
+    """Blocks that grow a token at a time, larger and larger: kept bytes move with the scale."""
+    g = np.random.default_rng(block)
+    p = Pair(*(C.Cache(2, 150, 2, block) for _ in "kv"))
+    sh = _shape(2, 1, 150, 2)
+    for j in range(100):
+        x = _random(g, 2, 1, 2, 3.0)
+        if j % 9 == 8:
+            x = [C.bf16(a * 2.0 ** 16)[0] for a in x]  # what was held falls below the least exponent
+        p.append(sh, block, x, [j, j + 31], [1, j % 3 > 0])
+    p.check()
+
+
+def test_append_extreme_values():
+    """NaN, infinities, zeros, subnormals, the largest values, and a border of the scale."""
+    p = Pair(*(C.Cache(1, 256, 2, 64) for _ in "kv"))
+    sh = _shape(1, 130, 256, 2)
+    x = np.zeros((2, 1, 130, 2, 128))
+    x[0, 0, 3, 0, 5], x[0, 0, 4, 0, 6], x[1, 0, 5, 1, 7] = np.nan, np.inf, -np.inf
+    x[0, 0, 6] = 448.0                      # exactly held by scale 1
+    x[0, 0, 70, 0] = 450.0                  # not by it
+    x[1, 0, 7, 0] = 3.38e38
+    x[1, 0, 8, 1] = -3.3895313892515355e38  # the largest bf16
+    x[1, 0, 75, 0] = 2.0 ** -133            # the least
+    x[1, 0, 76, 1] = 3 * 2.0 ** -108
+    x = [C.bf16(a)[0] for a in x]
+    p.append(sh, 64, x, [10], [130])
+    p.check()
+    assert p.k.scale[0, 0, 0] == 1.0 and p.k.scale[0, 1, 0] == 2.0 and p.v.scale[0, 1, 0] == 2.0 ** -100
+    x = [np.full_like(a, np.nan) for a in x]  # a block of NaN alone keeps its scale
+    p.append(sh, 64, x, [140], [20])
+    p.check()
+
+
+def test_append_begins_a_block_afresh():
+    """A block that the new tokens begin does not keep the larger scale of what was there."""
+    g = np.random.default_rng(1)
+    p = Pair(*(C.Cache(1, 128, 2, 32) for _ in "kv"))
+    sh = _shape(1, 40, 128, 2)
+    p.append(sh, 32, [a * 64 for a in _random(g, 1, 40, 2, 0.5)], [0], [40])
+    p.append(sh, 32, _random(g, 1, 40, 2, 0.5), [32], [20])
+    p.check()
+    assert (p.k.scale[0, 1] < p.k.scale[0, 0]).all()
+
+
+def test_append_out_of_range():
+    from paper_2606_06467_amd import binding as B
+    g = np.random.default_rng(2)
+    B.clsa_get_device_error()
+    for start, count, bits in (([0, 90], [8, 8], 0), ([95, 3], [8, 9], 4), ([-1, 101], [2, 2], 4),
+                               ([100, 0], [0, -3], 4), ([100, 5], [0, 0], 0), ([2 ** 31 - 1, 0], [8, 8], 4)):
+        p = Pair(*(C.Cache(2, 100, 2, 16) for _ in "kv"))
+        p.append(_shape(2, 8, 100, 2), 16, _random(g, 2, 8, 2), start, count)
+        p.check()
+        assert B.clsa_get_device_error() == bits, (start, count)
+
+
+def _attend(p, sh, block, q, idx=None, ns=None, lens=None, q_pos=None, with_lse=True):
+    import torch
+    from paper_2606_06467_amd import binding as B
+    qd = _bf16(q)
+    out = torch.full(qd.shape, float("nan"), dtype=torch.bfloat16, device="cuda")
+    lse = torch.full(qd.shape[:-1], float("nan"), device="cuda") if with_lse else None
+    if idx is not None:
+        ws = B.workspace(sh, B.CLSA_OP_ATTN8)
+        B.clsa_sparse_attn8(sh, block, qd, p.k8, p.v8, p.ks, p.vs, p.pt, _dev(idx), _dev(ns), out, lse, ws)
+    else:
+        ws = B.workspace(sh, B.CLSA_OP_DENSE8)
+        B.clsa_dense_attn8(sh, block, qd, p.k8, p.v8, p.ks, p.vs, p.pt, _dev(np.int32(lens)), _dev(q_pos),
+                           out, lse, ws)
+    torch.cuda.synchronize()
+    return B.bits_from_bf16(out), lse.cpu().numpy().astype(np.float64) if with_lse else None
+
+
+def _sets(g, lens, n_q, k, counts=None):
+    """Random ascending lists, -1 padded, and as sets."""
+    idx = np.full((len(lens), n_q, k), -1, np.int32)
+    ns = np.zeros((len(lens), n_q), np.int32)
+    sets = []
+    for b, n in enumerate(lens):
+        sets.append([])
+        for t in range(n_q):
+            m = min(k, n) if counts is None else min(counts[b][t], n, k)
+            s = np.sort(g.choice(n, size=m, replace=False)) if n else np.zeros(0, int)
+            idx[b, t, :m] = s
+            ns[b, t] = m
+            sets[-1].append(s)
+    return idx, ns, sets
+
+
+def _sparse_case(seed, lens, heads, group, k, block, page=0, n_q=1, counts=None, scale=None, with_lse=True):
+    g = np.random.default_rng(seed)
+    top = max(lens)
+    max_len = -(-top // page) * page if page else top
+    pt = C.page_table(seed, lens, page, max_len) if page else None
+    p = Pair(*(C.filled(seed + i, lens, heads, block, max_len, page, pt) for i in (1, 2)))
+    qv, q = C.bf16(g.standard_normal((len(lens), n_q, heads * group, 128)))
+    idx, ns, sets = _sets(g, lens, n_q, k, counts)
+    kw = {} if scale is None else dict(softmax_scale=scale)
+    sh = _shape(len(lens), n_q, max_len, heads, page, k, group, **kw)
+    out, lse = _attend(p, sh, block, q, idx, ns, with_lse=with_lse)
+    C.check_attention(out, lse, C.attention(qv, p.k, p.v, sets, SCALE if scale is None else np.float32(scale)))
+
+
+@pytest.mark.parametrize("group", [1, 2, 4, 5, 8])
+@pytest.mark.parametrize("page", [0, 64])
+def test_sparse_groups(group, page):
+    _sparse_case(group, (700, 450), 2, group, 300, 32, page)
+
+
+@pytest.mark.parametrize("k", [1, 2, 31, 32, 33, 127, 128, 129, 1000, 8192])
+def test_sparse_list_lengths(k):
+    _sparse_case(k, (max(40, min(k, 1500)), 40), 2, 4, k, 64)
+
+
+@pytest.mark.parametrize("block,page", [(16, 16), (16, 0), (32, 128), (128, 0), (128, 128), (64, 4096)])
+def test_sparse_blocks(block, page):
+    _sparse_case(block + page, (333, 1, 130), 4, 2, 200, block, page)
+
+
+def test_sparse_empty_and_partial_lists():
+    _sparse_case(5, (300, 200, 100), 2, 4, 256, 32, n_q=3,
+                 counts=[[0, 1, 256], [33, 0, 31], [64, 65, 0]])
+
+
+def test_sparse_many_rows():
+    """Rows enough that one workgroup takes a row's whole list."""
+    g = np.random.default_rng(6)
+    counts = [list(g.integers(0, 150, size=300))]
+    _sparse_case(6, (400,), 4, 2, 140, 64, n_q=300, counts=counts)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.25, 3.0])
+def test_sparse_softmax_scale(scale):
+    _sparse_case(7, (300, 200), 2, 4, 128, 64, scale=scale)
+
+
+def test_sparse_without_lse():
+    _sparse_case(8, (300, 200), 2, 4, 200, 64, with_lse=False)
+
+
+def test_sparse_nan_reaches_the_rows_that_select_it():
+    """Token 0 (where padding points) and a neighbour hold NaN: only lists with them see it."""
+    g = np.random.default_rng(9)
+    p = Pair(*(C.filled(9 + i, (300,), 2, 32, 300) for i in (1, 2)))
+    p.k.bytes[0, 0] = 0x7f
+    p.v.bytes[0, 0] = 0xff
+    p.v.bytes[0, 77, 1, 3] = 0x7f
+    p.k.bytes[0, 120, 0, 9] = 0xff
+    p.push()
+    lists = [[1, 5, 9], [0, 5, 9], [5, 77, 200], [76, 78, 119, 121], list(range(121, 290)), [120], []]
+    k = 200
+    idx, ns = np.full((1, 7, k), -1, np.int32), np.zeros((1, 7), np.int32)
+    for t, s in enumerate(lists):
+        idx[0, t, :len(s)], ns[0, t] = s, len(s)
+    qv, q = C.bf16(g.standard_normal((1, 7, 8, 128)))
+    out, lse = _attend(p, _shape(1, 7, 300, 2, 0, k, 4), 32, q, idx, ns)
+    C.check_attention(out, lse, C.attention(qv, p.k, p.v, [[np.array(s, int) for s in lists]], SCALE))
+
+
+def test_sparse_counts_out_of_range_are_clamped():
+    from paper_2606_06467_amd import binding as B
+    g = np.random.default_rng(10)
+    p = Pair(*(C.filled(10 + i, (300, 300), 2, 32, 300) for i in (1, 2)))
+    idx, ns, sets = _sets(g, (300, 300), 1, 64)
+    ns[0], ns[1] = -5, 70
+    B.clsa_get_device_error()
+    qv, q = C.bf16(g.standard_normal((2, 1, 2, 128)))
+    out, lse = _attend(p, _shape(2, 1, 300, 2, 0, 64), 32, q, idx, ns)
+    sets[0][0] = np.zeros(0, int)
+    C.check_attention(out, lse, C.attention(qv, p.k, p.v, sets, SCALE))
+    assert B.clsa_get_device_error() == B.CLSA_DEVERR_N_SEL
+
+
+@pytest.mark.parametrize("paged", [False, True])
+def test_sparse_offsets_past_32_bits(paged):
+    """Caches of over 4 GiB whose only numbers are the selected tokens, at the far end."""
+    import torch
+    from paper_2606_06467_amd import binding as B
+    g = np.random.default_rng(11)
+    heads, block, k, n = 64, 64, 40, 262080
+    batch, page = (3, 0) if not paged else (3, 64)
+    k8, v8 = (torch.full((batch * n, heads, 128), 0x7f, dtype=torch.uint8, device="cuda") for _ in "kv")
+    ks, vs = (torch.full((batch * n // block, heads), float("nan"), device="cuda") for _ in "kv")
+    pt = None
+    if paged:  # sequence 0 lies in the last pages
+        pt = torch.arange(batch * n // page, dtype=torch.int32).flip(0).view(batch, -1).contiguous()
+    idx = np.sort(np.concatenate([[0, n - 1], g.choice(np.arange(1, n - 1), k - 2, replace=False)]))
+    kv = np.zeros((2, batch, k, heads, 128))
+    row = []
+    for b in range(batch):
+        at = idx if not paged else (pt[b].numpy()[idx // page].astype(np.int64) * page + idx % page)
+        row.append(at if paged else at + b * n)
+        byte = np.where((r := g.integers(0, 256, (2, k, heads, 128))) % 128 == 127, r - 1, r).astype(np.uint8)
+        k8[torch.from_numpy(row[b]).cuda()] = _dev(byte[0])
+        v8[torch.from_numpy(row[b]).cuda()] = _dev(byte[1])
+        kv[:, b] = C.VALUES[byte] / 64
+        for s in (ks, vs):
+            s[torch.from_numpy(row[b] // block).cuda()] = 1 / 64
+    qv, q = C.bf16(g.standard_normal((batch, 1, heads, 128)) / 8)
+    sh = _shape(batch, 1, n, heads, page, k, softmax_scale=0.05)
+    out = torch.zeros((batch, 1, heads, 128), dtype=torch.bfloat16, device="cuda")
+    lse = torch.zeros((batch, 1, heads), device="cuda")
+    B.clsa_sparse_attn8(sh, block, _bf16(q), k8, v8, ks, vs, None if pt is None else pt.cuda(),
+                        _dev(np.tile(idx.astype(np.int32), (batch, 1, 1))),
+                        _dev(np.full((batch, 1), k, np.int32)), out, lse, B.workspace(sh, B.CLSA_OP_ATTN8))
+    torch.cuda.synchronize()
+    small = [C.Cache(batch, k, heads, 64) for _ in "kv"]
+    for c, x in zip(small, kv):
+        c.values = lambda x=x: x
+    want = C.attention(qv, *small, [[np.arange(k)]] * batch, np.float32(0.05))
+    C.check_attention(B.bits_from_bf16(out), lse.cpu().numpy().astype(np.float64), want)
+
+
+def _dense_case(seed, lens, heads, group, block, page=0, n_q=1, causal=False, tiles=None, max_len=None,
+                nan_at=None):
+    g = np.random.default_rng(seed)
+    top = max_len or max(max(lens), 1)
+    max_len = -(-top // page) * page if page else top
+    pt = C.page_table(seed, lens, page, max_len) if page else None
+    p = Pair(*(C.filled(seed + i, lens, heads, block, max_len, page, pt) for i in (1, 2)))
+    if nan_at is not None:
+        p.v.bytes[p.v.at(0, nan_at)][0, 7] = 0x7f
+        p.push()
+    qv, q = C.bf16(g.standard_normal((len(lens), n_q, heads * group, 128)))
+    q_pos = None
+    valid = [[n] * n_q for n in lens]
+    if causal:
+        q_pos = np.array([[n - n_q + t for t in range(n_q)] for n in lens], np.int32)
+        valid = [[max(0, n - n_q + t + 1) for t in range(n_q)] for n in lens]
+    sh = _shape(len(lens), n_q, max_len, heads, page, 64, group, causal)
+    if tiles is not None:
+        gm = U._Geometry(len(lens), n_q, len(lens) * n_q, max_len, page.bit_length() - 1,
+                         max_len // page if page else 0, 64, int(causal), heads * group, heads, group, SCALE)
+        from paper_2606_06467_amd import binding as B
+        f = B.lib()._ZN4clsa15dense8_in_tilesERKNS_8GeometryE
+        f.restype = ctypes.c_bool
+        assert f(ctypes.byref(gm)) == tiles
+    out, lse = _attend(p, sh, block, q, lens=lens, q_pos=q_pos)
+    C.check_attention(out, lse, C.attention(qv, p.k, p.v, [[np.arange(m) for m in v] for v in valid], SCALE))
+
+
+@pytest.mark.parametrize("page", [0, 64])
+def test_dense_lengths(page):
+    _dense_case(20 + page, (0, 1, 2, 31, 32, 33, 64, 127, 128, 129, 500), 2, 4, 16, page, max_len=513)
+
+
+@pytest.mark.parametrize("group,block", [(1, 128), (2, 64), (5, 32), (8, 16)])
+def test_dense_groups(group, block):
+    _dense_case(30 + group, (900, 333), 2, group, block, 128 if group < 4 else 0)
+
+
+def test_dense_long_split_over_many_ranges():
+    _dense_case(40, (9000,), 1, 4, 64)
+
+
+@pytest.mark.parametrize("page", [0, 128])
+def test_dense_causal_few_rows(page):
+    """Some rows before a sequence's first token see nothing."""
+    _dense_case(50, (200, 3, 77), 2, 2, 32, page, n_q=9, causal=True, tiles=False)
+
+
+@pytest.mark.parametrize("lens,heads,group,block,page,n_q,causal", [
+    ((700, 520), 4, 2, 64, 64, 300, True), ((600,), 4, 5, 16, 0, 600, True),
+    ((4000,), 4, 8, 128, 0, 33, False), ((3000, 1), 2, 4, 32, 64, 100, True)])
+def test_dense_tiles(lens, heads, group, block, page, n_q, causal):
+    _dense_case(60 + n_q, lens, heads, group, block, page, n_q, causal)
+
+
+@pytest.mark.parametrize("group,block,page", [(5, 16, 0), (8, 128, 128), (1, 32, 64)])
+def test_dense_tiles_of_a_long_context(group, block, page):
+    """Few rows over many keys: key ranges joined by the log-sum-exp rule."""
+    _dense_case(80 + group, (6000, 3500), 2, group, block, page, 70, True, tiles=True)
+
+
+def test_dense_tiles_nan_reaches_later_rows_only():
+    _dense_case(70, (500,), 4, 4, 32, 0, 500, True, nan_at=333)
+    _dense_case(72, (6000,), 2, 4, 32, 0, 70, True, tiles=True, nan_at=5960)
+
+
+def test_dense_rows_nan_reaches_later_rows_only():
+    _dense_case(71, (300,), 2, 4, 32, 0, 6, True, tiles=False, nan_at=297)
