@@ -242,52 +242,73 @@ def clsa_kd_loss(shape, abar, q_idx, k_idx, page_table, seq_lens, q_pos, loss, d
                               _ptr(ws, "ws"), wsb, _stream(stream)), "clsa_kd_loss")
 
 
+def _call(where, shape, block, args, ws, stream):
+    """An entry point of the 8-bit cache or of block routing: (name, tensor) arguments, and its
+    workspace (False: it takes none).  The call runs on the tensors' device; their stream is the
+    current one of that device unless one is given."""
+    ptrs, device = [], -1
+    for name, t in args if not isinstance(ws, torch.Tensor) else (*args, ("ws", ws)):
+        if t is None:
+            ptrs.append(None)
+            continue
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name} must be a torch.Tensor")
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a GPU tensor")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        at = t.get_device()
+        if at != device:
+            if device >= 0:
+                raise ValueError(f"{name} is on another device than the arguments before it")
+            device = at
+        ptrs.append(t.data_ptr())
+    if ws is None:
+        ptrs += (None, 0)
+    elif ws is not False:
+        ptrs.append(ws.numel() * ws.element_size())
+    if device >= 0 and device != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _call(where, shape, block, args, ws, stream)
+    # the raw handle: a torch Stream object costs 3 us, a quarter of a whole call
+    raw = torch._C._cuda_getCurrentRawStream(max(device, 0)) if stream is None else stream.cuda_stream
+    _check(getattr(lib(), where)(ctypes.byref(shape), block, *ptrs, raw), where)
+
+
 def clsa_cache_append8(shape, block, k, v, start, count, page_table, k8, v8, k_scale, v_scale,
                        stream=None):
-    _check(lib().clsa_cache_append8(ctypes.byref(shape), int(block), _ptr(k, "k"), _ptr(v, "v"),
-                                    _ptr(start, "start"), _ptr(count, "count"),
-                                    _ptr(page_table, "page_table"), _ptr(k8, "k8"), _ptr(v8, "v8"),
-                                    _ptr(k_scale, "k_scale"), _ptr(v_scale, "v_scale"),
-                                    _stream(stream)), "clsa_cache_append8")
+    _call("clsa_cache_append8", shape, block,
+          (("k", k), ("v", v), ("start", start), ("count", count), ("page_table", page_table),
+           ("k8", k8), ("v8", v8), ("k_scale", k_scale), ("v_scale", v_scale)), False, stream)
 
 
 def clsa_sparse_attn8(shape, block, q, k8, v8, k_scale, v_scale, page_table, idx, n_sel, out,
                       lse=None, ws=None, stream=None):
-    wsb = 0 if ws is None else ws.numel() * ws.element_size()
-    _check(lib().clsa_sparse_attn8(ctypes.byref(shape), int(block), _ptr(q, "q"), _ptr(k8, "k8"),
-                                   _ptr(v8, "v8"), _ptr(k_scale, "k_scale"),
-                                   _ptr(v_scale, "v_scale"), _ptr(page_table, "page_table"),
-                                   _ptr(idx, "idx"), _ptr(n_sel, "n_sel"), _ptr(out, "out"),
-                                   _ptr(lse, "lse"), _ptr(ws, "ws"), wsb, _stream(stream)),
-           "clsa_sparse_attn8")
+    _call("clsa_sparse_attn8", shape, block,
+          (("q", q), ("k8", k8), ("v8", v8), ("k_scale", k_scale), ("v_scale", v_scale),
+           ("page_table", page_table), ("idx", idx), ("n_sel", n_sel), ("out", out), ("lse", lse)),
+          ws, stream)
 
 
 def clsa_dense_attn8(shape, block, q, k8, v8, k_scale, v_scale, page_table, seq_lens, q_pos, out,
                      lse=None, ws=None, stream=None):
-    wsb = 0 if ws is None else ws.numel() * ws.element_size()
-    _check(lib().clsa_dense_attn8(ctypes.byref(shape), int(block), _ptr(q, "q"), _ptr(k8, "k8"),
-                                  _ptr(v8, "v8"), _ptr(k_scale, "k_scale"),
-                                  _ptr(v_scale, "v_scale"), _ptr(page_table, "page_table"),
-                                  _ptr(seq_lens, "seq_lens"), _ptr(q_pos, "q_pos"),
-                                  _ptr(out, "out"), _ptr(lse, "lse"), _ptr(ws, "ws"), wsb,
-                                  _stream(stream)), "clsa_dense_attn8")
+    _call("clsa_dense_attn8", shape, block,
+          (("q", q), ("k8", k8), ("v8", v8), ("k_scale", k_scale), ("v_scale", v_scale),
+           ("page_table", page_table), ("seq_lens", seq_lens), ("q_pos", q_pos), ("out", out),
+           ("lse", lse)), ws, stream)
 
 
 def clsa_block_means(shape, block, k_idx, start, count, page_table, means, stream=None):
-    _check(lib().clsa_block_means(ctypes.byref(shape), int(block), _ptr(k_idx, "k_idx"),
-                                  _ptr(start, "start"), _ptr(count, "count"),
-                                  _ptr(page_table, "page_table"), _ptr(means, "means"),
-                                  _stream(stream)), "clsa_block_means")
+    _call("clsa_block_means", shape, block,
+          (("k_idx", k_idx), ("start", start), ("count", count), ("page_table", page_table),
+           ("means", means)), False, stream)
 
 
-def clsa_block_topk(shape, block, q_idx, means, page_table, seq_lens, q_pos, idx, n_sel, ws,
+def clsa_block_topk(shape, block, q_idx, means, page_table, seq_lens, q_pos, idx, n_sel, ws=None,
                     stream=None):
-    wsb = 0 if ws is None else ws.numel() * ws.element_size()
-    _check(lib().clsa_block_topk(ctypes.byref(shape), int(block), _ptr(q_idx, "q_idx"),
-                                 _ptr(means, "means"), _ptr(page_table, "page_table"),
-                                 _ptr(seq_lens, "seq_lens"), _ptr(q_pos, "q_pos"),
-                                 _ptr(idx, "idx"), _ptr(n_sel, "n_sel"), _ptr(ws, "ws"), wsb,
-                                 _stream(stream)), "clsa_block_topk")
+    _call("clsa_block_topk", shape, block,
+          (("q_idx", q_idx), ("means", means), ("page_table", page_table), ("seq_lens", seq_lens),
+           ("q_pos", q_pos), ("idx", idx), ("n_sel", n_sel)), ws, stream)
 
 
 CLSA_DEVERR_SEQ_LEN = 1

@@ -13,8 +13,8 @@
 // its scores made again in 64 bits (about one row in ten of 32 out of 2048 blocks,
 // two or three blocks each).
 //
-// The scoring reads the means once (1 / block of the index keys); one wave then
-// chooses a row's blocks and writes its list.
+// The scoring reads the means once (1 / block of the index keys); a workgroup then
+// chooses a row's blocks, holding their scores in registers, and writes its list.
 #include "clsa_internal.h"
 #include "device_common.h"
 
@@ -26,18 +26,19 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kBrDim = 256;
-constexpr int kBrRows = 16;        // rows per scoring tile
-constexpr int kBrBlocks = 64;      // blocks per scoring workgroup (4 waves x 16)
+constexpr int kBrTile = 16;        // rows, and blocks, of a scoring tile
+constexpr int kBrWaves = 4;
+constexpr int kBrMostBlocks = kMaxLen / 16;
 constexpr float kBrEps = 0x1p-15f; // error of a score over sum_i |q_i kbar_i|
 
 struct RouteArgs {
     const uint16_t *q_idx, *means;
     const int32_t *page_table, *seq_lens, *q_pos;
     float *scores;     // [rows, nblk]
-    float *bound;      // [rows, nchunk]: largest sum of magnitudes of a chunk of blocks
+    float *bound;      // [rows, ntile]: largest sum of magnitudes of a tile of blocks
     int32_t *idx, *n_sel;
     int n_q, max_len, page_shift, max_pages, causal, top_k;
-    int block_shift, nblk, nchunk, row_tiles;
+    int block_shift, nblk, ntile, chunks, row_groups, group_tiles;
 };
 
 template <bool PAGED>
@@ -58,277 +59,304 @@ __device__ __forceinline__ int blocks_before(int n, int block_shift) {
     return n > 0 ? (n - 1) >> block_shift : 0;
 }
 
+// One wave: 16 blocks, held as B operands, against group_tiles tiles of 16 rows.  Lane
+// (grp, sub) supplies row / block sub, dimensions 8 grp + 32 step, and receives rows
+// 4 grp + r of block sub.
 template <bool PAGED>
-__global__ __launch_bounds__(256) void block_scores_kernel(RouteArgs a) {
-    __shared__ float s_top[4][kBrRows];
-    __shared__ int s_own[kBrRows];
-    const int chunk = blockIdx.x % a.nchunk;
-    int x = blockIdx.x / a.nchunk;
-    const int t0 = (x % a.row_tiles) * kBrRows, b = x / a.row_tiles;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+__global__ __launch_bounds__(64 * kBrWaves) void block_scores_kernel(RouteArgs a) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int grp = lane >> 4, sub = lane & 15;
-    if (tid < kBrRows) {
-        const int t = t0 + tid, row = b * a.n_q + min(t, a.n_q - 1);
-        s_own[tid] = t < a.n_q ? blocks_before(valid_keys(a.seq_lens, a.q_pos, a.causal, b, row,
-                                                          a.max_len), a.block_shift)
-                               : 0;
-    }
-    __syncthreads();
-    int most = 0;
-#pragma unroll
-    for (int i = 0; i < kBrRows; ++i) most = max(most, s_own[i]);
-    if (chunk * kBrBlocks >= most) return;  // uniform: no row sees these blocks
-    const int c = chunk * kBrBlocks + wave * 16 + sub;
-    const uint16_t *qp = a.q_idx + ((size_t)b * a.n_q + min(t0 + sub, a.n_q - 1)) * kBrDim + 8 * grp;
-    const uint16_t *kp = mean_row<PAGED>(a, b, min(c, most - 1)) + 8 * grp;
-    u32x4 qv[8], kv[8];
-#pragma unroll
-    for (int s = 0; s < 8; ++s) {
-        qv[s] = *reinterpret_cast<const u32x4 *>(qp + 32 * s);
-        kv[s] = *reinterpret_cast<const u32x4 *>(kp + 32 * s);
-    }
-    f32x4 z = {0.f, 0.f, 0.f, 0.f}, m = {0.f, 0.f, 0.f, 0.f};
+    const int tile = (blockIdx.x % a.chunks) * kBrWaves + wave;
+    int x = blockIdx.x / a.chunks;
+    const int first = (x % a.row_groups) * a.group_tiles * kBrTile, b = x / a.row_groups;
+    const int end = min(a.n_q, first + a.group_tiles * kBrTile);
+    // a causal row sees no more than the sequence's length allows
+    const int most = blocks_before(clamp_len(a.seq_lens[b], a.max_len), a.block_shift);
+    if (tile * kBrTile >= most) return;
+    const int c = tile * kBrTile + sub;
     const u32x4 mag = {0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu};
+    u32x4 kv[8];
+    {
+        const uint16_t *kp = mean_row<PAGED>(a, b, min(c, most - 1)) + 8 * grp;
 #pragma unroll
-    for (int s = 0; s < 8; ++s) {
-        z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, qv[s]),
-                                                    __builtin_bit_cast(bf16x8, kv[s]), z, 0, 0, 0);
-        m = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, qv[s] & mag),
-                                                    __builtin_bit_cast(bf16x8, kv[s] & mag), m, 0, 0, 0);
+        for (int s = 0; s < 8; ++s) kv[s] = *reinterpret_cast<const u32x4 *>(kp + 32 * s);
     }
+    for (int t0 = first; t0 < end; t0 += kBrTile) {
+        const int t = min(t0 + sub, a.n_q - 1), row = b * a.n_q + t;
+        const uint16_t *qp = a.q_idx + (size_t)row * kBrDim + 8 * grp;
+        u32x4 qv[8];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        const int i = 4 * grp + r;
-        const bool seen = c < s_own[i];
-        if (seen) a.scores[((size_t)b * a.n_q + t0 + i) * a.nblk + c] = z[r];
-        // NaN counts as infinite (the maximum would drop it)
-        float w = seen ? (m[r] == m[r] ? m[r] : INFINITY) : 0.0f;
-        w = fmaxf(w, row_partner<8>(w));
-        w = fmaxf(w, row_partner<4>(w));
-        w = fmaxf(w, row_partner<2>(w));
-        w = fmaxf(w, row_partner<1>(w));
-        if (sub == 0) s_top[wave][i] = w;
+        for (int s = 0; s < 8; ++s) qv[s] = *reinterpret_cast<const u32x4 *>(qp + 32 * s);
+        const int mine = t0 + sub < a.n_q
+                             ? blocks_before(valid_keys(a.seq_lens, a.q_pos, a.causal, b, row, a.max_len),
+                                             a.block_shift)
+                             : 0;
+        if (__ballot(tile * kBrTile < mine) == 0) continue;  // no row sees these blocks
+        f32x4 z = {0.f, 0.f, 0.f, 0.f}, m = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, qv[s]),
+                                                        __builtin_bit_cast(bf16x8, kv[s]), z, 0, 0, 0);
+            m = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, qv[s] & mag),
+                                                        __builtin_bit_cast(bf16x8, kv[s] & mag), m, 0, 0, 0);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = 4 * grp + r, own = __shfl(mine, i);
+            const bool seen = c < own;
+            const size_t at = (size_t)b * a.n_q + t0 + i;
+            if (seen) a.scores[at * a.nblk + c] = z[r];
+            // NaN counts as infinite (the maximum would drop it)
+            float w = seen ? (m[r] == m[r] ? m[r] : INFINITY) : 0.0f;
+            w = fmaxf(w, row_partner<8>(w));
+            w = fmaxf(w, row_partner<4>(w));
+            w = fmaxf(w, row_partner<2>(w));
+            w = fmaxf(w, row_partner<1>(w));
+            if (sub == 0 && tile * kBrTile < own) a.bound[at * a.ntile + tile] = w;
+        }
     }
-    __syncthreads();
-    if (tid < kBrRows && t0 + tid < a.n_q)
-        a.bound[((size_t)b * a.n_q + t0 + tid) * a.nchunk + chunk] =
-            fmaxf(fmaxf(s_top[0][tid], s_top[1][tid]), fmaxf(s_top[2][tid], s_top[3][tid]));
 }
 
 // The float that score_key() maps to a key.
 __device__ __forceinline__ float key_score(uint32_t k) {
     return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
-
-// What one wave needs in LDS to choose a row's blocks.
-struct RouteLds {
-    uint32_t *keys;     // [nblk]
-    uint32_t *in;       // [words] chosen
-    uint32_t *band;     // [words] undecided
-    uint16_t *list;     // [top_k / block] chosen blocks, ascending
-    double *q;          // [256] index query
-};
-__host__ __device__ inline size_t route_lds_bytes(int nblk, int chosen) {
-    const size_t words = (size_t)(nblk + 31) / 32;
-    return 8 * kBrDim + 4 * (((size_t)nblk + 1) / 2 * 2 + 2 * ((words + 1) / 2 * 2)) +
-           2 * (((size_t)chosen + 3) / 4 * 4);
-}
-__device__ __forceinline__ RouteLds route_lds(char *base, int nblk) {
-    const int words = (nblk + 31) / 32;
-    RouteLds l;
-    l.q = reinterpret_cast<double *>(base);
-    l.keys = reinterpret_cast<uint32_t *>(l.q + kBrDim);
-    l.in = l.keys + (nblk + 1) / 2 * 2;
-    l.band = l.in + (words + 1) / 2 * 2;
-    l.list = reinterpret_cast<uint16_t *>(l.band + (words + 1) / 2 * 2);
-    return l;
+// The same order of 64-bit scores (-0 as +0).
+__device__ __forceinline__ uint64_t score_key64(double s) {
+    uint64_t u = (uint64_t)__double_as_longlong(s);
+    if ((u << 1) == 0) u = 0;
+    return u >> 63 ? ~u : u | (1ull << 63);
 }
 
-// LDS written by one lane of a wave and read by another: the wave's LDS operations
-// keep their order; this keeps the compiler from changing it.
-__device__ __forceinline__ void wave_sync() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
-
-// Among blocks c < count (in the band, if given): the want-th largest key.
-__device__ __forceinline__ uint32_t kth_key(const uint32_t *keys, const uint32_t *band, int count,
-                                            int want, int lane) {
-    uint32_t t = 0u;
-    for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t trial = t | (1u << bit);
-        int have = 0;
-        for (int c0 = 0; c0 < count; c0 += 64) {
-            const int c = c0 + lane;
-            const bool live = c < count && (!band || ((band[c >> 5] >> (c & 31)) & 1u));
-            have += __popcll(__ballot(live && keys[min(c, count - 1)] >= trial));
-        }
-        if (have >= want) t = trial;
-    }
-    return t;
-}
-
-// Writes 64 blocks' flags as two words.
-__device__ __forceinline__ void put_bits(uint32_t *bits, int c0, uint64_t flags, int lane) {
-    if (lane < 2) bits[(c0 >> 5) + lane] = (uint32_t)(flags >> (32 * lane));
-}
-
-// One wave: the want best of `count` blocks into l.in.  l.keys holds their scores'
-// keys; mag: the row's largest sum of magnitudes; zero: every score is 0.
-template <bool PAGED>
-__device__ __forceinline__ void choose_blocks(const RouteArgs &a, const RouteLds &l, int b, int count,
-                                              int want, float mag, bool zero, int lane) {
-    uint32_t t = kth_key(l.keys, nullptr, count, want, lane);
-    const float tf = key_score(t);
-    // 2 eps, the rounding of t +- it, and products that are flushed to zero
-    const float eps = 2.1f * kBrEps * mag + 1e-34f;
-    uint32_t lo = score_key(tf - eps), hi = score_key(tf + eps);
-    if (!(eps < INFINITY)) lo = 0u, hi = ~0u;  // nothing is decided
-    int above = 0, within = 0;
-    for (int c0 = 0; c0 < count; c0 += 64) {
-        const int c = c0 + lane;
-        const uint32_t k = l.keys[min(c, count - 1)];
-        const uint64_t up = __ballot(c < count && k > hi);
-        const uint64_t mid = __ballot(c < count && k >= lo && k <= hi);
-        put_bits(l.in, c0, up, lane);
-        put_bits(l.band, c0, mid, lane);
-        above += __popcll(up);
-        within += __popcll(mid);
-    }
-    wave_sync();
-    want -= above;
-    // Three times 24 bits of what is left of I_c beside a base decide 64-bit scores;
-    // rounding keeps their order, so only equal ones stay undecided.
-    double base = tf - tf == 0.0f ? (double)tf : 0.0;
-    for (int round = 0; round < 3 && within > want && !zero; ++round) {
-        for (int c0 = 0; c0 < count; c0 += 64) {
-            const int c = c0 + lane;
-            const uint64_t mid = (uint64_t)l.band[c0 >> 5] | ((uint64_t)l.band[(c0 >> 5) + 1] << 32);
-            if (mid == 0) continue;  // uniform
-            if ((mid >> lane) & 1u) {
-                const uint16_t *kp = mean_row<PAGED>(a, b, c);
-                double s = 0.0;
-                for (int i = 0; i < kBrDim; i += 8) {
-                    const u32x4 v = *reinterpret_cast<const u32x4 *>(kp + i);
+// Sum of a wave-uniform count over the workgroup's waves (slot: alternates between calls,
+// so that one barrier per call is enough).
+__device__ __forceinline__ int over_waves(int count, int (*slots)[kBrWaves], int &slot, int wave, int lane) {
+    if (lane == 0) slots[slot][wave] = count;
+    __syncthreads();
+    int sum = 0;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        s = fma(l.q[i + 2 * e], (double)bf16_lo(v[e]), s);
-                        s = fma(l.q[i + 2 * e + 1], (double)bf16_hi(v[e]), s);
-                    }
-                }
-                l.keys[c] = score_key((float)(s - base));
-            }
-        }
-        wave_sync();
-        t = kth_key(l.keys, l.band, count, want, lane);
-        within = 0;
-        above = 0;
-        for (int c0 = 0; c0 < count; c0 += 64) {
-            const uint64_t mid = (uint64_t)l.band[c0 >> 5] | ((uint64_t)l.band[(c0 >> 5) + 1] << 32);
-            const uint64_t was = (uint64_t)l.in[c0 >> 5] | ((uint64_t)l.in[(c0 >> 5) + 1] << 32);
-            const uint32_t k = l.keys[min(c0 + lane, count - 1)];
-            const uint64_t up = __ballot(((mid >> lane) & 1u) && k > t);
-            const uint64_t same = __ballot(((mid >> lane) & 1u) && k == t);
-            wave_sync();
-            put_bits(l.in, c0, was | up, lane);
-            put_bits(l.band, c0, same, lane);
-            above += __popcll(up);
-            within += __popcll(same);
-        }
-        wave_sync();
-        want -= above;
-        const float more = key_score(t);
-        if (more == 0.0f) break;  // equal to the last bit
-        base += more - more == 0.0f ? (double)more : 0.0;
-    }
-    // the band's first `want` blocks (all of them, or equal ones: the lowest)
-    for (int c0 = 0; c0 < count && want > 0; c0 += 64) {
-        const uint64_t mid = (uint64_t)l.band[c0 >> 5] | ((uint64_t)l.band[(c0 >> 5) + 1] << 32);
-        const uint64_t was = (uint64_t)l.in[c0 >> 5] | ((uint64_t)l.in[(c0 >> 5) + 1] << 32);
-        const bool take = ((mid >> lane) & 1u) && __popcll(mid & ((1ull << lane) - 1)) < want;
-        const uint64_t taken = __ballot(take);
-        wave_sync();
-        put_bits(l.in, c0, was | taken, lane);
-        want -= __popcll(taken);
-    }
-    wave_sync();
+    for (int w = 0; w < kBrWaves; ++w) sum += slots[slot][w];
+    slot ^= 1;
+    return sum;
 }
 
-// One wave: the row's token list from l.in (blocks before `own`) and its own block.
-__device__ __forceinline__ void write_list(const RouteArgs &a, const RouteLds &l, size_t row, int n,
-                                           int own, bool all, int lane) {
-    const int block = 1 << a.block_shift, cap = a.top_k >> a.block_shift;
-    int chosen = 0;
-    if (n > 0 && !all) {
-        for (int w0 = 0; w0 < (own + 31) / 32; w0 += 64) {
-            uint32_t w = w0 + lane < (own + 31) / 32 ? l.in[w0 + lane] : 0u;
-            int before = __popc(w), total;
+// Counts [E] of blocks become the numbers of blocks before each (one wave).
+template <int E>
+__device__ __forceinline__ void scan_counts(uint32_t *counts, int lane) {
+    constexpr int PER = E > 64 ? E / 64 : 1;
+    uint32_t c[PER], sum = 0u;
 #pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int o = __shfl_up(before, d);
-                if (lane >= d) before += o;
-            }
-            total = __shfl(before, 63);
-            before += chosen - __popc(w);
-            for (; w; w &= w - 1u, ++before)
-                if (before < cap - 1) l.list[before] = (uint16_t)(32 * (w0 + lane) + __builtin_ctz(w));
-            chosen += total;
-        }
-        chosen = min(chosen, cap - 1);
-        if (lane == 0) l.list[chosen] = (uint16_t)own;
-        wave_sync();
-    } else {
-        chosen = own;
+    for (int i = 0; i < PER; ++i) {
+        c[i] = lane * PER + i < E ? counts[lane * PER + i] : 0u;
+        sum += c[i];
     }
-    const int tokens = n > 0 ? (chosen << a.block_shift) + n - (own << a.block_shift) : 0;
-    int32_t *out = a.idx + row * a.top_k;
-    for (int p = lane; p < a.top_k; p += 64) {
-        const int i = p >> a.block_shift;
-        int tok = -1;
-        if (p < tokens) tok = ((all ? i : (int)l.list[i]) << a.block_shift) + (p & (block - 1));
-        out[p] = tok;
+    uint32_t before = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t o = (uint32_t)__shfl_up((int)before, d);
+        if (lane >= d) before += o;
     }
-    if (lane == 0) a.n_sel[row] = tokens;
+    before -= sum;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        if (lane * PER + i < E) counts[lane * PER + i] = before;
+        before += c[i];
+    }
 }
 
-template <bool PAGED>
-__global__ __launch_bounds__(64) void block_choose_kernel(RouteArgs a) {
-    extern __shared__ __align__(16) char s_route[];
-    const RouteLds l = route_lds(s_route, a.nblk);
+// LDS of block_choose_kernel past its static part: the undecided blocks' exact scores,
+// the taken ones of them as bits, and the chosen blocks.
+inline __host__ __device__ int even_up(int x) { return (x + 1) / 2 * 2; }
+static size_t choose_lds_bytes(int nblk, int chosen) {
+    return (size_t)8 * nblk + 4 * even_up(div_up(nblk, 32)) + 2 * (size_t)chosen;
+}
+
+// One workgroup = one row.  Thread tid holds blocks 256 i + tid (i < VPL) as
+// order-preserving keys in registers; the want-th largest is found bit by bit from the
+// top, counting with ballots.
+template <int VPL, bool PAGED>
+__global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_kernel(RouteArgs a) {
+    constexpr int NT = 64 * kBrWaves;
+    extern __shared__ __align__(16) char s_dyn[];
+    __shared__ int s_slots[2][kBrWaves];
+    __shared__ float s_mag[kBrWaves];
+    __shared__ uint32_t s_count[VPL * kBrWaves];
+    __shared__ __align__(16) double s_q[kBrDim];
+    uint64_t *exact = reinterpret_cast<uint64_t *>(s_dyn);
+    uint32_t *taken = reinterpret_cast<uint32_t *>(exact + a.nblk);
+    uint16_t *list = reinterpret_cast<uint16_t *>(taken + even_up(div_up(a.nblk, 32)));
     const size_t row = blockIdx.x;
-    const int b = (int)row / a.n_q, lane = threadIdx.x;
+    // the undecided blocks' numbers take the place of the row's scores, which are in registers then
+    uint16_t *number = reinterpret_cast<uint16_t *>(a.scores + row * a.nblk);
+    const int b = (int)row / a.n_q, tid = threadIdx.x;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const uint64_t below = (1ull << lane) - 1;
     const int n = valid_keys(a.seq_lens, a.q_pos, a.causal, b, (int)row, a.max_len);
-    const int own = blocks_before(n, a.block_shift), want = (a.top_k >> a.block_shift) - 1;
+    const int own = blocks_before(n, a.block_shift);
+    int want = (a.top_k >> a.block_shift) - 1;
     const bool all = own <= want;
-    if (!all) {
+    const int rest = n > 0 ? n - (own << a.block_shift) : 0;  // of the row's own block
+    const int tokens = n > 0 ? ((all ? own : want) << a.block_shift) + rest : 0;
+    if (tid == 0) a.n_sel[row] = tokens;
+    int32_t *out = a.idx + row * a.top_k;
+    if (all) {  // uniform: every valid token
+        for (int p = tid; p < a.top_k; p += NT) out[p] = p < tokens ? p : -1;
+        return;
+    }
+    const int kept = want;
+    uint32_t key[VPL];
+    uint32_t lo = ~0u, hi = ~0u;  // keys above hi are in, keys from lo on undecided
+    bool some = false;            // of those the ones that `taken` marks (else all)
+    if (want > 0) {
+        int slot = 0;
         const float *s = a.scores + row * a.nblk;
-        for (int c = lane; c < own; c += 64) l.keys[c] = score_key(s[c]);
         float mag = 0.0f;
-        for (int i = lane; i < div_up(own, kBrBlocks); i += 64) mag = fmaxf(mag, a.bound[row * a.nchunk + i]);
+        for (int i = tid; i < div_up(own, kBrTile); i += NT) mag = fmaxf(mag, a.bound[row * a.ntile + i]);
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) {
+            const int c = NT * i + tid;
+            key[i] = 0u;  // below every score's key
+            if (NT * i < own && c < own) key[i] = score_key(s[c]);
+        }
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) mag = fmaxf(mag, __shfl_xor(mag, d));
-        const uint2 q = *reinterpret_cast<const uint2 *>(a.q_idx + row * kBrDim + 4 * lane);
-        l.q[4 * lane] = (double)bf16_lo(q.x);
-        l.q[4 * lane + 1] = (double)bf16_hi(q.x);
-        l.q[4 * lane + 2] = (double)bf16_lo(q.y);
-        l.q[4 * lane + 3] = (double)bf16_hi(q.y);
-        const bool zero = __ballot(((q.x | q.y) & 0x7fff7fffu) != 0u) == 0;
-        wave_sync();
-        if (want > 0) {
-            choose_blocks<PAGED>(a, l, b, own, want, mag, zero, lane);
-        } else {
-            for (int w = lane; w < (own + 31) / 32; w += 64) l.in[w] = 0u;
-            wave_sync();
+        if (lane == 0) s_mag[wave] = mag;
+        uint32_t t = 0u;
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t trial = t | (1u << bit);
+            int have = 0;
+#pragma unroll
+            for (int i = 0; i < VPL; ++i)
+                if (NT * i < own) have += __popcll(__ballot(key[i] >= trial));
+            if (over_waves(have, s_slots, slot, wave, lane) >= want) t = trial;
+        }
+        mag = fmaxf(fmaxf(s_mag[0], s_mag[1]), fmaxf(s_mag[2], s_mag[3]));
+        const float tf = key_score(t);
+        // 2 eps, the rounding of t +- it, and products that are flushed to zero
+        const float eps = 2.1f * kBrEps * mag + 1e-34f;
+        lo = score_key(tf - eps);
+        hi = score_key(tf + eps);
+        if (!(eps < INFINITY)) lo = 1u, hi = ~0u;  // nothing is decided
+        int above = 0, within = 0;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) {
+            if (NT * i < own) {
+                above += __popcll(__ballot(key[i] > hi));
+                const int c = __popcll(__ballot(key[i] >= lo && key[i] <= hi));
+                within += c;
+                if (lane == 0) s_count[i * kBrWaves + wave] = (uint32_t)c;
+            } else if (lane == 0) {
+                s_count[i * kBrWaves + wave] = 0u;
+            }
+        }
+        above = over_waves(above, s_slots, slot, wave, lane);
+        within = over_waves(within, s_slots, slot, wave, lane);
+        want -= above;
+        some = within > want;
+        if (some) {  // uniform: exact scores decide
+            s_q[tid] = (double)__uint_as_float((uint32_t)a.q_idx[row * kBrDim + tid] << 16);
+            for (int w = tid; w < div_up(own, 32); w += NT) taken[w] = 0u;
+            if (wave == 0) scan_counts<VPL * kBrWaves>(s_count, lane);
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) {  // undecided blocks in ascending order
+                const uint64_t band = __ballot(key[i] >= lo && key[i] <= hi);
+                if ((band >> lane) & 1u)
+                    number[s_count[i * kBrWaves + wave] + __popcll(band & below)] = (uint16_t)(NT * i + tid);
+            }
+            __syncthreads();
+            for (int p = tid; p < within; p += NT) {
+                const uint16_t *kp = mean_row<PAGED>(a, b, number[p]);
+                double sum = 0.0;
+#pragma unroll 4
+                for (int e = 0; e < kBrDim; e += 8) {
+                    const u32x4 v = *reinterpret_cast<const u32x4 *>(kp + e);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        sum = fma(s_q[e + 2 * j], (double)bf16_lo(v[j]), sum);
+                        sum = fma(s_q[e + 2 * j + 1], (double)bf16_hi(v[j]), sum);
+                    }
+                }
+                exact[p] = score_key64(sum);
+            }
+            __syncthreads();
+            uint64_t x = 0;  // the want-th largest
+            for (int bit = 63; bit >= 0; --bit) {
+                const uint64_t trial = x | (1ull << bit);
+                int have = 0;
+                for (int p0 = 0; p0 < within; p0 += NT) {
+                    const int p = p0 + tid;
+                    have += __popcll(__ballot(p < within && exact[min(p, within - 1)] >= trial));
+                }
+                if (over_waves(have, s_slots, slot, wave, lane) >= want) x = trial;
+            }
+            int more = 0;
+            for (int p0 = 0; p0 < within; p0 += NT)
+                more += __popcll(__ballot(p0 + tid < within && exact[min(p0 + tid, within - 1)] > x));
+            int ties = want - over_waves(more, s_slots, slot, wave, lane);
+            if (wave == 0) {  // the larger ones, and of equal ones the lowest
+                for (int p0 = 0; p0 < within; p0 += 64) {
+                    const int p = min(p0 + lane, within - 1);
+                    const uint64_t same = __ballot(p0 + lane < within && exact[p] == x);
+                    if (p0 + lane < within &&
+                        (exact[p] > x || (exact[p] == x && __popcll(same & below) < ties)))
+                        atomicOr(&taken[number[p] >> 5], 1u << (number[p] & 31));
+                    ties -= min(ties, (int)__popcll(same));
+                }
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) key[i] = 0u;
+    }
+    __syncthreads();  // `taken` is complete, and every wave is done with s_count
+    auto chosen = [&](int i) {
+        const int c = NT * i + tid;
+        const bool open = key[i] >= lo && key[i] <= hi;
+        return key[i] > hi || (open && (!some || ((taken[c >> 5] >> (c & 31)) & 1u)));
+    };
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+        int c = 0;
+        if (NT * i < own) c = __popcll(__ballot(chosen(i)));
+        if (lane == 0) s_count[i * kBrWaves + wave] = (uint32_t)c;
+    }
+    __syncthreads();
+    if (wave == 0) scan_counts<VPL * kBrWaves>(s_count, lane);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+        if (NT * i < own) {
+            const bool in = chosen(i);
+            const int p = (int)s_count[i * kBrWaves + wave] + __popcll(__ballot(in) & below);
+            if (in && p < kept) list[p] = (uint16_t)(NT * i + tid);
         }
     }
-    write_list(a, l, row, n, own, all, lane);
+    if (tid == 0) list[kept] = (uint16_t)own;
+    __syncthreads();
+    const int block = 1 << a.block_shift;
+    for (int p = tid; p < a.top_k; p += NT)
+        out[p] = p < tokens ? ((int)list[p >> a.block_shift] << a.block_shift) + (p & (block - 1)) : -1;
 }
 
 static size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 size_t block_topk_ws_bytes(const Geometry &g, int block) {
-    const size_t nblk = div_up(g.max_len, block), chunks = div_up((int)nblk, kBrBlocks);
-    return align256(4 * (size_t)g.rows * nblk) + align256(4 * (size_t)g.rows * chunks);
+    const size_t nblk = div_up(g.max_len, block), tiles = div_up((int)nblk, kBrTile);
+    return align256(4 * (size_t)g.rows * nblk) + align256(4 * (size_t)g.rows * tiles);
+}
+
+template <int VPL, bool PAGED>
+static hipError_t launch_choose(const RouteArgs &a, int rows, hipStream_t stream) {
+    static_assert(64 * 64 * kBrWaves >= kBrMostBlocks, "the larger form holds every sequence");
+    const size_t lds = choose_lds_bytes(a.nblk, a.top_k >> a.block_shift);
+    if (lds > 32768) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&block_choose_kernel<VPL, PAGED>),
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    block_choose_kernel<VPL, PAGED><<<dim3((unsigned)rows), dim3(64 * kBrWaves), lds, stream>>>(a);
+    return hipGetLastError();
 }
 
 hipError_t launch_block_topk(const Geometry &g, int block, const void *q_idx, const void *means,
@@ -351,28 +379,26 @@ hipError_t launch_block_topk(const Geometry &g, int block, const void *q_idx, co
     a.top_k = g.top_k;
     a.block_shift = __builtin_ctz((unsigned)block);
     a.nblk = div_up(g.max_len, block);
-    a.nchunk = div_up(a.nblk, kBrBlocks);
-    a.row_tiles = div_up(g.n_q, kBrRows);
+    a.ntile = div_up(a.nblk, kBrTile);
+    a.chunks = div_up(a.ntile, kBrWaves);
+    // a wave keeps its blocks for up to 8 tiles of rows while that leaves enough workgroups
+    const int tiles = div_up(g.n_q, kBrTile);
+    a.group_tiles = 1;
+    while (a.group_tiles < 8 && (long)g.batch * div_up(tiles, 2 * a.group_tiles) * a.chunks >= 1024)
+        a.group_tiles *= 2;
+    a.row_groups = div_up(tiles, a.group_tiles);
     a.scores = static_cast<float *>(ws);
     a.bound = reinterpret_cast<float *>(static_cast<char *>(ws) + align256(4 * (size_t)g.rows * a.nblk));
-    const size_t blocks = (size_t)g.batch * a.row_tiles * a.nchunk;
+    const size_t blocks = (size_t)g.batch * a.row_groups * a.chunks;
     if (blocks > 0x7fffffffull) return hipErrorInvalidConfiguration;
+    const dim3 grid((unsigned)blocks), wg(64 * kBrWaves);
     const bool paged = g.page_shift >= 0;
-    const size_t lds = route_lds_bytes(a.nblk, g.top_k / block);
-    const void *fn = paged ? reinterpret_cast<const void *>(&block_choose_kernel<true>)
-                           : reinterpret_cast<const void *>(&block_choose_kernel<false>);
-    if (lds > 65536) {
-        const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        if (e != hipSuccess) return e;
-    }
-    const dim3 sgrid((unsigned)blocks), swg(256), cgrid((unsigned)g.rows), cwg(64);
-    if (paged) block_scores_kernel<true><<<sgrid, swg, 0, stream>>>(a);
-    else block_scores_kernel<false><<<sgrid, swg, 0, stream>>>(a);
-    hipError_t e = hipGetLastError();
+    if (paged) block_scores_kernel<true><<<grid, wg, 0, stream>>>(a);
+    else block_scores_kernel<false><<<grid, wg, 0, stream>>>(a);
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (paged) block_choose_kernel<true><<<cgrid, cwg, lds, stream>>>(a);
-    else block_choose_kernel<false><<<cgrid, cwg, lds, stream>>>(a);
-    return hipGetLastError();
+    if (a.nblk <= 8 * 64 * kBrWaves) return paged ? launch_choose<8, true>(a, g.rows, stream) : launch_choose<8, false>(a, g.rows, stream);
+    return paged ? launch_choose<64, true>(a, g.rows, stream) : launch_choose<64, false>(a, g.rows, stream);
 }
 
 hipError_t take_device_error_block_route(uint32_t *bits) { return take_source_device_error(bits); }

@@ -182,7 +182,7 @@ struct MeansArgs {
     const uint16_t *k_idx;
     uint16_t *means;
     const int32_t *start, *count, *page_table;
-    int n_q, max_len, page_shift, max_pages, block, block_shift, slots;
+    int n_q, max_len, page_shift, max_pages, block_shift, slots;
 };
 
 // One workgroup = one (sequence, block completed by its new tokens): 32 lanes hold a
@@ -190,14 +190,14 @@ struct MeansArgs {
 // held in 64 bits, where a block's 128 bf16 values add up without rounding
 // unless they lie more than 2^37 apart: the mean is then rounded once (to fp32, and
 // that to bf16), whatever the order.
-template <bool PAGED>
+template <int S, bool PAGED>
 __global__ __launch_bounds__(256) void block_means_kernel(MeansArgs a) {
     __shared__ double part[8][256];
     const int slot = blockIdx.x % a.slots, b = blockIdx.x / a.slots;
     int first, end;
     append_range(a.start, a.count, b, a.n_q, a.max_len, first, end);
     const int blk = (first >> a.block_shift) + slot, base = blk << a.block_shift;
-    if (first >= end || base + a.block > end) return;  // uniform: not complete
+    if (first >= end || base + S > end) return;  // uniform: not complete
     const int tid = threadIdx.x, tok = tid >> 5, piece = tid & 31;
     size_t row, mrow;
     if (PAGED) {
@@ -206,13 +206,17 @@ __global__ __launch_bounds__(256) void block_means_kernel(MeansArgs a) {
         mrow = row >> a.block_shift;
     } else {
         row = (size_t)b * a.max_len + base;
-        mrow = (size_t)b * div_up(a.max_len, a.block) + blk;
+        mrow = (size_t)b * div_up(a.max_len, S) + blk;
     }
     const uint16_t *in = a.k_idx + row * 256 + piece * 8;
+    uint4 v[S / 8];
+#pragma unroll
+    for (int i = 0; i < S / 8; ++i)
+        v[i] = *reinterpret_cast<const uint4 *>(in + (size_t)(tok + 8 * i) * 256);
     double sum[8] = {0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0};
-    for (int j = tok; j < a.block; j += 8) {
-        const uint4 v = *reinterpret_cast<const uint4 *>(in + (size_t)j * 256);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < S / 8; ++i) {
+        const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             sum[2 * e] += (double)bf16_lo(w[e]);
@@ -225,7 +229,7 @@ __global__ __launch_bounds__(256) void block_means_kernel(MeansArgs a) {
     double s = part[0][tid];
 #pragma unroll
     for (int t = 1; t < 8; ++t) s += part[t][tid];
-    const __bf16 m = (__bf16)(float)(s / (double)a.block);
+    const __bf16 m = (__bf16)(float)(s * (1.0 / S));
     a.means[mrow * 256 + tid] = __builtin_bit_cast(uint16_t, m);
 }
 
@@ -242,14 +246,24 @@ hipError_t launch_block_means(const Geometry &g, int block, const void *k_idx,
     a.max_len = g.max_len;
     a.page_shift = g.page_shift;
     a.max_pages = g.max_pages;
-    a.block = block;
     a.block_shift = __builtin_ctz((unsigned)block);
     a.slots = append_slots(g, block);
     const size_t blocks = (size_t)g.batch * a.slots;
     if (blocks > 0x7fffffffull) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)blocks), wg(256);
-    if (g.page_shift >= 0) block_means_kernel<true><<<grid, wg, 0, stream>>>(a);
-    else block_means_kernel<false><<<grid, wg, 0, stream>>>(a);
+    const bool paged = g.page_shift >= 0;
+#define CLSA_MEANS(S)                                                        \
+    if (paged) block_means_kernel<S, true><<<grid, wg, 0, stream>>>(a);      \
+    else block_means_kernel<S, false><<<grid, wg, 0, stream>>>(a);           \
+    break
+    switch (block) {
+        case 16: CLSA_MEANS(16);
+        case 32: CLSA_MEANS(32);
+        case 64: CLSA_MEANS(64);
+        case 128: CLSA_MEANS(128);
+        default: return hipErrorInvalidValue;
+    }
+#undef CLSA_MEANS
     return hipGetLastError();
 }
 
