@@ -71,7 +71,8 @@ __global__ __launch_bounds__(64 * kBrWaves) void block_scores_kernel(RouteArgs a
     const int first = (x % a.row_groups) * a.group_tiles * kBrTile, b = x / a.row_groups;
     const int end = min(a.n_q, first + a.group_tiles * kBrTile);
     // a causal row sees no more than the sequence's length allows
-    const int most = blocks_before(clamp_len(a.seq_lens[b], a.max_len), a.block_shift);
+    const int len = clamp_len(a.seq_lens[b], a.max_len);
+    const int most = blocks_before(len, a.block_shift);
     if (tile * kBrTile >= most) return;
     const int c = tile * kBrTile + sub;
     const u32x4 mag = {0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu};
@@ -81,16 +82,24 @@ __global__ __launch_bounds__(64 * kBrWaves) void block_scores_kernel(RouteArgs a
 #pragma unroll
         for (int s = 0; s < 8; ++s) kv[s] = *reinterpret_cast<const u32x4 *>(kp + 32 * s);
     }
-    for (int t0 = first; t0 < end; t0 += kBrTile) {
+    // the next tile of rows is in flight during the products of this one
+    u32x4 qn[8];
+    int next = 0;  // blocks that row sub of the next tile sees
+    auto fetch = [&](int t0) {
         const int t = min(t0 + sub, a.n_q - 1), row = b * a.n_q + t;
         const uint16_t *qp = a.q_idx + (size_t)row * kBrDim + 8 * grp;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) qn[s] = *reinterpret_cast<const u32x4 *>(qp + 32 * s);
+        next = len;
+        if (a.causal) next = min(len, max(a.q_pos[row] + 1, 0));
+    };
+    fetch(first);
+    for (int t0 = first; t0 < end; t0 += kBrTile) {
         u32x4 qv[8];
 #pragma unroll
-        for (int s = 0; s < 8; ++s) qv[s] = *reinterpret_cast<const u32x4 *>(qp + 32 * s);
-        const int mine = t0 + sub < a.n_q
-                             ? blocks_before(valid_keys(a.seq_lens, a.q_pos, a.causal, b, row, a.max_len),
-                                             a.block_shift)
-                             : 0;
+        for (int s = 0; s < 8; ++s) qv[s] = qn[s];
+        const int mine = t0 + sub < a.n_q ? blocks_before(next, a.block_shift) : 0;
+        if (t0 + kBrTile < end) fetch(t0 + kBrTile);
         if (__ballot(tile * kBrTile < mine) == 0) continue;  // no row sees these blocks
         f32x4 z = {0.f, 0.f, 0.f, 0.f}, m = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -140,28 +149,32 @@ __device__ __forceinline__ int over_waves(int count, int (*slots)[kBrWaves], int
     return sum;
 }
 
-// Counts [E] of blocks become the numbers of blocks before each (one wave).
+// Every wave: words[w] marks blocks 64 w ..+ 64; before[w] of them lie in earlier words.
+// E words, 64-bit; a lane makes PER consecutive ones (every wave the same values).
 template <int E>
-__device__ __forceinline__ void scan_counts(uint32_t *counts, int lane) {
+__device__ __forceinline__ void scan_words(const uint64_t *words, uint32_t *before, int lane) {
     constexpr int PER = E > 64 ? E / 64 : 1;
     uint32_t c[PER], sum = 0u;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        c[i] = lane * PER + i < E ? counts[lane * PER + i] : 0u;
+        c[i] = lane * PER + i < E ? (uint32_t)__popcll(words[lane * PER + i]) : 0u;
         sum += c[i];
     }
-    uint32_t before = sum;
+    uint32_t past = sum;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t o = (uint32_t)__shfl_up((int)before, d);
-        if (lane >= d) before += o;
+        const uint32_t o = (uint32_t)__shfl_up((int)past, d);
+        if (lane >= d) past += o;
     }
-    before -= sum;
+    past -= sum;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        if (lane * PER + i < E) counts[lane * PER + i] = before;
-        before += c[i];
+        if (lane * PER + i < E) before[lane * PER + i] = past;
+        past += c[i];
     }
+    // the wave's other lanes read them: its LDS operations keep their order, if the compiler does
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 }
 
 // LDS of block_choose_kernel past its static part: the undecided blocks' exact scores,
@@ -172,16 +185,21 @@ static size_t choose_lds_bytes(int nblk, int chosen) {
 }
 
 // One workgroup = one row.  Thread tid holds blocks 256 i + tid (i < VPL) as
-// order-preserving keys in registers; the want-th largest is found bit by bit from the
-// top, counting with ballots.
+// order-preserving keys in registers.  The want-th largest is found in three histograms
+// in LDS (11, 11 and 10 bits from the top; bit by bit with ballots and a barrier each it
+// took 20000 of the kernel's 36000 cycles, so 6000).
+constexpr int kBrBins = 2048;
+
 template <int VPL, bool PAGED>
 __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_kernel(RouteArgs a) {
-    constexpr int NT = 64 * kBrWaves;
+    constexpr int NT = 64 * kBrWaves, WORDS = VPL * kBrWaves;
     extern __shared__ __align__(16) char s_dyn[];
     __shared__ int s_slots[2][kBrWaves];
     __shared__ float s_mag[kBrWaves];
-    __shared__ uint32_t s_count[VPL * kBrWaves];
-    __shared__ __align__(16) double s_q[kBrDim];
+    __shared__ uint64_t s_words[WORDS];
+    __shared__ uint32_t s_before[kBrWaves][WORDS];
+    __shared__ __align__(16) uint32_t s_bins[kBrBins];
+    __shared__ uint32_t s_pick[2];
     uint64_t *exact = reinterpret_cast<uint64_t *>(s_dyn);
     uint32_t *taken = reinterpret_cast<uint32_t *>(exact + a.nblk);
     uint16_t *list = reinterpret_cast<uint16_t *>(taken + even_up(div_up(a.nblk, 32)));
@@ -191,6 +209,12 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
     const int b = (int)row / a.n_q, tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const uint64_t below = (1ull << lane) - 1;
+    uint32_t key[VPL];
+    {  // before the row's length is known: those past its blocks are not used
+        const uint32_t *s = reinterpret_cast<const uint32_t *>(a.scores) + row * a.nblk;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) key[i] = s[min(NT * i + tid, a.nblk - 1)];
+    }
     const int n = valid_keys(a.seq_lens, a.q_pos, a.causal, b, (int)row, a.max_len);
     const int own = blocks_before(n, a.block_shift);
     int want = (a.top_k >> a.block_shift) - 1;
@@ -204,32 +228,69 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
         return;
     }
     const int kept = want;
-    uint32_t key[VPL];
     uint32_t lo = ~0u, hi = ~0u;  // keys above hi are in, keys from lo on undecided
     bool some = false;            // of those the ones that `taken` marks (else all)
+#pragma unroll
+    for (int i = 0; i < VPL; ++i)
+        key[i] = NT * i + tid < own && want > 0 ? score_key(__uint_as_float(key[i])) : 0u;
     if (want > 0) {
         int slot = 0;
-        const float *s = a.scores + row * a.nblk;
         float mag = 0.0f;
         for (int i = tid; i < div_up(own, kBrTile); i += NT) mag = fmaxf(mag, a.bound[row * a.ntile + i]);
+        // histograms of the digit at `shift` of the keys that agree with t above it
+        uint32_t t = 0u;
+        int left = want;
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) {
-            const int c = NT * i + tid;
-            key[i] = 0u;  // below every score's key
-            if (NT * i < own && c < own) key[i] = score_key(s[c]);
+        for (int pass = 0; pass < 3; ++pass) {
+            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+            const int width = pass == 2 ? 10 : 11;
+            constexpr int PER = kBrBins / NT;
+#pragma unroll
+            for (int i = 0; i < PER; i += 4)
+                *reinterpret_cast<uint4 *>(&s_bins[PER * tid + i]) = make_uint4(0u, 0u, 0u, 0u);
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < VPL; ++i)
+                if (NT * i + tid < own && (pass == 0 || (key[i] >> (shift + width)) == t))
+                    atomicAdd(&s_bins[(key[i] >> shift) & ((1u << width) - 1u)], 1u);
+            __syncthreads();
+            // thread tid: bins PER tid ..+ PER; keys in higher ones first
+            uint32_t c[PER], sum = 0u;
+#pragma unroll
+            for (int i = 0; i < PER; i += 4) {
+                const uint4 v = *reinterpret_cast<const uint4 *>(&s_bins[PER * tid + i]);
+                c[i] = v.x, c[i + 1] = v.y, c[i + 2] = v.z, c[i + 3] = v.w;
+                sum += (v.x + v.y) + (v.z + v.w);
+            }
+            uint32_t past = sum;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const uint32_t o = (uint32_t)__shfl_down((int)past, d);
+                if (lane + d < 64) past += o;
+            }
+            if (lane == 0) s_slots[slot][wave] = (int)past;
+            __syncthreads();
+            uint32_t higher = past - sum;
+            for (int w = wave + 1; w < kBrWaves; ++w) higher += (uint32_t)s_slots[slot][w];
+            slot ^= 1;
+            if (higher < (uint32_t)left && higher + sum >= (uint32_t)left) {  // one thread
+#pragma unroll
+                for (int i = PER - 1; i >= 0; --i) {
+                    if (higher < (uint32_t)left && higher + c[i] >= (uint32_t)left) {
+                        s_pick[0] = (uint32_t)(PER * tid + i);
+                        s_pick[1] = higher;
+                    }
+                    higher += c[i];
+                }
+            }
+            __syncthreads();
+            t = pass == 0 ? s_pick[0] : (t << width) | s_pick[0];
+            left -= (int)s_pick[1];
         }
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) mag = fmaxf(mag, __shfl_xor(mag, d));
         if (lane == 0) s_mag[wave] = mag;
-        uint32_t t = 0u;
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t trial = t | (1u << bit);
-            int have = 0;
-#pragma unroll
-            for (int i = 0; i < VPL; ++i)
-                if (NT * i < own) have += __popcll(__ballot(key[i] >= trial));
-            if (over_waves(have, s_slots, slot, wave, lane) >= want) t = trial;
-        }
+        __syncthreads();
         mag = fmaxf(fmaxf(s_mag[0], s_mag[1]), fmaxf(s_mag[2], s_mag[3]));
         const float tf = key_score(t);
         // 2 eps, the rounding of t +- it, and products that are flushed to zero
@@ -240,97 +301,94 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
         int above = 0, within = 0;
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
-            if (NT * i < own) {
-                above += __popcll(__ballot(key[i] > hi));
-                const int c = __popcll(__ballot(key[i] >= lo && key[i] <= hi));
-                within += c;
-                if (lane == 0) s_count[i * kBrWaves + wave] = (uint32_t)c;
-            } else if (lane == 0) {
-                s_count[i * kBrWaves + wave] = 0u;
-            }
+            const uint64_t band = __ballot(key[i] >= lo && key[i] <= hi);
+            above += __popcll(__ballot(key[i] > hi));
+            within += __popcll(band);
+            if (lane == 0) s_words[i * kBrWaves + wave] = band;
         }
         above = over_waves(above, s_slots, slot, wave, lane);
         within = over_waves(within, s_slots, slot, wave, lane);
         want -= above;
         some = within > want;
         if (some) {  // uniform: exact scores decide
-            s_q[tid] = (double)__uint_as_float((uint32_t)a.q_idx[row * kBrDim + tid] << 16);
+            scan_words<WORDS>(s_words, s_before[wave], lane);
+            double *q = reinterpret_cast<double *>(s_bins);
+            static_assert(sizeof(double) * kBrDim <= sizeof s_bins, "the query fits the bins");
+            q[tid] = (double)__uint_as_float((uint32_t)a.q_idx[row * kBrDim + tid] << 16);
             for (int w = tid; w < div_up(own, 32); w += NT) taken[w] = 0u;
-            if (wave == 0) scan_counts<VPL * kBrWaves>(s_count, lane);
-            __syncthreads();
 #pragma unroll
             for (int i = 0; i < VPL; ++i) {  // undecided blocks in ascending order
-                const uint64_t band = __ballot(key[i] >= lo && key[i] <= hi);
+                const uint64_t band = s_words[i * kBrWaves + wave];
                 if ((band >> lane) & 1u)
-                    number[s_count[i * kBrWaves + wave] + __popcll(band & below)] = (uint16_t)(NT * i + tid);
+                    number[s_before[wave][i * kBrWaves + wave] + __popcll(band & below)] = (uint16_t)(NT * i + tid);
             }
             __syncthreads();
             for (int p = tid; p < within; p += NT) {
                 const uint16_t *kp = mean_row<PAGED>(a, b, number[p]);
                 double sum = 0.0;
-#pragma unroll 4
+#pragma unroll 8
                 for (int e = 0; e < kBrDim; e += 8) {
                     const u32x4 v = *reinterpret_cast<const u32x4 *>(kp + e);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        sum = fma(s_q[e + 2 * j], (double)bf16_lo(v[j]), sum);
-                        sum = fma(s_q[e + 2 * j + 1], (double)bf16_hi(v[j]), sum);
+                        sum = fma(q[e + 2 * j], (double)bf16_lo(v[j]), sum);
+                        sum = fma(q[e + 2 * j + 1], (double)bf16_hi(v[j]), sum);
                     }
                 }
                 exact[p] = score_key64(sum);
             }
             __syncthreads();
-            uint64_t x = 0;  // the want-th largest
-            for (int bit = 63; bit >= 0; --bit) {
-                const uint64_t trial = x | (1ull << bit);
-                int have = 0;
-                for (int p0 = 0; p0 < within; p0 += NT) {
-                    const int p = p0 + tid;
-                    have += __popcll(__ballot(p < within && exact[min(p, within - 1)] >= trial));
+            if (within <= NT) {  // each counts those that go before it
+                const uint64_t x = tid < within ? exact[tid] : 0;
+                int before = 0;
+                for (int p = 0; p < within; ++p) {
+                    const uint64_t o = exact[p];
+                    before += o > x || (o == x && p < tid) ? 1 : 0;
                 }
-                if (over_waves(have, s_slots, slot, wave, lane) >= want) x = trial;
-            }
-            int more = 0;
-            for (int p0 = 0; p0 < within; p0 += NT)
-                more += __popcll(__ballot(p0 + tid < within && exact[min(p0 + tid, within - 1)] > x));
-            int ties = want - over_waves(more, s_slots, slot, wave, lane);
-            if (wave == 0) {  // the larger ones, and of equal ones the lowest
-                for (int p0 = 0; p0 < within; p0 += 64) {
-                    const int p = min(p0 + lane, within - 1);
-                    const uint64_t same = __ballot(p0 + lane < within && exact[p] == x);
-                    if (p0 + lane < within &&
-                        (exact[p] > x || (exact[p] == x && __popcll(same & below) < ties)))
-                        atomicOr(&taken[number[p] >> 5], 1u << (number[p] & 31));
-                    ties -= min(ties, (int)__popcll(same));
+                if (tid < within && before < want) atomicOr(&taken[number[tid] >> 5], 1u << (number[tid] & 31));
+            } else {  // many equal or nearly equal scores: bit by bit
+                uint64_t x = 0;  // the want-th largest
+                for (int bit = 63; bit >= 0; --bit) {
+                    const uint64_t trial = x | (1ull << bit);
+                    int have = 0;
+                    for (int p0 = 0; p0 < within; p0 += NT) {
+                        const int p = p0 + tid;
+                        have += __popcll(__ballot(p < within && exact[min(p, within - 1)] >= trial));
+                    }
+                    if (over_waves(have, s_slots, slot, wave, lane) >= want) x = trial;
+                }
+                int more = 0;
+                for (int p0 = 0; p0 < within; p0 += NT)
+                    more += __popcll(__ballot(p0 + tid < within && exact[min(p0 + tid, within - 1)] > x));
+                int ties = want - over_waves(more, s_slots, slot, wave, lane);
+                if (wave == 0) {  // the larger ones, and of equal ones the lowest
+                    for (int p0 = 0; p0 < within; p0 += 64) {
+                        const int p = min(p0 + lane, within - 1);
+                        const uint64_t same = __ballot(p0 + lane < within && exact[p] == x);
+                        if (p0 + lane < within &&
+                            (exact[p] > x || (exact[p] == x && __popcll(same & below) < ties)))
+                            atomicOr(&taken[number[p] >> 5], 1u << (number[p] & 31));
+                        ties -= min(ties, (int)__popcll(same));
+                    }
                 }
             }
+            __syncthreads();  // `taken` is complete
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < VPL; ++i) key[i] = 0u;
     }
-    __syncthreads();  // `taken` is complete, and every wave is done with s_count
-    auto chosen = [&](int i) {
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
         const int c = NT * i + tid;
         const bool open = key[i] >= lo && key[i] <= hi;
-        return key[i] > hi || (open && (!some || ((taken[c >> 5] >> (c & 31)) & 1u)));
-    };
-#pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-        int c = 0;
-        if (NT * i < own) c = __popcll(__ballot(chosen(i)));
-        if (lane == 0) s_count[i * kBrWaves + wave] = (uint32_t)c;
+        const uint64_t in = __ballot(key[i] > hi || (open && (!some || ((taken[c >> 5] >> (c & 31)) & 1u))));
+        if (lane == 0) s_words[i * kBrWaves + wave] = in;
     }
     __syncthreads();
-    if (wave == 0) scan_counts<VPL * kBrWaves>(s_count, lane);
-    __syncthreads();
+    scan_words<WORDS>(s_words, s_before[wave], lane);
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
-        if (NT * i < own) {
-            const bool in = chosen(i);
-            const int p = (int)s_count[i * kBrWaves + wave] + __popcll(__ballot(in) & below);
-            if (in && p < kept) list[p] = (uint16_t)(NT * i + tid);
-        }
+        const uint64_t in = s_words[i * kBrWaves + wave];
+        const int p = (int)s_before[wave][i * kBrWaves + wave] + __popcll(in & below);
+        if (((in >> lane) & 1u) && p < kept) list[p] = (uint16_t)(NT * i + tid);
     }
     if (tid == 0) list[kept] = (uint16_t)own;
     __syncthreads();
