@@ -33,8 +33,7 @@ typedef int i32x2 __attribute__((ext_vector_type(2)));
 constexpr int kA8Dim = 128;
 constexpr int kA8Pitch = kA8Dim + 16;  // bytes per staged row
 constexpr int kA8Tokens = 32;          // tokens per wave and step
-constexpr int kA8Waves = 4;
-constexpr int kA8Chunk = kA8Tokens * kA8Waves;
+constexpr int kA8ManyUnits = 768;      // (row, KV head) units from which a workgroup is one wave
 constexpr float kA8Log2e = 1.4426950408889634f;
 constexpr float kA8Ln2 = 0.6931471805599453f;
 
@@ -47,7 +46,7 @@ struct Attn8Args {
     const int32_t *seq_lens, *q_pos; // dense
     uint16_t *out;
     float *lse;                      // may be null
-    float *part_o, *part_ml;         // [rows, Hq, splits, 128 / 2] with several splits
+    float *part_o, *part_ml;         // [rows, Hq, splits, 128] and [.., 2] with several splits
     int n_q, max_len, page_shift, max_pages, block_shift, top_k, kv_heads, q_heads, splits, span;
     int causal;
     float scale_log2;
@@ -64,6 +63,13 @@ __device__ __forceinline__ int row_keys8(const Attn8Args &a, int row) {
     return m;
 }
 
+// 16 bytes of the cache; ONCE: no other workgroup reads them (non-temporal).
+template <bool ONCE>
+__device__ __forceinline__ u32x4 load16(const uint8_t *p) {
+    if (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
+    return *reinterpret_cast<const u32x4 *>(p);
+}
+
 // 8 e4m3 bytes -> 8 bf16 (exact)
 __device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi) {
     const bf16x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
@@ -73,23 +79,75 @@ __device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi) {
     return bf16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
 }
 
-// Maximum / sum over the four lanes (l, l ^ 16, l ^ 32, l ^ 48) of a head.
-__device__ __forceinline__ float quad_max(float x) {
+// The logits of a head come to the four lanes (qq, head) as 8 values each, token slots 4 qq
+// + r and 16 + 4 qq + r, and the columns past the heads are empty: F - 1 other lanes of
+// the row of 16, each 16 / F lanes on, take 8 / F of them (in order), so that the
+// softmax works on all lanes.  DPP moves whose bank mask picks the lanes that are
+// written (a bank: 4 lanes); row rotations by 4, 8 and 12.
+template <int CTRL, int BANKS>
+__device__ __forceinline__ float dpp_into(float old, float x) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(old), __float_as_int(x), CTRL, 0xf,
+                                                      BANKS, false));
+}
+template <int F, int E>
+__device__ __forceinline__ void spread(const f32x4 (&c)[2], float (&z)[E]) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        if constexpr (F == 4) {
+            z[e] = dpp_into<0x124, 0x2>(c[0][e], c[0][2 + e]);
+            z[e] = dpp_into<0x128, 0x4>(z[e], c[1][e]);
+            z[e] = dpp_into<0x12c, 0x8>(z[e], c[1][2 + e]);
+        } else {
+            z[e] = dpp_into<0x128, 0xc>(c[0][e], c[1][e]);
+        }
+    }
+}
+// Back to the lanes (qq, head) as bf16: the A operand (other lanes: rows past the heads).
+template <int F, int E>
+__device__ __forceinline__ bf16x8 collect(const float (&p)[E]) {
+    u32x4 w;
+    if constexpr (F == 4) {
+        const uint32_t x = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)p[0], (__bf16)p[1]});
+        w[0] = x;
+        w[1] = (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x12c, 0xf, 0xf, false);
+        w[2] = (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x128, 0xf, 0xf, false);
+        w[3] = (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x124, 0xf, 0xf, false);
+    } else {
+        w[0] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)p[0], (__bf16)p[1]});
+        w[1] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)p[2], (__bf16)p[3]});
+        w[2] = (uint32_t)__builtin_amdgcn_mov_dpp((int)w[0], 0x128, 0xf, 0xf, false);
+        w[3] = (uint32_t)__builtin_amdgcn_mov_dpp((int)w[1], 0x128, 0xf, 0xf, false);
+    }
+    return __builtin_bit_cast(bf16x8, w);
+}
+
+// Maximum / sum over the 4 F lanes of a head.
+template <int F>
+__device__ __forceinline__ float head_max(float x) {
     auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
     r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    x = fmaxf(x, dpp_f32<0x128>(x));
+    if (F == 4) x = fmaxf(x, dpp_f32<0x124>(x));
+    return x;
 }
-__device__ __forceinline__ float quad_sum(float x) {
+template <int F>
+__device__ __forceinline__ float head_sum(float x) {
     auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
     r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    x += dpp_f32<0x128>(x);
+    if (F == 4) x += dpp_f32<0x124>(x);
+    return x;
 }
 
-template <int G, bool PAGED, bool DENSE>
-__global__ __launch_bounds__(64 * kA8Waves) void attn8_kernel(Attn8Args a) {
-    constexpr int NW = kA8Waves;
+template <int G, bool PAGED, bool DENSE, bool ONCE, int HW, int TW>
+__global__ __launch_bounds__(64 * HW * TW, 4) void attn8_kernel(Attn8Args a) {
+    constexpr int NW = HW * TW;
+    constexpr int F = G <= 4 ? 4 : 2, E = 8 / F;  // lanes that share a head's logits; each one's share
+    constexpr int STEP = kA8Tokens * TW;  // tokens that the waves of a head take at a time
     // the waves' staged K and V rows; at the end their weighted values [NW][G * 128]
     __shared__ __align__(16) union {
         uint8_t rows[NW][2][kA8Tokens][kA8Pitch];
@@ -98,20 +156,29 @@ __global__ __launch_bounds__(64 * kA8Waves) void attn8_kernel(Attn8Args a) {
     __shared__ __align__(16) float s_sc[NW][2][kA8Tokens];  // key, value scales of the 32 tokens
     __shared__ float s_ml[NW][G][2];
     const int split = blockIdx.x % a.splits, rg = blockIdx.x / a.splits;
-    const int g = rg % a.kv_heads, row = rg / a.kv_heads;
+    const int groups = a.kv_heads / HW, row = rg / groups;
     const int b = row / a.n_q;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int g0 = (rg % groups) * HW, g = g0 + wave % HW, tw = wave / HW;
     const int qq = lane >> 4, sub = lane & 15;
-    const int n = row_keys8<DENSE>(a, row);
     const size_t rh0 = (size_t)row * a.q_heads + g * G;
+    const int32_t *sel = DENSE ? nullptr : a.idx + (size_t)row * a.top_k;
+    const int half = lane >> 5, tl = lane & 31;
+    const int begin = split * a.span, first = begin + tw * kA8Tokens;
+    // A step's 32 tokens: lane (half, tl) holds the list entry of token tl.  The entries of
+    // the first two steps are asked for before the row's count is known (any position
+    // below top_k is readable).
+    auto entry = [&](int c0) { return DENSE ? c0 + tl : sel[min(c0 + tl, a.top_k - 1)]; };
+    int j0 = entry(first), j1 = entry(first + STEP);
+    const int n = row_keys8<DENSE>(a, row);
     if (n == 0) {  // no keys: output 0, lse -inf
         if (split == 0) {
-            for (int e = tid; e < G * kA8Dim; e += 64 * NW) a.out[rh0 * kA8Dim + e] = 0;
-            if (a.lse && tid < G) a.lse[rh0 + tid] = -INFINITY;
+            const size_t h0 = (size_t)row * a.q_heads + g0 * G;
+            for (int e = tid; e < HW * G * kA8Dim; e += 64 * NW) a.out[h0 * kA8Dim + e] = 0;
+            if (a.lse && tid < HW * G) a.lse[h0 + tid] = -INFINITY;
         }
         return;
     }
-    const int begin = split * a.span;
     if (begin >= n) return;  // uniform; the merge masks splits past the last one
     const int end = min(n, begin + a.span);
 
@@ -124,55 +191,78 @@ __global__ __launch_bounds__(64 * kA8Waves) void attn8_kernel(Attn8Args a) {
             qb[st] = __builtin_bit_cast(bf16x8, sub < G ? v : u32x4{0u, 0u, 0u, 0u});
         }
     }
-    const int32_t *sel = DENSE ? nullptr : a.idx + (size_t)row * a.top_k;
-    const int half = lane >> 5, tl = lane & 31;
-    const float *scales = half ? a.v_scale : a.k_scale;
-    const int nblk = (a.max_len + (1 << a.block_shift) - 1) >> a.block_shift;
+    const int nblk = ((a.max_len - 1) >> a.block_shift) + 1;
     const uint32_t row_bytes = (uint32_t)a.kv_heads * kA8Dim;
+    // Contiguous caches: 32-bit offsets inside the sequence from a uniform base (one
+    // sequence's bytes are below 4 GiB, checked at the boundary).
+    const size_t head = (PAGED ? 0 : (size_t)b * a.max_len * row_bytes) + g * kA8Dim;
+    const uint8_t *kbase = a.k + head, *vbase = a.v + head;
+    const float *scales = (half ? a.v_scale : a.k_scale) + (PAGED ? 0 : (size_t)b * nblk * a.kv_heads) + g;
+    const float scale_log2 = half ? 1.0f : a.scale_log2;  // goes into the key scales
     uint8_t(*sk)[kA8Pitch] = s.rows[wave][0], (*sv)[kA8Pitch] = s.rows[wave][1];
+    // Cache row of this lane's token: an entry clamped into the sequence, for a token past
+    // the end the step's first one (with weight 0).
+    auto locate = [&](int j, int c0) {
+        j = min(max(j, 0), a.max_len - 1);
+        if (c0 + kA8Tokens > end) {
+            const int lead = __builtin_amdgcn_readfirstlane(j);
+            j = c0 + tl < end ? j : lead;
+        }
+        if (!PAGED) return (uint32_t)j;
+        const int page = a.page_table[(size_t)b * a.max_pages + (j >> a.page_shift)];
+        return ((uint32_t)page << a.page_shift) + (uint32_t)(j & ((1 << a.page_shift) - 1));
+    };
+    u32x4 kr[4], vr[4];
+    float sc;
+    auto gather = [&](uint32_t trow) {  // 8 lanes x 16 bytes a token, and its scales
+        // a row's place is made once and handed to the lanes that load it: its byte offset
+        // in the sequence, or (paged) its number of 128-byte vectors in the cache
+        const uint32_t place = PAGED ? trow * (uint32_t)a.kv_heads : trow * row_bytes;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const uint32_t r = (uint32_t)__shfl((int)place, 8 * x + (lane >> 3));
+            if (PAGED) {
+                const size_t off = ((size_t)r << 7) + (uint32_t)((lane & 7) * 16);
+                kr[x] = load16<ONCE>(kbase + off);
+                vr[x] = load16<ONCE>(vbase + off);
+            } else {
+                const uint32_t off = r + (uint32_t)((lane & 7) * 16);
+                kr[x] = load16<ONCE>(kbase + off);
+                vr[x] = load16<ONCE>(vbase + off);
+            }
+        }
+        const uint32_t blk = trow >> a.block_shift;
+        sc = scales[PAGED ? (size_t)blk * a.kv_heads : (size_t)(blk * (uint32_t)a.kv_heads)];
+    };
 
-    float m_run = -INFINITY, l_run = 0.0f;  // head sub (this wave)
-    f32x4 acc[8];                           // head 4 qq + r, dimension 16 d + sub
+    const int part = sub / (16 / F);  // this lane's share of head sub % (16 / F)
+    float m_run = -INFINITY, l_part = 0.0f;  // that head's maximum, and this lane's share of the sum
+    f32x4 acc[8];                            // head 4 qq + r, dimension 16 d + sub
 #pragma unroll
     for (int d = 0; d < 8; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    for (int c0 = begin + wave * kA8Tokens; c0 < end; c0 += kA8Chunk) {
-        // tokens past the end: the step's first one, with weight 0
-        int j = DENSE ? c0 + tl : sel[min(c0 + tl, a.top_k - 1)];
-        j = min(max(j, 0), a.max_len - 1);
-        const int j0 = __builtin_amdgcn_readfirstlane(j);
-        j = c0 + tl < end ? j : j0;
-        uint32_t trow;   // token row (paged: in the whole cache; else in the sequence)
-        size_t srow;
-        if (PAGED) {
-            const int page = a.page_table[(size_t)b * a.max_pages + (j >> a.page_shift)];
-            trow = ((uint32_t)page << a.page_shift) + (j & ((1 << a.page_shift) - 1));
-            srow = trow >> a.block_shift;
-        } else {
-            trow = (uint32_t)j;
-            srow = (size_t)b * nblk + (j >> a.block_shift);
-        }
-        const float sc = scales[srow * a.kv_heads + g];
-        u32x4 kr[4], vr[4];
+    // While a step is computed from LDS, the next one's rows are in flight, behind them the
+    // page of the one after it and the list entries of a third.
+    uint32_t t1 = 0u;
+    if (first < end) {
+        gather(locate(j0, first));
+        if (first + STEP < end) t1 = locate(j1, first + STEP);
+        j1 = entry(first + 2 * STEP);
+    }
+    for (int c0 = first; c0 < end; c0 += STEP) {
+        s_sc[wave][half][tl] = sc * scale_log2;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t r = (uint32_t)__shfl((int)trow, 8 * i + (lane >> 3));
-            const size_t off = ((size_t)r + (PAGED ? 0 : (size_t)b * a.max_len)) * row_bytes +
-                               (uint32_t)(g * kA8Dim + (lane & 7) * 16);
-            kr[i] = *reinterpret_cast<const u32x4 *>(a.k + off);
-            vr[i] = *reinterpret_cast<const u32x4 *>(a.v + off);
+        for (int x = 0; x < 4; ++x) {
+            *reinterpret_cast<u32x4 *>(&sk[8 * x + (lane >> 3)][(lane & 7) * 16]) = kr[x];
+            *reinterpret_cast<u32x4 *>(&sv[8 * x + (lane >> 3)][(lane & 7) * 16]) = vr[x];
         }
-        __builtin_amdgcn_sched_barrier(0);  // every gather in flight before the first wait
-        s_sc[wave][half][tl] = sc;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            *reinterpret_cast<u32x4 *>(&sk[8 * i + (lane >> 3)][(lane & 7) * 16]) = kr[i];
-            *reinterpret_cast<u32x4 *>(&sv[8 * i + (lane >> 3)][(lane & 7) * 16]) = vr[i];
+        if (c0 + STEP < end) {
+            gather(t1);
+            if (c0 + 2 * STEP < end) t1 = locate(j1, c0 + 2 * STEP);
+            j1 = entry(c0 + 3 * STEP);
         }
-        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_sched_barrier(0);
         f32x4 c[2];
-        float z[8], vs[8];
-        float mx = -INFINITY;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             c[t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -182,46 +272,57 @@ __global__ __launch_bounds__(64 * kA8Waves) void attn8_kernel(Attn8Args a) {
             c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(lo[2], lo[3]), qb[1], c[t], 0, 0, 0);
             c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(hi[0], hi[1]), qb[2], c[t], 0, 0, 0);
             c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(hi[2], hi[3]), qb[3], c[t], 0, 0, 0);
-            const f32x4 ks = *reinterpret_cast<const f32x4 *>(&s_sc[wave][0][16 * t + 4 * qq]);
-            const f32x4 vv = *reinterpret_cast<const f32x4 *>(&s_sc[wave][1][16 * t + 4 * qq]);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const bool live = sub < G && c0 + 16 * t + 4 * qq + r < end;
-                z[4 * t + r] = live ? c[t][r] * ks[r] * a.scale_log2 : -INFINITY;
-                vs[4 * t + r] = vv[r];
-                mx = fmaxf(mx, z[4 * t + r]);
-            }
         }
-        mx = quad_max(mx);
-        const float m_new = fmaxf(m_run, mx);
-        const float base = m_new == -INFINITY ? 0.0f : m_new;
-        const float f = __builtin_amdgcn_exp2f(m_run - base);  // m_run = -inf -> 0
-        bf16x8 pa;
-        float sum = 0.0f;
+        float z[E], p[E];
+        spread<F>(c, z);  // this lane's E logits: token slots 16 (part * E >> 2) + 4 qq + ...
+        const float *ksc = &s_sc[wave][0][16 * (part * E >> 2) + 4 * qq + (part * E & 3)];
+        const float *vsc = &s_sc[wave][1][16 * (part * E >> 2) + 4 * qq + (part * E & 3)];
+        float vs[E];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float p = __builtin_amdgcn_exp2f(z[e] - base);
-            sum += p;
-            pa[e] = (__bf16)(p * vs[e]);
+        for (int e = 0; e < E; ++e) {
+            z[e] *= ksc[e];
+            vs[e] = vsc[e];
         }
-        l_run = l_run * f + quad_sum(sum);
-        m_run = m_new;
-        float fr[4];  // of head 4 qq + r
+        if (c0 + kA8Tokens > end)  // uniform: tokens past the end
 #pragma unroll
-        for (int r = 0; r < 4; ++r) fr[r] = __shfl(f, 4 * qq + r);
+            for (int e = 0; e < E; ++e)
+                if (c0 + 16 * (part * E >> 2) + 4 * qq + (part * E & 3) + e >= end) z[e] = -INFINITY;
+        float mx = z[0];
+#pragma unroll
+        for (int e = 1; e < E; ++e) mx = fmaxf(mx, z[e]);
+        mx = fmaxf(m_run, head_max<F>(mx));
+        const float base = mx == -INFINITY ? 0.0f : mx;
+        if (__ballot(mx != m_run)) {  // some head's maximum has grown
+            const float f = __builtin_amdgcn_exp2f(m_run - base);  // m_run = -inf -> 0
+            l_part *= f;
+            float fr[4];  // of head 4 qq + r
+#pragma unroll
+            for (int r = 0; r < 4; ++r) fr[r] = __shfl(f, (4 * qq + r) & (16 / F - 1));
+#pragma unroll
+            for (int d = 0; d < 8; ++d)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[d][r] *= fr[r];
+            m_run = mx;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            p[e] = __builtin_amdgcn_exp2f(z[e] - base);
+            l_part += p[e];
+            p[e] *= vs[e];
+        }
+        const bf16x8 pa = collect<F>(p);
 #pragma unroll
         for (int d = 0; d < 8; ++d) {
             typedef __attribute__((address_space(3))) i32x2 lds2;
             const int j8 = (lane & 15) >> 1;  // token of the 8 that this lane's address names
             const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
                 (lds2 *)&sv[(j8 & 4 ? 12 : 0) + 4 * qq + j8][16 * d + 8 * (lane & 1)]);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[d][r] *= fr[r];
             acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa, widen8((uint32_t)v[0], (uint32_t)v[1]),
                                                              acc[d], 0, 0, 0);
         }
         __builtin_amdgcn_wave_barrier();
     }
+    const float l_run = head_sum<F>(l_part);
     __syncthreads();  // the staged rows become the reduction's
 #pragma unroll
     for (int r = 0; r < 4; ++r)
@@ -233,24 +334,26 @@ __global__ __launch_bounds__(64 * kA8Waves) void attn8_kernel(Attn8Args a) {
         s_ml[wave][sub][1] = l_run;
     }
     __syncthreads();
-    for (int e = tid; e < G * kA8Dim; e += 64 * NW) {
-        const int h = e / kA8Dim, dim = e - h * kA8Dim;
-        float m = s_ml[0][h][0];
+    const size_t h0 = (size_t)row * a.q_heads + g0 * G;
+    for (int e = tid; e < HW * G * kA8Dim; e += 64 * NW) {
+        const int hh = e / kA8Dim, dim = e - hh * kA8Dim;  // head of the workgroup's
+        const int w0 = hh / G, h = hh - w0 * G;            // its first wave, head there
+        float m = s_ml[w0][h][0];
 #pragma unroll
-        for (int w = 1; w < NW; ++w) m = fmaxf(m, s_ml[w][h][0]);
+        for (int w = 1; w < TW; ++w) m = fmaxf(m, s_ml[w * HW + w0][h][0]);
         float l = 0.0f, sum = 0.0f;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            const float mw = s_ml[w][h][0];
+        for (int w = 0; w < TW; ++w) {
+            const float mw = s_ml[w * HW + w0][h][0];
             const float fw = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - m);
-            l = fmaf(fw, s_ml[w][h][1], l);
-            sum = fmaf(fw, s.red[w][e], sum);
+            l = fmaf(fw, s_ml[w * HW + w0][h][1], l);
+            sum = fmaf(fw, s.red[w * HW + w0][h * kA8Dim + dim], sum);
         }
         if (a.splits == 1) {
-            a.out[(rh0 + h) * kA8Dim + dim] = (uint16_t)f32_to_bf16_bits(sum / l);
-            if (a.lse && dim == 0) a.lse[rh0 + h] = (m + log2f(l)) * kA8Ln2;
+            a.out[(h0 + hh) * kA8Dim + dim] = (uint16_t)f32_to_bf16_bits(sum / l);
+            if (a.lse && dim == 0) a.lse[h0 + hh] = (m + log2f(l)) * kA8Ln2;
         } else {
-            const size_t slot = (rh0 + h) * a.splits + split;
+            const size_t slot = (h0 + hh) * a.splits + split;
             a.part_o[slot * kA8Dim + dim] = sum;
             if (dim == 0) {
                 a.part_ml[slot * 2] = m;
@@ -260,45 +363,78 @@ __global__ __launch_bounds__(64 * kA8Waves) void attn8_kernel(Attn8Args a) {
     }
 }
 
-// Splits per (row, KV head): about 512 workgroups, two per CU.
-static void plan_splits8(const Geometry &g, int keys, int &splits, int &span) {
-    const int chunks = div_up(keys, kA8Chunk);
+// How a call is cut: heads and token groups per workgroup, key ranges per row.
+struct Plan8 {
+    int heads, waves;   // KV heads of a workgroup, waves of each
+    int splits, span;   // key ranges per row, keys per range
+};
+// Index lists: kA8ManyUnits (row, KV head) pairs or more take one wave and one range each;
+// fewer are cut into ranges for about one workgroup per CU, three on paged caches, whose
+// gathers wait for the page as well (32 rows of 2048 out of 40960 keys 31.2 us, 35.3
+// with two and 32.6 with three; paged 38.4, 37.0 and 35.1).  Dense: one workgroup per CU
+// reads each byte once; four heads a workgroup, whose 128-byte vectors lie side by side,
+// where that still leaves each 512 keys or more (8 rows of 32768 keys 87 us against 95
+// with one head; 32 rows of 1000 keys 18.6 against 21.6).  Several dense rows per sequence
+// find each other's bytes in the caches: four workgroups per CU (4 x 8 rows of 8192 keys
+// 39.8 us, 52.5 with one).
+static Plan8 plan_splits8(const Geometry &g, int keys, bool dense) {
+    Plan8 p{1, 4, 1, 0};
     const long units = (long)g.rows * g.kv_heads;
-    long want = (512 + units - 1) / units;
+    long target = dense ? (g.n_q == 1 ? 256 : 1024) : (g.page_shift >= 0 ? 768 : 256);
+    if (!dense && units >= kA8ManyUnits) {
+        p.waves = 1;
+        target = 1;
+    } else if (dense && g.n_q == 1 && g.kv_heads % 4 == 0 && units / 4 * (long)keys >= 256L * 512) {
+        p.heads = 4;
+        p.waves = 1;
+    }
+    const int step = p.waves * kA8Tokens, chunk = step < 64 ? 64 : step;
+    const int chunks = div_up(keys, chunk);
+    const long wgs = units / p.heads;
+    long want = (target + wgs - 1) / wgs;
     if (want > chunks) want = chunks;
     if (want > kMaxSplits) want = kMaxSplits;
-    if (want < 1) want = 1;
     const int per = div_up(chunks, (int)want);
-    span = per * kA8Chunk;
-    splits = div_up(chunks, per);
+    p.span = per * chunk;
+    p.splits = div_up(chunks, per);
+    return p;
 }
 
-static size_t partial_floats8(const Geometry &g, int keys) {
-    int splits, span;
-    plan_splits8(g, keys, splits, span);
-    return splits == 1 ? 0 : (size_t)g.rows * g.q_heads * splits * (kA8Dim + 2);
+static size_t partial_floats8(const Geometry &g, int keys, bool dense) {
+    const Plan8 p = plan_splits8(g, keys, dense);
+    return p.splits == 1 ? 0 : (size_t)g.rows * g.q_heads * p.splits * (kA8Dim + 2);
 }
 
-size_t sparse_attn8_floats(const Geometry &g) { return partial_floats8(g, g.top_k); }
+size_t sparse_attn8_floats(const Geometry &g) { return partial_floats8(g, g.top_k, false); }
 
 bool dense8_in_tiles(const Geometry &g) {
-    int splits, span;
-    plan_splits8(g, g.max_len, splits, span);
-    return tile_attn_dense(g, splits);
+    return tile_attn_dense(g, plan_splits8(g, g.max_len, true).splits);
 }
 
 size_t dense_attn8_floats(const Geometry &g) {
-    if (!dense8_in_tiles(g)) return partial_floats8(g, g.max_len);
+    if (!dense8_in_tiles(g)) return partial_floats8(g, g.max_len, true);
     int splits, span;
     tile_attn_plan(g, kMaxSplits, splits, span);
     return splits == 1 ? 0 : (size_t)g.rows * g.q_heads * splits * (kA8Dim + 2);
 }
 
+template <int G, bool DENSE, bool ONCE, int HW, int TW>
+static void launch_form(const Attn8Args &a, bool paged, dim3 grid, hipStream_t stream) {
+    const dim3 wg(64 * HW * TW);
+    if (paged) attn8_kernel<G, true, DENSE, ONCE, HW, TW><<<grid, wg, 0, stream>>>(a);
+    else attn8_kernel<G, false, DENSE, ONCE, HW, TW><<<grid, wg, 0, stream>>>(a);
+}
+
 template <int G, bool DENSE>
-static void launch_g(const Attn8Args &a, bool paged, dim3 grid, hipStream_t stream) {
-    const dim3 wg(64 * kA8Waves);
-    if (paged) attn8_kernel<G, true, DENSE><<<grid, wg, 0, stream>>>(a);
-    else attn8_kernel<G, false, DENSE><<<grid, wg, 0, stream>>>(a);
+static void launch_g(const Attn8Args &a, const Plan8 &p, bool paged, dim3 grid, hipStream_t stream) {
+    if constexpr (DENSE) {
+        if (a.n_q == 1 && p.heads == 4) return launch_form<G, true, true, 4, 1>(a, paged, grid, stream);
+        if (a.n_q == 1) return launch_form<G, true, true, 1, 4>(a, paged, grid, stream);
+    } else {
+        if (p.waves * p.heads == 1) return launch_form<G, false, false, 1, 1>(a, paged, grid, stream);
+    }
+    if (p.heads == 4) return launch_form<G, DENSE, false, 4, 1>(a, paged, grid, stream);
+    launch_form<G, DENSE, false, 1, 4>(a, paged, grid, stream);
 }
 
 template <bool DENSE>
@@ -329,20 +465,22 @@ static hipError_t launch_attn8(const Geometry &g, const Cache8 &c, const void *q
     a.q_heads = g.q_heads;
     a.causal = g.causal;
     a.scale_log2 = g.softmax_scale * kA8Log2e;
-    plan_splits8(g, DENSE ? g.max_len : g.top_k, a.splits, a.span);
+    const Plan8 p = plan_splits8(g, DENSE ? g.max_len : g.top_k, DENSE);
+    a.splits = p.splits;
+    a.span = p.span;
     a.part_o = a.splits > 1 ? partials : nullptr;
     a.part_ml = a.splits > 1 ? partials + (size_t)g.rows * g.q_heads * a.splits * kA8Dim : nullptr;
-    const size_t blocks = (size_t)g.rows * g.kv_heads * a.splits;
+    const size_t blocks = (size_t)g.rows * (g.kv_heads / p.heads) * a.splits;
     if (blocks == 0) return hipSuccess;
     if (blocks > 0x7fffffffull) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)blocks);
     const bool paged = g.page_shift >= 0;
     switch (g.group) {
-        case 1: launch_g<1, DENSE>(a, paged, grid, stream); break;
-        case 2: launch_g<2, DENSE>(a, paged, grid, stream); break;
-        case 4: launch_g<4, DENSE>(a, paged, grid, stream); break;
-        case 5: launch_g<5, DENSE>(a, paged, grid, stream); break;
-        case 8: launch_g<8, DENSE>(a, paged, grid, stream); break;
+        case 1: launch_g<1, DENSE>(a, p, paged, grid, stream); break;
+        case 2: launch_g<2, DENSE>(a, p, paged, grid, stream); break;
+        case 4: launch_g<4, DENSE>(a, p, paged, grid, stream); break;
+        case 5: launch_g<5, DENSE>(a, p, paged, grid, stream); break;
+        case 8: launch_g<8, DENSE>(a, p, paged, grid, stream); break;
         default: return hipErrorInvalidValue;
     }
     const hipError_t e = hipGetLastError();
