@@ -5,13 +5,12 @@
 //
 // The choice is exact: the blocks with the largest I_c, ties to the lowest.  The
 // scores come from the bf16 matrix cores in fp32 (16 rows x 16 blocks a wave,
-// v_mfma_f32_16x16x32_bf16, exact products), beside A = max_c sum_i |q_i kbar_ci| of
-// the row from the same operands without their signs.  256 additions that each err
-// by less than 2^-23 of the running sum leave |s_c - I_c| <= eps = 2^-15 A.  With T
-// the K-th largest score, blocks above T + 2 eps are in, those below T - 2 eps are
-// out, and only if the band between holds more blocks than are left to choose are
-// its scores made again in 64 bits (about one row in ten of 32 out of 2048 blocks,
-// two or three blocks each).
+// v_mfma_f32_16x16x32_bf16, exact products).  256 additions that each err by less than
+// 2^-23 of the sum of magnitudes leave |s_c - I_c| <= 2^-15 sum_i |q_i kbar_ci|, which is
+// at most eps = 2^-15 |q| max_c |kbar_c| (Cauchy-Schwarz).  With T the K-th largest
+// score, blocks above T + 2 eps are in, those below T - 2 eps are out, and only if the
+// band between holds more blocks than are left to choose are its scores made again in
+// 64 bits (about one row in ten of 32 out of 2048 blocks, two or three blocks each).
 //
 // The scoring reads the means once (1 / block of the index keys); a workgroup then
 // chooses a row's blocks, holding their scores in registers, and writes its list.
@@ -29,16 +28,16 @@ constexpr int kBrDim = 256;
 constexpr int kBrTile = 16;        // rows, and blocks, of a scoring tile
 constexpr int kBrWaves = 4;
 constexpr int kBrMostBlocks = kMaxLen / 16;
-constexpr float kBrEps = 0x1p-15f; // error of a score over sum_i |q_i kbar_i|
+constexpr float kBrEps = 0x1p-15f; // error of a score over |q| |kbar|
 
 struct RouteArgs {
     const uint16_t *q_idx, *means;
     const int32_t *page_table, *seq_lens, *q_pos;
-    float *scores;     // [rows, nblk]
-    float *bound;      // [rows, ntile]: largest sum of magnitudes of a tile of blocks
+    float *scores;     // [rows, pitch]
+    float *norm;       // [batch, ntile]: largest |kbar|^2 of a tile of blocks
     int32_t *idx, *n_sel;
     int n_q, max_len, page_shift, max_pages, causal, top_k;
-    int block_shift, nblk, ntile, chunks, row_groups, group_tiles;
+    int block_shift, nblk, pitch, ntile, chunks, row_groups, group_tiles;
 };
 
 template <bool PAGED>
@@ -59,70 +58,79 @@ __device__ __forceinline__ int blocks_before(int n, int block_shift) {
     return n > 0 ? (n - 1) >> block_shift : 0;
 }
 
-// One wave: 16 blocks, held as B operands, against group_tiles tiles of 16 rows.  Lane
-// (grp, sub) supplies row / block sub, dimensions 8 grp + 32 step, and receives rows
-// 4 grp + r of block sub.
+// One workgroup: 64 blocks, each wave 16 of them as B operands, against group_tiles tiles
+// of 16 rows, which pass through LDS (whole 512-byte rows from memory, one tile ahead,
+// double-buffered, one barrier a tile).  Lane (grp, sub) supplies row / block sub,
+// dimensions 8 grp + 32 step, and receives rows 4 grp + r of block sub.
+constexpr int kBrPitch = kBrDim + 8;  // bf16 per staged row
 template <bool PAGED>
 __global__ __launch_bounds__(64 * kBrWaves) void block_scores_kernel(RouteArgs a) {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    __shared__ __align__(16) uint16_t s_q[2][kBrTile][kBrPitch];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int grp = lane >> 4, sub = lane & 15;
-    const int tile = (blockIdx.x % a.chunks) * kBrWaves + wave;
+    const int chunk = blockIdx.x % a.chunks, tile = chunk * kBrWaves + wave;
     int x = blockIdx.x / a.chunks;
     const int first = (x % a.row_groups) * a.group_tiles * kBrTile, b = x / a.row_groups;
     const int end = min(a.n_q, first + a.group_tiles * kBrTile);
     // a causal row sees no more than the sequence's length allows
     const int len = clamp_len(a.seq_lens[b], a.max_len);
     const int most = blocks_before(len, a.block_shift);
-    if (tile * kBrTile >= most) return;
+    if (chunk * kBrWaves * kBrTile >= most) return;  // uniform over the workgroup
     const int c = tile * kBrTile + sub;
-    const u32x4 mag = {0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu};
     u32x4 kv[8];
     {
         const uint16_t *kp = mean_row<PAGED>(a, b, min(c, most - 1)) + 8 * grp;
 #pragma unroll
         for (int s = 0; s < 8; ++s) kv[s] = *reinterpret_cast<const u32x4 *>(kp + 32 * s);
     }
-    // the next tile of rows is in flight during the products of this one
-    u32x4 qn[8];
-    int next = 0;  // blocks that row sub of the next tile sees
+    // staging: thread -> 16-byte piece tid & 31 of rows tid >> 5 and 8 more
+    u32x4 qr[2];
+    int next = 0;  // keys that row sub of the staged tile sees
     auto fetch = [&](int t0) {
-        const int t = min(t0 + sub, a.n_q - 1), row = b * a.n_q + t;
-        const uint16_t *qp = a.q_idx + (size_t)row * kBrDim + 8 * grp;
 #pragma unroll
-        for (int s = 0; s < 8; ++s) qn[s] = *reinterpret_cast<const u32x4 *>(qp + 32 * s);
+        for (int i = 0; i < 2; ++i) {
+            const int t = min(t0 + (tid >> 5) + 8 * i, a.n_q - 1);
+            qr[i] = *reinterpret_cast<const u32x4 *>(a.q_idx + ((size_t)b * a.n_q + t) * kBrDim + 8 * (tid & 31));
+        }
         next = len;
-        if (a.causal) next = min(len, max(a.q_pos[row] + 1, 0));
+        if (a.causal) next = min(len, max(a.q_pos[b * a.n_q + min(t0 + sub, a.n_q - 1)] + 1, 0));
     };
     fetch(first);
-    for (int t0 = first; t0 < end; t0 += kBrTile) {
-        u32x4 qv[8];
+    int buf = 0;
+    for (int t0 = first; t0 < end; t0 += kBrTile, buf ^= 1) {
 #pragma unroll
-        for (int s = 0; s < 8; ++s) qv[s] = qn[s];
+        for (int i = 0; i < 2; ++i)
+            *reinterpret_cast<u32x4 *>(&s_q[buf][(tid >> 5) + 8 * i][8 * (tid & 31)]) = qr[i];
         const int mine = t0 + sub < a.n_q ? blocks_before(next, a.block_shift) : 0;
         if (t0 + kBrTile < end) fetch(t0 + kBrTile);
+        __syncthreads();  // staged; the other buffer's readers were done before they stored here
         if (__ballot(tile * kBrTile < mine) == 0) continue;  // no row sees these blocks
-        f32x4 z = {0.f, 0.f, 0.f, 0.f}, m = {0.f, 0.f, 0.f, 0.f};
+        f32x4 z = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < 8; ++s) {
-            z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, qv[s]),
-                                                        __builtin_bit_cast(bf16x8, kv[s]), z, 0, 0, 0);
-            m = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, qv[s] & mag),
-                                                        __builtin_bit_cast(bf16x8, kv[s] & mag), m, 0, 0, 0);
-        }
+        for (int s = 0; s < 8; ++s)
+            z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(&s_q[buf][sub][8 * grp + 32 * s])),
+                __builtin_bit_cast(bf16x8, kv[s]), z, 0, 0, 0);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int i = 4 * grp + r, own = __shfl(mine, i);
-            const bool seen = c < own;
-            const size_t at = (size_t)b * a.n_q + t0 + i;
-            if (seen) a.scores[at * a.nblk + c] = z[r];
-            // NaN counts as infinite (the maximum would drop it)
-            float w = seen ? (m[r] == m[r] ? m[r] : INFINITY) : 0.0f;
-            w = fmaxf(w, row_partner<8>(w));
-            w = fmaxf(w, row_partner<4>(w));
-            w = fmaxf(w, row_partner<2>(w));
-            w = fmaxf(w, row_partner<1>(w));
-            if (sub == 0 && tile * kBrTile < own) a.bound[at * a.ntile + tile] = w;
+            const int i = 4 * grp + r;
+            if (c < __shfl(mine, i)) a.scores[((size_t)b * a.n_q + t0 + i) * a.pitch + c] = z[r];
         }
+    }
+    if (first == 0 && tile * kBrTile < most) {  // one group of rows says how long the tile's longest mean is
+        float w = 0.0f;
+#pragma unroll
+        for (int s = 0; s < 8; ++s)
+            w = dot8_bf16(make_uint4(kv[s][0], kv[s][1], kv[s][2], kv[s][3]),
+                          make_uint4(kv[s][0], kv[s][1], kv[s][2], kv[s][3]), w);
+        w += __shfl_xor(w, 16);
+        w += __shfl_xor(w, 32);
+        w = w == w ? w : INFINITY;  // the maximum would drop a NaN
+        w = fmaxf(w, row_partner<8>(w));
+        w = fmaxf(w, row_partner<4>(w));
+        w = fmaxf(w, row_partner<2>(w));
+        w = fmaxf(w, row_partner<1>(w));
+        if (lane == 0) a.norm[(size_t)b * a.ntile + tile] = w;
     }
 }
 
@@ -195,7 +203,7 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
     constexpr int NT = 64 * kBrWaves, WORDS = VPL * kBrWaves;
     extern __shared__ __align__(16) char s_dyn[];
     __shared__ int s_slots[2][kBrWaves];
-    __shared__ float s_mag[kBrWaves];
+    __shared__ float2 s_mag[kBrWaves];
     __shared__ uint64_t s_words[WORDS];
     __shared__ uint32_t s_before[kBrWaves][WORDS];
     __shared__ __align__(16) uint32_t s_bins[kBrBins];
@@ -205,13 +213,13 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
     uint16_t *list = reinterpret_cast<uint16_t *>(taken + even_up(div_up(a.nblk, 32)));
     const size_t row = blockIdx.x;
     // the undecided blocks' numbers take the place of the row's scores, which are in registers then
-    uint16_t *number = reinterpret_cast<uint16_t *>(a.scores + row * a.nblk);
+    uint16_t *number = reinterpret_cast<uint16_t *>(a.scores + row * a.pitch);
     const int b = (int)row / a.n_q, tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const uint64_t below = (1ull << lane) - 1;
     uint32_t key[VPL];
     {  // before the row's length is known: those past its blocks are not used
-        const uint32_t *s = reinterpret_cast<const uint32_t *>(a.scores) + row * a.nblk;
+        const uint32_t *s = reinterpret_cast<const uint32_t *>(a.scores) + row * a.pitch;
 #pragma unroll
         for (int i = 0; i < VPL; ++i) key[i] = s[min(NT * i + tid, a.nblk - 1)];
     }
@@ -235,8 +243,10 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
         key[i] = NT * i + tid < own && want > 0 ? score_key(__uint_as_float(key[i])) : 0u;
     if (want > 0) {
         int slot = 0;
-        float mag = 0.0f;
-        for (int i = tid; i < div_up(own, kBrTile); i += NT) mag = fmaxf(mag, a.bound[row * a.ntile + i]);
+        float mag = 0.0f, qn = bf16_lo(a.q_idx[row * kBrDim + tid]);
+        static_assert(NT == kBrDim, "a component of the query per thread");
+        qn *= qn;
+        for (int i = tid; i < div_up(own, kBrTile); i += NT) mag = fmaxf(mag, a.norm[(size_t)b * a.ntile + i]);
         // histograms of the digit at `shift` of the keys that agree with t above it
         uint32_t t = 0u;
         int left = want;
@@ -288,12 +298,16 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
             left -= (int)s_pick[1];
         }
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) mag = fmaxf(mag, __shfl_xor(mag, d));
-        if (lane == 0) s_mag[wave] = mag;
+        for (int d = 1; d < 64; d <<= 1) {
+            mag = fmaxf(mag, __shfl_xor(mag, d));
+            qn += __shfl_xor(qn, d);
+        }
+        if (lane == 0) s_mag[wave] = make_float2(mag, qn);
         __syncthreads();
-        mag = fmaxf(fmaxf(s_mag[0], s_mag[1]), fmaxf(s_mag[2], s_mag[3]));
+        mag = fmaxf(fmaxf(s_mag[0].x, s_mag[1].x), fmaxf(s_mag[2].x, s_mag[3].x));
+        mag = sqrtf(mag) * sqrtf((s_mag[0].y + s_mag[1].y) + (s_mag[2].y + s_mag[3].y));
         const float tf = key_score(t);
-        // 2 eps, the rounding of t +- it, and products that are flushed to zero
+        // 2 eps, the rounding of it and of t +- it, and products that are flushed to zero
         const float eps = 2.1f * kBrEps * mag + 1e-34f;
         lo = score_key(tf - eps);
         hi = score_key(tf + eps);
@@ -399,9 +413,14 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
 
 static size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
+// Floats of a row of scores: an odd number of 256-byte pieces, so that the rows' pieces of
+// one block tile fall on all of an L2's channels (4096 rows of 2048 blocks at 8 KB a row
+// met on two of the sixteen: 40.8 us of scoring, now SCORE_US).
+static int score_pitch(int nblk) { return (div_up(nblk, 64) | 1) * 64; }
+
 size_t block_topk_ws_bytes(const Geometry &g, int block) {
-    const size_t nblk = div_up(g.max_len, block), tiles = div_up((int)nblk, kBrTile);
-    return align256(4 * (size_t)g.rows * nblk) + align256(4 * (size_t)g.rows * tiles);
+    const int nblk = div_up(g.max_len, block), tiles = div_up(nblk, kBrTile);
+    return 4 * (size_t)g.rows * score_pitch(nblk) + align256(4 * (size_t)g.batch * tiles);
 }
 
 template <int VPL, bool PAGED>
@@ -437,6 +456,7 @@ hipError_t launch_block_topk(const Geometry &g, int block, const void *q_idx, co
     a.top_k = g.top_k;
     a.block_shift = __builtin_ctz((unsigned)block);
     a.nblk = div_up(g.max_len, block);
+    a.pitch = score_pitch(a.nblk);
     a.ntile = div_up(a.nblk, kBrTile);
     a.chunks = div_up(a.ntile, kBrWaves);
     // a wave keeps its blocks for up to 8 tiles of rows while that leaves enough workgroups
@@ -446,7 +466,7 @@ hipError_t launch_block_topk(const Geometry &g, int block, const void *q_idx, co
         a.group_tiles *= 2;
     a.row_groups = div_up(tiles, a.group_tiles);
     a.scores = static_cast<float *>(ws);
-    a.bound = reinterpret_cast<float *>(static_cast<char *>(ws) + align256(4 * (size_t)g.rows * a.nblk));
+    a.norm = reinterpret_cast<float *>(static_cast<char *>(ws) + 4 * (size_t)g.rows * a.pitch);
     const size_t blocks = (size_t)g.batch * a.row_groups * a.chunks;
     if (blocks > 0x7fffffffull) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)blocks), wg(64 * kBrWaves);
