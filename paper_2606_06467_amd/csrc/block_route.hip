@@ -134,6 +134,11 @@ __global__ __launch_bounds__(64 * kBrWaves) void block_scores_kernel(RouteArgs a
     }
 }
 
+template <int N>
+struct Int {
+    static constexpr int value = N;
+};
+
 // The float that score_key() maps to a key.
 __device__ __forceinline__ float key_score(uint32_t k) {
     return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
@@ -157,6 +162,58 @@ __device__ __forceinline__ int over_waves(int count, int (*slots)[kBrWaves], int
     return sum;
 }
 
+// Inclusive prefix sum over the wave: DPP row shifts by 1, 2, 4 and 8, then lane 15 of a
+// row to the next row and lane 31 to the upper half.
+__device__ __forceinline__ uint32_t wave_prefix(uint32_t x) {
+    auto add = [&](auto ctrl, auto rows) {
+        x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+    };
+    add(Int<0x111>{}, Int<0xf>{});
+    add(Int<0x112>{}, Int<0xf>{});
+    add(Int<0x114>{}, Int<0xf>{});
+    add(Int<0x118>{}, Int<0xf>{});
+    add(Int<0x142>{}, Int<0xa>{});
+    add(Int<0x143>{}, Int<0xc>{});
+    return x;
+}
+
+// Maximum of m and sum of s over the wave.
+__device__ __forceinline__ void wave_max_sum(float &m, float &s) {
+    m = fmaxf(m, row_partner<8>(m));
+    s += row_partner<8>(s);
+    m = fmaxf(m, row_partner<4>(m));
+    s += row_partner<4>(s);
+    m = fmaxf(m, row_partner<2>(m));
+    s += row_partner<2>(s);
+    m = fmaxf(m, row_partner<1>(m));
+    s += row_partner<1>(s);
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+    m = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    a = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+    m = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    a = __builtin_amdgcn_permlane16_swap(__float_as_uint(s), __float_as_uint(s), false, false);
+    s = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    a = __builtin_amdgcn_permlane32_swap(__float_as_uint(s), __float_as_uint(s), false, false);
+    s = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+
+// Sum over the wave in 64 bits.
+__device__ __forceinline__ double wave_sum64(double x) {
+    auto partner = [](double v, auto ctrl) {
+        const uint64_t u = (uint64_t)__double_as_longlong(v);
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)u, decltype(ctrl)::value, 0xf, 0xf, false);
+        const uint32_t hi = (uint32_t)__builtin_amdgcn_mov_dpp((int)(u >> 32), decltype(ctrl)::value, 0xf, 0xf, false);
+        return __longlong_as_double((long long)(lo | ((uint64_t)hi << 32)));
+    };
+    x += partner(x, Int<0x140>{});
+    x += partner(x, Int<0x141>{});
+    x += partner(x, Int<0x4e>{});
+    x += partner(x, Int<0xb1>{});
+    x += __shfl_xor(x, 16);
+    x += __shfl_xor(x, 32);
+    return x;
+}
+
 // Every wave: words[w] marks blocks 64 w ..+ 64; before[w] of them lie in earlier words.
 // E words, 64-bit; a lane makes PER consecutive ones (every wave the same values).
 template <int E>
@@ -168,13 +225,7 @@ __device__ __forceinline__ void scan_words(const uint64_t *words, uint32_t *befo
         c[i] = lane * PER + i < E ? (uint32_t)__popcll(words[lane * PER + i]) : 0u;
         sum += c[i];
     }
-    uint32_t past = sum;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t o = (uint32_t)__shfl_up((int)past, d);
-        if (lane >= d) past += o;
-    }
-    past -= sum;
+    uint32_t past = wave_prefix(sum) - sum;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         if (lane * PER + i < E) before[lane * PER + i] = past;
@@ -185,19 +236,20 @@ __device__ __forceinline__ void scan_words(const uint64_t *words, uint32_t *befo
     __builtin_amdgcn_wave_barrier();
 }
 
-// LDS of block_choose_kernel past its static part: the undecided blocks' exact scores,
-// the taken ones of them as bits, and the chosen blocks.
+// LDS of block_choose_kernel past its static part: the histogram's bins, whose place the
+// undecided blocks' exact scores take; the query in 64 bits; the taken ones of the
+// undecided as bits; and the chosen blocks.
+constexpr int kBrBins = 2048;
 inline __host__ __device__ int even_up(int x) { return (x + 1) / 2 * 2; }
+inline __host__ __device__ int exact_slots(int nblk) { return nblk > kBrBins / 2 ? nblk : kBrBins / 2; }
 static size_t choose_lds_bytes(int nblk, int chosen) {
-    return (size_t)8 * nblk + 4 * even_up(div_up(nblk, 32)) + 2 * (size_t)chosen;
+    return 8 * (size_t)(exact_slots(nblk) + kBrDim) + 4 * even_up(div_up(nblk, 32)) + 2 * (size_t)chosen;
 }
 
 // One workgroup = one row.  Thread tid holds blocks 256 i + tid (i < VPL) as
 // order-preserving keys in registers.  The want-th largest is found in three histograms
 // in LDS (11, 11 and 10 bits from the top; bit by bit with ballots and a barrier each it
 // took 20000 of the kernel's 36000 cycles, so 6000).
-constexpr int kBrBins = 2048;
-
 template <int VPL, bool PAGED>
 __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_kernel(RouteArgs a) {
     constexpr int NT = 64 * kBrWaves, WORDS = VPL * kBrWaves;
@@ -206,10 +258,11 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
     __shared__ float2 s_mag[kBrWaves];
     __shared__ uint64_t s_words[WORDS];
     __shared__ uint32_t s_before[kBrWaves][WORDS];
-    __shared__ __align__(16) uint32_t s_bins[kBrBins];
     __shared__ uint32_t s_pick[2];
     uint64_t *exact = reinterpret_cast<uint64_t *>(s_dyn);
-    uint32_t *taken = reinterpret_cast<uint32_t *>(exact + a.nblk);
+    uint32_t *s_bins = reinterpret_cast<uint32_t *>(s_dyn);
+    double *q = reinterpret_cast<double *>(exact + exact_slots(a.nblk));
+    uint32_t *taken = reinterpret_cast<uint32_t *>(q + kBrDim);
     uint16_t *list = reinterpret_cast<uint16_t *>(taken + even_up(div_up(a.nblk, 32)));
     const size_t row = blockIdx.x;
     // the undecided blocks' numbers take the place of the row's scores, which are in registers then
@@ -272,15 +325,10 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
                 c[i] = v.x, c[i + 1] = v.y, c[i + 2] = v.z, c[i + 3] = v.w;
                 sum += (v.x + v.y) + (v.z + v.w);
             }
-            uint32_t past = sum;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const uint32_t o = (uint32_t)__shfl_down((int)past, d);
-                if (lane + d < 64) past += o;
-            }
-            if (lane == 0) s_slots[slot][wave] = (int)past;
+            const uint32_t upto = wave_prefix(sum), total = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+            if (lane == 0) s_slots[slot][wave] = (int)total;
             __syncthreads();
-            uint32_t higher = past - sum;
+            uint32_t higher = total - upto;
             for (int w = wave + 1; w < kBrWaves; ++w) higher += (uint32_t)s_slots[slot][w];
             slot ^= 1;
             if (higher < (uint32_t)left && higher + sum >= (uint32_t)left) {  // one thread
@@ -297,11 +345,7 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
             t = pass == 0 ? s_pick[0] : (t << width) | s_pick[0];
             left -= (int)s_pick[1];
         }
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            mag = fmaxf(mag, __shfl_xor(mag, d));
-            qn += __shfl_xor(qn, d);
-        }
+        wave_max_sum(mag, qn);
         if (lane == 0) s_mag[wave] = make_float2(mag, qn);
         __syncthreads();
         mag = fmaxf(fmaxf(s_mag[0].x, s_mag[1].x), fmaxf(s_mag[2].x, s_mag[3].x));
@@ -326,8 +370,6 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
         some = within > want;
         if (some) {  // uniform: exact scores decide
             scan_words<WORDS>(s_words, s_before[wave], lane);
-            double *q = reinterpret_cast<double *>(s_bins);
-            static_assert(sizeof(double) * kBrDim <= sizeof s_bins, "the query fits the bins");
             q[tid] = (double)__uint_as_float((uint32_t)a.q_idx[row * kBrDim + tid] << 16);
             for (int w = tid; w < div_up(own, 32); w += NT) taken[w] = 0u;
 #pragma unroll
@@ -337,19 +379,16 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
                     number[s_before[wave][i * kBrWaves + wave] + __popcll(band & below)] = (uint16_t)(NT * i + tid);
             }
             __syncthreads();
-            for (int p = tid; p < within; p += NT) {
-                const uint16_t *kp = mean_row<PAGED>(a, b, number[p]);
-                double sum = 0.0;
-#pragma unroll 8
-                for (int e = 0; e < kBrDim; e += 8) {
-                    const u32x4 v = *reinterpret_cast<const u32x4 *>(kp + e);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        sum = fma(q[e + 2 * j], (double)bf16_lo(v[j]), sum);
-                        sum = fma(q[e + 2 * j + 1], (double)bf16_hi(v[j]), sum);
-                    }
-                }
-                exact[p] = score_key64(sum);
+            // a wave per undecided block: lane holds dimensions 4 lane ..+ 4 (a thread per block,
+            // its 256 additions one after another, took 13500 cycles for two or three blocks)
+            for (int p = wave; p < within; p += kBrWaves) {
+                const uint2 v = *reinterpret_cast<const uint2 *>(mean_row<PAGED>(a, b, number[p]) + 4 * lane);
+                double sum = q[4 * lane] * (double)bf16_lo(v.x);
+                sum = fma(q[4 * lane + 1], (double)bf16_hi(v.x), sum);
+                sum = fma(q[4 * lane + 2], (double)bf16_lo(v.y), sum);
+                sum = fma(q[4 * lane + 3], (double)bf16_hi(v.y), sum);
+                sum = wave_sum64(sum);
+                if (lane == 0) exact[p] = score_key64(sum);
             }
             __syncthreads();
             if (within <= NT) {  // each counts those that go before it
