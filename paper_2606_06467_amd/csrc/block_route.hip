@@ -247,9 +247,11 @@ static size_t choose_lds_bytes(int nblk, int chosen) {
 }
 
 // One workgroup = one row.  Thread tid holds blocks 256 i + tid (i < VPL) as
-// order-preserving keys in registers.  The want-th largest is found in three histograms
-// in LDS (11, 11 and 10 bits from the top; bit by bit with ballots and a barrier each it
-// took 20000 of the kernel's 36000 cycles, so 6000).
+// order-preserving keys in registers.  The want-th largest is found by a histogram in LDS
+// of the top 11 bits (bins of a quarter octave: some thirty of 2048 scores share the
+// wanted one) and a count of each such key against the others, or, where more than 256
+// keys share it, by two more histograms.  (Bit by bit with ballots and a barrier each
+// it took 20000 of the kernel's 36000 cycles, with three histograms 7500 of 17500.)
 template <int VPL, bool PAGED>
 __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_kernel(RouteArgs a) {
     constexpr int NT = 64 * kBrWaves, WORDS = VPL * kBrWaves;
@@ -258,7 +260,7 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
     __shared__ float2 s_mag[kBrWaves];
     __shared__ uint64_t s_words[WORDS];
     __shared__ uint32_t s_before[kBrWaves][WORDS];
-    __shared__ uint32_t s_pick[2];
+    __shared__ uint32_t s_pick[4];  // the digit, keys above it, keys with it, a counter of these
     uint64_t *exact = reinterpret_cast<uint64_t *>(s_dyn);
     uint32_t *s_bins = reinterpret_cast<uint32_t *>(s_dyn);
     double *q = reinterpret_cast<double *>(exact + exact_slots(a.nblk));
@@ -337,6 +339,8 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
                     if (higher < (uint32_t)left && higher + c[i] >= (uint32_t)left) {
                         s_pick[0] = (uint32_t)(PER * tid + i);
                         s_pick[1] = higher;
+                        s_pick[2] = c[i];
+                        s_pick[3] = 0u;
                     }
                     higher += c[i];
                 }
@@ -344,6 +348,24 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
             __syncthreads();
             t = pass == 0 ? s_pick[0] : (t << width) | s_pick[0];
             left -= (int)s_pick[1];
+            if (pass == 0 && s_pick[2] <= NT) {  // uniform: few keys share the digit; they rank each other
+                uint32_t *few = s_bins;          // (every wave has read its bins)
+                const int m = (int)s_pick[2];
+#pragma unroll
+                for (int i = 0; i < VPL; ++i)
+                    if (NT * i + tid < own && (key[i] >> shift) == t) few[atomicAdd(&s_pick[3], 1u)] = key[i];
+                __syncthreads();
+                const uint32_t k = tid < m ? few[tid] : 0u;
+                int over = 0, same = 0;
+                for (int j = 0; j < m; ++j) {
+                    over += few[j] > k ? 1 : 0;
+                    same += few[j] == k ? 1 : 0;
+                }
+                if (tid < m && over < left && over + same >= left) s_pick[0] = k;  // equal ones: the same value
+                __syncthreads();
+                t = s_pick[0];
+                break;
+            }
         }
         wave_max_sum(mag, qn);
         if (lane == 0) s_mag[wave] = make_float2(mag, qn);
