@@ -368,25 +368,40 @@ struct Plan8 {
     int heads, waves;   // KV heads of a workgroup, waves of each
     int splits, span;   // key ranges per row, keys per range
 };
-// Index lists: kA8ManyUnits (row, KV head) pairs or more take one wave and one range each;
-// fewer are cut into ranges for about one workgroup per CU, three on paged caches, whose
-// gathers wait for the page as well (32 rows of 2048 out of 40960 keys 31.2 us, 35.3
-// with two and 32.6 with three; paged 38.4, 37.0 and 35.1).  Dense: one workgroup per CU
-// reads each byte once; four heads a workgroup, whose 128-byte vectors lie side by side,
-// where that still leaves each 512 keys or more (8 rows of 32768 keys 87 us against 95
-// with one head; 32 rows of 1000 keys 18.6 against 21.6).  Several dense rows per sequence
-// find each other's bytes in the caches: four workgroups per CU (4 x 8 rows of 8192 keys
-// 39.8 us, 52.5 with one).
+// Index lists: kA8ManyUnits (row, KV head) pairs or more take one wave and one range each
+// (800 pairs of 2048 keys 57 us against 66 in workgroups of four waves, 512 pairs 52
+// against 41).  Fewer are cut into ranges for one workgroup per CU: four waves, or on
+// paged caches, whose gathers wait for the page as well, eight (ragged 32 rows of 2048
+// out of 65536 keys, 64-token pages, 35.2 us against 38.8; contiguous 32.3 against 31.0).
+// Up to 512 keys make one range of eight waves, without a second launch to join ranges
+// (8 pairs of 512 keys 6.2 us against 6.5).
+// Dense, one row per sequence: a workgroup per CU reads each byte once, two on paged
+// caches (32 sequences of up to 2048 keys 24.7 us against 32.4); four heads a workgroup,
+// whose 128-byte vectors lie side by side, where that leaves each 512 keys or more (8
+// sequences of 32768 keys 87 us against 95 with one head; 32 of 1000 keys 21.6 against
+// 18.6).  Several rows per sequence find each other's bytes in the caches: four workgroups
+// per CU (4 x 8 rows of 8192 keys 39.8 us, 52.5 with one).
 static Plan8 plan_splits8(const Geometry &g, int keys, bool dense) {
     Plan8 p{1, 4, 1, 0};
     const long units = (long)g.rows * g.kv_heads;
-    long target = dense ? (g.n_q == 1 ? 256 : 1024) : (g.page_shift >= 0 ? 768 : 256);
+    const bool paged = g.page_shift >= 0;
+    long target = 256;
     if (!dense && units >= kA8ManyUnits) {
         p.waves = 1;
         target = 1;
-    } else if (dense && g.n_q == 1 && g.kv_heads % 4 == 0 && units / 4 * (long)keys >= 256L * 512) {
-        p.heads = 4;
-        p.waves = 1;
+    } else if (keys <= 512) {
+        p.waves = 8;
+        target = 1;
+    } else if (!dense) {
+        if (paged) p.waves = 8;
+    } else if (g.n_q > 1) {
+        target = 1024;
+    } else {
+        if (paged) target = 512;
+        if (g.kv_heads % 4 == 0 && units / 4 * (long)keys >= 256L * 512) {
+            p.heads = 4;
+            p.waves = 1;
+        }
     }
     const int step = p.waves * kA8Tokens, chunk = step < 64 ? 64 : step;
     const int chunks = div_up(keys, chunk);
@@ -428,12 +443,12 @@ static void launch_form(const Attn8Args &a, bool paged, dim3 grid, hipStream_t s
 template <int G, bool DENSE>
 static void launch_g(const Attn8Args &a, const Plan8 &p, bool paged, dim3 grid, hipStream_t stream) {
     if constexpr (DENSE) {
-        if (a.n_q == 1 && p.heads == 4) return launch_form<G, true, true, 4, 1>(a, paged, grid, stream);
-        if (a.n_q == 1) return launch_form<G, true, true, 1, 4>(a, paged, grid, stream);
+        if (p.heads == 4) return launch_form<G, true, true, 4, 1>(a, paged, grid, stream);
+        if (a.n_q == 1 && p.waves == 4) return launch_form<G, true, true, 1, 4>(a, paged, grid, stream);
     } else {
-        if (p.waves * p.heads == 1) return launch_form<G, false, false, 1, 1>(a, paged, grid, stream);
+        if (p.waves == 1) return launch_form<G, false, false, 1, 1>(a, paged, grid, stream);
     }
-    if (p.heads == 4) return launch_form<G, DENSE, false, 4, 1>(a, paged, grid, stream);
+    if (p.waves == 8) return launch_form<G, DENSE, false, 1, 8>(a, paged, grid, stream);
     launch_form<G, DENSE, false, 1, 4>(a, paged, grid, stream);
 }
 
