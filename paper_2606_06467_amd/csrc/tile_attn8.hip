@@ -13,13 +13,14 @@ struct Tile8Vec {
     float scale;
 };
 struct Tile8Raw {
-    u32x2 bytes;
+    u32x4 bytes;
     float scale;
 };
 
 struct TileE4m3 {
     typedef Tile8Vec Vec;
     typedef Tile8Raw Raw;
+    static constexpr int kDims = 16;
     template <bool PAGED>
     static __device__ __forceinline__ Vec vec(const TileAttnArgs &a, bool values, int b, int j,
                                               size_t tok, int g) {
@@ -29,17 +30,24 @@ struct TileE4m3 {
         return {static_cast<const uint8_t *>(values ? a.v : a.k) + (tok * a.kv_heads + g) * kTaDim,
                 (values ? a.v_scale : a.k_scale)[srow * a.kv_heads + g]};
     }
-    static __device__ __forceinline__ Raw eight(Vec v, int dim) {
-        return {*reinterpret_cast<const u32x2 *>(v.p + dim), v.scale};
+    static __device__ __forceinline__ Raw load(Vec v, int dim) {
+        return {*reinterpret_cast<const u32x4 *>(v.p + dim), v.scale};
     }
     static __device__ __forceinline__ uint32_t two(uint32_t w, float scale, bool high) {
         const bf16x2 x = high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true)
                               : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false);
         return __builtin_bit_cast(uint32_t, x);
     }
-    static __device__ __forceinline__ u32x4 widen(Raw x) {
-        return u32x4{two(x.bytes[0], x.scale, false), two(x.bytes[0], x.scale, true),
-                     two(x.bytes[1], x.scale, false), two(x.bytes[1], x.scale, true)};
+    static __device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi, float scale) {
+        return u32x4{two(lo, scale, false), two(lo, scale, true), two(hi, scale, false), two(hi, scale, true)};
+    }
+    static __device__ __forceinline__ void put(uint16_t *dst, Raw x) {
+        *reinterpret_cast<u32x4 *>(dst) = widen(x.bytes[0], x.bytes[1], x.scale);
+        *reinterpret_cast<u32x4 *>(dst + 8) = widen(x.bytes[2], x.bytes[3], x.scale);
+    }
+    static __device__ __forceinline__ u32x4 eight(Vec v, int dim) {
+        const u32x2 w = *reinterpret_cast<const u32x2 *>(v.p + dim);
+        return widen(w[0], w[1], v.scale);
     }
     static __device__ __forceinline__ u32x2 four(Vec v, int dim) {
         const uint32_t w = *reinterpret_cast<const uint32_t *>(v.p + dim);

@@ -67,19 +67,21 @@ __device__ __forceinline__ int wave_min_i(int x) {
     return x;
 }
 
-// How the kernel reads a cache.  Vec: a token's 128 values of one KV head; Raw: eight
-// of them as loaded; widen: those as bf16.
+// How the kernel reads a cache.  Vec: a token's 128 values of one KV head.  Staging: Raw is
+// kDims of them as loaded by one thread, put() stores them as bf16.  eight, four: as bf16.
 struct TileBf16 {
     typedef const uint16_t *Vec;
     typedef u32x4 Raw;
+    static constexpr int kDims = 8;
     template <bool PAGED>  // token j of sequence b, the cache's row tok
     static __device__ __forceinline__ Vec vec(const TileAttnArgs &a, bool values, int, int, size_t tok, int g) {
         return static_cast<const uint16_t *>(values ? a.v : a.k) + (tok * a.kv_heads + g) * kTaDim;
     }
-    static __device__ __forceinline__ Raw eight(Vec p, int dim) {
+    static __device__ __forceinline__ Raw load(Vec p, int dim) {
         return *reinterpret_cast<const u32x4 *>(p + dim);
     }
-    static __device__ __forceinline__ u32x4 widen(Raw x) { return x; }
+    static __device__ __forceinline__ void put(uint16_t *dst, Raw x) { *reinterpret_cast<u32x4 *>(dst) = x; }
+    static __device__ __forceinline__ u32x4 eight(Vec p, int dim) { return load(p, dim); }
     static __device__ __forceinline__ u32x2 four(Vec p, int dim) {
         return *reinterpret_cast<const u32x2 *>(p + dim);
     }
@@ -89,7 +91,9 @@ template <class Cache, int NW, bool PAGED, bool MASK>
 __global__ __launch_bounds__(64 * NW, 2) void tile_attn_kernel(TileAttnArgs a) {
     typedef typename Cache::Raw Raw;
     constexpr int NT = 64 * NW;
-    constexpr int PER = kTaKeys * kTaDim / 8 / NT;  // 16-byte pieces of a tile per thread
+    constexpr int PIECES = kTaDim / Cache::kDims;         // of a row
+    constexpr int ROWS = NT / PIECES;                     // that the workgroup stages at a time
+    constexpr int PER = kTaKeys / ROWS;                   // pieces of a tile per thread
     __shared__ __align__(16) uint16_t s_k[2][kTaKeys][kTaKPitch];
     __shared__ __align__(16) uint16_t s_v[2][kTaKeys][kTaVPitch];
     __shared__ int s_lim[NW];
@@ -139,9 +143,9 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_attn_kernel(TileAttnArgs a) {
         for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
     float m = -INFINITY, top = -INFINITY, l = 0.0f;  // base of o, maximum so far (base of l)
 
-    // staging: thread -> 16-byte piece (tid & 15) of key rows (tid >> 4) + i * NT / 16;
-    // keys past len are clamped (and masked)
-    const int srow = tid >> 4, spc = (tid & 15) * 8;
+    // staging: thread -> piece tid % PIECES of key rows tid / PIECES + i * ROWS; keys past
+    // len are clamped (and masked)
+    const int srow = tid / PIECES, spc = (tid % PIECES) * Cache::kDims;
     auto vector_at = [&](bool values, int j) {  // key or value j (at most the last)
         j = min(j, len - 1);
         size_t tok;
@@ -156,17 +160,17 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_attn_kernel(TileAttnArgs a) {
     auto fetch = [&](bool values, int j0, Raw (&v)[PER]) {
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-            v[i] = Cache::eight(vector_at(values, j0 + srow + i * (NT / 16)), spc);
+            v[i] = Cache::load(vector_at(values, j0 + srow + i * ROWS), spc);
     };
     auto stage_k = [&](int buf, const Raw (&v)[PER]) {
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-            *reinterpret_cast<u32x4 *>(&s_k[buf][srow + i * (NT / 16)][spc]) = Cache::widen(v[i]);
+            Cache::put(&s_k[buf][srow + i * ROWS][spc], v[i]);
     };
     auto stage_v = [&](int buf, const Raw (&v)[PER]) {
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-            *reinterpret_cast<u32x4 *>(&s_v[buf][srow + i * (NT / 16)][spc]) = Cache::widen(v[i]);
+            Cache::put(&s_v[buf][srow + i * ROWS][spc], v[i]);
     };
     // transposing V reads: lane i of a 16-lane group q reads row 4 hi + (i >> 2),
     // columns 16 (q & 1) + 4 (i & 3) .. + 4, and receives column i of the 4 x 16 block
@@ -367,7 +371,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_attn_kernel(TileAttnArgs a) {
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks)
                     s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        __builtin_bit_cast(bf16x8, Cache::widen(Cache::eight(kp, 16 * ks + 8 * hi))), qb[ks],
+                        __builtin_bit_cast(bf16x8, Cache::eight(kp, 16 * ks + 8 * hi)), qb[ks],
                         s[kt], 0, 0, 0);
             }
             const uint2 w = MASK ? words(j0) : make_uint2(0u, 0u);
@@ -382,7 +386,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tile_attn_kernel(TileAttnArgs a) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int r = 4 * i + (lane >> 4);
-                    u32x4 x = Cache::widen(Cache::eight(vector_at(true, j0 + 32 * kt + r), (lane & 15) * 8));
+                    u32x4 x = Cache::eight(vector_at(true, j0 + 32 * kt + r), (lane & 15) * 8);
                     bool some = false;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
