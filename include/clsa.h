@@ -114,7 +114,8 @@ typedef enum {
     CLSA_OP_KD_LOSS = 6,   /* clsa_kd_loss */
     CLSA_OP_ATTN8 = 7,     /* clsa_sparse_attn8 */
     CLSA_OP_DENSE8 = 8,    /* clsa_dense_attn8 */
-    CLSA_OP_BLOCK_TOPK = 9 /* clsa_block_topk (n_layers: the block)  */
+    CLSA_OP_BLOCK_TOPK = 9, /* clsa_block_topk (n_layers: the block)  */
+    CLSA_OP_PROJECT8 = 10  /* clsa_project_append8 */
 } clsa_op;
 
 typedef struct clsa_shape {
@@ -319,6 +320,17 @@ clsa_status clsa_cache_append8(const clsa_shape *shape, int32_t block, const voi
                                const int32_t *start, const int32_t *count,
                                const int32_t *page_table, void *k8, void *v8, float *k_scale,
                                float *v_scale, void *stream);
+
+/* clsa_project_append into an 8-bit cache: the projections of h with the same w, the
+ * index queries of every row to q_idx, and of rows 0 .. count[b]-1 of sequence b the
+ * index keys to positions start[b] .. of k_idx and K and V, rounded to bf16, to the
+ * cache as clsa_cache_append8 does it (with its conditions and errors).  Workspace:
+ * CLSA_OP_PROJECT8. */
+clsa_status clsa_project_append8(const clsa_shape *shape, int32_t block, int32_t d_model,
+                                 const void *h, const void *w, const int32_t *start,
+                                 const int32_t *count, const int32_t *page_table, void *q_idx,
+                                 void *k_idx, void *k8, void *v8, float *k_scale, float *v_scale,
+                                 void *ws, size_t ws_bytes, void *stream);
 
 /* clsa_sparse_attn over the 8-bit cache: the same index lists (of clsa_topk or
  * clsa_block_topk), outputs, conventions and errors.  Logits, softmax and sums in

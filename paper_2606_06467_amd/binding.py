@@ -36,6 +36,7 @@ CLSA_OP_KD_LOSS = 6
 CLSA_OP_ATTN8 = 7
 CLSA_OP_DENSE8 = 8
 CLSA_OP_BLOCK_TOPK = 9
+CLSA_OP_PROJECT8 = 10
 
 
 class ClsaError(RuntimeError):
@@ -93,6 +94,7 @@ def lib() -> ctypes.CDLL:
         "clsa_kd_target": (i32, [SP, i32, P, P, P, P, P, P, P, P, sz, P]),
         "clsa_kd_loss": (i32, [SP, P, P, P, P, P, P, P, P, P, P, sz, P]),
         "clsa_cache_append8": (i32, [SP, i32, P, P, P, P, P, P, P, P, P, P]),
+        "clsa_project_append8": (i32, [SP, i32, i32, P, P, P, P, P, P, P, P, P, P, P, P, sz, P]),
         "clsa_sparse_attn8": (i32, [SP, i32, P, P, P, P, P, P, P, P, P, P, P, sz, P]),
         "clsa_dense_attn8": (i32, [SP, i32, P, P, P, P, P, P, P, P, P, P, P, sz, P]),
         "clsa_block_means": (i32, [SP, i32, P, P, P, P, P, P]),
@@ -242,9 +244,9 @@ def clsa_kd_loss(shape, abar, q_idx, k_idx, page_table, seq_lens, q_pos, loss, d
                               _ptr(ws, "ws"), wsb, _stream(stream)), "clsa_kd_loss")
 
 
-def _call(where, shape, block, args, ws, stream):
-    """An entry point of the 8-bit cache or of block routing: (name, tensor) arguments, and its
-    workspace (False: it takes none).  The call runs on the tensors' device; their stream is the
+def _call(where, shape, block, args, ws, stream, sizes=()):
+    """An entry point of the 8-bit cache or of block routing: numbers after the block, (name,
+    tensor) arguments, and its workspace (False: it takes none).  The call runs on the tensors' device; their stream is the
     current one of that device unless one is given."""
     ptrs, device = [], -1
     for name, t in args if not isinstance(ws, torch.Tensor) else (*args, ("ws", ws)):
@@ -269,10 +271,10 @@ def _call(where, shape, block, args, ws, stream):
         ptrs.append(ws.numel() * ws.element_size())
     if device >= 0 and device != torch.cuda.current_device():
         with torch.cuda.device(device):
-            return _call(where, shape, block, args, ws, stream)
+            return _call(where, shape, block, args, ws, stream, sizes)
     # the raw handle: a torch Stream object costs 3 us, a quarter of a whole call
     raw = torch._C._cuda_getCurrentRawStream(max(device, 0)) if stream is None else stream.cuda_stream
-    _check(getattr(lib(), where)(ctypes.byref(shape), block, *ptrs, raw), where)
+    _check(getattr(lib(), where)(ctypes.byref(shape), block, *sizes, *ptrs, raw), where)
 
 
 def clsa_cache_append8(shape, block, k, v, start, count, page_table, k8, v8, k_scale, v_scale,
@@ -280,6 +282,14 @@ def clsa_cache_append8(shape, block, k, v, start, count, page_table, k8, v8, k_s
     _call("clsa_cache_append8", shape, block,
           (("k", k), ("v", v), ("start", start), ("count", count), ("page_table", page_table),
            ("k8", k8), ("v8", v8), ("k_scale", k_scale), ("v_scale", v_scale)), False, stream)
+
+
+def clsa_project_append8(shape, block, d_model, h, w, start, count, page_table, q_idx, k_idx, k8, v8,
+                         k_scale, v_scale, ws=None, stream=None):
+    _call("clsa_project_append8", shape, block,
+          (("h", h), ("w", w), ("start", start), ("count", count), ("page_table", page_table),
+           ("q_idx", q_idx), ("k_idx", k_idx), ("k8", k8), ("v8", v8), ("k_scale", k_scale),
+           ("v_scale", v_scale)), ws, stream, (d_model,))
 
 
 def clsa_sparse_attn8(shape, block, q, k8, v8, k_scale, v_scale, page_table, idx, n_sel, out,

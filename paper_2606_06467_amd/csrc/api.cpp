@@ -232,6 +232,11 @@ size_t attn_ws_bytes(const Geometry &g, bool dense = false) {
     return c.off;
 }
 
+// K (or V) rows of the new tokens between projection and append.
+size_t project8_row_bytes(const Geometry &g) {
+    return align_up(sizeof(uint16_t) * 128 * (size_t)g.rows * g.kv_heads);
+}
+
 size_t floats_ws_bytes(size_t floats) { return align_up(sizeof(float) * floats); }
 
 clsa_status check_cache8(const void *k8, const void *v8, const float *k_scale, const float *v_scale) {
@@ -282,6 +287,9 @@ size_t clsa_workspace_bytes(const clsa_shape *shape, int32_t op, int32_t n_layer
         case CLSA_OP_DENSE8:
             if (check_shape(shape, kAttn | kDense, &g) != CLSA_OK) return 0;
             return floats_ws_bytes(clsa::dense_attn8_floats(g));
+        case CLSA_OP_PROJECT8:
+            if (check_shape(shape, kIndex | kAttn, &g) != CLSA_OK) return 0;
+            return 2 * project8_row_bytes(g);
         case CLSA_OP_BLOCK_TOPK:  // n_layers: the block
             if (check_shape(shape, kIndex | kTopk, &g) != CLSA_OK ||
                 check_block(shape, n_layers) != CLSA_OK || g.top_k % n_layers != 0)
@@ -642,6 +650,33 @@ clsa_status clsa_cache_append8(const clsa_shape *shape, int32_t block, const voi
     CLSA_TRY(check_common(shape, page_table, nullptr, false, true));
     return from_hip(clsa::launch_append8(g, block, k, v, start, count, page_table, k8, v8, k_scale,
                                          v_scale, static_cast<hipStream_t>(stream)));
+}
+
+clsa_status clsa_project_append8(const clsa_shape *shape, int32_t block, int32_t d_model,
+                                 const void *h, const void *w, const int32_t *start,
+                                 const int32_t *count, const int32_t *page_table, void *q_idx,
+                                 void *k_idx, void *k8, void *v8, float *k_scale, float *v_scale,
+                                 void *ws, size_t ws_bytes, void *stream) {
+    Geometry g;
+    CLSA_TRY(check_shape(shape, kIndex | kAttn, &g));
+    CLSA_TRY(check_block(shape, block));
+    if (d_model < 1) return CLSA_ERR_INVALID_ARG;
+    if (!clsa::project_supported(d_model)) return CLSA_ERR_UNSUPPORTED;
+    CLSA_TRY(check_ptr(h, 16));
+    CLSA_TRY(check_ptr(w, 16));
+    CLSA_TRY(check_ptr(start, 4));
+    CLSA_TRY(check_ptr(count, 4));
+    CLSA_TRY(check_ptr(q_idx, 16));
+    CLSA_TRY(check_ptr(k_idx, 16));
+    CLSA_TRY(check_cache8(k8, v8, k_scale, v_scale));
+    CLSA_TRY(check_common(shape, page_table, nullptr, false, true));
+    if (!ws || ws_bytes < 2 * project8_row_bytes(g) || !aligned(ws, kAlign)) return CLSA_ERR_WORKSPACE;
+    char *k = static_cast<char *>(ws), *v = k + project8_row_bytes(g);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    CLSA_TRY(from_hip(clsa::launch_project_rows(g, d_model, h, w, start, count, page_table, q_idx,
+                                                k_idx, k, v, st)));
+    return from_hip(clsa::launch_append8(g, block, k, v, start, count, page_table, k8, v8, k_scale,
+                                         v_scale, st));
 }
 
 clsa_status clsa_sparse_attn8(const clsa_shape *shape, int32_t block, const void *q, const void *k8,

@@ -266,6 +266,13 @@ hipError_t launch_project(const Geometry &g, int d_model, const void *h, const v
                           const int32_t *pos, const int32_t *page_table, void *q_idx,
                           void *k_idx, void *k_cache, void *v_cache, hipStream_t stream);
 
+// The same with positions start[b] + t for t < count[b], and K and V left as rows
+// [rows, kv_heads, 128] instead of going to a cache.
+hipError_t launch_project_rows(const Geometry &g, int d_model, const void *h, const void *w,
+                               const int32_t *start, const int32_t *count,
+                               const int32_t *page_table, void *q_idx, void *k_idx, void *k_rows,
+                               void *v_rows, hipStream_t stream);
+
 // ---- kd.hip ----
 // Eq. 5 target: lse2 workspace of kd_target_ws_floats floats; lse_in, if not
 // null, holds the natural-log log-sum-exp of every (layer, row, query head)

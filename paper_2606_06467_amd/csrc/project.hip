@@ -42,17 +42,26 @@ constexpr int kSplitMaxRows = 128;
 struct ProjArgs {
     const uint16_t *h;         // [rows, d]
     const uint16_t *w;         // [n_feat, d]
-    const int32_t *pos;        // [rows]
+    const int32_t *pos;        // [rows], or null: rows 0 .. count[b]-1 of sequence b go to start[b] ..
+    const int32_t *start, *count;
     const int32_t *page_table;
     uint16_t *q_idx;           // [rows, 256]
     uint16_t *k_idx;           // index-key cache
     uint16_t *k_cache, *v_cache;
+    bool kv_rows;              // K and V stay in the rows' own order: [rows, kvw]
     int rows, d, n_q, max_len, page_shift, max_pages, kvw;  // kvw = kv_heads * 128
     int rtiles, ftiles, band;  // tiled kernel: 128-row and 128-feature tiles, row tiles per band
 };
 
 __device__ __forceinline__ bf16x8 ld8(const uint16_t *p) {
     return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(p));
+}
+
+// Position of row r of sequence b, negative for a row that has none.
+__device__ __forceinline__ int row_position(const ProjArgs &a, int b, int r) {
+    if (a.pos) return a.pos[r];
+    const int t = r - b * a.n_q, s = a.start[b];
+    return t < a.count[b] && s >= 0 && s <= a.max_len - 1 - t ? s + t : -1;
 }
 
 // Writes output feature f of row r (rows past the end are dropped; cache rows
@@ -65,15 +74,19 @@ __device__ __forceinline__ void store_feature(const ProjArgs &a, int r, int f, f
         a.q_idx[(size_t)r * 256 + f] = bits;
         return;
     }
-    const int p = a.pos[r];
-    if (p < 0 || p >= a.max_len) return;
     const int b = r / a.n_q;
     size_t row;
-    if (PAGED) {
-        const int page = a.page_table[(size_t)b * a.max_pages + (p >> a.page_shift)];
-        row = ((size_t)page << a.page_shift) + (p & ((1 << a.page_shift) - 1));
+    if (a.kv_rows && f >= 512) {  // uniform for a workgroup's features
+        row = r;
     } else {
-        row = (size_t)b * a.max_len + p;
+        const int p = row_position(a, b, r);
+        if (p < 0 || p >= a.max_len) return;
+        if (PAGED) {
+            const int page = a.page_table[(size_t)b * a.max_pages + (p >> a.page_shift)];
+            row = ((size_t)page << a.page_shift) + (p & ((1 << a.page_shift) - 1));
+        } else {
+            row = (size_t)b * a.max_len + p;
+        }
     }
     if (f < 512) a.k_idx[row * 256 + (f - 256)] = bits;
     else if (f < 512 + a.kvw) a.k_cache[row * a.kvw + (f - 512)] = bits;
@@ -273,10 +286,12 @@ __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
         uint16_t *dst;
         if (dst_kind == 0) {
             dst = a.q_idx + (size_t)r * 256;
+        } else if (a.kv_rows && dst_kind >= 2) {
+            dst = (dst_kind == 2 ? a.k_cache : a.v_cache) + (size_t)r * width;
         } else {
-            const int p = a.pos[r];
-            if (p < 0 || p >= a.max_len) continue;
             const int b = r / a.n_q;
+            const int p = row_position(a, b, r);
+            if (p < 0 || p >= a.max_len) continue;
             size_t row;
             if (PAGED) {
                 const int page = a.page_table[(size_t)b * a.max_pages + (p >> a.page_shift)];
@@ -309,14 +324,13 @@ static void launch_splitk(const ProjArgs &a, bool paged, int n_feat, hipStream_t
     else project_splitk_kernel<KS, NB, 1, false><<<grid, block, 0, stream>>>(a);
 }
 
-hipError_t launch_project(const Geometry &g, int d_model, const void *h, const void *w,
-                          const int32_t *pos, const int32_t *page_table, void *q_idx,
-                          void *k_idx, void *k_cache, void *v_cache, hipStream_t stream) {
+static hipError_t launch_project_args(const Geometry &g, int d_model, ProjArgs a, const void *h,
+                                      const void *w, const int32_t *page_table, void *q_idx,
+                                      void *k_idx, void *k_cache, void *v_cache,
+                                      hipStream_t stream) {
     if (!project_supported(d_model)) return hipErrorInvalidValue;
-    ProjArgs a;
     a.h = static_cast<const uint16_t *>(h);
     a.w = static_cast<const uint16_t *>(w);
-    a.pos = pos;
     a.page_table = page_table;
     a.q_idx = static_cast<uint16_t *>(q_idx);
     a.k_idx = static_cast<uint16_t *>(k_idx);
@@ -371,6 +385,25 @@ hipError_t launch_project(const Geometry &g, int d_model, const void *h, const v
     if (paged) project_gemm_kernel<true><<<grid, dim3(256), kGemmLds, stream>>>(a);
     else project_gemm_kernel<false><<<grid, dim3(256), kGemmLds, stream>>>(a);
     return hipGetLastError();
+}
+
+hipError_t launch_project(const Geometry &g, int d_model, const void *h, const void *w,
+                          const int32_t *pos, const int32_t *page_table, void *q_idx,
+                          void *k_idx, void *k_cache, void *v_cache, hipStream_t stream) {
+    ProjArgs a{};
+    a.pos = pos;
+    return launch_project_args(g, d_model, a, h, w, page_table, q_idx, k_idx, k_cache, v_cache, stream);
+}
+
+hipError_t launch_project_rows(const Geometry &g, int d_model, const void *h, const void *w,
+                               const int32_t *start, const int32_t *count,
+                               const int32_t *page_table, void *q_idx, void *k_idx, void *k_rows,
+                               void *v_rows, hipStream_t stream) {
+    ProjArgs a{};
+    a.start = start;
+    a.count = count;
+    a.kv_rows = true;
+    return launch_project_args(g, d_model, a, h, w, page_table, q_idx, k_idx, k_rows, v_rows, stream);
 }
 
 }  // namespace clsa

@@ -44,7 +44,13 @@ def _topk(sh, block=64, q=A, m=A, pt=None, sl=A, qp=None, idx=A, ns=A, ws=None, 
     return B.lib().clsa_block_topk(ctypes.byref(sh), block, q, m, pt, sl, qp, idx, ns, ws, wsb, None)
 
 
-CALLS = [_append, _sparse, _dense, _means, _topk]
+def _project(sh, block=64, d=512, h=A, w=A, start=A, count=A, pt=None, q=A, ki=A, k8=A, v8=A, ks=A, vs=A,
+             ws=None, wsb=0):
+    return B.lib().clsa_project_append8(ctypes.byref(sh), block, d, h, w, start, count, pt, q, ki, k8, v8, ks,
+                                        vs, ws, wsb, None)
+
+
+CALLS = [_append, _sparse, _dense, _means, _topk, _project]
 
 
 @pytest.mark.parametrize("call", CALLS)
@@ -65,15 +71,15 @@ def test_shapes(call):
     sh.causal = 2
     assert call(sh) == -1
     assert call(_shape(top_k=8193)) in (-1, -2)
-    if call in (_append, _sparse, _dense):
+    if call in (_append, _sparse, _dense, _project):
         assert call(_shape(head_dim=64)) == -2
         assert call(_shape(q_heads=48, kv_heads=8)) == -2
         assert call(_shape(q_heads=32, kv_heads=5)) == -1
         assert call(_shape(softmax_scale=float("nan"))) == -1
         assert call(_shape(max_len=262144, q_heads=64, kv_heads=64)) == -2
-    else:
+    if call in (_means, _topk, _project):
         assert call(_shape(idx_dim=32)) == -2
-    if call in (_dense, _topk, _means):
+    if call in (_dense, _topk, _means, _project):
         assert call(_shape(max_len=262145)) == -2
 
 
@@ -82,7 +88,8 @@ def test_shapes(call):
     (_sparse, ("q", "k8", "v8", "out"), 16), (_sparse, ("ks", "vs", "idx", "ns"), 4),
     (_dense, ("q", "k8", "v8", "out"), 16), (_dense, ("ks", "vs", "sl"), 4),
     (_means, ("ki", "m"), 16), (_means, ("start", "count"), 4),
-    (_topk, ("q", "m"), 16), (_topk, ("sl", "idx", "ns"), 4)])
+    (_topk, ("q", "m"), 16), (_topk, ("sl", "idx", "ns"), 4),
+    (_project, ("h", "w", "q", "ki", "k8", "v8"), 16), (_project, ("start", "count", "ks", "vs"), 4)])
 def test_pointers(call, names, align):
     sh = _shape()
     for n in names:
@@ -97,7 +104,7 @@ def test_pointers(call, names, align):
 def test_workspaces():
     sh = _shape(batch=1, max_len=8192, top_k=2048)
     for call, op, arg in ((_sparse, B.CLSA_OP_ATTN8, 0), (_dense, B.CLSA_OP_DENSE8, 0),
-                          (_topk, B.CLSA_OP_BLOCK_TOPK, 64)):
+                          (_topk, B.CLSA_OP_BLOCK_TOPK, 64), (_project, B.CLSA_OP_PROJECT8, 0)):
         need = B.clsa_workspace_bytes(sh, op, arg)
         assert need > 0 and need % 256 == 0
         assert call(sh, ws=None, wsb=need) == -3
@@ -106,6 +113,7 @@ def test_workspaces():
     assert B.clsa_workspace_bytes(sh, B.CLSA_OP_BLOCK_TOPK, 0) == 0   # the block is asked for
     assert B.clsa_workspace_bytes(sh, B.CLSA_OP_BLOCK_TOPK, 24) == 0
     assert B.clsa_workspace_bytes(_shape(head_dim=64), B.CLSA_OP_ATTN8) == 0
+    assert _project(sh, d=0) == -1 and _project(sh, d=500) == -2 and _project(sh, d=8704) == -2
     # a list of whole blocks
     assert _topk(_shape(top_k=100), ws=A, wsb=1 << 30) == -1
     assert _topk(_shape(top_k=32), ws=A, wsb=1 << 30) == -1

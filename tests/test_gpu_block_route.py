@@ -197,11 +197,6 @@ class Serving:
         self.means = z(*blocks, 256, dtype=torch.bfloat16)
         self.d_model = 512
         self.w = _bf16(C.bf16(self.g.standard_normal((512 + 2 * heads * 128, self.d_model)) / 16)[1])
-        # the new tokens' K and V leave the projection as rows of their own
-        self.new = _shape(batch, n_q, n_q, top_k, 0, True, **self.kw)
-        self.order = torch.arange(n_q, dtype=torch.int32, device="cuda").repeat(batch, 1)
-        self.kn, self.vn = (z(batch, n_q, heads, 128, dtype=torch.bfloat16) for _ in "kv")
-        self.kin = z(batch, n_q, 256, dtype=torch.bfloat16)
         self.h = z(batch, n_q, self.d_model, dtype=torch.bfloat16)
         self.q_idx = z(batch, n_q, 256, dtype=torch.bfloat16)
         self.q = z(layers, batch, n_q, heads * group, 128, dtype=torch.bfloat16)
@@ -213,7 +208,7 @@ class Serving:
         self.start, self.count, self.lens = (z(batch, dtype=torch.int32) for _ in range(3))
         self.pos = z(batch, n_q, dtype=torch.int32)
         self.ws = [B.workspace(self.sh, B.CLSA_OP_BLOCK_TOPK, block), B.workspace(self.sh, B.CLSA_OP_ATTN8),
-                   B.workspace(self.sh, B.CLSA_OP_DENSE8)]
+                   B.workspace(self.sh, B.CLSA_OP_DENSE8), B.workspace(self.sh, B.CLSA_OP_PROJECT8)]
         self.at = np.zeros(batch, np.int64)
 
     def feed(self, count):
@@ -234,13 +229,8 @@ class Serving:
 
     def step(self):
         B, sh, n = self.B, self.sh, self.block
-        # index keys into their cache; K and V rows aside
-        B.clsa_project_append(self.new, self.d_model, self.h, self.w, self.order, None, self.q_idx, self.kin,
-                              self.kn, self.vn)
-        B.clsa_project_append(sh, self.d_model, self.h, self.w, self.pos, self.d_pt, self.q_idx, self.k_idx,
-                              self.trash()[0], self.trash()[1])
-        B.clsa_cache_append8(sh, n, self.kn, self.vn, self.start, self.count, self.d_pt, self.k8, self.v8,
-                             self.ks, self.vs)
+        B.clsa_project_append8(sh, n, self.d_model, self.h, self.w, self.start, self.count, self.d_pt,
+                               self.q_idx, self.k_idx, self.k8, self.v8, self.ks, self.vs, self.ws[3])
         B.clsa_block_means(sh, n, self.k_idx, self.start, self.count, self.d_pt, self.means)
         B.clsa_block_topk(sh, n, self.q_idx, self.means, self.d_pt, self.lens, self.pos, self.idx, self.n_sel,
                           self.ws[0])
@@ -250,12 +240,16 @@ class Serving:
         B.clsa_dense_attn8(sh, n, self.q[0], self.k8, self.v8, self.ks, self.vs, self.d_pt, self.lens, self.pos,
                            self.dense, self.dense_lse, self.ws[2])
 
-    def trash(self):
+    def new_rows(self):
+        """K and V rows of the step's tokens, by the bf16 projection: [batch, n_q, heads, 128]."""
         import torch
-        if not hasattr(self, "_trash"):
-            s = tuple(self.k8.shape)
-            self._trash = [torch.zeros(s, dtype=torch.bfloat16, device="cuda") for _ in "kv"]
-        return self._trash
+        B = self.B
+        order = torch.arange(self.n_q, dtype=torch.int32, device="cuda").repeat(self.batch, 1)
+        rows = [torch.zeros(self.batch, self.n_q, *s, dtype=torch.bfloat16, device="cuda")
+                for s in ((256,), (256,), (self.heads, 128), (self.heads, 128))]
+        B.clsa_project_append(_shape(self.batch, self.n_q, self.n_q, self.sh.top_k, 0, True, **self.kw),
+                              self.d_model, self.h, self.w, order, None, *rows)
+        return rows
 
     def results(self):
         return [self.k8, self.v8, self.ks, self.vs, self.means, self.idx, self.n_sel, self.out, self.lse,
@@ -284,7 +278,13 @@ def test_serving_steps(page, block):
         pos = prog.feed(count)
         prog.step()
         torch.cuda.synchronize()
-        for c, x in zip(ref, (prog.kn, prog.vn)):
+        rows = prog.new_rows()
+        assert torch.equal(rows[0], prog.q_idx)
+        for b in range(3):  # index keys at their positions
+            for j in (0, count[b] - 1) if count[b] else ():
+                at = ref[0].at(b, int(first[b]) + j)
+                assert torch.equal(prog.k_idx[at], rows[1][b, j])
+        for c, x in zip(ref, rows[2:]):
             x = inputs.f32_from_bf16_bits(B.bits_from_bf16(x)).astype(np.float64)
             for b in range(3):
                 if count[b]:
@@ -339,8 +339,6 @@ def test_two_streams_at_once():
     import torch
     progs = [Serving(s, 2, 40, 512, 64, 128, 0) for s in (1, 2, 1, 2)]
     streams = [torch.cuda.Stream() for _ in range(2)]
-    for p in progs:
-        p.trash()
     for _ in range(5):
         for p in progs:
             p.feed([40, 13])
