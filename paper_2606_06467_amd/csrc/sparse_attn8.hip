@@ -2,10 +2,10 @@
 // tokens and KV head; see cache8.hip): over the tokens of an index list (Eq. 4),
 // or, for few query rows, over every valid key (Eq. 1).
 //
-// One workgroup (4 waves) = one (query row, KV head, split of the row's keys); a
-// wave takes 32 tokens at a time, on its own, with its own online softmax; the
-// waves' states are merged by the log-sum-exp rule at the end, and the splits' by
-// the merge kernels of sparse_attn.hip.  For the products the bytes become bf16,
+// One workgroup = one (query row, KV head or four of them, range of the row's keys): 1, 4
+// or 8 waves, see plan_splits8.  A wave takes 32 tokens at a time, on its own, with its
+// own online softmax; the states of a head's waves are merged by the log-sum-exp rule at
+// the end, and the ranges' by the merge kernels of sparse_attn.hip.  For the products the bytes become bf16,
 // which holds every e4m3 value; the scales stay outside: a logit is multiplied by
 // its token's key scale, and a weight by its value scale before it is rounded to
 // bf16 (a rounding of 2^-9 relative, of either sign, averaged over the keys).  (The
@@ -19,8 +19,18 @@
 // K is read back as A rows of v_mfma_f32_16x16x32_bf16 (lane (qq, sub): token sub,
 // dimensions 32 qq ..+ 32, the queries in the same order), V by the transposing
 // 8-bit read ds_read_b64_tr_b8, whose lane gets 8 tokens of one dimension: the
-// tokens (4 qq + r, 16 + 4 qq + r) of which the same lane holds the weights of head
-// sub, so that the weights never leave their registers.
+// tokens (4 qq + r, 16 + 4 qq + r) whose weights make up the lane's A row of head sub.
+// The next step's rows are in flight while one is computed.
+//
+// What bounds it (times of a call's kernels in a row of calls).  Dense, 8 x 32768 keys:
+// memory, 537 MB in 82 us, 6.6 TB/s.  Lists of 32 sequences, 134 MB: the gather of 128-byte
+// vectors, 31 us (a kernel that only loads them takes 31.2; 26 where a workgroup takes
+// whole 1 KB rows, which the joining of more ranges eats up).  4 x 2048 of 131072 keys
+// 9.1 us, one sequence 6.2 to 6.9: launches and four dependent memory latencies.  1024
+// rows of 2048 out of 65536 keys, 20 / 4 heads, 137 us: vector instructions (170 a step and
+// wave, 62% of the issue slots) and matrix products (20%) share the SIMDs with a gather
+// that the L2 serves to 77%.  (K read straight into operand registers, without LDS: 238
+// us, since a wave then asks for half lines.)
 #include "clsa_internal.h"
 #include "device_common.h"
 
@@ -34,6 +44,7 @@ constexpr int kA8Dim = 128;
 constexpr int kA8Pitch = kA8Dim + 16;  // bytes per staged row
 constexpr int kA8Tokens = 32;          // tokens per wave and step
 constexpr int kA8ManyUnits = 768;      // (row, KV head) units from which a workgroup is one wave
+constexpr int kA8StretchUnits = 8192;  // pairs from which lists are cut into stretches
 constexpr float kA8Log2e = 1.4426950408889634f;
 constexpr float kA8Ln2 = 0.6931471805599453f;
 
@@ -155,7 +166,10 @@ __global__ __launch_bounds__(64 * HW * TW, 4) void attn8_kernel(Attn8Args a) {
     } s;
     __shared__ __align__(16) float s_sc[NW][2][kA8Tokens];  // key, value scales of the 32 tokens
     __shared__ float s_ml[NW][G][2];
-    const int split = blockIdx.x % a.splits, rg = blockIdx.x / a.splits;
+    // one wave a workgroup: range by range over all rows (see plan_splits8)
+    const int all = gridDim.x / a.splits;
+    const int split = NW == 1 ? blockIdx.x / all : blockIdx.x % a.splits;
+    const int rg = NW == 1 ? blockIdx.x % all : blockIdx.x / a.splits;
     const int groups = a.kv_heads / HW, row = rg / groups;
     const int b = row / a.n_q;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -370,7 +384,13 @@ struct Plan8 {
 };
 // Index lists: kA8ManyUnits (row, KV head) pairs or more take one wave and one range each
 // (800 pairs of 2048 keys 57 us against 66 in workgroups of four waves, 512 pairs 52
-// against 41).  Fewer are cut into ranges for one workgroup per CU: four waves, or on
+// against 41).  From kA8StretchUnits pairs, twice what is resident, on, lists of 1024 keys
+// or more are cut into a stretch for each 8192 keys of the cache, 8 at most, issued stretch
+// by stretch over all rows: the lists are ascending, so what is gathered at a time comes
+// from one key range that the caches hold (4096 rows of 2048 out of 131072 keys, 8 KV heads,
+// 1.54 ms against 1.87, with 16 stretches 1.64; out of 32768 1.07 against 1.17, with eight
+// 1.22; 1024 rows out of 65536 346 us against 358; half as many pairs 172 against 139).
+// Fewer are cut into ranges for one workgroup per CU: four waves, or on
 // paged caches, whose gathers wait for the page as well, eight (ragged 32 rows of 2048
 // out of 65536 keys, 64-token pages, 35.2 us against 38.8; contiguous 32.3 against 31.0).
 // Up to 512 keys make one range of eight waves, without a second launch to join ranges
@@ -389,6 +409,8 @@ static Plan8 plan_splits8(const Geometry &g, int keys, bool dense) {
     if (!dense && units >= kA8ManyUnits) {
         p.waves = 1;
         target = 1;
+        if (units >= kA8StretchUnits && keys >= 1024 && g.max_len >= 8192)
+            target = units * (g.max_len < 65536 ? g.max_len / 8192 : 8);
     } else if (keys <= 512) {
         p.waves = 8;
         target = 1;

@@ -1,6 +1,7 @@
 """Host-only checks of the 8-bit cache and block routing entry points: what they refuse
 (before anything is enqueued), their workspaces, and the tests' own e4m3 reference."""
 import ctypes
+import types
 
 import numpy as np
 import pytest
@@ -129,3 +130,13 @@ def test_reference_rounding_is_the_formats():
     assert np.array_equal(C.encode(x.astype(np.float64)), t)
     assert np.array_equal(C.VALUES[np.arange(127)], torch.arange(127, dtype=torch.uint8)
                           .view(torch.float8_e4m3fn).double().numpy())
+
+
+def test_binding_refuses_what_is_no_gpu_tensor():
+    t = torch.zeros(16)
+    with pytest.raises(ValueError, match="k must be a GPU tensor"):
+        B.clsa_cache_append8(_shape(), 64, t, t, t, t, None, t, t, t, t)
+    with pytest.raises(TypeError, match="q_idx must be a torch.Tensor"):
+        B.clsa_block_topk(_shape(), 64, [1.0], t, None, t, None, t, t)
+    with pytest.raises(B.ClsaError, match="CLSA_ERR_INVALID_ARG"):
+        B.clsa_block_means(_shape(), 64, None, None, None, None, None, stream=types.SimpleNamespace(cuda_stream=0))

@@ -220,6 +220,23 @@ def test_sparse_many_rows():
     _sparse_case(6, (400,), 4, 2, 140, 64, n_q=300, counts=counts)
 
 
+@pytest.mark.parametrize("k,n_q,max_len", [(1030, 1030, 25000), (1500, 1025, 70000), (100, 1040, 25000),
+                                           (1100, 1030, 2000)])
+def test_sparse_rows_by_stretches(k, n_q, max_len):
+    """Over 8192 (row, KV head) pairs: long lists are cut into stretches that all rows take in turn
+    (checked on some rows of every kind)."""
+    g = np.random.default_rng(k)
+    n, heads, block = 2000, 8, 32
+    p = Pair(*(C.filled(k + i, (n,), heads, block, max_len) for i in (1, 2)))
+    counts = [list(np.where(g.random(n_q) < 0.3, g.integers(0, k + 1, size=n_q), k))]
+    counts[0][:5] = [0, 1, k // 8, k // 8 + 1, k - 1]
+    qv, q = C.bf16(g.standard_normal((1, n_q, heads, 128)))
+    idx, ns, sets = _sets(g, (n,), n_q, k, counts)
+    out, lse = _attend(p, _shape(1, n_q, max_len, heads, 0, k), block, q, idx, ns)
+    at = [*range(8), *g.integers(0, n_q, size=40), n_q - 1]
+    C.check_attention(out[:, at], lse[:, at], C.attention(qv[:, at], p.k, p.v, [[sets[0][t] for t in at]], SCALE))
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.25, 3.0])
 def test_sparse_softmax_scale(scale):
     _sparse_case(7, (300, 200), 2, 4, 128, 64, scale=scale)
@@ -303,14 +320,15 @@ def test_sparse_offsets_past_32_bits(paged):
 
 
 def _dense_case(seed, lens, heads, group, block, page=0, n_q=1, causal=False, tiles=None, max_len=None,
-                nan_at=None):
+                nan_at=None, of="v"):
     g = np.random.default_rng(seed)
     top = max_len or max(max(lens), 1)
     max_len = -(-top // page) * page if page else top
     pt = C.page_table(seed, lens, page, max_len) if page else None
     p = Pair(*(C.filled(seed + i, lens, heads, block, max_len, page, pt) for i in (1, 2)))
     if nan_at is not None:
-        p.v.bytes[p.v.at(0, nan_at)][0, 7] = 0x7f
+        c = getattr(p, of)
+        c.bytes[c.at(0, nan_at)][0, 7] = 0x7f
         p.push()
     qv, q = C.bf16(g.standard_normal((len(lens), n_q, heads * group, 128)))
     q_pos = None
@@ -363,10 +381,12 @@ def test_dense_tiles_of_a_long_context(group, block, page):
     _dense_case(80 + group, (6000, 3500), 2, group, block, page, 70, True, tiles=True)
 
 
-def test_dense_tiles_nan_reaches_later_rows_only():
-    _dense_case(70, (500,), 4, 4, 32, 0, 500, True, nan_at=333)
-    _dense_case(72, (6000,), 2, 4, 32, 0, 70, True, tiles=True, nan_at=5960)
+@pytest.mark.parametrize("of", ["k", "v"])
+def test_dense_tiles_nan_reaches_later_rows_only(of):
+    _dense_case(70, (500,), 4, 4, 32, 0, 500, True, nan_at=333, of=of)
+    _dense_case(72, (6000,), 2, 4, 32, 0, 70, True, tiles=True, nan_at=5960, of=of)
 
 
-def test_dense_rows_nan_reaches_later_rows_only():
-    _dense_case(71, (300,), 2, 4, 32, 0, 6, True, tiles=False, nan_at=297)
+@pytest.mark.parametrize("of", ["k", "v"])
+def test_dense_rows_nan_reaches_later_rows_only(of):
+    _dense_case(71, (300,), 2, 4, 32, 0, 6, True, tiles=False, nan_at=297, of=of)
