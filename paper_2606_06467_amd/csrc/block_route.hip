@@ -14,6 +14,13 @@
 //
 // The scoring reads the means once (1 / block of the index keys); a workgroup then
 // chooses a row's blocks, holding their scores in registers, and writes its list.
+//
+// What bounds it.  Single tokens: 4 sequences of 2048 blocks 4.3 us of scoring and 7.9 of
+// choosing (17 500 cycles of barriers, LDS and memory latency one after another, 36 000 at
+// first); 32 sequences of 512 to 2048 blocks 7.4 us of scoring, 44 MB of means at 5.9 TB/s.
+// 4096 rows of 2048 blocks: scoring 17.6 us (operands straight from memory, which asks for
+// half lines, took 40.8), choosing 32 us, of which the scores read and lists written, 67 MB,
+// need 14.
 #include "clsa_internal.h"
 #include "device_common.h"
 
@@ -152,12 +159,13 @@ __device__ __forceinline__ uint64_t score_key64(double s) {
 
 // Sum of a wave-uniform count over the workgroup's waves (slot: alternates between calls,
 // so that one barrier per call is enough).
-__device__ __forceinline__ int over_waves(int count, int (*slots)[kBrWaves], int &slot, int wave, int lane) {
+template <int NW>
+__device__ __forceinline__ int over_waves(int count, int (&slots)[2][NW], int &slot, int wave, int lane) {
     if (lane == 0) slots[slot][wave] = count;
     __syncthreads();
     int sum = 0;
 #pragma unroll
-    for (int w = 0; w < kBrWaves; ++w) sum += slots[slot][w];
+    for (int w = 0; w < NW; ++w) sum += slots[slot][w];
     slot ^= 1;
     return sum;
 }
@@ -246,20 +254,20 @@ static size_t choose_lds_bytes(int nblk, int chosen) {
     return 8 * (size_t)(exact_slots(nblk) + kBrDim) + 4 * even_up(div_up(nblk, 32)) + 2 * (size_t)chosen;
 }
 
-// One workgroup = one row.  Thread tid holds blocks 256 i + tid (i < VPL) as
+// One workgroup of NW waves = one row.  Thread tid holds blocks 64 NW i + tid (i < VPL) as
 // order-preserving keys in registers.  The want-th largest is found by a histogram in LDS
 // of the top 11 bits (bins of a quarter octave: some thirty of 2048 scores share the
 // wanted one) and a count of each such key against the others, or, where more than 256
 // keys share it, by two more histograms.  (Bit by bit with ballots and a barrier each
 // it took 20000 of the kernel's 36000 cycles, with three histograms 7500 of 17500.)
-template <int VPL, bool PAGED>
-__global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_kernel(RouteArgs a) {
-    constexpr int NT = 64 * kBrWaves, WORDS = VPL * kBrWaves;
+template <int VPL, int NW, bool PAGED>
+__global__ __launch_bounds__(64 * NW, 4) void block_choose_kernel(RouteArgs a) {
+    constexpr int NT = 64 * NW, WORDS = VPL * NW;
     extern __shared__ __align__(16) char s_dyn[];
-    __shared__ int s_slots[2][kBrWaves];
-    __shared__ float2 s_mag[kBrWaves];
+    __shared__ int s_slots[2][NW];
+    __shared__ float2 s_mag[NW];
     __shared__ uint64_t s_words[WORDS];
-    __shared__ uint32_t s_before[kBrWaves][WORDS];
+    __shared__ uint32_t s_before[NW][WORDS];
     __shared__ uint32_t s_pick[4];  // the digit, keys above it, keys with it, a counter of these
     uint64_t *exact = reinterpret_cast<uint64_t *>(s_dyn);
     uint32_t *s_bins = reinterpret_cast<uint32_t *>(s_dyn);
@@ -298,8 +306,8 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
         key[i] = NT * i + tid < own && want > 0 ? score_key(__uint_as_float(key[i])) : 0u;
     if (want > 0) {
         int slot = 0;
-        float mag = 0.0f, qn = bf16_lo(a.q_idx[row * kBrDim + tid]);
-        static_assert(NT == kBrDim, "a component of the query per thread");
+        static_assert(NT >= kBrDim, "a component of the query per thread");
+        float mag = 0.0f, qn = tid < kBrDim ? bf16_lo(a.q_idx[row * kBrDim + tid]) : 0.0f;
         qn *= qn;
         for (int i = tid; i < div_up(own, kBrTile); i += NT) mag = fmaxf(mag, a.norm[(size_t)b * a.ntile + i]);
         // histograms of the digit at `shift` of the keys that agree with t above it
@@ -311,8 +319,8 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
             const int width = pass == 2 ? 10 : 11;
             constexpr int PER = kBrBins / NT;
 #pragma unroll
-            for (int i = 0; i < PER; i += 4)
-                *reinterpret_cast<uint4 *>(&s_bins[PER * tid + i]) = make_uint4(0u, 0u, 0u, 0u);
+            for (int i = 0; i < PER; i += 2)
+                *reinterpret_cast<uint2 *>(&s_bins[PER * tid + i]) = make_uint2(0u, 0u);
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < VPL; ++i)
@@ -322,16 +330,16 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
             // thread tid: bins PER tid ..+ PER; keys in higher ones first
             uint32_t c[PER], sum = 0u;
 #pragma unroll
-            for (int i = 0; i < PER; i += 4) {
-                const uint4 v = *reinterpret_cast<const uint4 *>(&s_bins[PER * tid + i]);
-                c[i] = v.x, c[i + 1] = v.y, c[i + 2] = v.z, c[i + 3] = v.w;
-                sum += (v.x + v.y) + (v.z + v.w);
+            for (int i = 0; i < PER; i += 2) {
+                const uint2 v = *reinterpret_cast<const uint2 *>(&s_bins[PER * tid + i]);
+                c[i] = v.x, c[i + 1] = v.y;
+                sum += v.x + v.y;
             }
             const uint32_t upto = wave_prefix(sum), total = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
             if (lane == 0) s_slots[slot][wave] = (int)total;
             __syncthreads();
             uint32_t higher = total - upto;
-            for (int w = wave + 1; w < kBrWaves; ++w) higher += (uint32_t)s_slots[slot][w];
+            for (int w = wave + 1; w < NW; ++w) higher += (uint32_t)s_slots[slot][w];
             slot ^= 1;
             if (higher < (uint32_t)left && higher + sum >= (uint32_t)left) {  // one thread
 #pragma unroll
@@ -370,8 +378,14 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
         wave_max_sum(mag, qn);
         if (lane == 0) s_mag[wave] = make_float2(mag, qn);
         __syncthreads();
-        mag = fmaxf(fmaxf(s_mag[0].x, s_mag[1].x), fmaxf(s_mag[2].x, s_mag[3].x));
-        mag = sqrtf(mag) * sqrtf((s_mag[0].y + s_mag[1].y) + (s_mag[2].y + s_mag[3].y));
+        mag = s_mag[0].x;
+        qn = s_mag[0].y;
+#pragma unroll
+        for (int w = 1; w < NW; ++w) {
+            mag = fmaxf(mag, s_mag[w].x);
+            qn += s_mag[w].y;
+        }
+        mag = sqrtf(mag) * sqrtf(qn);
         const float tf = key_score(t);
         // 2 eps, the rounding of it and of t +- it, and products that are flushed to zero
         const float eps = 2.1f * kBrEps * mag + 1e-34f;
@@ -384,7 +398,7 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
             const uint64_t band = __ballot(key[i] >= lo && key[i] <= hi);
             above += __popcll(__ballot(key[i] > hi));
             within += __popcll(band);
-            if (lane == 0) s_words[i * kBrWaves + wave] = band;
+            if (lane == 0) s_words[i * NW + wave] = band;
         }
         above = over_waves(above, s_slots, slot, wave, lane);
         within = over_waves(within, s_slots, slot, wave, lane);
@@ -392,18 +406,18 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
         some = within > want;
         if (some) {  // uniform: exact scores decide
             scan_words<WORDS>(s_words, s_before[wave], lane);
-            q[tid] = (double)__uint_as_float((uint32_t)a.q_idx[row * kBrDim + tid] << 16);
+            if (tid < kBrDim) q[tid] = (double)__uint_as_float((uint32_t)a.q_idx[row * kBrDim + tid] << 16);
             for (int w = tid; w < div_up(own, 32); w += NT) taken[w] = 0u;
 #pragma unroll
             for (int i = 0; i < VPL; ++i) {  // undecided blocks in ascending order
-                const uint64_t band = s_words[i * kBrWaves + wave];
+                const uint64_t band = s_words[i * NW + wave];
                 if ((band >> lane) & 1u)
-                    number[s_before[wave][i * kBrWaves + wave] + __popcll(band & below)] = (uint16_t)(NT * i + tid);
+                    number[s_before[wave][i * NW + wave] + __popcll(band & below)] = (uint16_t)(NT * i + tid);
             }
             __syncthreads();
             // a wave per undecided block: lane holds dimensions 4 lane ..+ 4 (a thread per block,
             // its 256 additions one after another, took 13500 cycles for two or three blocks)
-            for (int p = wave; p < within; p += kBrWaves) {
+            for (int p = wave; p < within; p += NW) {
                 const uint2 v = *reinterpret_cast<const uint2 *>(mean_row<PAGED>(a, b, number[p]) + 4 * lane);
                 double sum = q[4 * lane] * (double)bf16_lo(v.x);
                 sum = fma(q[4 * lane + 1], (double)bf16_hi(v.x), sum);
@@ -455,14 +469,14 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
         const int c = NT * i + tid;
         const bool open = key[i] >= lo && key[i] <= hi;
         const uint64_t in = __ballot(key[i] > hi || (open && (!some || ((taken[c >> 5] >> (c & 31)) & 1u))));
-        if (lane == 0) s_words[i * kBrWaves + wave] = in;
+        if (lane == 0) s_words[i * NW + wave] = in;
     }
     __syncthreads();
     scan_words<WORDS>(s_words, s_before[wave], lane);
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
-        const uint64_t in = s_words[i * kBrWaves + wave];
-        const int p = (int)s_before[wave][i * kBrWaves + wave] + __popcll(in & below);
+        const uint64_t in = s_words[i * NW + wave];
+        const int p = (int)s_before[wave][i * NW + wave] + __popcll(in & below);
         if (((in >> lane) & 1u) && p < kept) list[p] = (uint16_t)(NT * i + tid);
     }
     if (tid == 0) list[kept] = (uint16_t)own;
@@ -474,26 +488,26 @@ __global__ __launch_bounds__(64 * kBrWaves, VPL > 8 ? 2 : 4) void block_choose_k
 
 static size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
-// Floats of a row of scores: an odd number of 256-byte pieces, so that the rows' pieces of
-// one block tile fall on all of an L2's channels (4096 rows of 2048 blocks at 8 KB a row
-// met on two of the sixteen: 40.8 us of scoring, now SCORE_US).
-static int score_pitch(int nblk) { return (div_up(nblk, 64) | 1) * 64; }
+// Floats of a row of scores: rows begin on 256-byte borders.
+static int score_pitch(int nblk) { return div_up(nblk, 64) * 64; }
 
 size_t block_topk_ws_bytes(const Geometry &g, int block) {
     const int nblk = div_up(g.max_len, block), tiles = div_up(nblk, kBrTile);
     return 4 * (size_t)g.rows * score_pitch(nblk) + align256(4 * (size_t)g.batch * tiles);
 }
 
-template <int VPL, bool PAGED>
-static hipError_t launch_choose(const RouteArgs &a, int rows, hipStream_t stream) {
-    static_assert(64 * 64 * kBrWaves >= kBrMostBlocks, "the larger form holds every sequence");
+template <int VPL, int NW>
+static hipError_t launch_choose(const RouteArgs &a, bool paged, int rows, hipStream_t stream) {
     const size_t lds = choose_lds_bytes(a.nblk, a.top_k >> a.block_shift);
+    const void *fn = paged ? reinterpret_cast<const void *>(&block_choose_kernel<VPL, NW, true>)
+                           : reinterpret_cast<const void *>(&block_choose_kernel<VPL, NW, false>);
     if (lds > 32768) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&block_choose_kernel<VPL, PAGED>),
-                                                 hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
     }
-    block_choose_kernel<VPL, PAGED><<<dim3((unsigned)rows), dim3(64 * kBrWaves), lds, stream>>>(a);
+    const dim3 grid((unsigned)rows), wg(64 * NW);
+    if (paged) block_choose_kernel<VPL, NW, true><<<grid, wg, lds, stream>>>(a);
+    else block_choose_kernel<VPL, NW, false><<<grid, wg, lds, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -536,8 +550,14 @@ hipError_t launch_block_topk(const Geometry &g, int block, const void *q_idx, co
     else block_scores_kernel<false><<<grid, wg, 0, stream>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (a.nblk <= 8 * 64 * kBrWaves) return paged ? launch_choose<8, true>(a, g.rows, stream) : launch_choose<8, false>(a, g.rows, stream);
-    return paged ? launch_choose<64, true>(a, g.rows, stream) : launch_choose<64, false>(a, g.rows, stream);
+    // Up to 8 blocks a thread in four waves, then 16, then sixteen waves (4 x 100000 tokens
+    // in blocks of 32, 3125 of them, 16.5 us; of 16, 6250 of them, 21.3 with sixteen waves of 8 a
+    // thread, 26.9 with four of 32)
+    static_assert(16 * 64 * 16 >= kBrMostBlocks, "the largest form holds every sequence");
+    if (a.nblk <= 8 * 64 * 4) return launch_choose<8, 4>(a, paged, g.rows, stream);
+    if (a.nblk <= 16 * 64 * 4) return launch_choose<16, 4>(a, paged, g.rows, stream);
+    if (a.nblk <= 8 * 64 * 16) return launch_choose<8, 16>(a, paged, g.rows, stream);
+    return launch_choose<16, 16>(a, paged, g.rows, stream);
 }
 
 hipError_t take_device_error_block_route(uint32_t *bits) { return take_source_device_error(bits); }

@@ -126,13 +126,20 @@ def test_causal_rows(block, page, top_k, n_q, lens):
     _case(block + n_q, lens, block, top_k, page, n_q, True)
 
 
-def test_most_blocks():
-    """The largest capacity: 16384 blocks of a sequence."""
-    _case(3, (262144, 200000), 16, 512)
-
-
 def _same(g, qv, mv, blk):
     mv[:] = mv[blk[0, 0]]
+
+
+@pytest.mark.parametrize("lens,page", [((262144, 200000), 0), ((100000, 131072), 64), ((65536, 33000), 0)])
+def test_many_blocks(lens, page):
+    """Up to the largest capacity: 4096, 8192 and 16384 blocks of a sequence."""
+    _case(3, lens, 16, 512, page)
+
+
+@pytest.mark.parametrize("lens,n_q", [((262144,), 3), ((120000,), 20), ((65536,), 20)])
+def test_many_blocks_alike(lens, n_q):
+    """Thousands of equal scores: the lowest blocks."""
+    _case(5, lens, 16, 8192, 0, n_q, True, _same)
 
 
 def _zero_query(g, qv, mv, blk):
