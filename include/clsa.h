@@ -300,8 +300,8 @@ clsa_status clsa_kd_loss(const clsa_shape *shape, const float *abar, const void 
  *   k_scale, v_scale  fp32 [batch, ceil(max_len / block), kv_heads]      contiguous
  *                     fp32 [num_pages, page_size / block, kv_heads]      paged
  * A cached value is its byte times its block's scale.  Half the bytes of a bf16
- * cache, each value off by at most 2^-4 of itself (or 2^-18 of the largest of its
- * block).  The index keys and the routing stay as they are. */
+ * cache, each value off by at most 2^-4 of itself or 2^-17 of the largest of its
+ * block.  The index keys and the routing stay as they are. */
 
 /* Appends new tokens' rows.  k, v: bf16 [batch, n_q, kv_heads, head_dim]; of
  * sequence b, rows 0 .. count[b]-1 go to positions start[b] .. start[b]+count[b]-1,
@@ -335,14 +335,16 @@ clsa_status clsa_project_append8(const clsa_shape *shape, int32_t block, int32_t
 /* clsa_sparse_attn over the 8-bit cache: the same index lists (of clsa_topk or
  * clsa_block_topk), outputs, conventions and errors.  Logits, softmax and sums in
  * fp32; each weight times its value's scale is rounded to bf16 for the product with
- * the values.  A NaN in the cache reaches the rows that select its token, and no
- * others.  Workspace: CLSA_OP_ATTN8. */
+ * the values, whose weighted sums are made in fp32 before they are divided (values
+ * from 2^108 on can overflow there).  A NaN in the cache reaches the rows that select
+ * its token, and no others.  Workspace: CLSA_OP_ATTN8. */
 clsa_status clsa_sparse_attn8(const clsa_shape *shape, int32_t block, const void *q, const void *k8,
                               const void *v8, const float *k_scale, const float *v_scale,
                               const int32_t *page_table, const int32_t *idx, const int32_t *n_sel,
                               void *out, float *lse, void *ws, size_t ws_bytes, void *stream);
 
-/* clsa_dense_attn over the 8-bit cache.  Workspace: CLSA_OP_DENSE8. */
+/* clsa_dense_attn over the 8-bit cache, with the conventions of clsa_sparse_attn8 (a NaN
+ * reaches the rows that see its token).  Workspace: CLSA_OP_DENSE8. */
 clsa_status clsa_dense_attn8(const clsa_shape *shape, int32_t block, const void *q, const void *k8,
                              const void *v8, const float *k_scale, const float *v_scale,
                              const int32_t *page_table, const int32_t *seq_lens,

@@ -13,8 +13,8 @@ LIB = os.path.join(PKG, "libclsa.so")
 BUILD_DIR = os.path.join(PKG, "_build")
 
 SOURCES = ["index_decode.hip", "index_prefill.hip", "topk.hip", "sparse_attn.hip", "tile_attn.hip",
-           "project.hip", "cache8.hip", "sparse_attn8.hip", "tile_attn8.hip", "block_route.hip", "kd.hip", "kd_loss.hip", "noalloc.hip",
-           "api.cpp"]
+           "project.hip", "cache8.hip", "sparse_attn8.hip", "tile_attn8.hip", "block_route.hip",
+           "kd.hip", "kd_loss.hip", "noalloc.hip", "api.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
@@ -30,9 +30,9 @@ COMMON_FLAGS = [
 # accumulator-register copies before the exponentials that consume them;
 # sparse_attn.hip: the chunked-prefill form of the layer kernel fits four waves
 # per SIMD; tile_attn.hip: the logits and the rescaled accumulators feed vector
-# instructions (so with tile_attn8.hip and sparse_attn8.hip).  kd_loss.hip goes without: its 128 gradient accumulators are
-# touched by matrix instructions only and fit beside the rest as accumulator
-# registers (3.2 ms; 4.3 ms in VGPRs).
+# instructions (so with tile_attn8.hip and sparse_attn8.hip).  kd_loss.hip goes
+# without: its 128 gradient accumulators are touched by matrix instructions only and
+# fit beside the rest as accumulator registers (3.2 ms; 4.3 ms in VGPRs).
 SOURCE_FLAGS = {"kd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                 "sparse_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                 "tile_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
