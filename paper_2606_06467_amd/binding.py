@@ -244,81 +244,84 @@ def clsa_kd_loss(shape, abar, q_idx, k_idx, page_table, seq_lens, q_pos, loss, d
                               _ptr(ws, "ws"), wsb, _stream(stream)), "clsa_kd_loss")
 
 
-def _call(where, shape, block, args, ws, stream, sizes=()):
-    """An entry point of the 8-bit cache or of block routing: numbers after the block, (name,
-    tensor) arguments, and its workspace (False: it takes none).  The call runs on the tensors' device; their stream is the
-    current one of that device unless one is given."""
-    ptrs, device = [], -1
-    for name, t in args if not isinstance(ws, torch.Tensor) else (*args, ("ws", ws)):
+_Tensor, _raw_stream = torch.Tensor, torch._C._cuda_getCurrentRawStream
+
+
+def _call(where, shape, block, names, tensors, ws, stream, sizes=()):
+    """An entry point of the 8-bit cache or of block routing: numbers after the block, its tensors
+    and their names, and its workspace (False: it takes none).  The call runs on the tensors'
+    device; their stream is the current one of that device unless one is given."""
+    args, device = [*sizes], -1
+    for i, t in enumerate(tensors):
         if t is None:
-            ptrs.append(None)
+            args.append(None)
             continue
-        if not isinstance(t, torch.Tensor):
-            raise TypeError(f"{name} must be a torch.Tensor")
-        if not t.is_cuda:
-            raise ValueError(f"{name} must be a GPU tensor")
-        if not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
-        at = t.get_device()
-        if at != device:
-            if device >= 0:
-                raise ValueError(f"{name} is on another device than the arguments before it")
+        at = t.get_device() if isinstance(t, _Tensor) else -1
+        if at < 0 or not t.is_contiguous() or at != device:
+            if device >= 0 or at < 0 or not t.is_contiguous():
+                _refuse(names[i], t)
             device = at
-        ptrs.append(t.data_ptr())
-    if ws is None:
-        ptrs += (None, 0)
-    elif ws is not False:
-        ptrs.append(ws.numel() * ws.element_size())
+        args.append(t.data_ptr())
+    if isinstance(ws, _Tensor):
+        if ws.get_device() != device or device < 0 or not ws.is_contiguous():
+            _refuse("ws", ws)
+        args += ws.data_ptr(), ws.numel() * ws.element_size()
+    elif ws is None:
+        args += None, 0
     if device >= 0 and device != torch.cuda.current_device():
         with torch.cuda.device(device):
-            return _call(where, shape, block, args, ws, stream, sizes)
-    # the raw handle: a torch Stream object costs 3 us, a quarter of a whole call
-    raw = torch._C._cuda_getCurrentRawStream(max(device, 0)) if stream is None else stream.cuda_stream
-    _check(getattr(lib(), where)(ctypes.byref(shape), block, *sizes, *ptrs, raw), where)
+            return _call(where, shape, block, names, tensors, ws, stream, sizes)
+    # the raw handle: making a torch Stream object takes 3 us, as long as the library's call
+    raw = _raw_stream(max(device, 0)) if stream is None else stream.cuda_stream
+    status = getattr(_lib_handle or lib(), where)(ctypes.byref(shape), block, *args, raw)
+    if status != CLSA_OK:
+        raise ClsaError(status, where)
+
+
+def _refuse(name, t):
+    _ptr(t, name)  # what is wrong with it alone
+    raise ValueError(f"{name} is on another device than the arguments before it")
 
 
 def clsa_cache_append8(shape, block, k, v, start, count, page_table, k8, v8, k_scale, v_scale,
                        stream=None):
     _call("clsa_cache_append8", shape, block,
-          (("k", k), ("v", v), ("start", start), ("count", count), ("page_table", page_table),
-           ("k8", k8), ("v8", v8), ("k_scale", k_scale), ("v_scale", v_scale)), False, stream)
+          ("k", "v", "start", "count", "page_table", "k8", "v8", "k_scale", "v_scale"),
+          (k, v, start, count, page_table, k8, v8, k_scale, v_scale), False, stream)
 
 
 def clsa_project_append8(shape, block, d_model, h, w, start, count, page_table, q_idx, k_idx, k8, v8,
                          k_scale, v_scale, ws=None, stream=None):
     _call("clsa_project_append8", shape, block,
-          (("h", h), ("w", w), ("start", start), ("count", count), ("page_table", page_table),
-           ("q_idx", q_idx), ("k_idx", k_idx), ("k8", k8), ("v8", v8), ("k_scale", k_scale),
-           ("v_scale", v_scale)), ws, stream, (d_model,))
+          ("h", "w", "start", "count", "page_table", "q_idx", "k_idx", "k8", "v8", "k_scale", "v_scale"),
+          (h, w, start, count, page_table, q_idx, k_idx, k8, v8, k_scale, v_scale), ws, stream,
+          (d_model,))
 
 
 def clsa_sparse_attn8(shape, block, q, k8, v8, k_scale, v_scale, page_table, idx, n_sel, out,
                       lse=None, ws=None, stream=None):
     _call("clsa_sparse_attn8", shape, block,
-          (("q", q), ("k8", k8), ("v8", v8), ("k_scale", k_scale), ("v_scale", v_scale),
-           ("page_table", page_table), ("idx", idx), ("n_sel", n_sel), ("out", out), ("lse", lse)),
-          ws, stream)
+          ("q", "k8", "v8", "k_scale", "v_scale", "page_table", "idx", "n_sel", "out", "lse"),
+          (q, k8, v8, k_scale, v_scale, page_table, idx, n_sel, out, lse), ws, stream)
 
 
 def clsa_dense_attn8(shape, block, q, k8, v8, k_scale, v_scale, page_table, seq_lens, q_pos, out,
                      lse=None, ws=None, stream=None):
     _call("clsa_dense_attn8", shape, block,
-          (("q", q), ("k8", k8), ("v8", v8), ("k_scale", k_scale), ("v_scale", v_scale),
-           ("page_table", page_table), ("seq_lens", seq_lens), ("q_pos", q_pos), ("out", out),
-           ("lse", lse)), ws, stream)
+          ("q", "k8", "v8", "k_scale", "v_scale", "page_table", "seq_lens", "q_pos", "out", "lse"),
+          (q, k8, v8, k_scale, v_scale, page_table, seq_lens, q_pos, out, lse), ws, stream)
 
 
 def clsa_block_means(shape, block, k_idx, start, count, page_table, means, stream=None):
-    _call("clsa_block_means", shape, block,
-          (("k_idx", k_idx), ("start", start), ("count", count), ("page_table", page_table),
-           ("means", means)), False, stream)
+    _call("clsa_block_means", shape, block, ("k_idx", "start", "count", "page_table", "means"),
+          (k_idx, start, count, page_table, means), False, stream)
 
 
 def clsa_block_topk(shape, block, q_idx, means, page_table, seq_lens, q_pos, idx, n_sel, ws=None,
                     stream=None):
     _call("clsa_block_topk", shape, block,
-          (("q_idx", q_idx), ("means", means), ("page_table", page_table), ("seq_lens", seq_lens),
-           ("q_pos", q_pos), ("idx", idx), ("n_sel", n_sel)), ws, stream)
+          ("q_idx", "means", "page_table", "seq_lens", "q_pos", "idx", "n_sel"),
+          (q_idx, means, page_table, seq_lens, q_pos, idx, n_sel), ws, stream)
 
 
 CLSA_DEVERR_SEQ_LEN = 1

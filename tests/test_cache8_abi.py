@@ -136,6 +136,8 @@ def test_binding_refuses_what_is_no_gpu_tensor():
     t = torch.zeros(16)
     with pytest.raises(ValueError, match="k must be a GPU tensor"):
         B.clsa_cache_append8(_shape(), 64, t, t, t, t, None, t, t, t, t)
+    with pytest.raises(ValueError, match="ws must be a GPU tensor"):
+        B.clsa_sparse_attn8(_shape(), 64, *[None] * 10, t)
     with pytest.raises(TypeError, match="q_idx must be a torch.Tensor"):
         B.clsa_block_topk(_shape(), 64, [1.0], t, None, t, None, t, t)
     with pytest.raises(B.ClsaError, match="CLSA_ERR_INVALID_ARG"):

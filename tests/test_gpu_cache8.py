@@ -390,3 +390,43 @@ def test_dense_tiles_nan_reaches_later_rows_only(of):
 @pytest.mark.parametrize("of", ["k", "v"])
 def test_dense_rows_nan_reaches_later_rows_only(of):
     _dense_case(71, (300,), 2, 4, 32, 0, 6, True, tiles=False, nan_at=297, of=of)
+
+
+def test_binding_refuses_tensors_that_are_not_contiguous():
+    import torch
+    from paper_2606_06467_amd import binding as B
+    p = Pair(*(C.filled(73 + i, (64,), 2, 32, 64) for i in (1, 2)))
+    x = torch.zeros((1, 8, 2, 256), dtype=torch.bfloat16, device="cuda")[..., ::2]
+    n = torch.ones(1, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError, match="v must be contiguous"):
+        B.clsa_cache_append8(_shape(1, 8, 64, 2), 32, x.contiguous(), x, n, n, None, p.k8, p.v8, p.ks, p.vs)
+    with pytest.raises(ValueError, match="k8 must be a GPU tensor"):
+        B.clsa_cache_append8(_shape(1, 8, 64, 2), 32, x.contiguous(), x.contiguous(), n, n, None, p.k8.cpu(),
+                             p.v8, p.ks, p.vs)
+
+
+def test_another_stream():
+    """The call's stream: the one given, or the current one."""
+    import torch
+    from paper_2606_06467_amd import binding as B
+    g = np.random.default_rng(74)
+    p = Pair(*(C.filled(74 + i, (700,), 2, 32, 700) for i in (1, 2)))
+    qv, q = C.bf16(g.standard_normal((1, 1, 8, 128)))
+    idx, ns, sets = _sets(g, (700,), 1, 300)
+    args = _bf16(q), p.k8, p.v8, p.ks, p.vs, None, _dev(idx), _dev(ns)
+    sh = _shape(1, 1, 700, 2, 0, 300, 4)
+    want = C.attention(qv, p.k, p.v, sets, SCALE)
+    torch.cuda.synchronize()
+    for given in (False, True):
+        st = torch.cuda.Stream()
+        out = torch.zeros((1, 1, 8, 128), dtype=torch.bfloat16, device="cuda")
+        lse = torch.zeros((1, 1, 8), device="cuda")
+        ws = B.workspace(sh, B.CLSA_OP_ATTN8)
+        torch.cuda.synchronize()
+        if given:
+            B.clsa_sparse_attn8(sh, 32, *args, out, lse, ws, stream=st)
+        else:
+            with torch.cuda.stream(st):
+                B.clsa_sparse_attn8(sh, 32, *args, out, lse, ws)
+        st.synchronize()
+        C.check_attention(B.bits_from_bf16(out), lse.cpu().numpy().astype(np.float64), want)
