@@ -26,10 +26,10 @@
 // vectors, 31 us (a kernel that only loads them takes 31.2; 26 where a workgroup takes
 // whole 1 KB rows, which the joining of more ranges eats up).  4 x 2048 of 131072 keys
 // 9.1 us, one sequence 6.2 to 6.9: launches and four dependent memory latencies.  1024
-// rows of 2048 out of 65536 keys, 20 / 4 heads, 137 us: vector instructions (170 a step and
-// wave, 62% of the issue slots) and matrix products (20%) share the SIMDs with a gather
-// that the L2 serves to 77%.  (K read straight into operand registers, without LDS: 238
-// us, since a wave then asks for half lines.)
+// rows of 2048 out of 65536 keys, 20 / 4 heads, 139 us: 2.27 GB asked of the L2 at 16 TB/s,
+// 77% found there (20 where all of it is); vector instructions (150 a step and wave) and
+// matrix products come to 95 us beside it.  (K read straight into operand registers,
+// without LDS: 238 us, since a wave then asks for half lines.)
 #include "clsa_internal.h"
 #include "device_common.h"
 

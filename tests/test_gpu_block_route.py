@@ -61,11 +61,13 @@ def test_means(block, page, n_q):
     assert np.array_equal(B.bits_from_bf16(md), means)
 
 
-def _topk(sh, block, q, means, lens, q_pos=None, pt=None, fill=-7):
+def _topk(sh, block, q, means, lens, q_pos=None, pt=None, fill=-7, shift=0):
+    """shift: elements by which the lists miss their 16 bytes."""
     import torch
     from paper_2606_06467_amd import binding as B
     rows = sh.batch * sh.n_q
-    buf = torch.full((rows + 2, sh.top_k), fill, dtype=torch.int32, device="cuda")
+    buf = torch.full(((rows + 2) * sh.top_k + shift,), fill, dtype=torch.int32, device="cuda")
+    buf = buf[shift:].view(rows + 2, sh.top_k)
     nb = torch.full((rows + 2,), fill, dtype=torch.int32, device="cuda")
     ws = B.workspace(sh, B.CLSA_OP_BLOCK_TOPK, block)
     ws.fill_(0xff)
@@ -87,7 +89,7 @@ def _check(sh, block, qv, mv, valid, got):
             assert np.array_equal(idx[b, t], want), (b, t)
 
 
-def _case(seed, lens, block, top_k, page=0, n_q=1, causal=False, tweak=None, max_len=None):
+def _case(seed, lens, block, top_k, page=0, n_q=1, causal=False, tweak=None, max_len=None, shift=0):
     g = np.random.default_rng(seed)
     batch, top = len(lens), max_len or max(max(lens), 1)
     max_len = -(-top // page) * page if page else top
@@ -106,7 +108,7 @@ def _case(seed, lens, block, top_k, page=0, n_q=1, causal=False, tweak=None, max
         q_pos = np.array([[n - n_q + t for t in range(n_q)] for n in lens], np.int32)
         valid = [[max(0, n - n_q + t + 1) for t in range(n_q)] for n in lens]
     sh = _shape(batch, n_q, max_len, top_k, page, causal)
-    got = _topk(sh, block, q, m, lens, q_pos, pt)
+    got = _topk(sh, block, q, m, lens, q_pos, pt, shift=shift)
     _check(sh, block, qv, [mv[np.maximum(blk[b], 0)] for b in range(batch)], valid, got)
 
 
@@ -124,6 +126,11 @@ def test_single_tokens(block, page, top_k):
 def test_causal_rows(block, page, top_k, n_q, lens):
     """Rows of a chunk: each its own block, none of the later ones; some rows see nothing."""
     _case(block + n_q, lens, block, top_k, page, n_q, True)
+
+
+@pytest.mark.parametrize("shift", [1, 2, 3])
+def test_lists_off_16_bytes(shift):
+    _case(shift, (0, 7, 64, 65, 300, 2000), 16, 48, shift=shift)
 
 
 def _same(g, qv, mv, blk):
