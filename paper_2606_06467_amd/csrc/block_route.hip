@@ -15,11 +15,11 @@
 // The scoring reads the means once (1 / block of the index keys); a workgroup then
 // chooses a row's blocks, holding their scores in registers, and writes its list.
 //
-// What bounds it.  Single tokens: 4 sequences of 2048 blocks 4.3 us of scoring and 7.9 of
+// What bounds it.  Single tokens: 4 sequences of 2048 blocks 4.3 us of scoring and 7.4 of
 // choosing (17 500 cycles of barriers, LDS and memory latency one after another, 36 000 at
 // first); 32 sequences of 512 to 2048 blocks 7.4 us of scoring, 44 MB of means at 5.9 TB/s.
 // 4096 rows of 2048 blocks: scoring 17.6 us (operands straight from memory, which asks for
-// half lines, took 40.8), choosing 32 us, of which the scores read and lists written, 67 MB,
+// half lines, took 40.8), choosing 31 us, of which the scores read and lists written, 67 MB,
 // need 14.
 #include "clsa_internal.h"
 #include "device_common.h"
