@@ -36,6 +36,11 @@ constexpr int kBrTile = 16;        // rows, and blocks, of a scoring tile
 constexpr int kBrWaves = 4;
 constexpr int kBrMostBlocks = kMaxLen / 16;
 constexpr float kBrEps = 0x1p-15f; // error of a score over |q| |kbar|
+// What fp32 can lose of a squared norm: 256 squares and 256 sums, each below 2^-126 at most.
+// With it |q| and |kbar| are no shorter than 2^-58, so that the bound of a score's error holds
+// for vectors whose squares vanish, and covers components that are taken for zero (2^-126
+// each, times the other vector's).
+constexpr float kBrNormLost = 0x1p-116f;
 
 struct RouteArgs {
     const uint16_t *q_idx, *means;
@@ -386,7 +391,7 @@ __global__ __launch_bounds__(64 * NW, 4) void block_choose_kernel(RouteArgs a) {
             mag = fmaxf(mag, s_mag[w].x);
             qn += s_mag[w].y;
         }
-        mag = sqrtf(mag) * sqrtf(qn);
+        mag = sqrtf(mag + kBrNormLost) * sqrtf(qn + kBrNormLost);
         const float tf = key_score(t);
         // 2 eps, the rounding of it and of t +- it, and products that are flushed to zero
         const float eps = 2.1f * kBrEps * mag + 1e-34f;

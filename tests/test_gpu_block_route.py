@@ -382,3 +382,20 @@ def test_workspace_contents_do_not_matter():
         torch.cuda.synchronize()
         for x, y in zip(a.results(), b.results()):
             assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+def _small(key_exp, query_exp):
+    """Equal exact scores that fp32 sums tell apart (the order of large and small terms differs),
+    of keys and queries whose squares fp32 cannot hold."""
+    def tweak(g, qv, mv, blk):
+        v = g.integers(-255, 256, size=256) * 2.0 ** g.integers(0, 15, size=256)
+        mv[:] = np.stack([g.permutation(v) for _ in range(len(mv))]) * 2.0 ** key_exp
+        qv[:] = 2.0 ** query_exp
+    return tweak
+
+
+@pytest.mark.parametrize("key_exp,query_exp", [(0, 0), (-88, 0), (-96, 0), (-104, 0), (0, -70), (0, -90),
+                                               (-88, 60), (-50, -52)])
+@pytest.mark.parametrize("n_q", [1, 40])
+def test_ties_of_small_scores(key_exp, query_exp, n_q):
+    _case(n_q, (6400, 3000), 32, 640, 0, n_q, n_q > 1, _small(key_exp, query_exp))
