@@ -334,7 +334,7 @@ clsa_status clsa_project_append8(const clsa_shape *shape, int32_t block, int32_t
 
 /* clsa_sparse_attn over the 8-bit cache: the same index lists (of clsa_topk or
  * clsa_block_topk), outputs, conventions and errors.  Logits, softmax and sums in
- * fp32; each weight times its value's scale is rounded to bf16 for the product with
+ * fp32, q . k before softmax_scale is applied; each weight times its value's scale is rounded to bf16 for the product with
  * the values, whose weighted sums are made in fp32 before they are divided (values
  * from 2^108 on can overflow there).  A NaN in the cache reaches the rows that select
  * its token, and no others.  Workspace: CLSA_OP_ATTN8. */

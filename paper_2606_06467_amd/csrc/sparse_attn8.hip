@@ -5,12 +5,13 @@
 // One workgroup = one (query row, KV head or four of them, range of the row's keys): 1, 4
 // or 8 waves, see plan_splits8.  A wave takes 32 tokens at a time, on its own, with its
 // own online softmax; the states of a head's waves are merged by the log-sum-exp rule at
-// the end, and the ranges' by the merge kernels of sparse_attn.hip.  For the products the bytes become bf16,
-// which holds every e4m3 value; the scales stay outside: a logit is multiplied by
-// its token's key scale, and a weight by its value scale before it is rounded to
-// bf16 (at most 2^-8 of it, of either sign, averaged over the keys).  (The 8-bit matrix
-// instructions would save the conversions, but they align the products that they add:
-// 2^-17 of the sum of magnitudes off on normal values, 2^-13 at worst, 2^-24 in bf16.)
+// the end, and the ranges' by the merge kernels of sparse_attn.hip.  For the products the
+// bytes become bf16: the keys' times their scale, which is exact, so that the sum of a
+// logit is q . k itself (of bytes alone it can overflow where q . k does not); the values'
+// without theirs, by which a weight is multiplied before it is rounded to bf16 (at most
+// 2^-8 of it, of either sign, averaged over the keys).  (The 8-bit matrix instructions
+// would save the conversions, but they align the products that they add: 2^-17 of the
+// sum of magnitudes off on normal values, 2^-13 at worst, 2^-24 in bf16.)
 //
 // Per 32 tokens: lane l loads token (l & 31)'s index (and page) and one of its two
 // scales, 8 lanes load a token's 128-byte row 16 bytes each (4 loads for K, 4 for
@@ -80,12 +81,12 @@ __device__ __forceinline__ u32x4 load16(const uint8_t *p) {
     return *reinterpret_cast<const u32x4 *>(p);
 }
 
-// 8 e4m3 bytes -> 8 bf16 (exact)
-__device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi) {
-    const bf16x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
-    const bf16x2 p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
-    const bf16x2 p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false);
-    const bf16x2 p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+// 8 e4m3 bytes times a scale -> 8 bf16 (exact: the scale is a power of two)
+__device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi, float scale) {
+    const bf16x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+    const bf16x2 p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+    const bf16x2 p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+    const bf16x2 p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
     return bf16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
 }
 
@@ -211,7 +212,6 @@ __global__ __launch_bounds__(64 * HW * TW, 4) void attn8_kernel(Attn8Args a) {
     const size_t head = (PAGED ? 0 : (size_t)b * a.max_len * row_bytes) + g * kA8Dim;
     const uint8_t *kbase = a.k + head, *vbase = a.v + head;
     const float *scales = (half ? a.v_scale : a.k_scale) + (PAGED ? 0 : (size_t)b * nblk * a.kv_heads) + g;
-    const float scale_log2 = half ? 1.0f : a.scale_log2;  // goes into the key scales
     uint8_t(*sk)[kA8Pitch] = s.rows[wave][0], (*sv)[kA8Pitch] = s.rows[wave][1];
     // Cache row of this lane's token: an entry clamped into the sequence, for a token past
     // the end the step's first one (with weight 0).
@@ -263,7 +263,7 @@ __global__ __launch_bounds__(64 * HW * TW, 4) void attn8_kernel(Attn8Args a) {
         j1 = entry(first + 2 * STEP);
     }
     for (int c0 = first; c0 < end; c0 += STEP) {
-        s_sc[wave][half][tl] = sc * scale_log2;
+        s_sc[wave][half][tl] = sc;
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
             *reinterpret_cast<u32x4 *>(&sk[8 * x + (lane >> 3)][(lane & 7) * 16]) = kr[x];
@@ -279,21 +279,21 @@ __global__ __launch_bounds__(64 * HW * TW, 4) void attn8_kernel(Attn8Args a) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             c[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            const float ks = s_sc[wave][0][16 * t + sub];
             const u32x4 lo = *reinterpret_cast<const u32x4 *>(&sk[16 * t + sub][32 * qq]);
             const u32x4 hi = *reinterpret_cast<const u32x4 *>(&sk[16 * t + sub][32 * qq + 16]);
-            c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(lo[0], lo[1]), qb[0], c[t], 0, 0, 0);
-            c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(lo[2], lo[3]), qb[1], c[t], 0, 0, 0);
-            c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(hi[0], hi[1]), qb[2], c[t], 0, 0, 0);
-            c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(hi[2], hi[3]), qb[3], c[t], 0, 0, 0);
+            c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(lo[0], lo[1], ks), qb[0], c[t], 0, 0, 0);
+            c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(lo[2], lo[3], ks), qb[1], c[t], 0, 0, 0);
+            c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(hi[0], hi[1], ks), qb[2], c[t], 0, 0, 0);
+            c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(hi[2], hi[3], ks), qb[3], c[t], 0, 0, 0);
         }
         float z[E], p[E];
         spread<F>(c, z);  // this lane's E logits: token slots 16 (part * E >> 2) + 4 qq + ...
-        const float *ksc = &s_sc[wave][0][16 * (part * E >> 2) + 4 * qq + (part * E & 3)];
         const float *vsc = &s_sc[wave][1][16 * (part * E >> 2) + 4 * qq + (part * E & 3)];
         float vs[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            z[e] *= ksc[e];
+            z[e] *= a.scale_log2;
             vs[e] = vsc[e];
         }
         if (c0 + kA8Tokens > end)  // uniform: tokens past the end
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(64 * HW * TW, 4) void attn8_kernel(Attn8Args a) {
             const int j8 = (lane & 15) >> 1;  // token of the 8 that this lane's address names
             const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
                 (lds2 *)&sv[(j8 & 4 ? 12 : 0) + 4 * qq + j8][16 * d + 8 * (lane & 1)]);
-            acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa, widen8((uint32_t)v[0], (uint32_t)v[1]),
+            acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa, widen8((uint32_t)v[0], (uint32_t)v[1], 1.0f),
                                                              acc[d], 0, 0, 0);
         }
         __builtin_amdgcn_wave_barrier();

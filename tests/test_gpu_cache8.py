@@ -430,3 +430,26 @@ def test_another_stream():
                 B.clsa_sparse_attn8(sh, 32, *args, out, lse, ws)
         st.synchronize()
         C.check_attention(B.bits_from_bf16(out), lse.cpu().numpy().astype(np.float64), want)
+
+
+@pytest.mark.parametrize("key_exp,query_exp,scale_exp", [(-100, 120, -28), (119, -119, -8)])
+@pytest.mark.parametrize("lens,heads,group,n_q,k", [
+    ((300, 200), 2, 4, 1, 128), ((400,), 4, 2, 200, 140), ((900, 333), 2, 5, 1, 0), ((200, 77), 2, 2, 9, 0),
+    ((3500,), 2, 5, 70, 0)])
+def test_logits_of_large_and_small_factors(lens, heads, group, n_q, k, key_exp, query_exp, scale_exp):
+    """Logits are finite where the products of the queries with the bytes alone are not (lists of k
+    tokens; k = 0: dense, the last case in key tiles)."""
+    g = np.random.default_rng(n_q + k)
+    p = Pair(*(C.filled(90 + i, lens, heads, 32, max(lens)) for i in (1, 2)))
+    p.k.scale[:] = 2.0 ** key_exp
+    p.push()
+    qv, q = C.bf16(g.standard_normal((len(lens), n_q, heads * group, 128)) * 2.0 ** query_exp)
+    scale = 2.0 ** scale_exp
+    sh = _shape(len(lens), n_q, max(lens), heads, 0, k or 64, group, softmax_scale=scale)
+    if k:
+        idx, ns, sets = _sets(g, lens, n_q, k)
+        out, lse = _attend(p, sh, 32, q, idx, ns)
+    else:
+        sets = [[np.arange(n)] * n_q for n in lens]
+        out, lse = _attend(p, sh, 32, q, lens=lens)
+    C.check_attention(out, lse, C.attention(qv, p.k, p.v, sets, scale))
