@@ -244,7 +244,16 @@ def clsa_kd_loss(shape, abar, q_idx, k_idx, page_table, seq_lens, q_pos, loss, d
                               _ptr(ws, "ws"), wsb, _stream(stream)), "clsa_kd_loss")
 
 
-_Tensor, _raw_stream = torch.Tensor, torch._C._cuda_getCurrentRawStream
+_Tensor = torch.Tensor
+
+
+def _stream_object(device):
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+# The current stream's raw handle: making a torch Stream object takes 3 us, as long as the
+# library's call.  It is no public name of torch, and a torch built without a GPU lacks it.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _stream_object)
 
 
 def _call(where, shape, block, names, tensors, ws, stream, sizes=()):
@@ -271,7 +280,6 @@ def _call(where, shape, block, names, tensors, ws, stream, sizes=()):
     if device >= 0 and device != torch.cuda.current_device():
         with torch.cuda.device(device):
             return _call(where, shape, block, names, tensors, ws, stream, sizes)
-    # the raw handle: making a torch Stream object takes 3 us, as long as the library's call
     raw = _raw_stream(max(device, 0)) if stream is None else stream.cuda_stream
     status = getattr(_lib_handle or lib(), where)(ctypes.byref(shape), block, *args, raw)
     if status != CLSA_OK:

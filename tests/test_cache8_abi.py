@@ -1,6 +1,7 @@
 """Host-only checks of the 8-bit cache and block routing entry points: what they refuse
 (before anything is enqueued), their workspaces, and the tests' own e4m3 reference."""
 import ctypes
+import importlib.util
 import types
 
 import numpy as np
@@ -142,3 +143,17 @@ def test_binding_refuses_what_is_no_gpu_tensor():
         B.clsa_block_topk(_shape(), 64, [1.0], t, None, t, None, t, t)
     with pytest.raises(B.ClsaError, match="CLSA_ERR_INVALID_ARG"):
         B.clsa_block_means(_shape(), 64, None, None, None, None, None, stream=types.SimpleNamespace(cuda_stream=0))
+
+
+def test_binding_where_torch_has_no_raw_stream_handle(monkeypatch):
+    """Such a torch loads the binding; a call takes the handle of torch's stream object."""
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream")
+    spec = importlib.util.spec_from_file_location("binding_alone", B.__file__)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    asked = []
+    monkeypatch.setattr(torch.cuda, "current_stream",
+                        lambda device=None: asked.append(device) or types.SimpleNamespace(cuda_stream=0))
+    with pytest.raises(m.ClsaError, match="CLSA_ERR_INVALID_ARG"):
+        m.clsa_block_means(m.make_shape(2, 1, 1024, 128), 64, None, None, None, None, None)
+    assert asked == [0]
