@@ -223,6 +223,13 @@ hipError_t launch_append8(const Geometry &g, int block, const void *k, const voi
 hipError_t launch_block_means(const Geometry &g, int block, const void *k_idx,
                               const int32_t *start, const int32_t *count,
                               const int32_t *page_table, void *means, hipStream_t stream);
+// How attention by rows is cut: heads and token groups per workgroup, key ranges per row
+// (keys: top_k, or dense max_len).
+struct Plan8 {
+    int heads, waves;   // KV heads of a workgroup, waves of each
+    int splits, span;   // key ranges per row, keys per range
+};
+Plan8 plan_splits8(const Geometry &g, int keys, bool dense);
 // Partial buffer floats of the two attention calls below (0 with one split).
 size_t sparse_attn8_floats(const Geometry &g);
 size_t dense_attn8_floats(const Geometry &g);

@@ -376,11 +376,6 @@ __global__ __launch_bounds__(64 * HW * TW, 4) void attn8_kernel(Attn8Args a) {
     }
 }
 
-// How a call is cut: heads and token groups per workgroup, key ranges per row.
-struct Plan8 {
-    int heads, waves;   // KV heads of a workgroup, waves of each
-    int splits, span;   // key ranges per row, keys per range
-};
 // Index lists: kA8ManyUnits (row, KV head) pairs or more take one wave and one range each
 // (800 pairs of 2048 keys 57 us against 66 in workgroups of four waves, 512 pairs 52
 // against 41).  From kA8StretchUnits pairs, twice what is resident, on, lists of 1024 keys
@@ -400,7 +395,7 @@ struct Plan8 {
 // sequences of 32768 keys 87 us against 95 with one head; 32 of 1000 keys 21.6 against
 // 18.6).  Several rows per sequence find each other's bytes in the caches: four workgroups
 // per CU (4 x 8 rows of 8192 keys 39.8 us, 52.5 with one).
-static Plan8 plan_splits8(const Geometry &g, int keys, bool dense) {
+Plan8 plan_splits8(const Geometry &g, int keys, bool dense) {
     Plan8 p{1, 4, 1, 0};
     const long units = (long)g.rows * g.kv_heads;
     const bool paged = g.page_shift >= 0;

@@ -453,3 +453,176 @@ def test_logits_of_large_and_small_factors(lens, heads, group, n_q, k, key_exp, 
         sets = [[np.arange(n)] * n_q for n in lens]
         out, lse = _attend(p, sh, 32, q, lens=lens)
     C.check_attention(out, lse, C.attention(qv, p.k, p.v, sets, scale))
+
+
+class _Plan8(ctypes.Structure):
+    """The library's cut of attention by rows (csrc/clsa_internal.h)."""
+    _fields_ = [(n, ctypes.c_int) for n in ("heads", "waves", "splits", "span")]
+
+
+def _geometry(batch, n_q, max_len, heads, group, page=0, top_k=64, causal=False):
+    return U._Geometry(batch, n_q, batch * n_q, max_len, page.bit_length() - 1, max_len // page if page else 0,
+                       top_k, int(causal), heads * group, heads, group, SCALE)
+
+
+def _plan(keys, dense, *a, **kw):
+    from paper_2606_06467_amd import binding as B
+    f = B.lib()._ZN4clsa12plan_splits8ERKNS_8GeometryEib
+    f.restype = _Plan8
+    p = f(ctypes.byref(_geometry(*a, **kw)), ctypes.c_int(keys), ctypes.c_bool(dense))
+    return p.heads, p.waves, p.splits
+
+
+def _tile_plan(*a, **kw):
+    """Whether dense attention runs over key tiles, and in how many key ranges it would."""
+    from paper_2606_06467_amd import binding as B
+    gm, n, span = _geometry(*a, **kw), ctypes.c_int(), ctypes.c_int()
+    f = B.lib()._ZN4clsa15dense8_in_tilesERKNS_8GeometryE
+    f.restype = ctypes.c_bool
+    B.lib()._ZN4clsa14tile_attn_planERKNS_8GeometryEiRiS3_(ctypes.byref(gm), ctypes.c_int(128), ctypes.byref(n),
+                                                         ctypes.byref(span))
+    return f(ctypes.byref(gm)), n.value
+
+
+def _widen_capacity(p, max_len):
+    """The caches in a larger capacity, what is new in it NaN; the references keep the small one."""
+    import torch
+    if p.k.page:
+        pt = torch.full((len(p.k.pt), max_len // p.k.page), -1, dtype=torch.int32, device="cuda")
+        pt[:, :p.pt.shape[1]] = p.pt
+        p.pt = pt
+        return
+    for name, n, fill in (("k8", max_len, 0x7f), ("v8", max_len, 0x7f), ("ks", -(-max_len // p.k.block), float("nan")),
+                          ("vs", -(-max_len // p.k.block), float("nan"))):
+        x = getattr(p, name)
+        y = torch.full((x.shape[0], n, *x.shape[2:]), fill, dtype=x.dtype, device="cuda")
+        y[:, :x.shape[1]] = x
+        setattr(p, name, y)
+
+
+@pytest.mark.parametrize("page", [0, 64])
+@pytest.mark.parametrize("group,heads", [(1, 4), (2, 4), (4, 8), (5, 4), (8, 4)])
+def test_dense_four_heads_a_workgroup(group, heads, page):
+    """Single tokens over capacities large enough that a workgroup takes four KV heads: key ranges of
+    one to several steps, ragged lengths, rows without keys, and NaN in one head of one sequence."""
+    g = np.random.default_rng(100 + group)
+    lens, block, capacity = (0, 1, 333, 2100, 640, 3001, 1280, 641, 0), 32, 131072 // heads
+    batch, small = len(lens), 3008
+    heads_, waves, splits = _plan(capacity, True, batch, 1, capacity, heads, group, page)
+    assert (heads_, waves) == (4, 1) and splits > 8
+    pt = C.page_table(group, lens, page, small) if page else None
+    p = Pair(*(C.filled(100 + group + i, lens, heads, block, small, page, pt) for i in (1, 2)))
+    p.k.bytes[p.k.at(3, 2040)][1, 7] = 0xff
+    p.v.bytes[p.v.at(5, 70)][3, 9] = 0x7f
+    p.push()
+    _widen_capacity(p, capacity)
+    qv, q = C.bf16(g.standard_normal((batch, 1, heads * group, 128)))
+    out, lse = _attend(p, _shape(batch, 1, capacity, heads, page, 64, group), block, q, lens=lens)
+    C.check_attention(out, lse, C.attention(qv, p.k, p.v, [[np.arange(n)] for n in lens], SCALE))
+
+
+def _sampled(p, sh, block, qv, q, lens, q_pos, valid, at):
+    out, lse = _attend(p, sh, block, q, lens=lens, q_pos=q_pos)
+    want = C.attention(qv[:, at], p.k, p.v, [[np.arange(v[t]) for t in at] for v in valid], SCALE)
+    C.check_attention(out[:, at], lse[:, at], want)
+
+
+@pytest.mark.parametrize("group,heads,n_q,lens,page,block,causal", [
+    (8, 4, 701, (701, 0, 433), 0, 16, True), (8, 4, 701, (701, 0, 433), 64, 64, True),
+    (5, 4, 1303, (1303, 700, 0), 128, 32, True), (5, 4, 1303, (1303, 700, 0), 0, 128, True),
+    (4, 8, 1025, (1100, 1), 0, 64, False), (2, 8, 1040, (1111, 64, 1000, 65), 16, 16, True),
+    (1, 8, 2100, (2100, 1500, 700, 2000), 0, 32, True)])
+@pytest.mark.parametrize("of", [None, "k", "v"])
+def test_dense_tiles_in_one_range(group, heads, n_q, lens, page, block, causal, of):
+    """Whole prompts: tiles whose workgroups write their rows' results themselves (checked on some rows
+    of every kind); with a NaN token in the first sequence."""
+    g = np.random.default_rng(n_q + page)
+    batch, max_len = len(lens), -(-max(lens) // (page or 1)) * (page or 1)
+    assert _tile_plan(batch, n_q, max_len, heads, group, page, 64, causal) == (True, 1)
+    pt = C.page_table(n_q, lens, page, max_len) if page else None
+    p = Pair(*(C.filled(n_q + i, lens, heads, block, max_len, page, pt) for i in (1, 2)))
+    if of:
+        c = getattr(p, of)
+        c.bytes[c.at(0, 333)][heads - 1, 7] = 0x7f
+        p.push()
+    qv, q = C.bf16(g.standard_normal((batch, n_q, heads * group, 128)))
+    q_pos, valid = None, [[n] * n_q for n in lens]
+    if causal:
+        q_pos = np.array([[n - n_q + t for t in range(n_q)] for n in lens], np.int32)
+        valid = [[max(0, n - n_q + t + 1) for t in range(n_q)] for n in lens]
+    # the first sequence's rows on both sides of the NaN token, the first and last ones, some more
+    nan_row = 333 - (lens[0] - n_q)
+    at = sorted({0, 1, 31, 32, 63, 64, nan_row - 1, nan_row, n_q - 2, n_q - 1, *g.integers(0, n_q, size=8).tolist()})
+    _sampled(p, _shape(batch, n_q, max_len, heads, page, 64, group, causal), block, qv, q, lens, q_pos, valid, at)
+
+
+@pytest.mark.parametrize("group,heads,n_q,lens,page,causal", [
+    (2, 4, 300, (700, 520), 64, True), (5, 4, 600, (600,), 0, True), (8, 4, 33, (4000,), 0, False),
+    (4, 2, 100, (3000, 1), 64, True), (4, 4, 500, (500,), 0, True)])
+@pytest.mark.parametrize("of", [None, "k", "v"])
+def test_dense_near_the_border_of_both_forms(group, heads, n_q, lens, page, causal, of):
+    """Shapes whose two prices lie near each other, in the form that the library takes for them."""
+    g = np.random.default_rng(n_q)
+    batch, max_len = len(lens), -(-max(lens) // (page or 1)) * (page or 1)
+    pt = C.page_table(n_q, lens, page, max_len) if page else None
+    p = Pair(*(C.filled(n_q + i, lens, heads, 32, max_len, page, pt) for i in (1, 2)))
+    nan_at = lens[0] - n_q // 2
+    if of:
+        c = getattr(p, of)
+        c.bytes[c.at(0, nan_at)][0, 100] = 0xff
+        p.push()
+    qv, q = C.bf16(g.standard_normal((batch, n_q, heads * group, 128)))
+    q_pos, valid = None, [[n] * n_q for n in lens]
+    if causal:
+        q_pos = np.array([[n - n_q + t for t in range(n_q)] for n in lens], np.int32)
+        valid = [[max(0, n - n_q + t + 1) for t in range(n_q)] for n in lens]
+    nan_row = n_q - n_q // 2
+    at = sorted({0, 1, 31, 32, nan_row - 1, nan_row, n_q - 1, *g.integers(0, n_q, size=8).tolist()})
+    _sampled(p, _shape(batch, n_q, max_len, heads, page, 64, group, causal), 32, qv, q, lens, q_pos, valid, at)
+
+
+@pytest.mark.parametrize("page,block", [(16, 16), (64, 32), (256, 128)])
+def test_sparse_paged_many_rows(page, block):
+    """One wave a workgroup over pages in any order: lists of many steps that end anywhere in one."""
+    g = np.random.default_rng(page)
+    n_q, heads, group, k, lens = 200, 4, 2, 900, (1500,)
+    max_len = -(-1500 // page) * page
+    assert _plan(k, False, 1, n_q, max_len, heads, group, page, k) == (1, 1, 1)
+    counts = [list(g.integers(0, k + 1, size=n_q))]
+    counts[0][:12] = [0, 1, 31, 32, 33, 63, 64, 65, 95, 96, 97, k]
+    _sparse_case(page, lens, heads, group, k, block, page, n_q, counts)
+
+
+@pytest.mark.parametrize("k,n_q,capacity", [(1030, 1030, 25088), (1500, 1025, 70016)])
+@pytest.mark.parametrize("page", [64, 4096])
+def test_sparse_paged_rows_by_stretches(page, k, n_q, capacity):
+    """Lists cut into stretches, over pages (checked on some rows of every kind)."""
+    g = np.random.default_rng(k + page)
+    n, heads, block = 2000, 8, 32
+    capacity = -(-capacity // page) * page
+    assert _plan(k, False, 1, n_q, capacity, heads, 1, page, k)[2] > 1
+    pt = C.page_table(k, (n,), page, capacity)
+    p = Pair(*(C.filled(k + i, (n,), heads, block, capacity, page, pt) for i in (1, 2)))
+    counts = [list(np.where(g.random(n_q) < 0.3, g.integers(0, k + 1, size=n_q), k))]
+    counts[0][:5] = [0, 1, k // 8, k // 8 + 1, k - 1]
+    qv, q = C.bf16(g.standard_normal((1, n_q, heads, 128)))
+    idx, ns, sets = _sets(g, (n,), n_q, k, counts)
+    out, lse = _attend(p, _shape(1, n_q, capacity, heads, page, k), block, q, idx, ns)
+    at = [*range(8), *g.integers(0, n_q, size=40), n_q - 1]
+    C.check_attention(out[:, at], lse[:, at], C.attention(qv[:, at], p.k, p.v, [[sets[0][t] for t in at]], SCALE))
+
+
+@pytest.mark.parametrize("page,block,k", [(16, 16, 1000), (64, 32, 2048), (128, 128, 1777), (64, 64, 8192)])
+@pytest.mark.parametrize("heads", [1, 8])
+def test_sparse_paged_long_lists(page, block, k, heads):
+    """Few rows over pages in any order: several steps a wave, or several ranges, ending anywhere."""
+    n = 3000 if k < 8192 else 8500
+    counts = [[m] for m in (k, k - 1, 0, 1, 255, 256, 257, 511, 513, k // 2 + 3, 97)]
+    _sparse_case(k + heads, [n] * len(counts), heads, 2, k, block, page, 1, counts)
+
+
+def test_sparse_paged_long_lists_of_several_rows():
+    """2 to 31 rows a sequence, as in checking several proposed tokens at once."""
+    g = np.random.default_rng(7)
+    _sparse_case(77, (2500, 2200, 1999), 2, 4, 1200, 64, 64, 5, [list(g.integers(0, 1201, size=5)) for _ in range(3)])
+    _sparse_case(78, (2500, 2200), 2, 5, 700, 32, 0, 31, [list(g.integers(0, 701, size=31)) for _ in range(2)])
