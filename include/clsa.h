@@ -334,17 +334,19 @@ clsa_status clsa_project_append8(const clsa_shape *shape, int32_t block, int32_t
 
 /* clsa_sparse_attn over the 8-bit cache: the same index lists (of clsa_topk or
  * clsa_block_topk), outputs, conventions and errors.  Logits, softmax and sums in
- * fp32, q . k before softmax_scale is applied; each weight times its value's scale is rounded to bf16 for the product with
- * the values, whose weighted sums are made in fp32 before they are divided (values
- * from 2^108 on can overflow there).  A NaN in the cache reaches the rows that select
- * its token, and no others.  Workspace: CLSA_OP_ATTN8. */
+ * fp32 (q . k before softmax_scale is applied); each weight times its value's scale
+ * enters the product with the values as two bf16, with 16 bits; the weighted sums are
+ * made in fp32 before they are divided (values from 2^108 on can overflow there).  A NaN
+ * in the cache reaches the rows that select its token, and no others.  Workspace:
+ * CLSA_OP_ATTN8. */
 clsa_status clsa_sparse_attn8(const clsa_shape *shape, int32_t block, const void *q, const void *k8,
                               const void *v8, const float *k_scale, const float *v_scale,
                               const int32_t *page_table, const int32_t *idx, const int32_t *n_sel,
                               void *out, float *lse, void *ws, size_t ws_bytes, void *stream);
 
 /* clsa_dense_attn over the 8-bit cache, with the conventions of clsa_sparse_attn8 (a NaN
- * reaches the rows that see its token).  Workspace: CLSA_OP_DENSE8. */
+ * reaches the rows that see its token).  Where many rows share key tiles, as the bf16
+ * call's do, each weight is rounded to one bf16.  Workspace: CLSA_OP_DENSE8. */
 clsa_status clsa_dense_attn8(const clsa_shape *shape, int32_t block, const void *q, const void *k8,
                              const void *v8, const float *k_scale, const float *v_scale,
                              const int32_t *page_table, const int32_t *seq_lens,

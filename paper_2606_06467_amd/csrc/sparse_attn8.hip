@@ -8,8 +8,11 @@
 // the end, and the ranges' by the merge kernels of sparse_attn.hip.  For the products the
 // bytes become bf16: the keys' times their scale, which is exact, so that the sum of a
 // logit is q . k itself (of bytes alone it can overflow where q . k does not); the values'
-// without theirs, by which a weight is multiplied before it is rounded to bf16 (at most
-// 2^-8 of it, of either sign, averaged over the keys).  (The 8-bit matrix instructions
+// without theirs, by which a weight is multiplied.  A weight enters its product in two
+// bf16 pieces, its rounding and what that left, 2^-16 of it off: the second takes rows of
+// the matrix operand that a group's few heads leave empty, so it costs no product (1% of
+// the lists of 1024 rows, 0.1 us of a single one), and the outputs' error is their own
+// rounding, 0.00166 (0.0019 to 0.0022 with one piece).  (The 8-bit matrix instructions
 // would save the conversions, but they align the products that they add: 2^-17 of the
 // sum of magnitudes off on normal values, 2^-13 at worst, 2^-24 in bf16.)
 //
@@ -96,9 +99,16 @@ __device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi, float scale) 
 // softmax works on all lanes.  DPP moves whose bank mask picks the lanes that are
 // written (a bank: 4 lanes); row rotations by 4, 8 and 12.
 template <int CTRL, int BANKS>
+__device__ __forceinline__ uint32_t dpp_put(uint32_t old, uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)x, CTRL, 0xf, BANKS, false);
+}
+template <int CTRL, int BANKS>
 __device__ __forceinline__ float dpp_into(float old, float x) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(old), __float_as_int(x), CTRL, 0xf,
-                                                      BANKS, false));
+    return __uint_as_float(dpp_put<CTRL, BANKS>(__float_as_uint(old), __float_as_uint(x)));
+}
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_take(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xf, 0xf, false);
 }
 template <int F, int E>
 __device__ __forceinline__ void spread(const f32x4 (&c)[2], float (&z)[E]) {
@@ -113,21 +123,31 @@ __device__ __forceinline__ void spread(const f32x4 (&c)[2], float (&z)[E]) {
         }
     }
 }
-// Back to the lanes (qq, head) as bf16: the A operand (other lanes: rows past the heads).
+__device__ __forceinline__ uint32_t pair_bf16(float x, float y) {
+    return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x, (__bf16)y});
+}
+// Back to the lanes (qq, head) as bf16: the A operand's rows of the heads.  The 16 / F rows
+// behind them take what the rounding left of the same weights (lane banks 1, or 2 and 3).
 template <int F, int E>
 __device__ __forceinline__ bf16x8 collect(const float (&p)[E]) {
     u32x4 w;
+    uint32_t x[E / 2], y[E / 2];
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e) {
+        x[e] = pair_bf16(p[2 * e], p[2 * e + 1]);
+        y[e] = pair_bf16(p[2 * e] - bf16_lo(x[e]), p[2 * e + 1] - bf16_hi(x[e]));
+    }
+    constexpr int kSame = 0xe4;  // quad permute: every lane itself
     if constexpr (F == 4) {
-        const uint32_t x = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)p[0], (__bf16)p[1]});
-        w[0] = x;
-        w[1] = (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x12c, 0xf, 0xf, false);
-        w[2] = (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x128, 0xf, 0xf, false);
-        w[3] = (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x124, 0xf, 0xf, false);
+        w[0] = dpp_put<0x124, 0x2>(x[0], y[0]);
+        w[1] = dpp_put<kSame, 0x2>(dpp_take<0x12c>(x[0]), y[0]);
+        w[2] = dpp_put<0x12c, 0x2>(dpp_take<0x128>(x[0]), y[0]);
+        w[3] = dpp_put<0x128, 0x2>(dpp_take<0x124>(x[0]), y[0]);
     } else {
-        w[0] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)p[0], (__bf16)p[1]});
-        w[1] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)p[2], (__bf16)p[3]});
-        w[2] = (uint32_t)__builtin_amdgcn_mov_dpp((int)w[0], 0x128, 0xf, 0xf, false);
-        w[3] = (uint32_t)__builtin_amdgcn_mov_dpp((int)w[1], 0x128, 0xf, 0xf, false);
+        w[0] = dpp_put<0x128, 0xc>(x[0], y[0]);
+        w[1] = dpp_put<0x128, 0xc>(x[1], y[1]);
+        w[2] = dpp_put<kSame, 0xc>(dpp_take<0x128>(x[0]), y[0]);
+        w[3] = dpp_put<kSame, 0xc>(dpp_take<0x128>(x[1]), y[1]);
     }
     return __builtin_bit_cast(bf16x8, w);
 }
@@ -159,10 +179,10 @@ __global__ __launch_bounds__(64 * HW * TW, 4) void attn8_kernel(Attn8Args a) {
     constexpr int NW = HW * TW;
     constexpr int F = G <= 4 ? 4 : 2, E = 8 / F;  // lanes that share a head's logits; each one's share
     constexpr int STEP = kA8Tokens * TW;  // tokens that the waves of a head take at a time
-    // the waves' staged K and V rows; at the end their weighted values [NW][G * 128]
+    // the waves' staged K and V rows; at the end their weighted values
     __shared__ __align__(16) union {
         uint8_t rows[NW][2][kA8Tokens][kA8Pitch];
-        float red[NW][G * kA8Dim];
+        float red[NW][2][G * kA8Dim + 16];  // padded: the two rows of a head in other banks
     } s;
     __shared__ __align__(16) float s_sc[NW][2][kA8Tokens];  // key, value scales of the 32 tokens
     __shared__ float s_ml[NW][G][2];
@@ -338,10 +358,12 @@ __global__ __launch_bounds__(64 * HW * TW, 4) void attn8_kernel(Attn8Args a) {
     const float l_run = head_sum<F>(l_part);
     __syncthreads();  // the staged rows become the reduction's
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-        if (4 * qq + r < G)
+    for (int r = 0; r < 4; ++r) {  // row h, and 16 / F rows on what rounding left of its weights
+        const int at = 4 * qq + r, h = at & (16 / F - 1);
+        if (h < G && at < 32 / F)
 #pragma unroll
-            for (int d = 0; d < 8; ++d) s.red[wave][(4 * qq + r) * kA8Dim + 16 * d + sub] = acc[d][r];
+            for (int d = 0; d < 8; ++d) s.red[wave][at / (16 / F)][h * kA8Dim + 16 * d + sub] = acc[d][r];
+    }
     if (qq == 0 && sub < G) {
         s_ml[wave][sub][0] = m_run;
         s_ml[wave][sub][1] = l_run;
@@ -360,7 +382,8 @@ __global__ __launch_bounds__(64 * HW * TW, 4) void attn8_kernel(Attn8Args a) {
             const float mw = s_ml[w * HW + w0][h][0];
             const float fw = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - m);
             l = fmaf(fw, s_ml[w * HW + w0][h][1], l);
-            sum = fmaf(fw, s.red[w * HW + w0][h * kA8Dim + dim], sum);
+            const float *red = &s.red[w * HW + w0][0][h * kA8Dim + dim];
+            sum = fmaf(fw, red[0] + red[G * kA8Dim + 16], sum);
         }
         if (a.splits == 1) {
             a.out[(h0 + hh) * kA8Dim + dim] = (uint16_t)f32_to_bf16_bits(sum / l);

@@ -626,3 +626,47 @@ def test_sparse_paged_long_lists_of_several_rows():
     g = np.random.default_rng(7)
     _sparse_case(77, (2500, 2200, 1999), 2, 4, 1200, 64, 64, 5, [list(g.integers(0, 1201, size=5)) for _ in range(3)])
     _sparse_case(78, (2500, 2200), 2, 5, 700, 32, 0, 31, [list(g.integers(0, 701, size=31)) for _ in range(2)])
+
+
+@pytest.mark.parametrize("lens,heads,group,n_q,k,page", [
+    ((300, 260), 2, 4, 1, 256, 0), ((700, 600), 1, 1, 1, 600, 64), ((500,), 2, 2, 400, 450, 0),
+    ((500, 400), 4, 5, 100, 400, 64), ((400, 300), 2, 8, 1, 0, 0), ((900, 800), 2, 5, 1, 0, 64),
+    ((600, 200), 2, 8, 7, 0, 0)])
+def test_weights_keep_16_bits(lens, heads, group, n_q, k, page):
+    """Logits that fp32 holds exactly, so that the weights' rounding is what the outputs show beside their own.
+
+    A weight is off by 2^-8 of what its first piece left, 2^-16 of it; the exponent's product with the scale
+    by 2^-24 of up to 40, twice with the maximum's, and the exponential by a few 2^-24 (2^-17 in all), of
+    which the sum of weights carries as much; both sums over n keys by n 2^-24, the merging by 2^-20."""
+    g = np.random.default_rng(heads + n_q + k)
+    max_len = -(-max(lens) // page) * page if page else max(lens)
+    pt = C.page_table(n_q, lens, page, max_len) if page else None
+    p = Pair(*(C.filled(95 + i, lens, heads, 32, max_len, page, pt) for i in (1, 2)))
+    held = (p.k.bytes & 0x7f) != 0x7f
+    p.k.bytes[held] = C.encode(g.integers(-4, 5, size=p.k.bytes.shape).astype(np.float64))[held]
+    p.k.scale[:] = 1.0
+    p.push()
+    qv = g.integers(-4, 5, size=(len(lens), n_q, heads * group, 128)).astype(np.float64)
+    q, scale = C.bf16(qv)[1], 2.0 ** -5
+    sh = _shape(len(lens), n_q, max_len, heads, page, k or 64, group, softmax_scale=scale)
+    if k:
+        idx, ns, sets = _sets(g, lens, n_q, k)
+        out = _attend(p, sh, 32, q, idx, ns, with_lse=False)[0]
+    else:
+        assert not _tile_plan(len(lens), n_q, max_len, heads, group, page)[0]
+        sets = [[np.arange(n)] * n_q for n in lens]
+        out = _attend(p, sh, 32, q, lens=lens, with_lse=False)[0]
+    out = inputs.f32_from_bf16_bits(out).astype(np.float64)
+    for b, n in enumerate(lens):
+        kb, vb = p.k.rows(b, n), p.v.rows(b, n)
+        for t in range(0, n_q, 1 if n_q < 50 else 17):
+            for h in range(heads * group):
+                z = kb[sets[b][t], h // group] @ qv[b, t, h] * scale
+                w = np.exp(z - z.max())
+                w /= w.sum()
+                v = vb[sets[b][t], h // group]
+                o = w @ v
+                tol = w @ np.abs(v) * (2.0 ** -16 + 2 * 2.0 ** -17 + 2 * len(z) * 2.0 ** -24 + 2.0 ** -20) + \
+                    2.0 ** -8 * np.abs(o) * 1.001
+                off = np.abs(out[b, t, h] - o) / tol
+                assert off.max() <= 1.0, (b, t, h, off.max())
