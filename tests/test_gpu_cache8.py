@@ -670,3 +670,23 @@ def test_weights_keep_16_bits(lens, heads, group, n_q, k, page):
                     2.0 ** -8 * np.abs(o) * 1.001
                 off = np.abs(out[b, t, h] - o) / tol
                 assert off.max() <= 1.0, (b, t, h, off.max())
+
+
+@pytest.mark.parametrize("value_exp", [-100, 96])
+@pytest.mark.parametrize("lens,heads,group,n_q,k", [
+    ((300, 200), 2, 4, 1, 128), ((400,), 4, 5, 200, 140), ((900, 333), 2, 8, 1, 0), ((3500,), 2, 5, 70, 0)])
+def test_smallest_and_large_values(lens, heads, group, n_q, k, value_exp):
+    """Value scales at their least, and as large as sums of values may be (k = 0: dense, the last in tiles)."""
+    g = np.random.default_rng(n_q + k)
+    p = Pair(*(C.filled(97 + i, lens, heads, 32, max(lens)) for i in (1, 2)))
+    p.v.scale[:] = 2.0 ** value_exp
+    p.push()
+    qv, q = C.bf16(g.standard_normal((len(lens), n_q, heads * group, 128)))
+    sh = _shape(len(lens), n_q, max(lens), heads, 0, k or 64, group)
+    if k:
+        idx, ns, sets = _sets(g, lens, n_q, k)
+        out, lse = _attend(p, sh, 32, q, idx, ns)
+    else:
+        sets = [[np.arange(n)] * n_q for n in lens]
+        out, lse = _attend(p, sh, 32, q, lens=lens)
+    C.check_attention(out, lse, C.attention(qv, p.k, p.v, sets, SCALE))
