@@ -15,12 +15,12 @@
 // The scoring reads the means once (1 / block of the index keys); a workgroup then
 // chooses a row's blocks, holding their scores in registers, and writes its list.
 //
-// What bounds it.  Single tokens: 4 sequences of 2048 blocks 4.3 us of scoring and 7.4 of
-// choosing (17 500 cycles of barriers, LDS and memory latency one after another, 36 000 at
-// first); 32 sequences of 512 to 2048 blocks 7.4 us of scoring, 44 MB of means at 5.9 TB/s.
-// 4096 rows of 2048 blocks: scoring 17.6 us (operands straight from memory, which asks for
-// half lines, took 40.8), choosing 31 us, of which the scores read and lists written, 67 MB,
-// need 14.
+// What bounds it.  Single tokens: 4 sequences of 2048 blocks 4.3 us of scoring and 7.3 of
+// choosing, which is barriers, LDS and memory latency one after another (790 vector and 93
+// LDS instructions in a wave's 20 000 cycles); 32 sequences of 512 to 2048 blocks 8 us of
+// scoring, 44 MB of means at 5.5 TB/s.  4096 rows of 2048 blocks: scoring 17.5 us (operands
+// straight from memory, which asks for half lines, took 40.8), choosing 31 us, of which the
+// scores read and lists written, 67 MB, need 14.
 #include "clsa_internal.h"
 #include "device_common.h"
 
@@ -264,8 +264,8 @@ static size_t choose_lds_bytes(int nblk, int chosen) {
 // order-preserving keys in registers.  The want-th largest is found by a histogram in LDS
 // of the top 11 bits (bins of a quarter octave: some thirty of 2048 scores share the
 // wanted one) and a count of each such key against the others, or, where more than 256
-// keys share it, by two more histograms.  (Bit by bit with ballots and a barrier each
-// it took 20000 of the kernel's 36000 cycles, with three histograms 7500 of 17500.)
+// keys share it, by two more histograms.  (Routing of 4 x 128K: 22.5 us bit by bit, with
+// ballots and a barrier each; 16.3 with three histograms; 13.0 now.)
 template <int VPL, int NW, bool PAGED>
 __global__ __launch_bounds__(64 * NW, 4) void block_choose_kernel(RouteArgs a) {
     constexpr int NT = 64 * NW, WORDS = VPL * NW;
@@ -421,8 +421,8 @@ __global__ __launch_bounds__(64 * NW, 4) void block_choose_kernel(RouteArgs a) {
                     number[s_before[wave][i * NW + wave] + __popcll(band & below)] = (uint16_t)(NT * i + tid);
             }
             __syncthreads();
-            // a wave per undecided block: lane holds dimensions 4 lane ..+ 4 (a thread per block,
-            // its 256 additions one after another, took 13500 cycles for two or three blocks)
+            // a wave per undecided block: lane holds dimensions 4 lane ..+ 4 (with a thread per
+            // block, its 256 additions one after another, 32 ragged sequences 25.4 us; so 19.4)
             for (int p = wave; p < within; p += NW) {
                 const uint2 v = *reinterpret_cast<const uint2 *>(mean_row<PAGED>(a, b, number[p]) + 4 * lane);
                 double sum = q[4 * lane] * (double)bf16_lo(v.x);

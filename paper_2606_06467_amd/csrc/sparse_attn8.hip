@@ -25,15 +25,15 @@
 // tokens (4 qq + r, 16 + 4 qq + r) whose weights make up the lane's A row of head sub.
 // The next step's rows are in flight while one is computed.
 //
-// What bounds it (times of a call's kernels in a row of calls).  Dense, 8 x 32768 keys:
-// memory, 537 MB in 82 us, 6.6 TB/s.  Lists of 32 sequences, 134 MB: the gather of 128-byte
-// vectors, 31 us (a kernel that only loads them takes 31.2; 26 where a workgroup takes
-// whole 1 KB rows, which the joining of more ranges eats up).  4 x 2048 of 131072 keys
-// 9.1 us, one sequence 6.2 to 6.9: launches and four dependent memory latencies.  1024
-// rows of 2048 out of 65536 keys, 20 / 4 heads, 139 us: 2.27 GB asked of the L2 at 16 TB/s,
-// 77% found there (20 where all of it is); vector instructions (150 a step and wave) and
-// matrix products come to 95 us beside it.  (K read straight into operand registers,
-// without LDS: 238 us, since a wave then asks for half lines.)
+// What bounds it (times of a call's kernels in a row of calls whose inputs change).  Dense,
+// 8 x 32768 keys: memory, 537 MB in 79 to 82 us, 6.6 to 6.8 TB/s.  Lists of 32 sequences,
+// 134 MB: the gather of 128-byte vectors, 34 us (a kernel that only loads them takes
+// 31.2; 26 where a workgroup takes whole 1 KB rows, which the joining of more ranges eats
+// up).  4 x 2048 of 131072 keys 9.4 us, one sequence 6.0 to 6.9: launches and four
+// dependent memory latencies.  1024 rows of 2048 out of 65536 keys, 20 / 4 heads, 141 us:
+// 17.9 million requests of 128 bytes to the L2, 2.29 GB at 16 TB/s, 77% found there; beside
+// it 160 vector instructions and 16 matrix products a step and wave.  (K read straight
+// into operand registers, without LDS: 238 us, since a wave then asks for half lines.)
 #include "clsa_internal.h"
 #include "device_common.h"
 
@@ -461,6 +461,12 @@ static size_t partial_floats8(const Geometry &g, int keys, bool dense) {
 
 size_t sparse_attn8_floats(const Geometry &g) { return partial_floats8(g, g.top_k, false); }
 
+// Key tiles where they are priced below the rows' gathers, by the price that the bf16 shapes
+// gave (tile_attn_dense).  It holds here: of 260 shapes (16 to 4096 rows, 48 to 40000 keys,
+// 1 to 32 sequences, groups of 1 to 8, contiguous and paged; 14 to 19 ps per (row, KV head,
+// key) gathered) it takes the slower form by more than 2% for 13 and by more than 20% for
+// five, all of rows with few keys: 28 sequences x 35 rows x 94 keys, 20 / 4 heads 31.9 us by
+// rows and 15.5 in tiles, 4 x 266 x 267, 32 / 8 64 and 38.
 bool dense8_in_tiles(const Geometry &g) {
     return tile_attn_dense(g, plan_splits8(g, g.max_len, true).splits);
 }
