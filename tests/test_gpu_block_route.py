@@ -399,3 +399,38 @@ def _small(key_exp, query_exp):
 @pytest.mark.parametrize("n_q", [1, 40])
 def test_ties_of_small_scores(key_exp, query_exp, n_q):
     _case(n_q, (6400, 3000), 32, 640, 0, n_q, n_q > 1, _small(key_exp, query_exp))
+
+
+def test_captured_choice_of_many_blocks():
+    """The largest form, captured first and replayed between eager calls with other inputs."""
+    import torch
+    from paper_2606_06467_amd import binding as B
+    g = torch.Generator(device="cuda").manual_seed(3)
+    sh = _shape(2, 1, 262144, 512)
+    lens = torch.tensor([262144, 150001], dtype=torch.int32, device="cuda")
+    means = torch.zeros((2, 16384, 256), dtype=torch.bfloat16, device="cuda")
+    sides = []
+    for _ in "ge":
+        sides.append((torch.zeros((2, 1, 256), dtype=torch.bfloat16, device="cuda"), means, None, lens, None,
+                      torch.zeros((2, 1, 512), dtype=torch.int32, device="cuda"),
+                      torch.zeros((2, 1), dtype=torch.int32, device="cuda"),
+                      B.workspace(sh, B.CLSA_OP_BLOCK_TOPK, 16)))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.clsa_block_topk(sh, 16, *sides[0])
+    for _ in range(4):
+        means.copy_(torch.randn(means.shape, generator=g, device="cuda") / 64)
+        for s in sides:
+            s[0].copy_(torch.randn(s[0].shape, generator=torch.Generator(device="cuda").manual_seed(5), device="cuda"))
+        graph.replay()
+        B.clsa_block_topk(sh, 16, *sides[1])
+        torch.cuda.synchronize()
+        for a, b in zip(sides[0][5:7], sides[1][5:7]):
+            assert torch.equal(a, b)
+        z = (means.double() @ sides[0][0].double().transpose(1, 2)).squeeze(-1)
+        for b, n in enumerate(lens.tolist()):
+            own = (n - 1) // 16
+            best = set(torch.topk(z[b, :own], 31).indices.tolist()) | {own}
+            want = sorted(c * 16 + i for c in best for i in range(16) if c * 16 + i < n)
+            assert sides[0][5][b, 0, :len(want)].tolist() == want and int(sides[0][6][b, 0]) == len(want)

@@ -690,3 +690,59 @@ def test_smallest_and_large_values(lens, heads, group, n_q, k, value_exp):
         sets = [[np.arange(n)] * n_q for n in lens]
         out, lse = _attend(p, sh, 32, q, lens=lens)
     C.check_attention(out, lse, C.attention(qv, p.k, p.v, sets, SCALE))
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.25, 3.0])
+@pytest.mark.parametrize("lens,heads,group,n_q,page,tiles", [
+    ((300, 0, 201), 3, 4, 1, 0, False), ((2100, 1999), 3, 5, 4, 64, False), ((3500, 2900), 3, 2, 70, 64, True)])
+def test_dense_softmax_scale(lens, heads, group, n_q, page, tiles, scale):
+    g = np.random.default_rng(n_q)
+    max_len = -(-max(lens) // page) * page if page else max(lens)
+    assert _tile_plan(len(lens), n_q, max_len, heads, group, page, 64, True)[0] == tiles
+    pt = C.page_table(n_q, lens, page, max_len) if page else None
+    p = Pair(*(C.filled(98 + i, lens, heads, 32, max_len, page, pt) for i in (1, 2)))
+    qv, q = C.bf16(g.standard_normal((len(lens), n_q, heads * group, 128)))
+    q_pos = np.array([[n - n_q + t for t in range(n_q)] for n in lens], np.int32)
+    sets = [[np.arange(max(0, n - n_q + t + 1)) for t in range(n_q)] for n in lens]
+    sh = _shape(len(lens), n_q, max_len, heads, page, 64, group, True, softmax_scale=scale)
+    out, lse = _attend(p, sh, 32, q, lens=lens, q_pos=q_pos)
+    C.check_attention(out, lse, C.attention(qv, p.k, p.v, sets, np.float32(scale)))
+
+
+@pytest.mark.parametrize("n_q,k,capacity", [(1030, 1500, 70016), (1, 2048, 4096), (40, 300, 4096)])
+def test_captured_lists(n_q, k, capacity):
+    """Lists in stretches, in ranges and whole, replayed between eager calls with other queries and lists."""
+    import torch
+    from paper_2606_06467_amd import binding as B
+    g = np.random.default_rng(k)
+    n, heads = 3000, 8
+    p = Pair(*(C.filled(k + i, (n,), heads, 64, n) for i in (1, 2)))
+    _widen_capacity(p, capacity)
+    sh = _shape(1, n_q, capacity, heads, 0, k)
+    bufs = []
+    for _ in "ge":
+        q = torch.zeros((1, n_q, heads, 128), dtype=torch.bfloat16, device="cuda")
+        bufs.append((q, torch.full((1, n_q, k), -1, dtype=torch.int32, device="cuda"),
+                     torch.zeros((1, n_q), dtype=torch.int32, device="cuda"), torch.zeros_like(q),
+                     torch.zeros((1, n_q, heads), device="cuda"), B.workspace(sh, B.CLSA_OP_ATTN8)))
+
+    def call(q, idx, ns, out, lse, ws):
+        B.clsa_sparse_attn8(sh, 64, q, p.k8, p.v8, p.ks, p.vs, None, idx, ns, out, lse, ws)
+
+    call(*bufs[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(*bufs[0])
+    for _ in range(3):
+        idx, ns, _ = _sets(g, (n,), n_q, k, [list(g.integers(0, k + 1, size=n_q))])
+        q = _bf16(C.bf16(g.standard_normal((1, n_q, heads, 128)))[1])
+        for b in bufs:
+            b[0].copy_(q)
+            b[1].copy_(torch.from_numpy(idx))
+            b[2].copy_(torch.from_numpy(ns))
+        graph.replay()
+        call(*bufs[1])
+        torch.cuda.synchronize()
+        for a, b in zip(bufs[0][3:5], bufs[1][3:5]):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
