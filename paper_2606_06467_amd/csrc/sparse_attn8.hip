@@ -382,8 +382,8 @@ __global__ __launch_bounds__(64 * HW * TW, 4) void attn8_kernel(Attn8Args a) {
             const float mw = s_ml[w * HW + w0][h][0];
             const float fw = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - m);
             l = fmaf(fw, s_ml[w * HW + w0][h][1], l);
-            const float *red = &s.red[w * HW + w0][0][h * kA8Dim + dim];
-            sum = fmaf(fw, red[0] + red[G * kA8Dim + 16], sum);
+            const auto &red = s.red[w * HW + w0];
+            sum = fmaf(fw, red[0][h * kA8Dim + dim] + red[1][h * kA8Dim + dim], sum);
         }
         if (a.splits == 1) {
             a.out[(h0 + hh) * kA8Dim + dim] = (uint16_t)f32_to_bf16_bits(sum / l);
