@@ -101,7 +101,10 @@ typedef enum {
 enum {
     CLSA_DEVERR_SEQ_LEN = 1, /* a seq_lens[b] outside [0, max_len] was clamped        */
     CLSA_DEVERR_N_SEL = 2,   /* an n_sel[r] outside [0, top_k] was clamped            */
-    CLSA_DEVERR_APPEND = 4   /* start / count of appended tokens that do not fit      */
+    CLSA_DEVERR_APPEND = 4,  /* start / count of appended tokens that do not fit      */
+    CLSA_DEVERR_ADAPTER = 8, /* an adapter[b] outside [-1, n_adapters): none was used */
+    CLSA_DEVERR_PAGES = 16   /* clsa_pages_*: a page or slot number out of range, or  */
+                             /* fewer free pages than needed                          */
 };
 
 typedef enum {
@@ -115,7 +118,12 @@ typedef enum {
     CLSA_OP_ATTN8 = 7,     /* clsa_sparse_attn8 */
     CLSA_OP_DENSE8 = 8,    /* clsa_dense_attn8 */
     CLSA_OP_BLOCK_TOPK = 9, /* clsa_block_topk (n_layers: the block)  */
-    CLSA_OP_PROJECT8 = 10  /* clsa_project_append8 */
+    CLSA_OP_PROJECT8 = 10, /* clsa_project_append8 */
+    CLSA_OP_ADAPTED = 11,  /* clsa_project_append_adapted (n_layers: the rank)       */
+    CLSA_OP_ADAPTED8 = 12, /* clsa_project_append8_adapted (n_layers: the rank)      */
+    CLSA_OP_NORM_GRAD = 13, /* clsa_residual_norm_grad (n_layers: d_model)           */
+    CLSA_OP_PAGES_RESERVE = 14, /* clsa_pages_reserve                                */
+    CLSA_OP_PAGES_COMPACT = 15  /* clsa_pages_compact (n_layers: num_pages)          */
 } clsa_op;
 
 typedef struct clsa_shape {
@@ -137,7 +145,8 @@ typedef struct clsa_shape {
 
 /* Bytes of workspace `op` needs for `shape` (n_layers matters for
  * CLSA_OP_KD_TARGET, whose statistics buffer grows with the layer count, and for
- * CLSA_OP_BLOCK_TOPK, where it holds the tokens per block;
+ * CLSA_OP_BLOCK_TOPK, where it holds the tokens per block; the operations below it
+ * in clsa_op say there what it holds for them;
  * for CLSA_OP_DECODE it never changes the size: layers reuse the same buffers).
  * Returns 0 for CLSA_OP_INDEX, and also 0 when the shape is invalid or
  * unsupported (the entry point then reports the reason). */
@@ -382,6 +391,127 @@ clsa_status clsa_block_topk(const clsa_shape *shape, int32_t block, const void *
                             const void *means, const int32_t *page_table, const int32_t *seq_lens,
                             const int32_t *q_pos, int32_t *idx, int32_t *n_sel, void *ws,
                             size_t ws_bytes, void *stream);
+
+/* ---- Projections with an adapter of each request ----
+ *
+ * clsa_project_append with a low-rank addition to the weights that each sequence chooses:
+ *   feature f of row (b,t) = bf16( sum_i h_i w[f,i]
+ *        + alpha[m] * sum_j B[m,f,j] * (sum_i A[m,j,i] h_i) ),   m = adapter[b],
+ * over all features of w (index query, index key, K and V of every head).
+ *   a        bf16 [n_adapters, rank, d_model]
+ *   b        bf16 [n_adapters, 512 + 2*kv_heads*head_dim, rank]
+ *   alpha    fp32 [n_adapters]
+ *   adapter  int32 [batch]; -1: the sequence has none.  A number outside
+ *            [-1, n_adapters) counts as -1 and raises CLSA_DEVERR_ADAPTER.
+ * rank: a multiple of 8 up to 128, the same for all adapters (fill up smaller ones with
+ * zeros).  bf16 inputs; fp32 products and sums, one rounding at the end; with many rows
+ * the inner sum enters its product with B as two bf16, with 16 bits.  One adapter's
+ * infinities and NaN stay with the sequences that use it.  Everything else as in
+ * clsa_project_append.  Workspace: CLSA_OP_ADAPTED, whose size asks for the rank in
+ * n_layers. */
+clsa_status clsa_project_append_adapted(const clsa_shape *shape, int32_t d_model,
+                                        int32_t n_adapters, int32_t rank, const void *h,
+                                        const void *w, const void *a, const void *b,
+                                        const float *alpha, const int32_t *adapter,
+                                        const int32_t *pos, const int32_t *page_table, void *q_idx,
+                                        void *k_idx, void *k_cache, void *v_cache, void *ws,
+                                        size_t ws_bytes, void *stream);
+
+/* The same beside clsa_project_append8, into the 8-bit cache.  Workspace:
+ * CLSA_OP_ADAPTED8 (n_layers: the rank). */
+clsa_status clsa_project_append8_adapted(const clsa_shape *shape, int32_t block, int32_t d_model,
+                                         int32_t n_adapters, int32_t rank, const void *h,
+                                         const void *w, const void *a, const void *b,
+                                         const float *alpha, const int32_t *adapter,
+                                         const int32_t *start, const int32_t *count,
+                                         const int32_t *page_table, void *q_idx, void *k_idx,
+                                         void *k8, void *v8, float *k_scale, float *v_scale,
+                                         void *ws, size_t ws_bytes, void *stream);
+
+/* ---- The norm in front of the projections ----
+ *
+ * For every row r of the batch * n_q rows (up to 2^22) of d_model values (a multiple of 8
+ * up to 16384; nothing else of the shape is read):
+ *   s = bf16(x + residual) (x itself if residual is NULL),
+ *   rstd = 1 / sqrt(mean(s^2) + eps),   y = s * rstd * weight.
+ * x, residual, sum, y: bf16 [batch, n_q, d_model]; weight: bf16 [d_model].  sum receives s
+ * and may be x or residual; so may y.  The norm is that of the rounded s, which goes on as
+ * the residual stream.  y8 receives y as e4m3 bytes over y_scale, fp32 [batch, n_q,
+ * ceil(d_model / group)], one power of two for each `group` consecutive values of a row (32,
+ * 64, 128, or d_model: one a row; the last group of a row may be shorter): the least 2^e
+ * (e >= -100) that holds the group's largest finite magnitude within 448 * 2^e; infinities
+ * and NaN are held as NaN.  rstd: fp32 [batch, n_q].  sum, rstd, and one of y and y8 may be
+ * NULL (y_scale with y8; group then is not read).  The squares are summed in 64 bits, the
+ * rest is fp32, rounded once.  eps: a normal fp32 value above zero.  Needs no workspace. */
+clsa_status clsa_residual_norm(const clsa_shape *shape, int32_t d_model, double eps, int32_t group,
+                               const void *x, const void *residual, const void *weight, void *sum,
+                               void *y, void *y8, float *y_scale, float *rstd, void *stream);
+
+/* Its backward pass, from s and rstd as above: with g = dy * weight and xhat = s * rstd,
+ *   dx = dsum + rstd * (g - xhat * mean(g * xhat)),   dweight = sum over rows of dy * xhat.
+ * dy: bf16, the gradient of y; dsum: bf16, that of s from what follows it, or NULL; dx: bf16,
+ * the gradient of s, i.e. of x and of residual alike (may be dy or dsum).  dweight: fp32
+ * [d_model], added up in an order that the sizes alone decide.  fp32 products and sums.
+ * Workspace: CLSA_OP_NORM_GRAD, whose size asks for d_model in n_layers. */
+clsa_status clsa_residual_norm_grad(const clsa_shape *shape, int32_t d_model, const void *s,
+                                    const float *rstd, const void *weight, const void *dy,
+                                    const void *dsum, void *dx, float *dweight, void *ws,
+                                    size_t ws_bytes, void *stream);
+
+/* ---- Pages of the shared cache among many sequences ----
+ *
+ * For paged shapes.  refs: int32 [num_pages] (num_pages up to 2^24), the holders of each
+ * physical page: the entries of page_table that name it, and whatever else the caller
+ * counts there (a prefix kept for later sequences).  A page with refs 0 is free.  Entries
+ * of page_table are -1 where a sequence has no page; other numbers outside
+ * [0, num_pages) count as -1 and raise CLSA_DEVERR_PAGES.  refs that do not count the
+ * table's entries give undefined tables, never an access outside the buffers.
+ * The tensors of the cache (index keys, K, V, and what else has a row for each page: scales,
+ * block keys) are a host array, which the call copies: */
+typedef struct clsa_paged {
+    void *data;         /* [num_pages, page_bytes], 4-byte aligned (16 for full speed) */
+    int64_t page_bytes; /* a multiple of 4 (16 for full speed), up to 2^30             */
+} clsa_paged;           /* up to 16 of them; they must not overlap                     */
+
+/* Every slot b of the batch takes the pages of slot parent[b] as they were before the
+ * call, and its length: b itself leaves it as it is, -1 empties it, and any other slot makes
+ * b a fork that shares all of that slot's pages (also if that one changes or is emptied by
+ * the same call).  Pages that a slot no longer holds lose a holder.  parent: int32
+ * [batch]; a number outside [-1, batch) leaves the slot as it is and raises
+ * CLSA_DEVERR_PAGES.  seq_lens: int32 [batch].  batch up to 16384. */
+clsa_status clsa_pages_fork(const clsa_shape *shape, int32_t num_pages, const int32_t *parent,
+                            int32_t *page_table, int32_t *seq_lens, int32_t *refs, void *stream);
+
+/* Makes positions start[b] .. start[b]+count[b]-1 of every sequence writable (count up to
+ * n_q; ranges and errors as in clsa_cache_append8): where the table has no page for them it gets a
+ * free one, and where it has a page with other holders it gets a free page with a copy of
+ * that one's content in every tensor, and the old page loses a holder.  If all holders of
+ * a page write to it in this call, the last of them (the highest b) keeps it.  Pages are
+ * taken in ascending order, for sequences and positions in ascending order.  Where fewer pages are
+ * free than needed nothing is changed, *missing (int32) receives the number that lacks,
+ * and CLSA_DEVERR_PAGES is raised; else *missing is 0.  batch * ceil(n_q / page_size)
+ * below about 2^24.  n_tensors may be 0 (the tables alone).  Workspace:
+ * CLSA_OP_PAGES_RESERVE. */
+clsa_status clsa_pages_reserve(const clsa_shape *shape, int32_t num_pages, int32_t n_tensors,
+                               const clsa_paged *tensors, const int32_t *start,
+                               const int32_t *count, int32_t *page_table, int32_t *refs,
+                               int32_t *missing, void *ws, size_t ws_bytes, void *stream);
+
+/* Moves pages to the front of the pool: with U pages in use, the pages from U on, in
+ * ascending order, to the free pages below U, in ascending order, with their content in
+ * every tensor, their refs and the table's entries.  A page with holders beside the
+ * table's entries stays where it is.  *bound (int32) receives 1 + the highest page in use:
+ * what lies from there on is free.  Workspace: CLSA_OP_PAGES_COMPACT, whose size asks for
+ * num_pages in n_layers. */
+clsa_status clsa_pages_compact(const clsa_shape *shape, int32_t num_pages, int32_t n_tensors,
+                               const clsa_paged *tensors, int32_t *page_table, int32_t *refs,
+                               int32_t *bound, void *ws, size_t ws_bytes, void *stream);
+
+/* Copies page src[i] to page dst[i] in every tensor, for i < n (int32 [n] each); a pair
+ * with src -1 is skipped, one with a number outside [0, num_pages) too, and raises
+ * CLSA_DEVERR_PAGES.  No dst may be another pair's src or dst.  Needs no workspace. */
+clsa_status clsa_pages_copy(int32_t num_pages, int32_t n_tensors, const clsa_paged *tensors,
+                            int32_t n, const int32_t *src, const int32_t *dst, void *stream);
 
 /* Static, human-readable name of a status code. */
 const char *clsa_status_string(clsa_status status);

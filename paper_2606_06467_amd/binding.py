@@ -37,6 +37,11 @@ CLSA_OP_ATTN8 = 7
 CLSA_OP_DENSE8 = 8
 CLSA_OP_BLOCK_TOPK = 9
 CLSA_OP_PROJECT8 = 10
+CLSA_OP_ADAPTED = 11
+CLSA_OP_ADAPTED8 = 12
+CLSA_OP_NORM_GRAD = 13
+CLSA_OP_PAGES_RESERVE = 14
+CLSA_OP_PAGES_COMPACT = 15
 
 
 class ClsaError(RuntimeError):
@@ -54,6 +59,11 @@ class ClsaShape(ctypes.Structure):
                 ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32),
                 ("top_k", ctypes.c_int32), ("causal", ctypes.c_int32),
                 ("softmax_scale", ctypes.c_float)]
+
+
+class ClsaPaged(ctypes.Structure):
+    """Mirror of ``clsa_paged``."""
+    _fields_ = [("data", ctypes.c_void_p), ("page_bytes", ctypes.c_int64)]
 
 
 def make_shape(batch: int, n_q: int, max_len: int, top_k: int, *, idx_heads: int = 4,
@@ -79,7 +89,7 @@ def lib() -> ctypes.CDLL:
                            "(there is no fallback implementation)")
     L = ctypes.CDLL(LIB_PATH)
     P, SP = ctypes.c_void_p, ctypes.POINTER(ClsaShape)
-    i32, i64, sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+    i32, i64, sz, dbl = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_double
     sig = {
         "clsa_workspace_bytes": (sz, [SP, i32, i32]),
         "clsa_index_scores": (i32, [SP, P, P, P, P, P, P, P]),
@@ -99,6 +109,15 @@ def lib() -> ctypes.CDLL:
         "clsa_dense_attn8": (i32, [SP, i32, P, P, P, P, P, P, P, P, P, P, P, sz, P]),
         "clsa_block_means": (i32, [SP, i32, P, P, P, P, P, P]),
         "clsa_block_topk": (i32, [SP, i32, P, P, P, P, P, P, P, P, sz, P]),
+        "clsa_project_append_adapted": (i32, [SP, i32, i32, i32, P, P, P, P, P, P, P, P, P, P, P, P, P, sz, P]),
+        "clsa_project_append8_adapted": (i32, [SP, i32, i32, i32, i32, P, P, P, P, P, P, P, P, P, P, P, P, P,
+                                               P, P, P, sz, P]),
+        "clsa_residual_norm": (i32, [SP, i32, dbl, i32, P, P, P, P, P, P, P, P, P]),
+        "clsa_residual_norm_grad": (i32, [SP, i32, P, P, P, P, P, P, P, P, sz, P]),
+        "clsa_pages_fork": (i32, [SP, i32, P, P, P, P, P]),
+        "clsa_pages_reserve": (i32, [SP, i32, i32, P, P, P, P, P, P, P, sz, P]),
+        "clsa_pages_compact": (i32, [SP, i32, i32, P, P, P, P, P, sz, P]),
+        "clsa_pages_copy": (i32, [i32, i32, P, i32, P, P, P]),
         "clsa_status_string": (ctypes.c_char_p, [i32]),
         "clsa_set_phase_events": (i32, [ctypes.POINTER(P), i32]),
         "clsa_get_device_error": (i32, [ctypes.POINTER(ctypes.c_uint32)]),
@@ -256,11 +275,12 @@ def _stream_object(device):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _stream_object)
 
 
-def _call(where, shape, block, names, tensors, ws, stream, sizes=()):
-    """An entry point of the 8-bit cache or of block routing: numbers after the block, its tensors
-    and their names, and its workspace (False: it takes none).  The call runs on the tensors'
-    device; their stream is the current one of that device unless one is given."""
-    args, device = [*sizes], -1
+def _call(where, shape, block, names, tensors, ws, stream, sizes=(), device=-1):
+    """An entry point of the 8-bit cache or of what came after it: numbers after the block (or
+    d_model, or the pool's pages), its tensors and their names, and its workspace (False: it takes
+    none).  The call runs on the tensors' device (that of tensors among the numbers: device); their
+    stream is the current one of that device unless one is given."""
+    args, given = [*sizes], device
     for i, t in enumerate(tensors):
         if t is None:
             args.append(None)
@@ -279,9 +299,10 @@ def _call(where, shape, block, names, tensors, ws, stream, sizes=()):
         args += None, 0
     if device >= 0 and device != torch.cuda.current_device():
         with torch.cuda.device(device):
-            return _call(where, shape, block, names, tensors, ws, stream, sizes)
+            return _call(where, shape, block, names, tensors, ws, stream, sizes, given)
     raw = _raw_stream(max(device, 0)) if stream is None else stream.cuda_stream
-    status = getattr(_lib_handle or lib(), where)(ctypes.byref(shape), block, *args, raw)
+    head = (block,) if shape is None else (ctypes.byref(shape), block)
+    status = getattr(_lib_handle or lib(), where)(*head, *args, raw)
     if status != CLSA_OK:
         raise ClsaError(status, where)
 
@@ -332,9 +353,90 @@ def clsa_block_topk(shape, block, q_idx, means, page_table, seq_lens, q_pos, idx
           (q_idx, means, page_table, seq_lens, q_pos, idx, n_sel), ws, stream)
 
 
+def clsa_project_append_adapted(shape, d_model, h, w, a, b, alpha, adapter, pos, page_table, q_idx, k_idx,
+                                k_cache, v_cache, ws=None, stream=None):
+    """a: [adapters, rank, d_model], b: [adapters, features, rank]."""
+    _call("clsa_project_append_adapted", shape, d_model,
+          ("h", "w", "a", "b", "alpha", "adapter", "pos", "page_table", "q_idx", "k_idx", "k_cache", "v_cache"),
+          (h, w, a, b, alpha, adapter, pos, page_table, q_idx, k_idx, k_cache, v_cache), ws, stream,
+          a.shape[:2])
+
+
+def clsa_project_append8_adapted(shape, block, d_model, h, w, a, b, alpha, adapter, start, count, page_table,
+                                 q_idx, k_idx, k8, v8, k_scale, v_scale, ws=None, stream=None):
+    _call("clsa_project_append8_adapted", shape, block,
+          ("h", "w", "a", "b", "alpha", "adapter", "start", "count", "page_table", "q_idx", "k_idx", "k8", "v8",
+           "k_scale", "v_scale"),
+          (h, w, a, b, alpha, adapter, start, count, page_table, q_idx, k_idx, k8, v8, k_scale, v_scale), ws,
+          stream, (d_model, *a.shape[:2]))
+
+
+def clsa_residual_norm(shape, d_model, eps, x, residual, weight, sum=None, y=None, y8=None, y_scale=None,
+                       rstd=None, stream=None, *, group=128):
+    _call("clsa_residual_norm", shape, d_model,
+          ("x", "residual", "weight", "sum", "y", "y8", "y_scale", "rstd"),
+          (x, residual, weight, sum, y, y8, y_scale, rstd), False, stream, (eps, group))
+
+
+def clsa_residual_norm_grad(shape, d_model, s, rstd, weight, dy, dsum, dx, dweight, ws=None, stream=None):
+    _call("clsa_residual_norm_grad", shape, d_model,
+          ("s", "rstd", "weight", "dy", "dsum", "dx", "dweight"),
+          (s, rstd, weight, dy, dsum, dx, dweight), ws, stream)
+
+
+def _paged(tensors, pages):
+    """The host array of a paged cache's tensors, their number and their device."""
+    n, device = len(tensors), -1
+    arr = (ClsaPaged * max(1, n))()
+    for i, t in enumerate(tensors):
+        if not isinstance(t, _Tensor):
+            raise TypeError(f"tensors[{i}] must be a torch.Tensor")
+        at = t.get_device()
+        if at < 0 or not t.is_contiguous() or (at != device and device >= 0):
+            _refuse(f"tensors[{i}]", t)
+        if t.dim() < 1 or t.shape[0] != pages:
+            raise ValueError(f"tensors[{i}] must have one row for each of the {pages} pages of refs")
+        device = at
+        arr[i].data = t.data_ptr()
+        arr[i].page_bytes = t.nbytes // pages
+    return n, arr, device
+
+
+def clsa_pages_fork(shape, parent, page_table, seq_lens, refs, stream=None):
+    _call("clsa_pages_fork", shape, refs.numel(), ("parent", "page_table", "seq_lens", "refs"),
+          (parent, page_table, seq_lens, refs), False, stream)
+
+
+def clsa_pages_reserve(shape, tensors, start, count, page_table, refs, missing, ws=None, stream=None):
+    """tensors: the cache's tensors, each with a leading dimension of refs.numel() pages."""
+    pages = refs.numel()
+    n, arr, device = _paged(tensors, pages)
+    _call("clsa_pages_reserve", shape, pages, ("start", "count", "page_table", "refs", "missing"),
+          (start, count, page_table, refs, missing), ws, stream, (n, arr), device)
+
+
+def clsa_pages_compact(shape, tensors, page_table, refs, bound, ws=None, stream=None):
+    pages = refs.numel()
+    n, arr, device = _paged(tensors, pages)
+    _call("clsa_pages_compact", shape, pages, ("page_table", "refs", "bound"), (page_table, refs, bound), ws,
+          stream, (n, arr), device)
+
+
+def clsa_pages_copy(tensors, src, dst, stream=None):
+    """Pages src[i] to dst[i] of every tensor (they have the same number of pages)."""
+    pages = tensors[0].shape[0] if tensors else 1
+    n, arr, device = _paged(tensors, pages)
+    if src.numel() != dst.numel():
+        raise ValueError("src and dst must have one length")
+    _call("clsa_pages_copy", None, pages, ("src", "dst"), (src, dst), False, stream, (n, arr, src.numel()),
+          device)
+
+
 CLSA_DEVERR_SEQ_LEN = 1
 CLSA_DEVERR_N_SEL = 2
 CLSA_DEVERR_APPEND = 4
+CLSA_DEVERR_ADAPTER = 8
+CLSA_DEVERR_PAGES = 16
 
 
 def clsa_get_device_error() -> int:
@@ -358,7 +460,9 @@ def clsa_set_phase_events(events: Optional[Sequence[int]]) -> None:
 
 def workspace(shape: ClsaShape, op: int, n_layers: int = 0, device="cuda") -> Optional[torch.Tensor]:
     """A device byte tensor large enough for ``op`` (None if none is needed); for
-    CLSA_OP_BLOCK_TOPK ``n_layers`` is the tokens per block."""
+    CLSA_OP_BLOCK_TOPK ``n_layers`` is the tokens per block, for CLSA_OP_ADAPTED and
+    CLSA_OP_ADAPTED8 the rank, for CLSA_OP_NORM_GRAD d_model, for CLSA_OP_PAGES_COMPACT the
+    pool's pages."""
     n = clsa_workspace_bytes(shape, op, n_layers)
     if n == 0:
         return None

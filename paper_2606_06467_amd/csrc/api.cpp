@@ -3,6 +3,7 @@
 // call clsa_get_device_error synchronises.
 #include "clsa.h"
 
+#include <float.h>
 #include <math.h>
 #include <stdint.h>
 
@@ -252,6 +253,53 @@ clsa::Cache8 cache8(const void *k8, const void *v8, const float *k_scale, const 
     return {k8, v8, k_scale, v_scale, page_table, log2i(block)};
 }
 
+// Adapters beside the projections.
+clsa_status check_adapters(int32_t n, int32_t rank, const void *a, const void *b,
+                           const float *alpha, const int32_t *adapter) {
+    if (n < 1 || rank < 1) return CLSA_ERR_INVALID_ARG;
+    if (rank % 8 || rank > clsa::kMaxRank) return CLSA_ERR_UNSUPPORTED;
+    CLSA_TRY(check_ptr(a, 16));
+    CLSA_TRY(check_ptr(b, 16));
+    CLSA_TRY(check_ptr(alpha, 4));
+    CLSA_TRY(check_ptr(adapter, 4));
+    return CLSA_OK;
+}
+
+bool rank_supported(int32_t rank) { return rank >= 8 && rank <= clsa::kMaxRank && rank % 8 == 0; }
+
+// alpha A h of every row.
+size_t adapted_bytes(const Geometry &g, int32_t rank) {
+    return align_up(sizeof(float) * (size_t)g.rows * rank);
+}
+
+// A shape whose rows alone matter, and the width of a row.
+clsa_status check_norm(const clsa_shape *s, int32_t d_model) {
+    if (!s || s->batch < 1 || s->n_q < 1 || d_model < 1) return CLSA_ERR_INVALID_ARG;
+    if ((int64_t)s->batch * s->n_q > clsa::kNormMaxRows || !clsa::norm_supported(d_model))
+        return CLSA_ERR_UNSUPPORTED;
+    return CLSA_OK;
+}
+
+// A paged shape, the pool's pages and its tensors.
+static_assert(sizeof(clsa_paged) == sizeof(clsa::PagedTensor), "one layout");
+clsa_status check_pool(const clsa_shape *s, int32_t pages, Geometry *g) {
+    CLSA_TRY(check_shape(s, 0u, g));
+    if (!s->page_size || pages < 1) return CLSA_ERR_INVALID_ARG;
+    return pages <= clsa::kMaxPoolPages ? CLSA_OK : CLSA_ERR_UNSUPPORTED;
+}
+
+clsa_status check_paged(int32_t n, const clsa_paged *t, clsa::PagedTensor *out) {
+    if (n < 0 || (n > 0 && !t)) return CLSA_ERR_INVALID_ARG;
+    if (n > clsa::kMaxPaged) return CLSA_ERR_UNSUPPORTED;
+    for (int i = 0; i < n; ++i) {
+        CLSA_TRY(check_ptr(t[i].data, 4));
+        if (t[i].page_bytes < 4 || t[i].page_bytes % 4) return CLSA_ERR_INVALID_ARG;
+        if (t[i].page_bytes > (int64_t)1 << 30) return CLSA_ERR_UNSUPPORTED;
+        out[i] = {t[i].data, t[i].page_bytes};
+    }
+    return CLSA_OK;
+}
+
 clsa_status from_hip(hipError_t e) { return e == hipSuccess ? CLSA_OK : CLSA_ERR_HIP; }
 
 }  // namespace
@@ -290,6 +338,19 @@ size_t clsa_workspace_bytes(const clsa_shape *shape, int32_t op, int32_t n_layer
         case CLSA_OP_PROJECT8:
             if (check_shape(shape, kIndex | kAttn, &g) != CLSA_OK) return 0;
             return 2 * project8_row_bytes(g);
+        case CLSA_OP_NORM_GRAD:  // n_layers: d_model
+            if (check_norm(shape, n_layers) != CLSA_OK) return 0;
+            return floats_ws_bytes((size_t)clsa::norm_grad_parts(shape->batch * shape->n_q, n_layers) * n_layers);
+        case CLSA_OP_ADAPTED:    // n_layers: the rank
+        case CLSA_OP_ADAPTED8:
+            if (check_shape(shape, kIndex | kAttn, &g) != CLSA_OK || !rank_supported(n_layers)) return 0;
+            return adapted_bytes(g, n_layers) + (op == CLSA_OP_ADAPTED8 ? 2 * project8_row_bytes(g) : 0);
+        case CLSA_OP_PAGES_RESERVE:
+            if (check_pool(shape, 1, &g) != CLSA_OK || !clsa::reserve_supported(g)) return 0;
+            return align_up(sizeof(int32_t) * clsa::reserve_ws_ints(g));
+        case CLSA_OP_PAGES_COMPACT:  // n_layers: the pool's pages
+            if (check_pool(shape, n_layers, &g) != CLSA_OK) return 0;
+            return align_up(sizeof(int32_t) * clsa::compact_ws_ints(n_layers));
         case CLSA_OP_BLOCK_TOPK:  // n_layers: the block
             if (check_shape(shape, kIndex | kTopk, &g) != CLSA_OK ||
                 check_block(shape, n_layers) != CLSA_OK || g.top_k % n_layers != 0)
@@ -756,6 +817,171 @@ clsa_status clsa_block_topk(const clsa_shape *shape, int32_t block, const void *
                                             n_sel, ws, static_cast<hipStream_t>(stream)));
 }
 
+clsa_status clsa_project_append_adapted(const clsa_shape *shape, int32_t d_model,
+                                        int32_t n_adapters, int32_t rank, const void *h,
+                                        const void *w, const void *a, const void *b,
+                                        const float *alpha, const int32_t *adapter,
+                                        const int32_t *pos, const int32_t *page_table, void *q_idx,
+                                        void *k_idx, void *k_cache, void *v_cache, void *ws,
+                                        size_t ws_bytes, void *stream) {
+    Geometry g;
+    CLSA_TRY(check_shape(shape, kIndex | kAttn, &g));
+    if (d_model < 1) return CLSA_ERR_INVALID_ARG;
+    if (!clsa::project_supported(d_model)) return CLSA_ERR_UNSUPPORTED;
+    CLSA_TRY(check_adapters(n_adapters, rank, a, b, alpha, adapter));
+    CLSA_TRY(check_ptr(h, 16));
+    CLSA_TRY(check_ptr(w, 16));
+    CLSA_TRY(check_ptr(pos, 4));
+    CLSA_TRY(check_ptr(q_idx, 16));
+    CLSA_TRY(check_ptr(k_idx, 16));
+    CLSA_TRY(check_ptr(k_cache, 16));
+    CLSA_TRY(check_ptr(v_cache, 16));
+    CLSA_TRY(check_common(shape, page_table, nullptr, false, true));
+    if (!ws || ws_bytes < adapted_bytes(g, rank) || !aligned(ws, kAlign)) return CLSA_ERR_WORKSPACE;
+    const clsa::Adapters l{a, b, alpha, adapter, n_adapters, rank, static_cast<float *>(ws)};
+    return from_hip(clsa::launch_project_adapted(g, d_model, l, h, w, pos, page_table, q_idx, k_idx,
+                                                 k_cache, v_cache, static_cast<hipStream_t>(stream)));
+}
+
+clsa_status clsa_project_append8_adapted(const clsa_shape *shape, int32_t block, int32_t d_model,
+                                         int32_t n_adapters, int32_t rank, const void *h,
+                                         const void *w, const void *a, const void *b,
+                                         const float *alpha, const int32_t *adapter,
+                                         const int32_t *start, const int32_t *count,
+                                         const int32_t *page_table, void *q_idx, void *k_idx,
+                                         void *k8, void *v8, float *k_scale, float *v_scale,
+                                         void *ws, size_t ws_bytes, void *stream) {
+    Geometry g;
+    CLSA_TRY(check_shape(shape, kIndex | kAttn, &g));
+    CLSA_TRY(check_block(shape, block));
+    if (d_model < 1) return CLSA_ERR_INVALID_ARG;
+    if (!clsa::project_supported(d_model)) return CLSA_ERR_UNSUPPORTED;
+    CLSA_TRY(check_adapters(n_adapters, rank, a, b, alpha, adapter));
+    CLSA_TRY(check_ptr(h, 16));
+    CLSA_TRY(check_ptr(w, 16));
+    CLSA_TRY(check_ptr(start, 4));
+    CLSA_TRY(check_ptr(count, 4));
+    CLSA_TRY(check_ptr(q_idx, 16));
+    CLSA_TRY(check_ptr(k_idx, 16));
+    CLSA_TRY(check_cache8(k8, v8, k_scale, v_scale));
+    CLSA_TRY(check_common(shape, page_table, nullptr, false, true));
+    if (!ws || ws_bytes < 2 * project8_row_bytes(g) + adapted_bytes(g, rank) || !aligned(ws, kAlign))
+        return CLSA_ERR_WORKSPACE;
+    char *k = static_cast<char *>(ws), *v = k + project8_row_bytes(g);
+    const clsa::Adapters l{a, b, alpha, adapter, n_adapters, rank,
+                           reinterpret_cast<float *>(v + project8_row_bytes(g))};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    CLSA_TRY(from_hip(clsa::launch_project_rows_adapted(g, d_model, l, h, w, start, count, page_table,
+                                                        q_idx, k_idx, k, v, st)));
+    return from_hip(clsa::launch_append8(g, block, k, v, start, count, page_table, k8, v8, k_scale,
+                                         v_scale, st));
+}
+
+clsa_status clsa_residual_norm(const clsa_shape *shape, int32_t d_model, double eps, int32_t group,
+                               const void *x, const void *residual, const void *weight, void *sum,
+                               void *y, void *y8, float *y_scale, float *rstd, void *stream) {
+    CLSA_TRY(check_norm(shape, d_model));
+    if (!(eps >= FLT_MIN) || !isfinite(eps)) return CLSA_ERR_INVALID_ARG;
+    CLSA_TRY(check_ptr(x, 16));
+    CLSA_TRY(check_ptr(weight, 16));
+    if (residual) CLSA_TRY(check_ptr(residual, 16));
+    if (sum) CLSA_TRY(check_ptr(sum, 16));
+    if (y) CLSA_TRY(check_ptr(y, 16));
+    if (rstd) CLSA_TRY(check_ptr(rstd, 4));
+    if (!y8 != !y_scale || (!y && !y8)) return CLSA_ERR_INVALID_ARG;
+    if (y8) {
+        CLSA_TRY(check_ptr(y8, 8));
+        CLSA_TRY(check_ptr(y_scale, 4));
+        if (group < 1) return CLSA_ERR_INVALID_ARG;
+        if (group != 32 && group != 64 && group != 128 && group != d_model) return CLSA_ERR_UNSUPPORTED;
+    }
+    return from_hip(clsa::launch_norm(shape->batch * shape->n_q, d_model, eps, x, residual, weight, sum, y,
+                                      group, y8, y_scale, rstd, static_cast<hipStream_t>(stream)));
+}
+
+clsa_status clsa_residual_norm_grad(const clsa_shape *shape, int32_t d_model, const void *s,
+                                    const float *rstd, const void *weight, const void *dy,
+                                    const void *dsum, void *dx, float *dweight, void *ws,
+                                    size_t ws_bytes, void *stream) {
+    CLSA_TRY(check_norm(shape, d_model));
+    CLSA_TRY(check_ptr(s, 16));
+    CLSA_TRY(check_ptr(rstd, 4));
+    CLSA_TRY(check_ptr(weight, 16));
+    CLSA_TRY(check_ptr(dy, 16));
+    if (dsum) CLSA_TRY(check_ptr(dsum, 16));
+    CLSA_TRY(check_ptr(dx, 16));
+    CLSA_TRY(check_ptr(dweight, 4));
+    const int rows = shape->batch * shape->n_q;
+    const size_t need = floats_ws_bytes((size_t)clsa::norm_grad_parts(rows, d_model) * d_model);
+    if (!ws || ws_bytes < need || !aligned(ws, kAlign)) return CLSA_ERR_WORKSPACE;
+    return from_hip(clsa::launch_norm_grad(rows, d_model, s, rstd, weight, dy, dsum, dx, dweight,
+                                           static_cast<float *>(ws), static_cast<hipStream_t>(stream)));
+}
+
+clsa_status clsa_pages_fork(const clsa_shape *shape, int32_t num_pages, const int32_t *parent,
+                            int32_t *page_table, int32_t *seq_lens, int32_t *refs, void *stream) {
+    Geometry g;
+    CLSA_TRY(check_pool(shape, num_pages, &g));
+    if (g.batch > clsa::kMaxForkBatch) return CLSA_ERR_UNSUPPORTED;
+    CLSA_TRY(check_ptr(parent, 4));
+    CLSA_TRY(check_ptr(page_table, 4));
+    CLSA_TRY(check_ptr(seq_lens, 4));
+    CLSA_TRY(check_ptr(refs, 4));
+    return from_hip(clsa::launch_pages_fork(g, num_pages, parent, page_table, seq_lens, refs,
+                                            static_cast<hipStream_t>(stream)));
+}
+
+clsa_status clsa_pages_reserve(const clsa_shape *shape, int32_t num_pages, int32_t n_tensors,
+                               const clsa_paged *tensors, const int32_t *start,
+                               const int32_t *count, int32_t *page_table, int32_t *refs,
+                               int32_t *missing, void *ws, size_t ws_bytes, void *stream) {
+    Geometry g;
+    clsa::PagedTensor t[clsa::kMaxPaged];
+    CLSA_TRY(check_pool(shape, num_pages, &g));
+    CLSA_TRY(check_paged(n_tensors, tensors, t));
+    if (!clsa::reserve_supported(g)) return CLSA_ERR_UNSUPPORTED;
+    CLSA_TRY(check_ptr(start, 4));
+    CLSA_TRY(check_ptr(count, 4));
+    CLSA_TRY(check_ptr(page_table, 4));
+    CLSA_TRY(check_ptr(refs, 4));
+    CLSA_TRY(check_ptr(missing, 4));
+    if (!ws || ws_bytes < align_up(sizeof(int32_t) * clsa::reserve_ws_ints(g)) || !aligned(ws, kAlign))
+        return CLSA_ERR_WORKSPACE;
+    return from_hip(clsa::launch_pages_reserve(g, num_pages, n_tensors, t, start, count, page_table, refs,
+                                               missing, static_cast<int32_t *>(ws),
+                                               static_cast<hipStream_t>(stream)));
+}
+
+clsa_status clsa_pages_compact(const clsa_shape *shape, int32_t num_pages, int32_t n_tensors,
+                               const clsa_paged *tensors, int32_t *page_table, int32_t *refs,
+                               int32_t *bound, void *ws, size_t ws_bytes, void *stream) {
+    Geometry g;
+    clsa::PagedTensor t[clsa::kMaxPaged];
+    CLSA_TRY(check_pool(shape, num_pages, &g));
+    CLSA_TRY(check_paged(n_tensors, tensors, t));
+    CLSA_TRY(check_ptr(page_table, 4));
+    CLSA_TRY(check_ptr(refs, 4));
+    CLSA_TRY(check_ptr(bound, 4));
+    if (!ws || ws_bytes < align_up(sizeof(int32_t) * clsa::compact_ws_ints(num_pages)) || !aligned(ws, kAlign))
+        return CLSA_ERR_WORKSPACE;
+    return from_hip(clsa::launch_pages_compact(g, num_pages, n_tensors, t, page_table, refs, bound,
+                                               static_cast<int32_t *>(ws),
+                                               static_cast<hipStream_t>(stream)));
+}
+
+clsa_status clsa_pages_copy(int32_t num_pages, int32_t n_tensors, const clsa_paged *tensors,
+                            int32_t n, const int32_t *src, const int32_t *dst, void *stream) {
+    clsa::PagedTensor t[clsa::kMaxPaged];
+    if (num_pages < 1 || n < 0) return CLSA_ERR_INVALID_ARG;
+    if (num_pages > clsa::kMaxPoolPages) return CLSA_ERR_UNSUPPORTED;
+    CLSA_TRY(check_paged(n_tensors, tensors, t));
+    if (n == 0) return CLSA_OK;
+    CLSA_TRY(check_ptr(src, 4));
+    CLSA_TRY(check_ptr(dst, 4));
+    return from_hip(clsa::launch_pages_copy(num_pages, n_tensors, t, n, src, dst,
+                                            static_cast<hipStream_t>(stream)));
+}
+
 const char *clsa_status_string(clsa_status status) {
     switch (status) {
         case CLSA_OK: return "CLSA_OK";
@@ -784,6 +1010,8 @@ clsa_status clsa_get_device_error(uint32_t *bits) {
     CLSA_TRY(from_hip(clsa::take_device_error_sparse_attn8(&v)));
     CLSA_TRY(from_hip(clsa::take_device_error_tile_attn8(&v)));
     CLSA_TRY(from_hip(clsa::take_device_error_block_route(&v)));
+    CLSA_TRY(from_hip(clsa::take_device_error_project(&v)));
+    CLSA_TRY(from_hip(clsa::take_device_error_pages(&v)));
     *bits = v;
     return CLSA_OK;
 }

@@ -13,12 +13,11 @@
 // copy's rate; the token of 32 sequences 4.2 us, which is a launch.
 #include "clsa_internal.h"
 #include "device_common.h"
+#include "e4m3.h"
 
 namespace clsa {
 
 constexpr int kC8Dim = 128;
-constexpr int kC8MinExp = -100;          // least scale 2^-100
-constexpr float kC8Top = 0x1.ep+127f;    // 240 * 2^120: magnitudes above would round past fp32
 
 struct AppendArgs {
     const uint16_t *x[2];    // new K, V rows [batch, n_q, kv_heads, 128]
@@ -37,11 +36,6 @@ __device__ __forceinline__ void append_range(const int32_t *start, const int32_t
     if (n != m || !inside || m > max_len - first) note_device_error(kDevErrAppend);
     if (!inside) first = 0;
     end = inside ? first + min(m, max_len - first) : 0;
-}
-
-// Two e4m3 bytes (low halfword) of two values that lie within +-448; NaN stays NaN.
-__device__ __forceinline__ uint32_t e4m3_pair(float x, float y) {
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, y, 0, false) & 0xffffu;
 }
 
 // One workgroup = one (sequence, block that its new tokens reach, KV head), K or V.
@@ -100,11 +94,7 @@ __global__ __launch_bounds__(256) void append8_kernel(AppendArgs a) {
     if ((tid & 63) == 0) s_max[tid >> 6] = top;
     __syncthreads();
     top = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
-    top = min(top, __float_as_uint(kC8Top));
-    // 448 = 1.75 * 2^8: the exponent of top / 448, one more above 1.75
-    int e = (int)(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
-    e = max(e, kC8MinExp);
-    const float fresh = __uint_as_float((uint32_t)(e + 127) << 23);
+    const float fresh = e4m3_scale(top);
     const float now = keeps ? fmaxf(old, fresh) : fresh;
     const float inv = 1.0f / now;  // a power of two: exact
 #pragma unroll
@@ -116,11 +106,7 @@ __global__ __launch_bounds__(256) void append8_kernel(AppendArgs a) {
             uint32_t h[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                float lo = bf16_lo(w[k]), hi = bf16_hi(w[k]);
-                // not finite -> NaN (e4m3 has no infinity); else within the largest value held
-                lo = lo - lo == 0.0f ? fminf(fmaxf(lo, -kC8Top), kC8Top) * inv : NAN;
-                hi = hi - hi == 0.0f ? fminf(fmaxf(hi, -kC8Top), kC8Top) * inv : NAN;
-                h[k] = e4m3_pair(lo, hi);
+                h[k] = e4m3_pair(e4m3_scaled(bf16_lo(w[k]), inv), e4m3_scaled(bf16_hi(w[k]), inv));
             }
             *dst = make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
         } else if (p < first && now > old) {  // kept bytes move to the larger scale

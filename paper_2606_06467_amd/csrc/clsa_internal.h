@@ -280,6 +280,65 @@ hipError_t launch_project_rows(const Geometry &g, int d_model, const void *h, co
                                const int32_t *page_table, void *q_idx, void *k_idx, void *k_rows,
                                void *v_rows, hipStream_t stream);
 
+// Low-rank adapters beside the projections: sequence b adds alpha B (A h) of adapter
+// adapter[b] (-1: none) to its rows.  a: [n, rank, d_model], b: [n, features, rank];
+// u: [rows, rank] scratch for alpha A h.
+struct Adapters {
+    const void *a, *b;
+    const float *alpha;
+    const int32_t *adapter;
+    int n, rank;
+    float *u;
+};
+constexpr int kMaxRank = 128;  // a multiple of 8
+// The two calls above with adapters.
+hipError_t launch_project_adapted(const Geometry &g, int d_model, const Adapters &l, const void *h,
+                                  const void *w, const int32_t *pos, const int32_t *page_table,
+                                  void *q_idx, void *k_idx, void *k_cache, void *v_cache,
+                                  hipStream_t stream);
+hipError_t launch_project_rows_adapted(const Geometry &g, int d_model, const Adapters &l,
+                                       const void *h, const void *w, const int32_t *start,
+                                       const int32_t *count, const int32_t *page_table, void *q_idx,
+                                       void *k_idx, void *k_rows, void *v_rows, hipStream_t stream);
+hipError_t take_device_error_project(uint32_t *bits);
+
+// ---- norm.hip ----
+constexpr int kNormMaxDim = 16384;
+constexpr int kNormMaxRows = 1 << 22;
+bool norm_supported(int d);
+// group: 32, 64, 128 or d (a whole row); residual, sum, y, y8 (with y_scale) and rstd may be null.
+hipError_t launch_norm(int rows, int d, double eps, const void *x, const void *residual,
+                       const void *weight, void *sum, void *y, int group, void *y8, float *y_scale,
+                       float *rstd, hipStream_t stream);
+// part: [norm_grad_parts(rows, d), d] floats.
+int norm_grad_parts(int rows, int d);
+hipError_t launch_norm_grad(int rows, int d, const void *s, const float *rstd, const void *weight,
+                            const void *dy, const void *dsum, void *dx, float *dweight, float *part,
+                            hipStream_t stream);
+
+// ---- pages.hip ----
+constexpr int kMaxPaged = 16;            // tensors of a paged cache
+constexpr int kMaxPoolPages = 1 << 24;   // physical pages
+constexpr int kMaxForkBatch = 16384;     // slots of a fork
+struct PagedTensor {                     // clsa_paged of clsa.h
+    void *data;
+    int64_t page_bytes;
+};
+hipError_t launch_pages_fork(const Geometry &g, int pages, const int32_t *parent, int32_t *table,
+                             int32_t *seq_lens, int32_t *refs, hipStream_t stream);
+hipError_t launch_pages_copy(int pages, int tensors, const PagedTensor *t, int n, const int32_t *src,
+                             const int32_t *dst, hipStream_t stream);
+bool reserve_supported(const Geometry &g);
+size_t reserve_ws_ints(const Geometry &g);
+hipError_t launch_pages_reserve(const Geometry &g, int pages, int tensors, const PagedTensor *t,
+                                const int32_t *start, const int32_t *count, int32_t *table,
+                                int32_t *refs, int32_t *missing, int32_t *ws, hipStream_t stream);
+size_t compact_ws_ints(int pages);
+hipError_t launch_pages_compact(const Geometry &g, int pages, int tensors, const PagedTensor *t,
+                                int32_t *table, int32_t *refs, int32_t *bound, int32_t *ws,
+                                hipStream_t stream);
+hipError_t take_device_error_pages(uint32_t *bits);
+
 // ---- kd.hip ----
 // Eq. 5 target: lse2 workspace of kd_target_ws_floats floats; lse_in, if not
 // null, holds the natural-log log-sum-exp of every (layer, row, query head)

@@ -105,6 +105,8 @@ __device__ __forceinline__ uint32_t score_key(float s) {
 constexpr uint32_t kDevErrSeqLen = 1u;  // seq_lens[b] outside [0, max_len]
 constexpr uint32_t kDevErrNSel = 2u;    // n_sel[r] outside [0, top_k]
 constexpr uint32_t kDevErrAppend = 4u;  // appended tokens that do not fit
+constexpr uint32_t kDevErrAdapter = 8u; // adapter[b] outside [-1, n_adapters)
+constexpr uint32_t kDevErrPages = 16u;  // page numbers or slots out of range, or too few free pages
 static __device__ uint32_t g_device_error;
 
 // One atomic per wave that meets the condition (called inside the branch that

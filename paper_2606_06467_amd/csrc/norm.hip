@@ -1,0 +1,389 @@
+// The residual's addition and the root-mean-square norm in front of the projections:
+//   s = bf16(x + residual),  rstd = 1 / sqrt(mean(s^2) + eps),  y = s rstd w,
+// y as bf16, as e4m3 bytes with a power-of-two scale per group of a row's values, or
+// both from one pass; and the backward pass
+//   dx = dsum + rstd (g - xhat mean(g xhat)),  dw = sum over rows of dy xhat,
+//   g = dy w,  xhat = s rstd.
+// The norm is that of the rounded sum: the residual stream goes on as s, and the
+// backward pass, which has only s, then differentiates the very function that ran.
+//
+// The squares are summed in 64 bits: a bf16's square is exact there and cannot
+// overflow, so rstd has one rounding whatever the order of the sum, and a group's scale
+// does not depend on how a row is cut.  It costs two 64-bit instructions a value,
+// under a tenth of the pass's time, which the bytes bound.
+//
+// Bound by memory: every value is read once and written once; a row is held in
+// registers (8 values of 16 bytes a lane and piece) between the sum and the output.
+#include "clsa_internal.h"
+#include "device_common.h"
+#include "e4m3.h"
+
+namespace clsa {
+
+struct NormArgs {
+    const uint16_t *x, *residual, *weight;
+    uint16_t *sum, *y;
+    uint8_t *y8;
+    float *y_scale, *rstd;
+    double eps;
+    int rows, d, pieces;         // pieces = d / 8
+    int group_shift, groups;     // log2 of a group's pieces (-1: the row is one group), groups of a row
+};
+
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+    const __bf16 l = (__bf16)lo, h = (__bf16)hi;
+    return (uint32_t)__builtin_bit_cast(uint16_t, l) | ((uint32_t)__builtin_bit_cast(uint16_t, h) << 16);
+}
+
+__device__ __forceinline__ void unpack8(uint4 v, float (&f)[8]) {
+    f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x); f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
+    f[4] = bf16_lo(v.z); f[5] = bf16_hi(v.z); f[6] = bf16_lo(v.w); f[7] = bf16_hi(v.w);
+}
+
+__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
+    return make_uint4(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]), bf16_pair(f[4], f[5]), bf16_pair(f[6], f[7]));
+}
+
+__device__ __forceinline__ uint4 ld16(const uint16_t *p) { return *reinterpret_cast<const uint4 *>(p); }
+
+// Sum (or largest) of a row's values: over the wave, then over the workgroup's waves
+// where they share the row.
+template <bool WAVE, class T, class F>
+__device__ __forceinline__ T row_reduce(T v, T *s, F f) {
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) v = f(v, __shfl_xor(v, m));
+    if (WAVE) return v;
+    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    if ((threadIdx.x & 63) == 0) s[wave] = v;
+    __syncthreads();
+    v = s[0];
+    for (int w = 1; w < waves; ++w) v = f(v, s[w]);
+    return v;
+}
+
+// A row's P pieces a thread; WAVE: a wave holds a row, else the workgroup does.
+template <int P, bool WAVE>
+__global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_kernel(NormArgs a) {
+    __shared__ double s_sum[16];
+    __shared__ uint32_t s_top[16];
+    const int t = WAVE ? threadIdx.x & 63 : threadIdx.x, width = WAVE ? 64 : blockDim.x;
+    const int row = WAVE ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+    if (row >= a.rows) return;  // a whole wave or workgroup
+    const size_t at = (size_t)row * a.d;
+    uint4 v[P], r[P], w[P];
+    bool live[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        const int p = t + i * width;
+        live[i] = p < a.pieces;
+        v[i] = r[i] = w[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (live[i]) {
+            v[i] = ld16(a.x + at + 8 * p);
+            if (a.residual) r[i] = ld16(a.residual + at + 8 * p);
+            w[i] = ld16(a.weight + 8 * p);
+        }
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        float f[8];
+        unpack8(v[i], f);
+        if (a.residual) {
+            float g[8];
+            unpack8(r[i], g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] += g[e];
+            v[i] = pack8(f);
+            unpack8(v[i], f);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum = fma((double)f[e], (double)f[e], sum);
+    }
+    sum = row_reduce<WAVE>(sum, s_sum, [](double x, double y) { return x + y; });
+    const float rstd = (float)(1.0 / sqrt(sum / a.d + a.eps));
+    if (a.rstd && t == 0) a.rstd[row] = rstd;
+    if (a.sum) {
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+            if (live[i]) *reinterpret_cast<uint4 *>(a.sum + at + 8 * (t + i * width)) = v[i];
+    }
+    float whole = 0.0f;  // the row's scale, where the row is one group
+    if (a.y8 && a.group_shift < 0) {
+        uint32_t top = 0u;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            float f[8], g[8];
+            unpack8(v[i], f);
+            unpack8(w[i], g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t m = __float_as_uint(f[e] * rstd * g[e]) & 0x7fffffffu;
+                top = max(top, m < 0x7f800000u ? m : 0u);
+            }
+        }
+        top = row_reduce<WAVE>(top, s_top, [](uint32_t x, uint32_t y) { return max(x, y); });
+        whole = e4m3_scale(top);
+        if (t == 0) a.y_scale[row] = whole;
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        const int p = t + i * width;
+        float f[8], g[8];
+        unpack8(v[i], f);
+        unpack8(w[i], g);
+        uint32_t top = 0u;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            f[e] = f[e] * rstd * g[e];
+            const uint32_t m = __float_as_uint(f[e]) & 0x7fffffffu;
+            top = max(top, m < 0x7f800000u ? m : 0u);
+        }
+        if (a.y && live[i]) *reinterpret_cast<uint4 *>(a.y + at + 8 * p) = pack8(f);
+        if (a.y8) {
+            float scale = whole;
+            if (a.group_shift >= 0) {  // 4, 8 or 16 neighbouring lanes hold a group
+                for (int m = 1; m < (1 << a.group_shift); m <<= 1)
+                    top = max(top, (uint32_t)__shfl_xor((int)top, m));
+                scale = e4m3_scale(top);
+                if (live[i] && (p & ((1 << a.group_shift) - 1)) == 0)
+                    a.y_scale[(size_t)row * a.groups + (p >> a.group_shift)] = scale;
+            }
+            const float inv = 1.0f / scale;  // a power of two: exact
+            if (live[i]) {
+                uint32_t h[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    h[e] = e4m3_pair(e4m3_scaled(f[2 * e], inv), e4m3_scaled(f[2 * e + 1], inv));
+                *reinterpret_cast<uint2 *>(a.y8 + at + 8 * p) = make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
+            }
+        }
+    }
+}
+
+struct NormGradArgs {
+    const uint16_t *s, *weight, *dy, *dsum;
+    const float *rstd;
+    uint16_t *dx;
+    float *dweight, *part;  // part: [workgroups, d] sums of dy xhat
+    int rows, d, pieces, parts;
+};
+
+// Rows in turn, each held by a wave (or the workgroup): the sum g xhat, then dx; dy xhat
+// stays in registers until the last row, so that each workgroup writes one row of sums.
+template <int P, bool WAVE>
+__global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_grad_kernel(NormGradArgs a) {
+    __shared__ float s_sum[2][16];
+    extern __shared__ float s_dw[];  // WAVE: the waves' sums meet here, [d]
+    const int t = WAVE ? threadIdx.x & 63 : threadIdx.x, width = WAVE ? 64 : blockDim.x;
+    const int wave = threadIdx.x >> 6;
+    const int first = WAVE ? blockIdx.x * 4 + wave : blockIdx.x, step = WAVE ? gridDim.x * 4 : gridDim.x;
+    uint4 w[P];
+    float dw[P][8];
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        const int p = t + i * width;
+        w[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (p < a.pieces) w[i] = ld16(a.weight + 8 * p);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dw[i][e] = 0.0f;
+    }
+    const float inv_d = 1.0f / a.d;
+    int turn = 0;
+    for (int row = first; row < a.rows; row += step, turn ^= 1) {
+        const size_t at = (size_t)row * a.d;
+        uint4 v[P], y[P], u[P];
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const int p = t + i * width;
+            v[i] = y[i] = u[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (p < a.pieces) {
+                v[i] = ld16(a.s + at + 8 * p);
+                y[i] = ld16(a.dy + at + 8 * p);
+                if (a.dsum) u[i] = ld16(a.dsum + at + 8 * p);
+            }
+        }
+        const float rstd = a.rstd[row];
+        float dot = 0.0f;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            float f[8], g[8], h[8];
+            unpack8(v[i], f);
+            unpack8(y[i], g);
+            unpack8(w[i], h);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float q = g[e] * (f[e] * rstd);
+                dw[i][e] += q;
+                dot = fmaf(q, h[e], dot);
+            }
+        }
+        dot = row_reduce<WAVE>(dot, s_sum[turn], [](float x, float y) { return x + y; });
+        const float c = dot * inv_d;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const int p = t + i * width;
+            float f[8], g[8], h[8], o[8];
+            unpack8(v[i], f);
+            unpack8(y[i], g);
+            unpack8(w[i], h);
+            unpack8(u[i], o);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float z = (g[e] * h[e] - f[e] * rstd * c) * rstd;
+                f[e] = a.dsum ? z + o[e] : z;
+            }
+            if (p < a.pieces) *reinterpret_cast<uint4 *>(a.dx + at + 8 * p) = pack8(f);
+        }
+    }
+    float *part = a.part + (size_t)blockIdx.x * a.d;
+    if (WAVE) {  // wave after wave, in a fixed order
+        for (int k = 0; k < 4; ++k) {
+            if (wave == k) {
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    const int p = t + i * width;
+                    if (p < a.pieces) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float z = k ? s_dw[8 * p + e] + dw[i][e] : dw[i][e];
+                            if (k < 3) s_dw[8 * p + e] = z;
+                            else part[8 * p + e] = z;
+                        }
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        const int p = t + i * width;
+        if (p < a.pieces) {
+            float4 *o = reinterpret_cast<float4 *>(part + 8 * p);
+            o[0] = make_float4(dw[i][0], dw[i][1], dw[i][2], dw[i][3]);
+            o[1] = make_float4(dw[i][4], dw[i][5], dw[i][6], dw[i][7]);
+        }
+    }
+}
+
+// dw: the workgroups' sums, added in a fixed order: 16 threads take every 16th, for 16 columns.
+__global__ __launch_bounds__(256) void norm_grad_join_kernel(NormGradArgs a) {
+    __shared__ float s[16][17];
+    const int c = threadIdx.x & 15, k = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
+    float sum = 0.0f;
+    if (col < a.d)
+        for (int p = k; p < a.parts; p += 16) sum += a.part[(size_t)p * a.d + col];
+    s[k][c] = sum;
+    __syncthreads();
+    if (k == 0 && col < a.d) {
+#pragma unroll
+        for (int j = 1; j < 16; ++j) sum += s[j][c];
+        a.dweight[col] = sum;
+    }
+}
+
+// Rows from which a wave holds a row (below, a workgroup).
+constexpr int kNormWaveRows = 1024;
+constexpr int kNormWavePieces = 512;  // pieces of a row that a wave can hold (8 a lane: d 4096)
+
+bool norm_supported(int d) { return d >= 8 && d <= kNormMaxDim && d % 8 == 0; }
+
+static bool norm_by_wave(int rows, int pieces) { return rows >= kNormWaveRows && pieces <= kNormWavePieces; }
+
+// Workgroup threads for a row, and pieces a thread.
+static int norm_threads(int pieces, int &per) {
+    per = pieces <= 1024 ? 1 : 2;
+    return div_up(pieces, 64 * per) * 64;
+}
+
+hipError_t launch_norm(int rows, int d, double eps, const void *x, const void *residual,
+                       const void *weight, void *sum, void *y, int group, void *y8, float *y_scale,
+                       float *rstd, hipStream_t stream) {
+    if (!norm_supported(d)) return hipErrorInvalidValue;
+    NormArgs a{};
+    a.x = static_cast<const uint16_t *>(x);
+    a.residual = static_cast<const uint16_t *>(residual);
+    a.weight = static_cast<const uint16_t *>(weight);
+    a.sum = static_cast<uint16_t *>(sum);
+    a.y = static_cast<uint16_t *>(y);
+    a.y8 = static_cast<uint8_t *>(y8);
+    a.y_scale = y_scale;
+    a.rstd = rstd;
+    a.eps = eps;
+    a.rows = rows;
+    a.d = d;
+    a.pieces = d / 8;
+    a.group_shift = !y8 || group == d ? -1 : __builtin_ctz((unsigned)group / 8);
+    a.groups = !y8 ? 0 : div_up(d, group);
+    if (norm_by_wave(rows, a.pieces)) {
+        const dim3 grid(div_up(rows, 4)), wg(256);
+        switch (div_up(a.pieces, 64)) {
+            case 1: norm_kernel<1, true><<<grid, wg, 0, stream>>>(a); break;
+            case 2: norm_kernel<2, true><<<grid, wg, 0, stream>>>(a); break;
+            case 3: norm_kernel<3, true><<<grid, wg, 0, stream>>>(a); break;
+            case 4: norm_kernel<4, true><<<grid, wg, 0, stream>>>(a); break;
+            case 5: norm_kernel<5, true><<<grid, wg, 0, stream>>>(a); break;
+            case 6: norm_kernel<6, true><<<grid, wg, 0, stream>>>(a); break;
+            case 7: norm_kernel<7, true><<<grid, wg, 0, stream>>>(a); break;
+            default: norm_kernel<8, true><<<grid, wg, 0, stream>>>(a); break;
+        }
+        return hipGetLastError();
+    }
+    int per;
+    const dim3 grid(rows), wg(norm_threads(a.pieces, per));
+    if (per == 1) norm_kernel<1, false><<<grid, wg, 0, stream>>>(a);
+    else norm_kernel<2, false><<<grid, wg, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+// Workgroups of the backward pass: two per CU of rows that waves hold, else one a row up
+// to the same number.
+int norm_grad_parts(int rows, int d) {
+    return norm_by_wave(rows, d / 8) ? (div_up(rows, 4) < 512 ? div_up(rows, 4) : 512) : (rows < 512 ? rows : 512);
+}
+
+hipError_t launch_norm_grad(int rows, int d, const void *s, const float *rstd, const void *weight,
+                            const void *dy, const void *dsum, void *dx, float *dweight, float *part,
+                            hipStream_t stream) {
+    if (!norm_supported(d)) return hipErrorInvalidValue;
+    NormGradArgs a{};
+    a.s = static_cast<const uint16_t *>(s);
+    a.weight = static_cast<const uint16_t *>(weight);
+    a.dy = static_cast<const uint16_t *>(dy);
+    a.dsum = static_cast<const uint16_t *>(dsum);
+    a.rstd = rstd;
+    a.dx = static_cast<uint16_t *>(dx);
+    a.dweight = dweight;
+    a.part = part;
+    a.rows = rows;
+    a.d = d;
+    a.pieces = d / 8;
+    a.parts = norm_grad_parts(rows, d);
+    const dim3 grid(a.parts);
+    if (norm_by_wave(rows, a.pieces)) {
+        const dim3 wg(256);
+        const size_t lds = sizeof(float) * d;
+        switch (div_up(a.pieces, 64)) {
+            case 1: norm_grad_kernel<1, true><<<grid, wg, lds, stream>>>(a); break;
+            case 2: norm_grad_kernel<2, true><<<grid, wg, lds, stream>>>(a); break;
+            case 3: norm_grad_kernel<3, true><<<grid, wg, lds, stream>>>(a); break;
+            case 4: norm_grad_kernel<4, true><<<grid, wg, lds, stream>>>(a); break;
+            case 5: norm_grad_kernel<5, true><<<grid, wg, lds, stream>>>(a); break;
+            case 6: norm_grad_kernel<6, true><<<grid, wg, lds, stream>>>(a); break;
+            case 7: norm_grad_kernel<7, true><<<grid, wg, lds, stream>>>(a); break;
+            default: norm_grad_kernel<8, true><<<grid, wg, lds, stream>>>(a); break;
+        }
+    } else {
+        int per;
+        const dim3 wg(norm_threads(a.pieces, per));
+        if (per == 1) norm_grad_kernel<1, false><<<grid, wg, 0, stream>>>(a);
+        else norm_grad_kernel<2, false><<<grid, wg, 0, stream>>>(a);
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    norm_grad_join_kernel<<<dim3(div_up(d, 16)), dim3(256), 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace clsa

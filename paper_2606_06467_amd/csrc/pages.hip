@@ -1,0 +1,468 @@
+// Pages of the shared cache among many sequences: forks that share them, pages for new
+// tokens with a copy of each one that others hold too, and compaction of the pool.
+//
+// refs[p] counts the holders of physical page p: entries of the page table, and whatever
+// else the caller keeps (a prefix that outlives its sequence).  A page with no holder is
+// free; there is no list of free pages, the lowest ones are taken first, so that a call's
+// result depends on its inputs alone.
+//
+// The tables are small beside the cache: one workgroup plans (what it needs is an order
+// over all entries, a scan), and a launch of many workgroups moves the pages, which the
+// memory bounds.
+#include "clsa_internal.h"
+#include "device_common.h"
+
+namespace clsa {
+
+constexpr int kPlanThreads = 1024;
+constexpr int kForkEntries = kMaxForkBatch;  // table entries of a fork's workgroup (64 KB of LDS)
+constexpr int kCopyBytes = 8192;       // a copying workgroup's piece of a page
+
+struct PageArgs {
+    int32_t *table, *refs;
+    int batch, max_pages, pages;
+};
+
+// ---- fork ----
+
+struct ForkArgs : PageArgs {
+    const int32_t *parent;
+    int32_t *seq_lens;
+    int cols;
+};
+
+// One workgroup = `cols` columns of the table, whole; the last one takes the lengths.
+// Every entry is read before one is written, so that a slot may take from one that
+// changes in the same call.
+__global__ __launch_bounds__(256) void pages_fork_kernel(ForkArgs a) {
+    __shared__ int32_t s_old[kForkEntries];
+    if (blockIdx.x == gridDim.x - 1) {
+        for (int b = threadIdx.x; b < a.batch; b += 256) s_old[b] = a.seq_lens[b];
+        __syncthreads();
+        for (int b = threadIdx.x; b < a.batch; b += 256) {
+            const int up = a.parent[b];
+            if (up < -1 || up >= a.batch) note_device_error(kDevErrPages);  // stays as it is
+            else if (up != b) a.seq_lens[b] = up < 0 ? 0 : s_old[up];
+        }
+        return;
+    }
+    const int c0 = blockIdx.x * a.cols, width = min(a.cols, a.max_pages - c0), n = a.batch * width;
+    for (int i = threadIdx.x; i < n; i += 256)
+        s_old[i] = a.table[(size_t)(i / width) * a.max_pages + c0 + i % width];
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += 256) {
+        const int b = i / width, c = i % width, up = a.parent[b];
+        if (up < -1 || up >= a.batch || up == b) continue;
+        const int old = s_old[i], from = up < 0 ? -1 : s_old[up * width + c];
+        const bool held = from >= 0 && from < a.pages;
+        if (from >= a.pages || old >= a.pages) note_device_error(kDevErrPages);
+        const int now = held ? from : -1;
+        if (now == old) continue;
+        a.table[(size_t)b * a.max_pages + c0 + c] = now;
+        if (held) atomicAdd(a.refs + now, 1);
+        if (old >= 0 && old < a.pages) atomicSub(a.refs + old, 1);
+    }
+}
+
+hipError_t launch_pages_fork(const Geometry &g, int pages, const int32_t *parent, int32_t *table,
+                             int32_t *seq_lens, int32_t *refs, hipStream_t stream) {
+    if (g.batch > kForkEntries) return hipErrorInvalidValue;
+    ForkArgs a{{table, refs, g.batch, g.max_pages, pages}, parent, seq_lens, kForkEntries / g.batch};
+    a.cols = a.cols < 64 ? a.cols : 64;
+    pages_fork_kernel<<<dim3(div_up(g.max_pages, a.cols) + 1), dim3(256), 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+// ---- moving pages ----
+
+// Pairs of pages (source, destination), their number known on the device; a pair without
+// a source (-1) is skipped.  A page is cut into pieces over all of its tensors.
+struct CopyArgs {
+    char *data[kMaxPaged];
+    int64_t bytes[kMaxPaged];   // of a page
+    int first[kMaxPaged + 1];   // piece numbers
+    int tensors, pages;
+    const int32_t *src, *dst, *count;  // count: null if n is known
+    int n;
+};
+
+__device__ __forceinline__ void copy_pages(const CopyArgs &a, int n) {
+    const int per = a.first[a.tensors];
+    const int64_t all = (int64_t)n * per;
+    for (int64_t i = blockIdx.x; i < all; i += gridDim.x) {
+        const int k = (int)(i / per), piece = (int)(i % per);
+        const int src = a.src[k], dst = a.dst[k];
+        if (src == -1 || src == dst) continue;
+        if (src < 0 || src >= a.pages || dst < 0 || dst >= a.pages) {
+            if (piece == 0) note_device_error(kDevErrPages);
+            continue;
+        }
+        int t = 0;
+        while (piece >= a.first[t + 1]) ++t;
+        const int64_t bytes = a.bytes[t], at = (int64_t)(piece - a.first[t]) * kCopyBytes;
+        const int len = (int)min((int64_t)kCopyBytes, bytes - at);
+        const char *from = a.data[t] + src * bytes + at;
+        char *to = a.data[t] + dst * bytes + at;
+        if (((uintptr_t)a.data[t] | bytes) % 16 == 0) {
+            constexpr int N = kCopyBytes / 16 / 256;
+            u32x4 v[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const int o = (threadIdx.x + 256 * j) * 16;
+                if (o < len) v[j] = *reinterpret_cast<const u32x4 *>(from + o);
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const int o = (threadIdx.x + 256 * j) * 16;
+                if (o < len) *reinterpret_cast<u32x4 *>(to + o) = v[j];
+            }
+        } else {
+            for (int o = threadIdx.x * 4; o < len; o += 1024)
+                *reinterpret_cast<uint32_t *>(to + o) = *reinterpret_cast<const uint32_t *>(from + o);
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void pages_copy_kernel(CopyArgs a) {
+    copy_pages(a, a.count ? *a.count : a.n);
+}
+
+static int copy_args(CopyArgs &a, int pages, int tensors, const PagedTensor *t) {
+    a.pages = pages;
+    a.tensors = tensors;
+    int at = 0;
+    for (int i = 0; i < tensors; ++i) {
+        a.data[i] = static_cast<char *>(t[i].data);
+        a.bytes[i] = t[i].page_bytes;
+        a.first[i] = at;
+        at += (int)((t[i].page_bytes + kCopyBytes - 1) / kCopyBytes);
+    }
+    a.first[tensors] = at;
+    return at;
+}
+
+// Workgroups for at most n pairs of `per` pieces: eight a CU.
+static unsigned copy_grid(int64_t n, int per) {
+    const int64_t all = n * per;
+    return (unsigned)(all < 2048 ? (all < 1 ? 1 : all) : 2048);
+}
+
+hipError_t launch_pages_copy(int pages, int tensors, const PagedTensor *t, int n,
+                             const int32_t *src, const int32_t *dst, hipStream_t stream) {
+    if (n == 0 || tensors == 0) return hipSuccess;
+    CopyArgs a{};
+    const int per = copy_args(a, pages, tensors, t);
+    a.src = src;
+    a.dst = dst;
+    a.n = n;
+    pages_copy_kernel<<<dim3(copy_grid(n, per)), dim3(256), 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+// ---- reserve ----
+
+// Sum of v over the threads before this one, and over all of them.
+__device__ __forceinline__ int block_scan(int v, int *s, int &all) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int x = v;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const int y = __shfl_up(x, m);
+        if (lane >= m) x += y;
+    }
+    if (lane == 63) s[wave] = x;
+    __syncthreads();
+    int before = 0;
+    all = 0;
+    for (int w = 0; w < kPlanThreads / 64; ++w) {
+        if (w < wave) before += s[w];
+        all += s[w];
+    }
+    __syncthreads();
+    return before + x - v;
+}
+
+// refs are counted by atomics and read past the first-level cache.
+__device__ __forceinline__ int ref_of(const int32_t *p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+struct ReserveArgs {
+    PageArgs p;
+    const int32_t *start, *count;
+    int32_t *missing;
+    int32_t *state, *src, *dst, *n_pairs;  // workspace: [entries] each, and one number
+    int n_q, max_len, page_shift, slots;
+};
+
+// The table entry of (sequence, slot) i, where its new tokens reach it: the page index.
+__device__ __forceinline__ bool reserve_entry(const ReserveArgs &a, int i, size_t &at) {
+    const int b = i / a.slots, slot = i - b * a.slots;
+    const int first = a.start[b], n = min(max(a.count[b], 0), a.n_q);
+    if (first < 0 || first > a.max_len) return false;
+    const int end = first + min(n, a.max_len - first), page = (first >> a.page_shift) + slot;
+    at = (size_t)b * a.p.max_pages + page;
+    return first < end && (int64_t)page << a.page_shift < end;
+}
+
+// One workgroup.  An entry without a page needs one; so does an entry whose page others
+// hold and that do not all write now: it gets a copy.  Where every holder of a page
+// writes, the last of them (by sequence) keeps it.  To find out, each writer drops its
+// count; a count of zero says that all holders write, and the counter itself then takes
+// the largest entry number, as the least negative value below zero.
+__global__ __launch_bounds__(kPlanThreads) void pages_reserve_kernel(ReserveArgs a) {
+    __shared__ int s_scan[kPlanThreads / 64];
+    const int tid = threadIdx.x, entries = a.p.batch * a.slots;
+    int32_t *refs = a.p.refs;
+    __shared__ uint32_t s_odd;
+    if (tid == 0) s_odd = 0u;
+    __syncthreads();
+    uint32_t odd = 0u;  // what the entries and ranges hold that they should not
+    for (int b = tid; b < a.p.batch; b += kPlanThreads) {
+        const int first = a.start[b], n = a.count[b];
+        if (first < 0 || first > a.max_len || n < 0 || n > a.n_q || n > a.max_len - first) odd |= kDevErrAppend;
+    }
+    constexpr int kNone = -2, kNew = -1;  // state: not reached, has no page; else its page
+    for (int i = tid; i < entries; i += kPlanThreads) {
+        size_t at;
+        int st = kNone;
+        if (reserve_entry(a, i, at)) {
+            st = a.p.table[at];
+            if (st < 0 || st >= a.p.pages) {
+                if (st != -1) odd |= kDevErrPages;
+                st = kNew;
+            } else {
+                atomicSub(refs + st, 1);
+            }
+        }
+        a.state[i] = st;
+    }
+    if (odd) atomicOr(&s_odd, odd);
+    __threadfence();
+    __syncthreads();
+    for (int i = tid; i < entries; i += kPlanThreads) {
+        const int st = a.state[i];
+        if (st >= 0 && ref_of(refs + st) <= 0) atomicMin(refs + st, -(i + 1));
+    }
+    __threadfence();
+    __syncthreads();
+    // needs in the order of entries; a keeper leaves the list once everyone has looked
+    int need = 0;
+    for (int i0 = 0; i0 < entries; i0 += kPlanThreads) {
+        const int i = i0 + tid;
+        const int st = i < entries ? a.state[i] : kNone;
+        const bool keeps = st >= 0 && ref_of(refs + st) == -(i + 1);
+        const bool wants = st != kNone && !keeps;
+        int all;
+        const int k = need + block_scan(wants, s_scan, all);
+        if (wants) {
+            a.src[k] = st;   // -1: nothing to copy
+            a.dst[k] = i;    // the entry, until its page is known
+        }
+        if (keeps) a.state[i] = -3 - st;
+        need += all;
+    }
+    __threadfence();
+    __syncthreads();
+    for (int i = tid; i < entries; i += kPlanThreads)
+        if (a.state[i] <= -3) __hip_atomic_store(refs + (-3 - a.state[i]), 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __threadfence();
+    __syncthreads();
+    // the lowest free pages, as many as are needed (state holds them from here on)
+    int found = 0;
+    for (int p0 = 0; p0 < a.p.pages && found < need; p0 += 4 * kPlanThreads) {
+        const int p = p0 + 4 * tid;
+        int free[4], n = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            free[j] = p + j < a.p.pages && ref_of(refs + p + j) == 0;
+            n += free[j];
+        }
+        int all;
+        int k = found + block_scan(n, s_scan, all);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (free[j] && k < need) a.state[k] = p + j;
+            k += free[j];
+        }
+        found += all;
+    }
+    __threadfence();
+    __syncthreads();
+    const bool enough = found >= need;
+    for (int k = tid; k < need; k += kPlanThreads) {
+        const int src = a.src[k];
+        if (enough) {
+            size_t at;
+            reserve_entry(a, a.dst[k], at);
+            const int page = a.state[k];
+            a.p.table[at] = page;
+            refs[page] = 1;
+            a.dst[k] = page;
+        } else if (src >= 0) {
+            atomicAdd(refs + src, 1);  // nothing happens: its holder holds it still
+        }
+    }
+    if (tid == 0) {
+        *a.n_pairs = enough ? need : 0;
+        *a.missing = enough ? 0 : need - found;
+        const uint32_t bits = s_odd | (enough ? 0u : kDevErrPages);
+        if (bits) note_device_error(bits);
+    }
+}
+
+static int reserve_slots(const Geometry &g) {
+    return (int)(((int64_t)g.n_q + (1 << g.page_shift) - 2) / (1 << g.page_shift) + 1);
+}
+
+size_t reserve_ws_ints(const Geometry &g) {
+    return (size_t)g.batch * reserve_slots(g) * 3 + 64;
+}
+
+bool reserve_supported(const Geometry &g) { return (int64_t)g.batch * reserve_slots(g) < (1 << 24); }
+
+hipError_t launch_pages_reserve(const Geometry &g, int pages, int tensors, const PagedTensor *t,
+                                const int32_t *start, const int32_t *count, int32_t *table,
+                                int32_t *refs, int32_t *missing, int32_t *ws, hipStream_t stream) {
+    if (!reserve_supported(g)) return hipErrorInvalidValue;
+    ReserveArgs a;
+    a.p = {table, refs, g.batch, g.max_pages, pages};
+    a.start = start;
+    a.count = count;
+    a.missing = missing;
+    a.n_q = g.n_q;
+    a.max_len = g.max_len;
+    a.page_shift = g.page_shift;
+    a.slots = reserve_slots(g);
+    const size_t entries = (size_t)g.batch * a.slots;
+    a.n_pairs = ws;
+    a.state = ws + 64;
+    a.src = a.state + entries;
+    a.dst = a.src + entries;
+    pages_reserve_kernel<<<dim3(1), dim3(kPlanThreads), 0, stream>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || tensors == 0) return e;
+    CopyArgs c{};
+    const int per = copy_args(c, pages, tensors, t);
+    c.src = a.src;
+    c.dst = a.dst;
+    c.count = a.n_pairs;
+    pages_copy_kernel<<<dim3(copy_grid((int64_t)entries, per)), dim3(256), 0, stream>>>(c);
+    return hipGetLastError();
+}
+
+// ---- compact ----
+
+struct CompactArgs {
+    PageArgs p;
+    int32_t *bound;
+    int32_t *held, *to, *src, *dst, *n_pairs;  // workspace: [pages] each, and one number
+};
+
+// Table entries that hold each page (held: zero on entry).
+__global__ __launch_bounds__(256) void pages_count_kernel(CompactArgs a) {
+    const size_t n = (size_t)a.p.batch * a.p.max_pages;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) {
+        const int e = a.p.table[i];
+        if (e >= 0 && e < a.p.pages) atomicAdd(a.held + e, 1);
+        else if (e != -1) note_device_error(kDevErrPages);
+    }
+}
+
+// One workgroup: with U pages in use, the k-th page from U on that the table alone holds
+// moves to the k-th free page below U.  There are at least as many of those; a page that
+// something else holds stays.
+__global__ __launch_bounds__(kPlanThreads) void pages_compact_kernel(CompactArgs a) {
+    __shared__ int s_scan[kPlanThreads / 64];
+    __shared__ int s_bound;
+    const int tid = threadIdx.x;
+    int used = 0;
+    for (int p0 = 0; p0 < a.p.pages; p0 += kPlanThreads) {
+        const int p = p0 + tid;
+        int all;
+        block_scan(p < a.p.pages && a.p.refs[p] > 0, s_scan, all);
+        used += all;
+    }
+    if (tid == 0) s_bound = 0;
+    __syncthreads();
+    int holes = 0, moves = 0, bound = 0;
+    for (int p0 = 0; p0 < a.p.pages; p0 += kPlanThreads) {
+        const int p = p0 + tid;
+        const bool in = p < a.p.pages;
+        const int r = in ? a.p.refs[p] : 0;
+        const bool hole = in && p < used && r <= 0, move = in && p >= used && r > 0 && r == a.held[p];
+        int all;
+        const int h = holes + block_scan(hole, s_scan, all);
+        holes += all;
+        if (hole) a.dst[h] = p;
+        const int m = moves + block_scan(move, s_scan, all);
+        moves += all;
+        if (move) a.src[m] = p;
+        if (in) a.to[p] = p;
+        if (r > 0 && !move) bound = p + 1;
+    }
+    if (bound) atomicMax(&s_bound, bound);
+    __threadfence();
+    __syncthreads();
+    for (int k = tid; k < moves; k += kPlanThreads) {
+        const int src = a.src[k], dst = a.dst[k];
+        a.to[src] = dst;
+        a.p.refs[dst] = a.p.refs[src];
+        a.p.refs[src] = 0;
+    }
+    if (tid == 0) {
+        *a.n_pairs = moves;
+        *a.bound = max(s_bound, moves ? a.dst[moves - 1] + 1 : 0);
+    }
+}
+
+struct MoveArgs {
+    CompactArgs a;
+    CopyArgs c;
+};
+
+__global__ __launch_bounds__(256) void pages_move_kernel(MoveArgs m) {
+    const CompactArgs &a = m.a;
+    const size_t n = (size_t)a.p.batch * a.p.max_pages;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) {
+        const int e = a.p.table[i];
+        if (e >= 0 && e < a.p.pages) {
+            const int now = a.to[e];
+            if (now != e) a.p.table[i] = now;
+        }
+    }
+    if (m.c.tensors) copy_pages(m.c, *m.c.count);
+}
+
+size_t compact_ws_ints(int pages) { return (size_t)pages * 4 + 64; }
+
+hipError_t launch_pages_compact(const Geometry &g, int pages, int tensors, const PagedTensor *t,
+                                int32_t *table, int32_t *refs, int32_t *bound, int32_t *ws,
+                                hipStream_t stream) {
+    CompactArgs a;
+    a.p = {table, refs, g.batch, g.max_pages, pages};
+    a.bound = bound;
+    a.n_pairs = ws;
+    a.held = ws + 64;
+    a.to = a.held + pages;
+    a.src = a.to + pages;
+    a.dst = a.src + pages;
+    hipError_t e = launch_zero_u32(reinterpret_cast<uint32_t *>(a.held), (size_t)pages, stream);
+    if (e != hipSuccess) return e;
+    const size_t n = (size_t)g.batch * g.max_pages;
+    const unsigned grid = (unsigned)(n < 2048 * 256 ? (n + 255) / 256 : 2048);
+    pages_count_kernel<<<dim3(grid), dim3(256), 0, stream>>>(a);
+    pages_compact_kernel<<<dim3(1), dim3(kPlanThreads), 0, stream>>>(a);
+    MoveArgs m{a, {}};
+    const int per = tensors ? copy_args(m.c, pages, tensors, t) : 0;
+    m.c.src = a.src;
+    m.c.dst = a.dst;
+    m.c.count = a.n_pairs;
+    const unsigned copies = copy_grid(pages / 2, per);
+    pages_move_kernel<<<dim3(grid > copies ? grid : copies), dim3(256), 0, stream>>>(m);
+    return hipGetLastError();
+}
+
+hipError_t take_device_error_pages(uint32_t *bits) { return take_source_device_error(bits); }
+
+}  // namespace clsa

@@ -51,7 +51,24 @@ struct ProjArgs {
     bool kv_rows;              // K and V stay in the rows' own order: [rows, kvw]
     int rows, d, n_q, max_len, page_shift, max_pages, kvw;  // kvw = kv_heads * 128
     int rtiles, ftiles, band;  // tiled kernel: 128-row and 128-feature tiles, row tiles per band
+    // adapters (adapted kernels only)
+    const uint16_t *down;      // [n_adapters, rank, d]
+    const uint16_t *up;        // [n_adapters, features, rank]
+    const float *alpha;
+    const int32_t *adapter;    // [batch]
+    float *u;                  // [rows, rank]: alpha A h of the rows that have an adapter
+    int n_adapters, rank, n_feat;
 };
+
+// Adapter of sequence b, -1 for none.
+__device__ __forceinline__ int adapter_of(const ProjArgs &a, int b) {
+    const int id = a.adapter[b];
+    if (id < -1 || id >= a.n_adapters) {
+        note_device_error(kDevErrAdapter);
+        return -1;
+    }
+    return id;
+}
 
 __device__ __forceinline__ bf16x8 ld8(const uint16_t *p) {
     return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(p));
@@ -93,10 +110,30 @@ __device__ __forceinline__ void store_feature(const ProjArgs &a, int r, int f, f
     else a.v_cache[row * a.kvw + (f - 512 - a.kvw)] = bits;
 }
 
+// (alpha A h) . B of row r and output feature f: fp32 products and sums.
+__device__ __forceinline__ float adapter_dot(const ProjArgs &a, int id, int r, int f) {
+    const uint16_t *bp = a.up + ((size_t)id * a.n_feat + f) * a.rank;
+    const float4 *up = reinterpret_cast<const float4 *>(a.u + (size_t)r * a.rank);
+    float sum = 0.0f;
+    for (int j = 0; j < a.rank / 8; ++j) {
+        const uint4 b = *reinterpret_cast<const uint4 *>(bp + 8 * j);
+        const float4 x = up[2 * j], y = up[2 * j + 1];
+        sum = fmaf(x.x, bf16_lo(b.x), sum);
+        sum = fmaf(x.y, bf16_hi(b.x), sum);
+        sum = fmaf(x.z, bf16_lo(b.y), sum);
+        sum = fmaf(x.w, bf16_hi(b.y), sum);
+        sum = fmaf(y.x, bf16_lo(b.z), sum);
+        sum = fmaf(y.y, bf16_hi(b.z), sum);
+        sum = fmaf(y.z, bf16_lo(b.w), sum);
+        sum = fmaf(y.w, bf16_hi(b.w), sum);
+    }
+    return sum;
+}
+
 // Few rows: one 16 RT-row x 16-feature tile per workgroup, d_model split over 8
 // waves of NB * KS 32-dim steps each (d_model = 256 * NB * KS), KS at a time.
 // RT = 2: a weight is read once for 32 rows (launch_splitk: when).
-template <int KS, int NB, int RT, bool PAGED>
+template <int KS, int NB, int RT, bool PAGED, bool ADAPTED>
 __global__ __launch_bounds__(512) void project_splitk_kernel(ProjArgs a) {
     __shared__ float part[kSplitWaves][16 * RT][16 + 1];
     const int ft = blockIdx.x, rt = blockIdx.y;
@@ -137,7 +174,12 @@ __global__ __launch_bounds__(512) void project_splitk_kernel(ProjArgs a) {
         float sum = 0.0f;
 #pragma unroll
         for (int w = 0; w < kSplitWaves; ++w) sum += part[w][rr][f];
-        store_feature<PAGED>(a, rt * 16 * RT + rr, ft * 16 + f, sum);
+        const int r = rt * 16 * RT + rr;
+        if (ADAPTED && r < a.rows) {
+            const int id = adapter_of(a, r / a.n_q);
+            if (id >= 0) sum += adapter_dot(a, id, r, ft * 16 + f);
+        }
+        store_feature<PAGED>(a, r, ft * 16 + f, sum);
     }
 }
 
@@ -151,7 +193,71 @@ constexpr int kGemmPitch = kGemmK;           // bf16 per staged row
 constexpr int kGemmOutPitch = kGemmN + 8;    // bf16 per staged output row
 constexpr size_t kGemmLds = sizeof(uint16_t) * 2 * 2 * kGemmM * kGemmPitch;
 
-template <bool PAGED>
+// u as the A operand of a 16-row product: the lane's row, ranks ro .. ro + 8, as the
+// high or the low bf16 of each fp32 (together 16 bits: hi cut off, lo the rest rounded, so
+// that an infinity stays one).
+__device__ __forceinline__ bf16x8 adapter_operand(const float *u, bool low) {
+    const float4 x = *reinterpret_cast<const float4 *>(u), y = *reinterpret_cast<const float4 *>(u + 4);
+    const float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+    bf16x8 o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float hi = __uint_as_float(__float_as_uint(f[e]) & 0xffff0000u);
+        const float rest = f[e] - hi;
+        o[e] = low ? (rest == rest ? (__bf16)rest : (__bf16)0.0f) : (__bf16)hi;
+    }
+    return o;
+}
+
+// Adds the adapters' part to a wave's 64 x 64 tile of the tiled product (c[mt][nt]: rows
+// r0 + 16 mt, features f0 + 16 nt).  A 32-wide step holds 16 ranks twice, the high and the
+// low parts of u against the same B.  Rows of different sequences can share a 16-row
+// tile: the tile is then made once for each adapter in it and added to that adapter's rows
+// only (a factor of zero would carry one adapter's infinities to another's rows).
+__device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, f32x4 (&c)[4][4]) {
+    const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
+    const bool low = grp >= 2;
+    for (int mt = 0; mt < 4; ++mt) {
+        if (r0 + 16 * mt >= a.rows) break;
+        const int r = min(r0 + 16 * mt + col, a.rows - 1);
+        const int mine = adapter_of(a, r / a.n_q);
+        uint64_t todo = __ballot(mine >= 0) & 0xffffull;
+        while (todo) {
+            const int id = __builtin_amdgcn_readlane(mine, __builtin_ctzll(todo));
+            const uint64_t same = __ballot(mine == id) & 0xffffull;
+            todo &= ~same;
+            f32x4 t[4];
+#pragma unroll
+            for (int nt = 0; nt < 4; ++nt) t[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < a.rank; j += 16) {
+                const int ro = j + (grp & 1) * 8;
+                bf16x8 av = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u}), bv[4];
+                const bool in = ro < a.rank;
+                if (in && mine == id) av = adapter_operand(a.u + (size_t)r * a.rank + ro, low);
+#pragma unroll
+                for (int nt = 0; nt < 4; ++nt) {
+                    bv[nt] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
+                    if (in) bv[nt] = ld8(a.up + ((size_t)id * a.n_feat + f0 + 16 * nt + col) * a.rank + ro);
+                }
+#pragma unroll
+                for (int nt = 0; nt < 4; ++nt)
+                    t[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, bv[nt], t[nt], 0, 0, 0);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (!((same >> (4 * grp + e)) & 1)) continue;
+#pragma unroll
+                for (int nt = 0; nt < 4; ++nt) {
+#pragma unroll
+                    for (int m = 0; m < 4; ++m)
+                        if (m == mt) c[m][nt][e] += t[nt][e];
+                }
+            }
+        }
+    }
+}
+
+template <bool PAGED, bool ADAPTED>
 __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
     // two stages of A (rows of h) and B (features of w), 128 x 64 bf16 each
     // (dynamic LDS, kGemmLds bytes); the output tile (128 x 128 bf16) reuses it
@@ -260,6 +366,7 @@ __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
         __syncthreads();
       }
     }
+    if (ADAPTED) adapter_tile(a, r0 + wm * 64, f0 + wn * 64, c);
     // bf16 results into LDS: C tile (mt, nt) row 4 grp + r, column col
     uint16_t(*s_out)[kGemmOutPitch] = reinterpret_cast<uint16_t(*)[kGemmOutPitch]>(&s_ab[0][0][0][0]);
     static_assert(kGemmLds >= sizeof(uint16_t) * kGemmM * kGemmOutPitch, "output tile fits");
@@ -309,7 +416,22 @@ bool project_supported(int d_model) {
     return d_model >= 512 && d_model <= 8192 && d_model % 512 == 0;
 }
 
-template <int KS, int NB = 1>
+// u = alpha A h.  A wave makes one rank of one row.
+__global__ __launch_bounds__(256) void adapter_down_kernel(ProjArgs a) {
+    const int per_row = a.rank / 4, row = blockIdx.x / per_row;
+    const int j = (blockIdx.x % per_row) * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int id = adapter_of(a, row / a.n_q);
+    if (id < 0) return;
+    const uint16_t *hp = a.h + (size_t)row * a.d, *ap = a.down + ((size_t)id * a.rank + j) * a.d;
+    float sum = 0.0f;
+    for (int i = lane * 8; i < a.d; i += 512)
+        sum = dot8_bf16(*reinterpret_cast<const uint4 *>(hp + i), *reinterpret_cast<const uint4 *>(ap + i), sum);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) sum += __shfl_xor(sum, m);
+    if (lane == 0) a.u[(size_t)row * a.rank + j] = sum * a.alpha[id];
+}
+
+template <int KS, int NB = 1, bool ADAPTED = false>
 static void launch_splitk(const ProjArgs &a, bool paged, int n_feat, hipStream_t stream) {
     // 32 rows a workgroup where 16 would not fit the chip in one round but 32 do
     // (32 rows x 2560 features, d_model 2560: 9.1 us against 11.3; 4096: 13.2 against
@@ -318,12 +440,13 @@ static void launch_splitk(const ProjArgs &a, bool paged, int n_feat, hipStream_t
     const int tiles = n_feat / 16;
     const bool two = tiles * div_up(a.rows, 16) > 256 && (tiles * div_up(a.rows, 32) <= 256 || a.rows > 64);
     const dim3 grid(tiles, div_up(a.rows, two ? 32 : 16)), block(512);
-    if (two && paged) project_splitk_kernel<KS, NB, 2, true><<<grid, block, 0, stream>>>(a);
-    else if (two) project_splitk_kernel<KS, NB, 2, false><<<grid, block, 0, stream>>>(a);
-    else if (paged) project_splitk_kernel<KS, NB, 1, true><<<grid, block, 0, stream>>>(a);
-    else project_splitk_kernel<KS, NB, 1, false><<<grid, block, 0, stream>>>(a);
+    if (two && paged) project_splitk_kernel<KS, NB, 2, true, ADAPTED><<<grid, block, 0, stream>>>(a);
+    else if (two) project_splitk_kernel<KS, NB, 2, false, ADAPTED><<<grid, block, 0, stream>>>(a);
+    else if (paged) project_splitk_kernel<KS, NB, 1, true, ADAPTED><<<grid, block, 0, stream>>>(a);
+    else project_splitk_kernel<KS, NB, 1, false, ADAPTED><<<grid, block, 0, stream>>>(a);
 }
 
+template <bool ADAPTED = false>
 static hipError_t launch_project_args(const Geometry &g, int d_model, ProjArgs a, const void *h,
                                       const void *w, const int32_t *page_table, void *q_idx,
                                       void *k_idx, void *k_cache, void *v_cache,
@@ -346,25 +469,33 @@ static hipError_t launch_project_args(const Geometry &g, int d_model, ProjArgs a
     if (g.rows == 0) return hipSuccess;
     const int n_feat = 512 + 2 * a.kvw;  // a multiple of 256 (kv_heads * 128 per K and V)
     const bool paged = g.page_shift >= 0;
+    if (ADAPTED) {
+        a.n_feat = n_feat;
+        const int64_t blocks = (int64_t)g.rows * (a.rank / 4);
+        if (blocks > 0xffffff) return hipErrorInvalidConfiguration;  // 2^32 threads a launch
+        adapter_down_kernel<<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
     if (g.rows <= kSplitMaxRows) {
         switch (d_model / 512) {
-            case 1: launch_splitk<2>(a, paged, n_feat, stream); break;
-            case 2: launch_splitk<4>(a, paged, n_feat, stream); break;
-            case 3: launch_splitk<6>(a, paged, n_feat, stream); break;
-            case 4: launch_splitk<8>(a, paged, n_feat, stream); break;
-            case 5: launch_splitk<10>(a, paged, n_feat, stream); break;
-            case 6: launch_splitk<12>(a, paged, n_feat, stream); break;
+            case 1: launch_splitk<2, 1, ADAPTED>(a, paged, n_feat, stream); break;
+            case 2: launch_splitk<4, 1, ADAPTED>(a, paged, n_feat, stream); break;
+            case 3: launch_splitk<6, 1, ADAPTED>(a, paged, n_feat, stream); break;
+            case 4: launch_splitk<8, 1, ADAPTED>(a, paged, n_feat, stream); break;
+            case 5: launch_splitk<10, 1, ADAPTED>(a, paged, n_feat, stream); break;
+            case 6: launch_splitk<12, 1, ADAPTED>(a, paged, n_feat, stream); break;
             // past 3072 (96 operand registers) in two batches
-            case 7: launch_splitk<7, 2>(a, paged, n_feat, stream); break;
-            case 8: launch_splitk<8, 2>(a, paged, n_feat, stream); break;
-            case 9: launch_splitk<9, 2>(a, paged, n_feat, stream); break;
-            case 10: launch_splitk<10, 2>(a, paged, n_feat, stream); break;
-            case 11: launch_splitk<11, 2>(a, paged, n_feat, stream); break;
-            case 12: launch_splitk<12, 2>(a, paged, n_feat, stream); break;
-            case 13: launch_splitk<13, 2>(a, paged, n_feat, stream); break;
-            case 14: launch_splitk<14, 2>(a, paged, n_feat, stream); break;
-            case 15: launch_splitk<15, 2>(a, paged, n_feat, stream); break;
-            case 16: launch_splitk<16, 2>(a, paged, n_feat, stream); break;
+            case 7: launch_splitk<7, 2, ADAPTED>(a, paged, n_feat, stream); break;
+            case 8: launch_splitk<8, 2, ADAPTED>(a, paged, n_feat, stream); break;
+            case 9: launch_splitk<9, 2, ADAPTED>(a, paged, n_feat, stream); break;
+            case 10: launch_splitk<10, 2, ADAPTED>(a, paged, n_feat, stream); break;
+            case 11: launch_splitk<11, 2, ADAPTED>(a, paged, n_feat, stream); break;
+            case 12: launch_splitk<12, 2, ADAPTED>(a, paged, n_feat, stream); break;
+            case 13: launch_splitk<13, 2, ADAPTED>(a, paged, n_feat, stream); break;
+            case 14: launch_splitk<14, 2, ADAPTED>(a, paged, n_feat, stream); break;
+            case 15: launch_splitk<15, 2, ADAPTED>(a, paged, n_feat, stream); break;
+            case 16: launch_splitk<16, 2, ADAPTED>(a, paged, n_feat, stream); break;
             default: return hipErrorInvalidValue;
         }
         return hipGetLastError();
@@ -378,12 +509,12 @@ static hipError_t launch_project_args(const Geometry &g, int d_model, ProjArgs a
     const long blocks = div_up((int)bands, 8) * 8 * (long)a.band * a.ftiles;
     if (blocks > 0x7fffffffL) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)blocks);
-    const void *fn = paged ? reinterpret_cast<const void *>(&project_gemm_kernel<true>)
-                           : reinterpret_cast<const void *>(&project_gemm_kernel<false>);
+    const void *fn = paged ? reinterpret_cast<const void *>(&project_gemm_kernel<true, ADAPTED>)
+                           : reinterpret_cast<const void *>(&project_gemm_kernel<false, ADAPTED>);
     hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kGemmLds);
     if (e != hipSuccess) return e;
-    if (paged) project_gemm_kernel<true><<<grid, dim3(256), kGemmLds, stream>>>(a);
-    else project_gemm_kernel<false><<<grid, dim3(256), kGemmLds, stream>>>(a);
+    if (paged) project_gemm_kernel<true, ADAPTED><<<grid, dim3(256), kGemmLds, stream>>>(a);
+    else project_gemm_kernel<false, ADAPTED><<<grid, dim3(256), kGemmLds, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -405,5 +536,39 @@ hipError_t launch_project_rows(const Geometry &g, int d_model, const void *h, co
     a.kv_rows = true;
     return launch_project_args(g, d_model, a, h, w, page_table, q_idx, k_idx, k_rows, v_rows, stream);
 }
+
+static ProjArgs adapted_args(const Adapters &l) {
+    ProjArgs a{};
+    a.down = static_cast<const uint16_t *>(l.a);
+    a.up = static_cast<const uint16_t *>(l.b);
+    a.alpha = l.alpha;
+    a.adapter = l.adapter;
+    a.u = l.u;
+    a.n_adapters = l.n;
+    a.rank = l.rank;
+    return a;
+}
+
+hipError_t launch_project_adapted(const Geometry &g, int d_model, const Adapters &l, const void *h,
+                                  const void *w, const int32_t *pos, const int32_t *page_table,
+                                  void *q_idx, void *k_idx, void *k_cache, void *v_cache,
+                                  hipStream_t stream) {
+    ProjArgs a = adapted_args(l);
+    a.pos = pos;
+    return launch_project_args<true>(g, d_model, a, h, w, page_table, q_idx, k_idx, k_cache, v_cache, stream);
+}
+
+hipError_t launch_project_rows_adapted(const Geometry &g, int d_model, const Adapters &l,
+                                       const void *h, const void *w, const int32_t *start,
+                                       const int32_t *count, const int32_t *page_table, void *q_idx,
+                                       void *k_idx, void *k_rows, void *v_rows, hipStream_t stream) {
+    ProjArgs a = adapted_args(l);
+    a.start = start;
+    a.count = count;
+    a.kv_rows = true;
+    return launch_project_args<true>(g, d_model, a, h, w, page_table, q_idx, k_idx, k_rows, v_rows, stream);
+}
+
+hipError_t take_device_error_project(uint32_t *bits) { return take_source_device_error(bits); }
 
 }  // namespace clsa

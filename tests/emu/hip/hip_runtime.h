@@ -40,6 +40,11 @@ inline float __uint_as_float(uint32_t x) { return __builtin_bit_cast(float, x); 
 inline int __float_as_int(float x) { return __builtin_bit_cast(int, x); }
 inline float __int_as_float(int x) { return __builtin_bit_cast(float, x); }
 inline uint32_t atomicOr(uint32_t *p, uint32_t v) { const uint32_t o = *p; *p |= v; return o; }
+inline int atomicAdd(int *p, int v) { const int o = *p; *p += v; return o; }
+inline int atomicSub(int *p, int v) { const int o = *p; *p -= v; return o; }
+inline int atomicMin(int *p, int v) { const int o = *p; *p = v < o ? v : o; return o; }
+inline int atomicMax(int *p, int v) { const int o = *p; *p = v > o ? v : o; return o; }
+template <class T> inline T emu_atomic_load(const T *p) { return *p; }
 template <class... A> inline hipError_t hipMemcpyFromSymbol(A...) { return hipSuccess; }
 template <class... A> inline hipError_t hipMemcpyToSymbol(A...) { return hipSuccess; }
 
@@ -148,6 +153,15 @@ template <class T> inline T shfl_xor(T v, int d) {
     });
     return a.r;
 }
+template <class T> inline T shfl_up(T v, int d) {
+    struct A { T v; int d; T r; } a{v, d, v};
+    wave_op(a, [](void *const *l) {
+        for (int i = 0; i < 64; ++i)
+            if (A *x = (A *)l[i])
+                if (i >= x->d && l[i - x->d]) x->r = ((A *)l[i - x->d])->v;
+    });
+    return a.r;
+}
 template <int M> inline pair_u32 permlane_swap(uint32_t x, uint32_t y) {
     struct A { uint32_t x, y; pair_u32 r; } a{x, y, {}};
     wave_op(a, [](void *const *l) {
@@ -244,6 +258,10 @@ inline uint32_t perm(uint32_t hi, uint32_t lo, uint32_t sel) {
 #define gridDim emu::grid_dim
 #define __syncthreads() emu::yield_as(emu::Fibre::kBarrier)
 #define __shfl_xor emu::shfl_xor
+#define __shfl_up emu::shfl_up
+#define __threadfence() ((void)0)
+#define __hip_atomic_load(p, order, scope) emu_atomic_load(p)
+#define __hip_atomic_store(p, v, order, scope) ((void)(*(p) = (v)))
 #define __ballot emu::ballot
 #define __lane_id() (emu::thread_idx.x & 63)
 #define __builtin_amdgcn_ballot_w64 emu::ballot

@@ -1,0 +1,246 @@
+"""Projections with an adapter of each request on the GPU against the formula in 64 bits.
+
+Bounds: sums of n fp32 products, at most gamma_n = n u / (1 - n u) times the sum of magnitudes
+(doubled, as for the projections without adapters); the inner sum's two bf16 hold it to 2^-15;
+one rounding to bf16, 2^-8."""
+import numpy as np
+import pytest
+
+from paper_2606_06467_amd import inputs
+from tests import gpu_util as U
+
+pytestmark = pytest.mark.gpu
+
+
+def gamma(n):
+    return n * U.U32 / (1 - n * U.U32)
+
+
+def f64(bits):
+    return inputs.f32_from_bf16_bits(bits).astype(np.float64)
+
+
+class Case:
+    """Inputs, the cache that they are written to, and the result in 64 bits."""
+
+    def __init__(self, batch, n_q, d, rank, n_adapters, ids, heads=2, page=0, max_len=128, seed=1):
+        self.batch, self.n_q, self.d, self.rank, self.heads, self.page, self.max_len = batch, n_q, d, rank, heads, page, max_len
+        self.kvw = heads * 128
+        self.feats = 512 + 2 * self.kvw
+        rng = np.random.default_rng(seed)
+        self.h = inputs.normal_bf16(seed, (batch * n_q, d), 1.0)
+        self.w = inputs.normal_bf16(seed + 1, (self.feats, d), 0.02)
+        self.a = inputs.normal_bf16(seed + 2, (n_adapters, rank, d), 0.05)
+        self.b = inputs.normal_bf16(seed + 3, (n_adapters, self.feats, rank), 0.3)
+        self.alpha = (rng.random(n_adapters) * 3 - 1).astype(np.float32)
+        self.ids = np.asarray(ids, np.int32)
+        self.start = rng.integers(0, max_len - n_q + 1, batch).astype(np.int32)
+        self.pos = self.start[:, None] + np.arange(n_q, dtype=np.int32)
+        self.pos[rng.random(self.pos.shape) < 0.05] = -1
+        self.table = None
+        if page:
+            cols = max_len // page
+            self.table = rng.permutation(batch * cols).reshape(batch, cols).astype(np.int32)
+
+    def shape(self):
+        from paper_2606_06467_amd import binding as B
+        return B.make_shape(self.batch, self.n_q, self.max_len, 1, q_heads=self.heads, kv_heads=self.heads,
+                            page_size=self.page, max_pages=self.max_len // self.page if self.page else 0)
+
+    def dev(self):
+        import torch
+        from paper_2606_06467_amd import binding as B
+        bf = {k: B.bf16_from_bits(getattr(self, k)) for k in ("h", "w", "a", "b")}
+        it = {k: torch.from_numpy(np.ascontiguousarray(getattr(self, k))).cuda() for k in ("alpha", "ids", "start", "pos")}
+        it["table"] = None if self.table is None else torch.from_numpy(self.table).cuda()
+        return {**bf, **it}
+
+    def caches(self):
+        import torch
+        n = self.batch * self.max_len
+        return (torch.full((self.batch * self.n_q, 256), 3.0, dtype=torch.bfloat16, device="cuda"),
+                *[torch.full((n, k), 3.0, dtype=torch.bfloat16, device="cuda") for k in (256, self.kvw, self.kvw)])
+
+    def run(self, d=None, ws=None):
+        from paper_2606_06467_amd import binding as B
+        import torch
+        d, out = d or self.dev(), self.caches()
+        ws = B.workspace(self.shape(), B.CLSA_OP_ADAPTED, self.rank) if ws is None else ws
+        ws.fill_(0xFF)   # NaN
+        B.clsa_project_append_adapted(self.shape(), self.d, d["h"], d["w"], d["a"], d["b"], d["alpha"], d["ids"],
+                                      d["pos"], d["table"], *out, ws)
+        torch.cuda.synchronize()
+        return [B.bits_from_bf16(t) for t in out]
+
+    def rows(self):
+        """Cache row of every token, -1 for none."""
+        p = self.pos
+        if self.page:
+            at = self.table[np.arange(self.batch)[:, None], np.maximum(p, 0) // self.page].astype(np.int64) * self.page + p % self.page
+        else:
+            at = np.arange(self.batch)[:, None] * self.max_len + p
+        return np.where(p >= 0, at, -1).reshape(-1)
+
+    def reference(self):
+        h, w = f64(self.h), f64(self.w)
+        ref, tol = h @ w.T, 2 * gamma(self.d) * (np.abs(h) @ np.abs(w).T)
+        for b, m in enumerate(self.ids):
+            if not 0 <= m < len(self.a):
+                continue
+            r = slice(b * self.n_q, (b + 1) * self.n_q)
+            a, up, al = f64(self.a[m]), f64(self.b[m]), float(self.alpha[m])
+            ref[r] += al * (h[r] @ a.T) @ up.T
+            tol[r] += abs(al) * (2 * gamma(self.d) + 2 * gamma(2 * self.rank) + 2.0 ** -15) * (np.abs(h[r]) @ np.abs(a).T) @ np.abs(up).T
+        return ref, tol + np.abs(ref) * 2.0 ** -8 + 1e-30
+
+    def check(self, got, only=None):
+        ref, tol = self.reference()
+        rows, kvw = self.rows(), self.kvw
+        keep = np.ones(len(ref), bool) if only is None else np.repeat(only, self.n_q)
+        err = np.abs(f64(got[0]) - ref[:, :256])
+        assert np.all(err[keep] <= tol[keep, :256]), float((err[keep] / tol[keep, :256]).max())
+        for x, c0, c1 in ((got[1], 256, 512), (got[2], 512, 512 + kvw), (got[3], 512 + kvw, 512 + 2 * kvw)):
+            live = (rows >= 0) & keep
+            err = np.abs(f64(x[rows[live]]) - ref[live, c0:c1])
+            assert np.all(err <= tol[live, c0:c1]), float((err / tol[live, c0:c1]).max())
+            idle = np.ones(len(x), bool)
+            idle[rows[rows >= 0]] = False
+            assert np.all(x[idle] == 0x4040)  # 3.0: left as it was
+
+
+CASES = [  # batch, n_q, d_model, rank, adapters, page
+    (1, 1, 512, 8, 1, 0), (5, 1, 2560, 16, 3, 16), (32, 1, 2560, 16, 40, 16), (33, 1, 1024, 64, 5, 0), (70, 1, 4096, 8, 9, 16),
+    (128, 1, 512, 128, 130, 0), (200, 1, 512, 16, 11, 16), (3, 5, 1536, 24, 2, 0), (300, 2, 512, 40, 250, 0),
+    (7, 37, 512, 16, 3, 16), (1, 300, 2560, 16, 2, 0), (9, 33, 1024, 128, 9, 16), (2, 100, 512, 8, 2, 0), (4, 64, 3584, 56, 3, 0)]
+
+
+@pytest.mark.parametrize("batch,n_q,d,rank,n,page", CASES)
+def test_adapted(batch, n_q, d, rank, n, page):
+    rng = np.random.default_rng(batch + n_q)
+    ids = rng.integers(-1, n, batch)
+    if batch > 2:
+        ids[1], ids[2] = -1, n - 1
+    max_len = -(-max(n_q + 20, 48) // 16) * 16
+    c = Case(batch, n_q, d, rank, n, ids, page=page, max_len=max_len, seed=batch * 7 + rank)
+    got = c.run()
+    c.check(got)
+    for a, b in zip(got, c.run()):
+        assert np.array_equal(a, b)
+
+
+@pytest.mark.parametrize("batch,n_q", [(6, 1), (150, 1), (3, 70)])
+def test_no_adapters_are_the_plain_projections(batch, n_q):
+    import torch
+    from paper_2606_06467_amd import binding as B
+    c = Case(batch, n_q, 1024, 16, 2, np.full(batch, -1), page=16, max_len=96, seed=5)
+    d, out = c.dev(), c.caches()
+    B.clsa_project_append(c.shape(), c.d, d["h"], d["w"], d["pos"], d["table"], *out)
+    torch.cuda.synchronize()
+    for a, b in zip(c.run(), out):
+        assert np.array_equal(a, B.bits_from_bf16(b))
+
+
+@pytest.mark.parametrize("batch,n_q", [(6, 1), (150, 1), (5, 70)])
+def test_infinities_stay_with_their_adapter(batch, n_q):
+    c = Case(batch, n_q, 512, 16, 3, np.arange(batch) % 3 - 1, max_len=96, seed=6)
+    c.b[0, :, 3] = 0x7F80      # an infinity against every feature
+    c.b[0, 5, 2] = 0x7FC0      # a NaN
+    got = c.run()
+    others = c.ids != 0
+    c.check(got, others)
+    q = f64(got[0]).reshape(batch, n_q, 256)
+    assert not np.isfinite(q[~others]).any() and np.isnan(q[~others][..., 5]).all()
+    # an inner sum that is infinite gives infinities of its features' signs, or NaN where B is zero
+    c = Case(batch, n_q, 512, 16, 3, np.arange(batch) % 3 - 1, max_len=96, seed=6)
+    c.h[:] = 0x3F80            # ones
+    c.a[0, 2] = 0x7F00         # 1.7e38 each: the sum overflows
+    c.b[0, 7, 2] = 0
+    got = c.run()
+    c.check(got, others)
+    q = f64(got[0]).reshape(batch, n_q, 256)
+    bad = q[~others]
+    want = np.sign(f64(c.b[0, :256, 2])) * np.sign(c.alpha[0]) * np.inf
+    assert np.isnan(bad[..., 7]).all()
+    fine = np.arange(256) != 7
+    fine &= np.isfinite(want) | np.isinf(want)
+    assert np.array_equal(bad[..., fine], np.broadcast_to(want[fine], bad[..., fine].shape))
+
+
+@pytest.mark.parametrize("batch,n_q", [(6, 1), (150, 1), (5, 70)])
+def test_adapter_numbers_out_of_range(batch, n_q):
+    from paper_2606_06467_amd import binding as B
+    ids = np.arange(batch) % 4
+    ids[1], ids[2], ids[3] = 4, -2, 2 ** 31 - 1
+    c = Case(batch, n_q, 512, 8, 4, ids, max_len=96, seed=7)
+    B.clsa_get_device_error()
+    got = c.run()
+    assert B.clsa_get_device_error() == B.CLSA_DEVERR_ADAPTER
+    c.check(got)
+
+
+@pytest.mark.parametrize("batch,n_q,rank,block,page", [(4, 1, 16, 16, 0), (140, 1, 8, 16, 16), (5, 77, 64, 32, 64),
+                                                       (1, 200, 16, 64, 0)])
+def test_adapted_into_the_8bit_cache(batch, n_q, rank, block, page):
+    """The same bytes as the rows of the bf16 call, appended."""
+    import torch
+    from paper_2606_06467_amd import binding as B
+    rng = np.random.default_rng(batch)
+    max_len = -(-(n_q + 40) // 64) * 64
+    c = Case(batch, n_q, 1024, rank, 6, rng.integers(-1, 6, batch), page=page, max_len=max_len, seed=9)
+    count = rng.integers(0, n_q + 1, batch).astype(np.int32)
+    count[0] = n_q
+    c.pos = np.where(np.arange(n_q) < count[:, None], c.start[:, None] + np.arange(n_q), -1).astype(np.int32)
+    sh, d, out = c.shape(), c.dev(), c.caches()
+    d["count"] = torch.from_numpy(count).cuda()
+    ws = B.workspace(sh, B.CLSA_OP_ADAPTED, rank)
+    lora = d["a"], d["b"], d["alpha"], d["ids"]
+    B.clsa_project_append_adapted(sh, c.d, d["h"], d["w"], *lora, d["pos"], d["table"], *out, ws)
+    # rows of K and V in the order of h, from the cache
+    rows = torch.from_numpy(np.maximum(c.rows(), 0)).cuda()
+    k, v = (out[i][rows].contiguous() for i in (2, 3))
+
+    def cache():
+        n = batch * max_len
+        return [torch.full((n, c.kvw), 0x20, dtype=torch.uint8, device="cuda") for _ in "kv"] + \
+               [torch.full((n // block if page else batch * -(-max_len // block), c.heads), 0.25, device="cuda") for _ in "kv"]
+
+    want, got = cache(), cache()
+    B.clsa_cache_append8(sh, block, k, v, d["start"], d["count"], d["table"], *want)
+    q, ki = torch.zeros_like(out[0]), torch.full_like(out[1], 3.0)
+    ws8 = B.workspace(sh, B.CLSA_OP_ADAPTED8, rank)
+    ws8.fill_(0xFF)
+    B.clsa_project_append8_adapted(sh, block, c.d, d["h"], d["w"], *lora, d["start"], d["count"], d["table"], q, ki, *got,
+                                   ws8)
+    torch.cuda.synchronize()
+    assert torch.equal(q.view(torch.int16), out[0].view(torch.int16))
+    assert torch.equal(ki.view(torch.int16), out[1].view(torch.int16))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("batch,n_q", [(12, 1), (3, 90)])
+def test_adapted_replayed(batch, n_q):
+    import torch
+    from paper_2606_06467_amd import binding as B
+    c = Case(batch, n_q, 1024, 16, 4, np.arange(batch) % 5 - 1, max_len=96, seed=3)
+    want = c.run()
+    d, out, sh = c.dev(), c.caches(), c.shape()
+    ws = B.workspace(sh, B.CLSA_OP_ADAPTED, c.rank)
+
+    def step():
+        B.clsa_project_append_adapted(sh, c.d, d["h"], d["w"], d["a"], d["b"], d["alpha"], d["ids"], d["pos"],
+                                      d["table"], *out, ws)
+
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for _ in range(3):
+        for t in out:
+            t.fill_(3.0)
+        ws.fill_(0xFF)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(np.array_equal(B.bits_from_bf16(t), w) for t, w in zip(out, want))
+        step()
+        torch.cuda.synchronize()
