@@ -56,7 +56,9 @@ struct ProjArgs {
     const uint16_t *up;        // [n_adapters, features, rank]
     const float *alpha;
     const int32_t *adapter;    // [batch]
-    float *u;                  // [rows, rank]: alpha A h of the rows that have an adapter
+    // alpha A h of the rows that have an adapter: fp32 [rows, rank] for the few-rows kernel, two
+    // bf16 [rows, rank / 16, 2, 16] (adapter_halves) for the tiled one
+    float *u;
     int n_adapters, rank, n_feat;
 };
 
@@ -193,64 +195,57 @@ constexpr int kGemmPitch = kGemmK;           // bf16 per staged row
 constexpr int kGemmOutPitch = kGemmN + 8;    // bf16 per staged output row
 constexpr size_t kGemmLds = sizeof(uint16_t) * 2 * 2 * kGemmM * kGemmPitch;
 
-// u as the A operand of a 16-row product: the lane's row, ranks ro .. ro + 8, as the
-// high or the low bf16 of each fp32 (together 16 bits: hi cut off, lo the rest rounded, so
-// that an infinity stays one).
-__device__ __forceinline__ bf16x8 adapter_operand(const float *u, bool low) {
-    const float4 x = *reinterpret_cast<const float4 *>(u), y = *reinterpret_cast<const float4 *>(u + 4);
-    const float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-    bf16x8 o;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float hi = __uint_as_float(__float_as_uint(f[e]) & 0xffff0000u);
-        const float rest = f[e] - hi;
-        o[e] = low ? (rest == rest ? (__bf16)rest : (__bf16)0.0f) : (__bf16)hi;
-    }
-    return o;
-}
-
 // Adds the adapters' part to a wave's 64 x 64 tile of the tiled product (c[mt][nt]: rows
-// r0 + 16 mt, features f0 + 16 nt).  A 32-wide step holds 16 ranks twice, the high and the
-// low parts of u against the same B.  Rows of different sequences can share a 16-row
-// tile: the tile is then made once for each adapter in it and added to that adapter's rows
+// r0 + 16 mt, features f0 + 16 nt).  A 32-wide product step holds 16 ranks twice, the high and
+// the low parts of u against the same B.  Rows of different sequences can share a 16-row
+// tile: the step is then made once for each adapter in it and added to that adapter's rows
 // only (a factor of zero would carry one adapter's infinities to another's rows).
 __device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, f32x4 (&c)[4][4]) {
     const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
-    const bool low = grp >= 2;
+    const uint16_t *halves = reinterpret_cast<const uint16_t *>(a.u);
+    const int pitch = div_up(a.rank, 16) * 32;
+    int mine[4];
+#pragma unroll
     for (int mt = 0; mt < 4; ++mt) {
-        if (r0 + 16 * mt >= a.rows) break;
-        const int r = min(r0 + 16 * mt + col, a.rows - 1);
-        const int mine = adapter_of(a, r / a.n_q);
-        uint64_t todo = __ballot(mine >= 0) & 0xffffull;
-        while (todo) {
-            const int id = __builtin_amdgcn_readlane(mine, __builtin_ctzll(todo));
-            const uint64_t same = __ballot(mine == id) & 0xffffull;
-            todo &= ~same;
-            f32x4 t[4];
+        const int r = r0 + 16 * mt + col;
+        mine[mt] = r < a.rows ? adapter_of(a, r / a.n_q) : -1;
+    }
+    for (int j = 0; j < a.rank; j += 16) {
+        bf16x8 av[4], bv[4];
 #pragma unroll
-            for (int nt = 0; nt < 4; ++nt) t[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
-            for (int j = 0; j < a.rank; j += 16) {
-                const int ro = j + (grp & 1) * 8;
-                bf16x8 av = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u}), bv[4];
-                const bool in = ro < a.rank;
-                if (in && mine == id) av = adapter_operand(a.u + (size_t)r * a.rank + ro, low);
+        for (int mt = 0; mt < 4; ++mt) {
+            av[mt] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
+            if (mine[mt] >= 0) av[mt] = ld8(halves + (size_t)(r0 + 16 * mt + col) * pitch + 2 * j + grp * 8);
+        }
+        const int ro = j + (grp & 1) * 8;
+        int held = -1;  // the adapter that bv holds
 #pragma unroll
-                for (int nt = 0; nt < 4; ++nt) {
-                    bv[nt] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
-                    if (in) bv[nt] = ld8(a.up + ((size_t)id * a.n_feat + f0 + 16 * nt + col) * a.rank + ro);
+        for (int mt = 0; mt < 4; ++mt) {
+            uint64_t todo = __ballot(mine[mt] >= 0) & 0xffffull;
+            while (todo) {
+                const int id = __builtin_amdgcn_readlane(mine[mt], __builtin_ctzll(todo));
+                const uint64_t same = __ballot(mine[mt] == id) & 0xffffull;
+                todo &= ~same;
+                if (id != held) {
+#pragma unroll
+                    for (int nt = 0; nt < 4; ++nt) {
+                        bv[nt] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
+                        if (ro < a.rank) bv[nt] = ld8(a.up + ((size_t)id * a.n_feat + f0 + 16 * nt + col) * a.rank + ro);
+                    }
+                    held = id;
                 }
+                if (same == 0xffffull) {
 #pragma unroll
-                for (int nt = 0; nt < 4; ++nt)
-                    t[nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, bv[nt], t[nt], 0, 0, 0);
-            }
+                    for (int nt = 0; nt < 4; ++nt)
+                        c[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[mt], bv[nt], c[mt][nt], 0, 0, 0);
+                } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (!((same >> (4 * grp + e)) & 1)) continue;
+                    for (int nt = 0; nt < 4; ++nt) {
+                        const f32x4 t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[mt], bv[nt], c[mt][nt], 0, 0, 0);
 #pragma unroll
-                for (int nt = 0; nt < 4; ++nt) {
-#pragma unroll
-                    for (int m = 0; m < 4; ++m)
-                        if (m == mt) c[m][nt][e] += t[nt][e];
+                        for (int e = 0; e < 4; ++e)
+                            c[mt][nt][e] = (same >> (4 * grp + e)) & 1 ? t[e] : c[mt][nt][e];
+                    }
                 }
             }
         }
@@ -416,7 +411,87 @@ bool project_supported(int d_model) {
     return d_model >= 512 && d_model <= 8192 && d_model % 512 == 0;
 }
 
-// u = alpha A h.  A wave makes one rank of one row.
+// alpha A h in two bf16: the high one cut off, the low one the rest rounded, together 16
+// bits (so that an infinity stays one; its rest is none).
+__device__ __forceinline__ void adapter_halves(float u, uint16_t *p) {
+    const uint32_t hi = __float_as_uint(u) & 0xffff0000u;
+    const float rest = u - __uint_as_float(hi);
+    const __bf16 lo = rest == rest ? (__bf16)rest : (__bf16)0.0f;
+    p[0] = (uint16_t)(hi >> 16);
+    p[16] = __builtin_bit_cast(uint16_t, lo);
+}
+
+// u = alpha A h of many rows: one workgroup = up to 16 RT rows of one sequence x 16 NT ranks,
+// d_model split over 8 waves whose parts meet in LDS.  h is read once (for each 32 ranks),
+// which bounds it; A comes from the caches.
+template <int RT, int NT>
+__global__ __launch_bounds__(512) void adapter_down_tile_kernel(ProjArgs a) {
+    constexpr int S = 4;  // 32-wide steps whose loads are in flight together
+    __shared__ float part[kSplitWaves][16 * RT][16 * NT + 1];
+    const int tiles = div_up(a.n_q, 16 * RT), b = blockIdx.x / tiles, t0 = (blockIdx.x % tiles) * 16 * RT;
+    const int id = adapter_of(a, b);
+    if (id < 0) return;  // uniform
+    const int j0 = blockIdx.y * 16 * NT, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int col = lane & 15, grp = lane >> 4, steps = a.d / 256;
+    const uint16_t *hp[RT], *ap[NT];
+#pragma unroll
+    for (int m = 0; m < RT; ++m)
+        hp[m] = a.h + ((size_t)b * a.n_q + min(t0 + 16 * m + col, a.n_q - 1)) * a.d + wave * steps * 32 + grp * 8;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+        ap[n] = a.down + ((size_t)id * a.rank + min(j0 + 16 * n + col, a.rank - 1)) * a.d + wave * steps * 32 + grp * 8;
+    f32x4 c[RT][NT];
+#pragma unroll
+    for (int m = 0; m < RT; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) c[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < steps; s0 += S) {
+        bf16x8 av[S][RT], bv[S][NT];
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const bool in = s0 + s < steps;  // uniform
+#pragma unroll
+            for (int m = 0; m < RT; ++m) {
+                av[s][m] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
+                if (in) av[s][m] = ld8(hp[m] + (s0 + s) * 32);
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                bv[s][n] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
+                if (in) bv[s][n] = ld8(ap[n] + (s0 + s) * 32);
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int m = 0; m < RT; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    c[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[s][m], bv[s][n], c[m][n], 0, 0, 0);
+    }
+#pragma unroll
+    for (int m = 0; m < RT; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) part[wave][16 * m + 4 * grp + e][16 * n + col] = c[m][n][e];
+    __syncthreads();
+    uint16_t *halves = reinterpret_cast<uint16_t *>(a.u);
+    const int pitch = div_up(a.rank, 16) * 32;
+    const float alpha = a.alpha[id];
+    for (int i = threadIdx.x; i < 16 * RT * 16 * NT; i += 512) {
+        const int m = i / (16 * NT), n = i % (16 * NT), j = j0 + n;
+        if (t0 + m >= a.n_q || j >= div_up(a.rank, 16) * 16) continue;
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kSplitWaves; ++w) sum += part[w][m][n];
+        // ranks past the last fill up a step with zeros
+        adapter_halves(j < a.rank ? sum * alpha : 0.0f,
+                       halves + ((size_t)b * a.n_q + t0 + m) * pitch + (j >> 4) * 32 + (j & 15));
+    }
+}
+
+// u = alpha A h of few rows: a wave makes one rank of one row.
 __global__ __launch_bounds__(256) void adapter_down_kernel(ProjArgs a) {
     const int per_row = a.rank / 4, row = blockIdx.x / per_row;
     const int j = (blockIdx.x % per_row) * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -429,6 +504,23 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(ProjArgs a) {
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) sum += __shfl_xor(sum, m);
     if (lane == 0) a.u[(size_t)row * a.rank + j] = sum * a.alpha[id];
+}
+
+static hipError_t launch_adapter_down(const ProjArgs &a, int batch, hipStream_t stream) {
+    if (a.rows <= kSplitMaxRows) {
+        adapter_down_kernel<<<dim3(a.rows * (a.rank / 4)), dim3(256), 0, stream>>>(a);
+        return hipGetLastError();
+    }
+    // 32 rows a workgroup where that still fills the chip
+    const bool two = (int64_t)batch * div_up(a.n_q, 32) >= 256 && a.n_q > 16, wide = a.rank > 16;
+    const int64_t tiles = (int64_t)batch * div_up(a.n_q, two ? 32 : 16);
+    if (tiles > 0x7fffff) return hipErrorInvalidConfiguration;  // 2^32 threads a launch
+    const dim3 grid((unsigned)tiles, div_up(a.rank, wide ? 32 : 16)), wg(512);
+    if (two && wide) adapter_down_tile_kernel<2, 2><<<grid, wg, 0, stream>>>(a);
+    else if (two) adapter_down_tile_kernel<2, 1><<<grid, wg, 0, stream>>>(a);
+    else if (wide) adapter_down_tile_kernel<1, 2><<<grid, wg, 0, stream>>>(a);
+    else adapter_down_tile_kernel<1, 1><<<grid, wg, 0, stream>>>(a);
+    return hipGetLastError();
 }
 
 template <int KS, int NB = 1, bool ADAPTED = false>
@@ -471,10 +563,7 @@ static hipError_t launch_project_args(const Geometry &g, int d_model, ProjArgs a
     const bool paged = g.page_shift >= 0;
     if (ADAPTED) {
         a.n_feat = n_feat;
-        const int64_t blocks = (int64_t)g.rows * (a.rank / 4);
-        if (blocks > 0xffffff) return hipErrorInvalidConfiguration;  // 2^32 threads a launch
-        adapter_down_kernel<<<dim3((unsigned)blocks), dim3(256), 0, stream>>>(a);
-        const hipError_t e = hipGetLastError();
+        const hipError_t e = launch_adapter_down(a, g.batch, stream);
         if (e != hipSuccess) return e;
     }
     if (g.rows <= kSplitMaxRows) {
