@@ -170,13 +170,15 @@ struct NormGradArgs {
 
 // Rows in turn, each held by a wave (or the workgroup): the sum g xhat, then dx; dy xhat
 // stays in registers until the last row, so that each workgroup writes one row of sums.
+constexpr int kGradWaves = 8;  // of a workgroup whose waves hold a row each
 template <int P, bool WAVE>
-__global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_grad_kernel(NormGradArgs a) {
+__global__ __launch_bounds__(WAVE ? 64 * kGradWaves : 1024) void norm_grad_kernel(NormGradArgs a) {
     __shared__ float s_sum[2][16];
     extern __shared__ float s_dw[];  // WAVE: the waves' sums meet here, [d]
     const int t = WAVE ? threadIdx.x & 63 : threadIdx.x, width = WAVE ? 64 : blockDim.x;
     const int wave = threadIdx.x >> 6;
-    const int first = WAVE ? blockIdx.x * 4 + wave : blockIdx.x, step = WAVE ? gridDim.x * 4 : gridDim.x;
+    const int first = WAVE ? blockIdx.x * kGradWaves + wave : blockIdx.x;
+    const int step = WAVE ? gridDim.x * kGradWaves : gridDim.x;
     uint4 w[P];
     float dw[P][8];
 #pragma unroll
@@ -237,7 +239,7 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_grad_kernel(NormGradAr
     }
     float *part = a.part + (size_t)blockIdx.x * a.d;
     if (WAVE) {  // wave after wave, in a fixed order
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < kGradWaves; ++k) {
             if (wave == k) {
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
@@ -246,7 +248,7 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_grad_kernel(NormGradAr
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
                             const float z = k ? s_dw[8 * p + e] + dw[i][e] : dw[i][e];
-                            if (k < 3) s_dw[8 * p + e] = z;
+                            if (k < kGradWaves - 1) s_dw[8 * p + e] = z;
                             else part[8 * p + e] = z;
                         }
                     }
@@ -267,19 +269,36 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_grad_kernel(NormGradAr
     }
 }
 
-// dw: the workgroups' sums, added in a fixed order: 16 threads take every 16th, for 16 columns.
+// dw: the workgroups' sums, added in a fixed order: 16 threads take every 16th, for 4 columns
+// of 64 each.  Their loads are independent, so that what counts is few rounds of them.
 __global__ __launch_bounds__(256) void norm_grad_join_kernel(NormGradArgs a) {
-    __shared__ float s[16][17];
-    const int c = threadIdx.x & 15, k = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
-    float sum = 0.0f;
-    if (col < a.d)
-        for (int p = k; p < a.parts; p += 16) sum += a.part[(size_t)p * a.d + col];
+    __shared__ float4 s[16][16];
+    const int c = threadIdx.x & 15, k = threadIdx.x >> 4, col = blockIdx.x * 64 + c * 4;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (col < a.d) {
+#pragma unroll 8
+        for (int p = k; p < a.parts; p += 16) {
+            const float4 v = *reinterpret_cast<const float4 *>(a.part + (size_t)p * a.d + col);
+            sum.x += v.x;
+            sum.y += v.y;
+            sum.z += v.z;
+            sum.w += v.w;
+        }
+    }
     s[k][c] = sum;
     __syncthreads();
     if (k == 0 && col < a.d) {
 #pragma unroll
-        for (int j = 1; j < 16; ++j) sum += s[j][c];
-        a.dweight[col] = sum;
+        for (int j = 1; j < 16; ++j) {
+            sum.x += s[j][c].x;
+            sum.y += s[j][c].y;
+            sum.z += s[j][c].z;
+            sum.w += s[j][c].w;
+        }
+        a.dweight[col] = sum.x;  // 4-byte aligned: one at a time
+        a.dweight[col + 1] = sum.y;
+        a.dweight[col + 2] = sum.z;
+        a.dweight[col + 3] = sum.w;
     }
 }
 
@@ -337,10 +356,11 @@ hipError_t launch_norm(int rows, int d, double eps, const void *x, const void *r
     return hipGetLastError();
 }
 
-// Workgroups of the backward pass: two per CU of rows that waves hold, else one a row up
-// to the same number.
+// Workgroups of the backward pass: one a CU where waves hold rows, else one a row up to
+// two a CU.
 int norm_grad_parts(int rows, int d) {
-    return norm_by_wave(rows, d / 8) ? (div_up(rows, 4) < 512 ? div_up(rows, 4) : 512) : (rows < 512 ? rows : 512);
+    if (norm_by_wave(rows, d / 8)) return rows < 256 * kGradWaves ? div_up(rows, kGradWaves) : 256;
+    return rows < 512 ? rows : 512;
 }
 
 hipError_t launch_norm_grad(int rows, int d, const void *s, const float *rstd, const void *weight,
@@ -362,7 +382,7 @@ hipError_t launch_norm_grad(int rows, int d, const void *s, const float *rstd, c
     a.parts = norm_grad_parts(rows, d);
     const dim3 grid(a.parts);
     if (norm_by_wave(rows, a.pieces)) {
-        const dim3 wg(256);
+        const dim3 wg(64 * kGradWaves);
         const size_t lds = sizeof(float) * d;
         switch (div_up(a.pieces, 64)) {
             case 1: norm_grad_kernel<1, true><<<grid, wg, lds, stream>>>(a); break;
@@ -382,7 +402,7 @@ hipError_t launch_norm_grad(int rows, int d, const void *s, const float *rstd, c
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    norm_grad_join_kernel<<<dim3(div_up(d, 16)), dim3(256), 0, stream>>>(a);
+    norm_grad_join_kernel<<<dim3(div_up(d, 64)), dim3(256), 0, stream>>>(a);
     return hipGetLastError();
 }
 

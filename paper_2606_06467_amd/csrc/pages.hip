@@ -67,8 +67,10 @@ __global__ __launch_bounds__(256) void pages_fork_kernel(ForkArgs a) {
 hipError_t launch_pages_fork(const Geometry &g, int pages, const int32_t *parent, int32_t *table,
                              int32_t *seq_lens, int32_t *refs, hipStream_t stream) {
     if (g.batch > kForkEntries) return hipErrorInvalidValue;
-    ForkArgs a{{table, refs, g.batch, g.max_pages, pages}, parent, seq_lens, kForkEntries / g.batch};
-    a.cols = a.cols < 64 ? a.cols : 64;
+    // about 1024 entries a workgroup, whole 16-byte pieces of a row where that many fit
+    // (72 slots x 235 pages: 64 columns 13.1 us, 12 3.9)
+    ForkArgs a{{table, refs, g.batch, g.max_pages, pages}, parent, seq_lens, 1024 / g.batch / 4 * 4};
+    a.cols = a.cols < 4 ? (4 * g.batch <= kForkEntries ? 4 : kForkEntries / g.batch) : a.cols < 64 ? a.cols : 64;
     pages_fork_kernel<<<dim3(div_up(g.max_pages, a.cols) + 1), dim3(256), 0, stream>>>(a);
     return hipGetLastError();
 }
@@ -161,7 +163,8 @@ hipError_t launch_pages_copy(int pages, int tensors, const PagedTensor *t, int n
 
 // ---- reserve ----
 
-// Sum of v over the threads before this one, and over all of them.
+// Sum of v over the threads before this one, and over all of them (T threads).
+template <int T>
 __device__ __forceinline__ int block_scan(int v, int *s, int &all) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int x = v;
@@ -174,7 +177,8 @@ __device__ __forceinline__ int block_scan(int v, int *s, int &all) {
     __syncthreads();
     int before = 0;
     all = 0;
-    for (int w = 0; w < kPlanThreads / 64; ++w) {
+#pragma unroll
+    for (int w = 0; w < T / 64; ++w) {
         if (w < wave) before += s[w];
         all += s[w];
     }
@@ -254,7 +258,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_reserve_kernel(ReserveArgs
         const bool keeps = st >= 0 && ref_of(refs + st) == -(i + 1);
         const bool wants = st != kNone && !keeps;
         int all;
-        const int k = need + block_scan(wants, s_scan, all);
+        const int k = need + block_scan<kPlanThreads>(wants, s_scan, all);
         if (wants) {
             a.src[k] = st;   // -1: nothing to copy
             a.dst[k] = i;    // the entry, until its page is known
@@ -279,7 +283,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_reserve_kernel(ReserveArgs
             n += free[j];
         }
         int all;
-        int k = found + block_scan(n, s_scan, all);
+        int k = found + block_scan<kPlanThreads>(n, s_scan, all);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if (free[j] && k < need) a.state[k] = p + j;
@@ -302,6 +306,95 @@ __global__ __launch_bounds__(kPlanThreads) void pages_reserve_kernel(ReserveArgs
         } else if (src >= 0) {
             atomicAdd(refs + src, 1);  // nothing happens: its holder holds it still
         }
+    }
+    if (tid == 0) {
+        *a.n_pairs = enough ? need : 0;
+        *a.missing = enough ? 0 : need - found;
+        const uint32_t bits = s_odd | (enough ? 0u : kDevErrPages);
+        if (bits) note_device_error(bits);
+    }
+}
+
+// The same for at most T entries, one a thread.  A page that is free stays free until it is
+// taken, so the first free ones are looked up while the entries are on their way, and the
+// writers of a page that others hold meet in a hash table in LDS: no counter changes
+// before the call is known to have enough pages.
+template <int T>
+__global__ __launch_bounds__(T) void pages_reserve_few_kernel(ReserveArgs a) {
+    constexpr int H = 2 * T, N = 2048 / T;  // hash slots; pages a thread looks at in a turn
+    __shared__ int s_scan[T / 64], s_key[H], s_writers[H], s_last[H], s_free[T];
+    __shared__ uint32_t s_odd;
+    const int tid = threadIdx.x;
+    int32_t *refs = a.p.refs;
+    bool free[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) free[j] = N * tid + j < a.p.pages && refs[N * tid + j] == 0;
+    if (tid == 0) s_odd = 0u;
+    for (int h = tid; h < H; h += T) {
+        s_key[h] = -1;
+        s_writers[h] = 0;
+        s_last[h] = -1;
+    }
+    __syncthreads();
+    uint32_t odd = 0u;
+    for (int b = tid; b < a.p.batch; b += T) {
+        const int first = a.start[b], n = a.count[b];
+        if (first < 0 || first > a.max_len || n < 0 || n > a.n_q || n > a.max_len - first) odd |= kDevErrAppend;
+    }
+    size_t at = 0;
+    const bool reached = tid < a.p.batch * a.slots && reserve_entry(a, tid, at);
+    int src = -1, held = 0, h = 0;
+    if (reached) {
+        src = a.p.table[at];
+        if (src < -1 || src >= a.p.pages) odd |= kDevErrPages;
+        if (src < 0 || src >= a.p.pages) src = -1;
+        else held = refs[src];
+        if (src >= 0 && held != 1) {
+            h = (int)(((uint32_t)src * 2654435761u) >> 16) & (H - 1);
+            for (;;) {  // at most T keys in 2 T slots
+                const int key = atomicCAS(&s_key[h], -1, src);
+                if (key == -1 || key == src) break;
+                h = (h + 1) & (H - 1);
+            }
+            atomicAdd(&s_writers[h], 1);
+            atomicMax(&s_last[h], tid);
+        }
+    }
+    if (odd) atomicOr(&s_odd, odd);
+    __syncthreads();
+    const bool keeps = src >= 0 && (held == 1 || (s_writers[h] == held && s_last[h] == tid));
+    const bool wants = reached && !keeps;
+    int need;
+    const int k = block_scan<T>(wants, s_scan, need);
+    int found = 0;
+    for (int p0 = 0; found < need;) {
+        int n = 0, all;
+#pragma unroll
+        for (int j = 0; j < N; ++j) n += free[j];
+        int f = found + block_scan<T>(n, s_scan, all);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            if (free[j] && f < need) s_free[f] = p0 + N * tid + j;
+            f += free[j];
+        }
+        found += all;
+        p0 += N * T;
+        if (p0 >= a.p.pages) break;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int p = p0 + N * tid + j;
+            free[j] = p < a.p.pages && refs[p] == 0;
+        }
+    }
+    __syncthreads();
+    const bool enough = found >= need;
+    if (wants && enough) {
+        const int page = s_free[k];
+        a.p.table[at] = page;
+        refs[page] = 1;
+        a.src[k] = src;  // -1: nothing to copy
+        a.dst[k] = page;
+        if (src >= 0) atomicSub(refs + src, 1);
     }
     if (tid == 0) {
         *a.n_pairs = enough ? need : 0;
@@ -339,7 +432,9 @@ hipError_t launch_pages_reserve(const Geometry &g, int pages, int tensors, const
     a.state = ws + 64;
     a.src = a.state + entries;
     a.dst = a.src + entries;
-    pages_reserve_kernel<<<dim3(1), dim3(kPlanThreads), 0, stream>>>(a);
+    if (entries <= 256) pages_reserve_few_kernel<256><<<dim3(1), dim3(256), 0, stream>>>(a);
+    else if (entries <= kPlanThreads) pages_reserve_few_kernel<kPlanThreads><<<dim3(1), dim3(kPlanThreads), 0, stream>>>(a);
+    else pages_reserve_kernel<<<dim3(1), dim3(kPlanThreads), 0, stream>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || tensors == 0) return e;
     CopyArgs c{};
@@ -369,40 +464,81 @@ __global__ __launch_bounds__(256) void pages_count_kernel(CompactArgs a) {
     }
 }
 
+// Pools whose pages one workgroup counts in LDS, and the tables that it goes through itself.
+constexpr int kLdsPages = 8192;
+constexpr int kLdsEntries = 32768;
+
 // One workgroup: with U pages in use, the k-th page from U on that the table alone holds
 // moves to the k-th free page below U.  There are at least as many of those; a page that
-// something else holds stays.
+// something else holds stays.  COUNT: it makes the table's counts as well, in LDS.
+template <bool COUNT>
 __global__ __launch_bounds__(kPlanThreads) void pages_compact_kernel(CompactArgs a) {
+    constexpr int N = 8;  // consecutive pages a thread looks at in a turn
     __shared__ int s_scan[kPlanThreads / 64];
-    __shared__ int s_bound;
+    __shared__ int s_bound, s_odd;
+    __shared__ int32_t s_held[COUNT ? kLdsPages : 1];
     const int tid = threadIdx.x;
-    int used = 0;
-    for (int p0 = 0; p0 < a.p.pages; p0 += kPlanThreads) {
-        const int p = p0 + tid;
-        int all;
-        block_scan(p < a.p.pages && a.p.refs[p] > 0, s_scan, all);
-        used += all;
+    int r[N], mine = 0;
+    if (COUNT)
+        for (int p = tid; p < a.p.pages; p += kPlanThreads) s_held[p] = 0;
+    if (tid == 0) s_bound = s_odd = 0;
+    for (int p0 = 0; p0 < a.p.pages; p0 += N * kPlanThreads)
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int p = p0 + N * tid + j;
+            r[j] = p < a.p.pages ? a.p.refs[p] : 0;
+            mine += r[j] > 0;
+        }
+    int used;
+    block_scan<kPlanThreads>(mine, s_scan, used);
+    if (COUNT) {
+        bool odd = false;
+        const int n = a.p.batch * a.p.max_pages;
+        for (int i0 = 0; i0 < n; i0 += 4 * kPlanThreads) {
+            int e[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int i = i0 + j * kPlanThreads + tid;
+                e[j] = i < n ? a.p.table[i] : -1;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (e[j] >= 0 && e[j] < a.p.pages) atomicAdd(&s_held[e[j]], 1);
+                else odd |= e[j] != -1;
+            }
+        }
+        if (odd) s_odd = 1;
+        __syncthreads();
     }
-    if (tid == 0) s_bound = 0;
-    __syncthreads();
     int holes = 0, moves = 0, bound = 0;
-    for (int p0 = 0; p0 < a.p.pages; p0 += kPlanThreads) {
-        const int p = p0 + tid;
-        const bool in = p < a.p.pages;
-        const int r = in ? a.p.refs[p] : 0;
-        const bool hole = in && p < used && r <= 0, move = in && p >= used && r > 0 && r == a.held[p];
+    for (int p0 = 0; p0 < a.p.pages; p0 += N * kPlanThreads) {
+        const int first = p0 + N * tid;
+        int n = 0;  // holes, and moves in the high half
+        bool hole[N], move[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int p = first + j;
+            const bool in = p < a.p.pages;
+            if (a.p.pages > N * kPlanThreads) r[j] = in ? a.p.refs[p] : 0;
+            hole[j] = in && p < used && r[j] <= 0;
+            move[j] = in && p >= used && r[j] > 0 && r[j] == (COUNT ? s_held[p] : a.held[p]);
+            n += hole[j] + (move[j] << 16);
+            if (in) a.to[p] = p;
+            if (r[j] > 0 && !move[j]) bound = p + 1;
+        }
         int all;
-        const int h = holes + block_scan(hole, s_scan, all);
-        holes += all;
-        if (hole) a.dst[h] = p;
-        const int m = moves + block_scan(move, s_scan, all);
-        moves += all;
-        if (move) a.src[m] = p;
-        if (in) a.to[p] = p;
-        if (r > 0 && !move) bound = p + 1;
+        const int before = block_scan<kPlanThreads>(n, s_scan, all);
+        int h = holes + (before & 0xffff), m = moves + (before >> 16);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            if (hole[j]) a.dst[h++] = first + j;
+            if (move[j]) a.src[m++] = first + j;
+        }
+        holes += all & 0xffff;
+        moves += all >> 16;
     }
     if (bound) atomicMax(&s_bound, bound);
-    __threadfence();
+    __threadfence_block();
     __syncthreads();
     for (int k = tid; k < moves; k += kPlanThreads) {
         const int src = a.src[k], dst = a.dst[k];
@@ -413,6 +549,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_compact_kernel(CompactArgs
     if (tid == 0) {
         *a.n_pairs = moves;
         *a.bound = max(s_bound, moves ? a.dst[moves - 1] + 1 : 0);
+        if (s_odd) note_device_error(kDevErrPages);
     }
 }
 
@@ -447,12 +584,16 @@ hipError_t launch_pages_compact(const Geometry &g, int pages, int tensors, const
     a.to = a.held + pages;
     a.src = a.to + pages;
     a.dst = a.src + pages;
-    hipError_t e = launch_zero_u32(reinterpret_cast<uint32_t *>(a.held), (size_t)pages, stream);
-    if (e != hipSuccess) return e;
     const size_t n = (size_t)g.batch * g.max_pages;
     const unsigned grid = (unsigned)(n < 2048 * 256 ? (n + 255) / 256 : 2048);
-    pages_count_kernel<<<dim3(grid), dim3(256), 0, stream>>>(a);
-    pages_compact_kernel<<<dim3(1), dim3(kPlanThreads), 0, stream>>>(a);
+    if (pages <= kLdsPages && n <= kLdsEntries) {
+        pages_compact_kernel<true><<<dim3(1), dim3(kPlanThreads), 0, stream>>>(a);
+    } else {
+        hipError_t e = launch_zero_u32(reinterpret_cast<uint32_t *>(a.held), (size_t)pages, stream);
+        if (e != hipSuccess) return e;
+        pages_count_kernel<<<dim3(grid), dim3(256), 0, stream>>>(a);
+        pages_compact_kernel<false><<<dim3(1), dim3(kPlanThreads), 0, stream>>>(a);
+    }
     MoveArgs m{a, {}};
     const int per = tensors ? copy_args(m.c, pages, tensors, t) : 0;
     m.c.src = a.src;

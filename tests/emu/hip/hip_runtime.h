@@ -44,6 +44,7 @@ inline int atomicAdd(int *p, int v) { const int o = *p; *p += v; return o; }
 inline int atomicSub(int *p, int v) { const int o = *p; *p -= v; return o; }
 inline int atomicMin(int *p, int v) { const int o = *p; *p = v < o ? v : o; return o; }
 inline int atomicMax(int *p, int v) { const int o = *p; *p = v > o ? v : o; return o; }
+inline int atomicCAS(int *p, int c, int v) { const int o = *p; if (o == c) *p = v; return o; }
 template <class T> inline T emu_atomic_load(const T *p) { return *p; }
 template <class... A> inline hipError_t hipMemcpyFromSymbol(A...) { return hipSuccess; }
 template <class... A> inline hipError_t hipMemcpyToSymbol(A...) { return hipSuccess; }
@@ -260,6 +261,7 @@ inline uint32_t perm(uint32_t hi, uint32_t lo, uint32_t sel) {
 #define __shfl_xor emu::shfl_xor
 #define __shfl_up emu::shfl_up
 #define __threadfence() ((void)0)
+#define __threadfence_block() ((void)0)
 #define __hip_atomic_load(p, order, scope) emu_atomic_load(p)
 #define __hip_atomic_store(p, v, order, scope) ((void)(*(p) = (v)))
 #define __ballot emu::ballot

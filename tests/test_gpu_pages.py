@@ -66,11 +66,12 @@ def test_fork(batch, cols, bad):
 
 @pytest.mark.parametrize("bits8", [False, True])
 @pytest.mark.parametrize("batch,cols,n_q,spare,page", [(1, 4, 1, 9, 64), (6, 9, 1, 99, 64), (40, 30, 300, 1500, 16),
-                                                       (3000, 3, 1, 200, 16), (5, 6, 900, 40, 128), (12, 9, 4, 3, 64)])
+                                                       (3000, 3, 1, 200, 16), (5, 6, 900, 40, 128), (12, 9, 4, 3, 64), (700, 4, 1, 900, 16),
+                                                       (300, 9, 40, 5000, 16)])
 def test_reserve(bits8, batch, cols, n_q, spare, page):
     from paper_2606_06467_amd import binding as B
     rng = np.random.default_rng(batch * cols + n_q)
-    heads = 1 if batch > 1000 else 4
+    heads = 1 if batch >= 300 else 4
     pages = batch * cols // 2 + spare
     table, refs = P.state(rng, batch, cols, pages, shared=0.7, pinned=2)
     start = rng.integers(0, cols * page + 1, batch).astype(np.int32)
@@ -92,7 +93,7 @@ def test_reserve(bits8, batch, cols, n_q, spare, page):
 
 @pytest.mark.parametrize("bits8", [False, True])
 @pytest.mark.parametrize("batch,cols,pages,pinned", [(1, 1, 1, 0), (7, 9, 60, 0), (30, 40, 2000, 12), (50, 3, 5000, 0),
-                                                     (9, 6, 54, 54)])
+                                                     (9, 6, 54, 54), (40, 300, 9001, 4), (700, 64, 4000, 0)])
 def test_compact(bits8, batch, cols, pages, pinned):
     from paper_2606_06467_amd import binding as B
     rng = np.random.default_rng(pages)

@@ -136,7 +136,8 @@ def _reserve(emu, rng, table, refs, start, count, n_q, page, order, tensors=True
 
 @pytest.mark.parametrize("order", [0, 1])
 @pytest.mark.parametrize("batch,cols,n_q,spare", [(1, 4, 1, 9), (5, 6, 1, 20), (33, 9, 40, 200), (1100, 3, 1, 1200),
-                                                  (20, 8, 100, 6000), (17, 6, 3, 4)])
+                                                  (20, 8, 100, 6000), (17, 6, 3, 4), (700, 4, 1, 900),
+                                                  (400, 6, 20, 9000), (400, 6, 20, 10)])
 def test_reserve(emu, batch, cols, n_q, spare, order):
     rng = np.random.default_rng(batch + cols + n_q)
     pages = batch * cols + spare
@@ -150,18 +151,18 @@ def test_reserve(emu, batch, cols, n_q, spare, order):
 
 
 @pytest.mark.parametrize("order", [0, 1])
-def test_reserve_all_holders_write(emu, order):
+@pytest.mark.parametrize("batch", [150, 603, 1500])
+def test_reserve_all_holders_write(emu, batch, order):
     """Every holder of a page writes: all but the last get copies, also across waves."""
     rng = np.random.default_rng(5)
-    batch = 150
     table = np.full((batch, 2), -1, np.int32)
     table[:, 0] = np.arange(batch) % 3 + 400
-    refs = P.holders(table, 600)
+    refs = P.holders(table, 450 + batch)
     _, copies, missing = _reserve(emu, rng, table, refs, [3] * batch, [1] * batch, 1, 16, order)
     assert len(copies) == batch - 3 and not missing
     # one holder of each page does not write: every other one gets a copy
     count = np.ones(batch, np.int32)
-    count[[10, 80, 149 - 149 % 3 + 0]] = 0
+    count[[10, 80, batch - 3]] = 0
     _reserve(emu, rng, table, refs, [3] * batch, count, 1, 16, order)
     # the page of 400 is held from elsewhere too
     refs[400] += 1
@@ -209,7 +210,8 @@ def test_reserve_out_of_range(emu, order):
 
 @pytest.mark.parametrize("order", [0, 1])
 @pytest.mark.parametrize("batch,cols,pages,pinned,bad", [(1, 1, 1, 0, 0), (6, 5, 31, 0, 0), (30, 9, 500, 9, 0),
-                                                         (4, 3, 2100, 0, 0), (8, 8, 64, 3, 0.1)])
+                                                         (4, 3, 2100, 0, 0), (8, 8, 64, 3, 0.1), (5, 900, 9001, 5, 0),
+                                                         (5, 9, 8200, 2, 0.1)])
 def test_compact(emu, batch, cols, pages, pinned, bad, order):
     rng = np.random.default_rng(pages)
     table, refs = P.state(rng, batch, cols, pages, shared=0.6, pinned=pinned, bad=bad)
