@@ -60,6 +60,7 @@ struct ProjArgs {
     // bf16 [rows, rank / 16, 2, 16] (adapter_halves) for the tiled one
     float *u;
     int n_adapters, rank, n_feat;
+    int seq_tiles;             // kOwnTiles: 128-row tiles of a sequence
 };
 
 // Adapter of sequence b, -1 for none.
@@ -195,7 +196,7 @@ constexpr int kGemmPitch = kGemmK;           // bf16 per staged row
 constexpr int kGemmOutPitch = kGemmN + 8;    // bf16 per staged output row
 constexpr size_t kGemmLds = sizeof(uint16_t) * 2 * 2 * kGemmM * kGemmPitch;
 
-// Adds the adapters' part to a wave's 64 x 64 tile of the tiled product (c[mt][nt]: rows
+// kMixed: adds the adapters' part to a wave's 64 x 64 tile of the tiled product (c[mt][nt]: rows
 // r0 + 16 mt, features f0 + 16 nt).  A 32-wide product step holds 16 ranks twice, the high and
 // the low parts of u against the same B.  Rows of different sequences can share a 16-row
 // tile: the step is then made once for each adapter in it and added to that adapter's rows
@@ -210,41 +211,46 @@ __device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, 
         const int r = r0 + 16 * mt + col;
         mine[mt] = r < a.rows ? adapter_of(a, r / a.n_q) : -1;
     }
+#pragma unroll 1
     for (int j = 0; j < a.rank; j += 16) {
-        bf16x8 av[4], bv[4];
+        bf16x8 av[4], bv[2][4];
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt) {
             av[mt] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
             if (mine[mt] >= 0) av[mt] = ld8(halves + (size_t)(r0 + 16 * mt + col) * pitch + 2 * j + grp * 8);
         }
         const int ro = j + (grp & 1) * 8;
-        int held = -1;  // the adapter that bv holds
+        auto load = [&](int id, bf16x8 (&b)[4]) {
+#pragma unroll
+            for (int nt = 0; nt < 4; ++nt) {
+                b[nt] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
+                if (ro < a.rank) b[nt] = ld8(a.up + ((size_t)id * a.n_feat + f0 + 16 * nt + col) * a.rank + ro);
+            }
+        };
 #pragma unroll
         for (int mt = 0; mt < 4; ++mt) {
             uint64_t todo = __ballot(mine[mt] >= 0) & 0xffffull;
-            while (todo) {
-                const int id = __builtin_amdgcn_readlane(mine[mt], __builtin_ctzll(todo));
-                const uint64_t same = __ballot(mine[mt] == id) & 0xffffull;
-                todo &= ~same;
-                if (id != held) {
+            while (todo) {  // two adapters at a time: their loads in flight together
+                uint64_t same[2];
 #pragma unroll
-                    for (int nt = 0; nt < 4; ++nt) {
-                        bv[nt] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
-                        if (ro < a.rank) bv[nt] = ld8(a.up + ((size_t)id * a.n_feat + f0 + 16 * nt + col) * a.rank + ro);
+                for (int q = 0; q < 2; ++q) {
+                    same[q] = 0;
+                    if (todo) {
+                        const int id = __builtin_amdgcn_readlane(mine[mt], __builtin_ctzll(todo));
+                        same[q] = __ballot(mine[mt] == id) & 0xffffull;
+                        todo &= ~same[q];
+                        load(id, bv[q]);
                     }
-                    held = id;
                 }
-                if (same == 0xffffull) {
 #pragma unroll
-                    for (int nt = 0; nt < 4; ++nt)
-                        c[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[mt], bv[nt], c[mt][nt], 0, 0, 0);
-                } else {
+                for (int q = 0; q < 2; ++q) {
+                    if (!same[q]) break;
 #pragma unroll
                     for (int nt = 0; nt < 4; ++nt) {
-                        const f32x4 t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[mt], bv[nt], c[mt][nt], 0, 0, 0);
+                        const f32x4 t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[mt], bv[q][nt], c[mt][nt], 0, 0, 0);
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            c[mt][nt][e] = (same >> (4 * grp + e)) & 1 ? t[e] : c[mt][nt][e];
+                            c[mt][nt][e] = (same[q] >> (4 * grp + e)) & 1 ? t[e] : c[mt][nt][e];
                     }
                 }
             }
@@ -252,7 +258,12 @@ __device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, 
     }
 }
 
-template <bool PAGED, bool ADAPTED>
+// The tiled product's adapters.  kOwnTiles: no row tile holds two sequences; the ranks of its
+// adapter are more of the sum's dimensions, a 64-wide step for every 32 (16 ranks twice,
+// the high and the low parts of u against the same B).  kMixed: adapter_tile above.
+enum GemmMode { kPlain, kOwnTiles, kMixed };
+
+template <bool PAGED, GemmMode MODE>
 __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
     // two stages of A (rows of h) and B (features of w), 128 x 64 bf16 each
     // (dynamic LDS, kGemmLds bytes); the output tile (128 x 128 bf16) reuses it
@@ -278,7 +289,14 @@ __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
         ft = qi / a.band;
     }
     if (rt >= a.rtiles) return;  // uniform: padding workgroups of the last bands
-    const int f0 = ft * kGemmN, r0 = rt * kGemmM;
+    const int f0 = ft * kGemmN;
+    int r0 = rt * kGemmM, row_end = a.rows, id = -1;
+    if (MODE == kOwnTiles) {
+        const int b = rt / a.seq_tiles;
+        r0 = b * a.n_q + (rt - b * a.seq_tiles) * kGemmM;
+        row_end = (b + 1) * a.n_q;
+        id = adapter_of(a, b);
+    }
     // staging: thread t moves 16-byte pieces t + 256 i (i < 4) of each 128 x 64
     // tile: row (t >> 3) + 32 i, columns 8 (t & 7) .. + 8
     const int lrow = tid >> 3, lcol = (tid & 7) * 8;
@@ -286,14 +304,11 @@ __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
     const uint16_t *hp[4], *wp[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        hp[i] = a.h + (size_t)min(r0 + lrow + 32 * i, a.rows - 1) * a.d + lcol;  // tail rows: never stored
+        hp[i] = a.h + (size_t)min(r0 + lrow + 32 * i, row_end - 1) * a.d + lcol;  // tail rows: never stored
         wp[i] = a.w + (size_t)(f0 + lrow + 32 * i) * a.d + lcol;
     }
     // two register sets: the loads for step k + 2 are issued while step k is
-    // computed, and step k + 1 (loaded a step earlier) goes to LDS after it;
-    // every step issues its loads (the last two reload a valid step that is
-    // never stored), so that the compiler's wait before each LDS store leaves
-    // the newest 8 loads in flight
+    // computed, and step k + 1 (loaded a step earlier) goes to LDS after it
     u32x4 ra[2][4], rb[2][4];
     auto gload = [&](int set, int k0) {
 #pragma unroll
@@ -315,15 +330,30 @@ __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
 #pragma unroll
         for (int nt = 0; nt < 4; ++nt) c[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int nk = a.d / kGemmK;  // even (d_model is a multiple of 512)
+    const int steps = nk + (MODE == kOwnTiles && id >= 0 ? div_up(a.rank, 32) : 0);
+    // step e of the adapter's ranks: this thread's pieces of u and of B
+    auto xload = [&](int set, int e) {
+        const int chunk = 2 * e + (lcol >> 5), ro = chunk * 16 + (lcol & 8), pitch = div_up(a.rank, 16) * 32;
+        const uint16_t *halves = reinterpret_cast<const uint16_t *>(a.u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            ra[set][i] = rb[set][i] = u32x4{0u, 0u, 0u, 0u};
+            if (chunk * 16 < a.rank)
+                ra[set][i] = *reinterpret_cast<const u32x4 *>(
+                    halves + (size_t)min(r0 + lrow + 32 * i, row_end - 1) * pitch + e * 64 + lcol);
+            if (ro < a.rank)
+                rb[set][i] = *reinterpret_cast<const u32x4 *>(
+                    a.up + ((size_t)id * a.n_feat + f0 + lrow + 32 * i) * a.rank + ro);
+        }
+    };
     gload(0, 0);
     gload(1, kGemmK);
     lstore(0, 0);
     __syncthreads();
-    for (int kt = 0; kt < nk; kt += 2) {
-      for (int h = 0; h < 2; ++h) {   // unrolled by two so that register sets are static
-        const int k = kt + h;
+    // The products of step k (stage and register set h = k & 1), after the loads for step
+    // k + 2 were issued; step k + 1 goes to the other stage meanwhile.
+    auto step = [&](int h) {
         const int st = h;
-        gload(h, min(k + 2, nk - 1) * kGemmK);  // unconditional (the last steps reload a valid step, never stored): a static load count
         // operand o of 32-wide half ks: A rows (o < 4) and B features of the wave's quadrant
         bf16x8 op[2][8];
         auto read_op = [&](int ks, int o) {
@@ -359,9 +389,25 @@ __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
             __builtin_amdgcn_sched_barrier(0);
         }
         __syncthreads();
-      }
+    };
+    // every step but the last two issues loads: a static count, so that the compiler's wait
+    // before each LDS store leaves the newest 8 loads in flight
+    for (int k = 0; k < nk - 2; k += 2) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {   // unrolled by two so that register sets are static
+            gload(h, (k + h + 2) * kGemmK);
+            step(h);
+        }
     }
-    if (ADAPTED) adapter_tile(a, r0 + wm * 64, f0 + wn * 64, c);
+    for (int k = nk - 2; k < steps; k += 2) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (k + h >= steps) break;
+            if (MODE == kOwnTiles && k + h + 2 < steps) xload(h, k + h + 2 - nk);
+            step(h);
+        }
+    }
+    if (MODE == kMixed) adapter_tile(a, r0 + wm * 64, f0 + wn * 64, c);
     // bf16 results into LDS: C tile (mt, nt) row 4 grp + r, column col
     uint16_t(*s_out)[kGemmOutPitch] = reinterpret_cast<uint16_t(*)[kGemmOutPitch]>(&s_ab[0][0][0][0]);
     static_assert(kGemmLds >= sizeof(uint16_t) * kGemmM * kGemmOutPitch, "output tile fits");
@@ -383,7 +429,7 @@ __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
     else { dst_kind = 3; width = a.kvw; fo = f0 - 512 - a.kvw; }
     for (int rr = tid >> 4; rr < kGemmM; rr += 16) {
         const int r = r0 + rr;
-        if (r >= a.rows) break;
+        if (r >= row_end) break;
         const u32x4 v = *reinterpret_cast<const u32x4 *>(&s_out[rr][piece * 8]);
         uint16_t *dst;
         if (dst_kind == 0) {
@@ -421,18 +467,22 @@ __device__ __forceinline__ void adapter_halves(float u, uint16_t *p) {
     p[16] = __builtin_bit_cast(uint16_t, lo);
 }
 
-// u = alpha A h of many rows: one workgroup = up to 16 RT rows of one sequence x 16 NT ranks,
-// d_model split over 8 waves whose parts meet in LDS.  h is read once (for each 32 ranks),
-// which bounds it; A comes from the caches.
+// u = alpha A h of many rows: one workgroup = up to 16 RT rows of one sequence and 16 NT
+// ranks, d_model split over 8 waves whose parts meet in LDS, 32 ranks at a time.  Where there
+// are rows enough, all ranks: h is then read once, which bounds it, and A comes from the
+// caches (8192 rows, d_model 2560, rank 128: 30 us; 41 with a workgroup for each 32 ranks).
+// Few rows take 32 ranks a workgroup (1505 rows, d_model 4096, rank 64: 14 us, 21 with all).
 template <int RT, int NT>
 __global__ __launch_bounds__(512) void adapter_down_tile_kernel(ProjArgs a) {
-    constexpr int S = 4;  // 32-wide steps whose loads are in flight together
-    __shared__ float part[kSplitWaves][16 * RT][16 * NT + 1];
+    constexpr int S = NT > 4 ? 2 : RT + NT > 3 ? 4 : 8;  // 32-wide steps whose loads are in flight together
+    constexpr int J = NT > 2 ? 2 : NT;     // rank tiles that meet in LDS at a time
+    __shared__ float part[kSplitWaves][16 * RT][16 * J + 1];
     const int tiles = div_up(a.n_q, 16 * RT), b = blockIdx.x / tiles, t0 = (blockIdx.x % tiles) * 16 * RT;
     const int id = adapter_of(a, b);
     if (id < 0) return;  // uniform
-    const int j0 = blockIdx.y * 16 * NT, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int col = lane & 15, grp = lane >> 4, steps = a.d / 256;
+    const int ranks = div_up(a.rank, 16) * 16, j0 = blockIdx.y * 16 * NT;
     const uint16_t *hp[RT], *ap[NT];
 #pragma unroll
     for (int m = 0; m < RT; ++m)
@@ -469,25 +519,29 @@ __global__ __launch_bounds__(512) void adapter_down_tile_kernel(ProjArgs a) {
                 for (int n = 0; n < NT; ++n)
                     c[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[s][m], bv[s][n], c[m][n], 0, 0, 0);
     }
-#pragma unroll
-    for (int m = 0; m < RT; ++m)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) part[wave][16 * m + 4 * grp + e][16 * n + col] = c[m][n][e];
-    __syncthreads();
     uint16_t *halves = reinterpret_cast<uint16_t *>(a.u);
-    const int pitch = div_up(a.rank, 16) * 32;
     const float alpha = a.alpha[id];
-    for (int i = threadIdx.x; i < 16 * RT * 16 * NT; i += 512) {
-        const int m = i / (16 * NT), n = i % (16 * NT), j = j0 + n;
-        if (t0 + m >= a.n_q || j >= div_up(a.rank, 16) * 16) continue;
-        float sum = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kSplitWaves; ++w) sum += part[w][m][n];
-        // ranks past the last fill up a step with zeros
-        adapter_halves(j < a.rank ? sum * alpha : 0.0f,
-                       halves + ((size_t)b * a.n_q + t0 + m) * pitch + (j >> 4) * 32 + (j & 15));
+    for (int n0 = 0; n0 < NT; n0 += J) {
+        if (j0 + 16 * n0 >= ranks) break;  // uniform
+        if (n0) __syncthreads();
+#pragma unroll
+        for (int m = 0; m < RT; ++m)
+#pragma unroll
+            for (int n = 0; n < J; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) part[wave][16 * m + 4 * grp + e][16 * n + col] = c[m][n0 + n][e];
+        __syncthreads();
+        for (int i = threadIdx.x; i < 16 * RT * 16 * J; i += 512) {
+            const int m = i / (16 * J), n = i % (16 * J), j = j0 + 16 * n0 + n;
+            if (t0 + m >= a.n_q || j >= ranks) continue;
+            float sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kSplitWaves; ++w) sum += part[w][m][n];
+            // ranks past the last fill up a step with zeros
+            adapter_halves(j < a.rank ? sum * alpha : 0.0f,
+                           halves + ((size_t)b * a.n_q + t0 + m) * (2 * ranks) + (j >> 4) * 32 + (j & 15));
+        }
     }
 }
 
@@ -506,20 +560,28 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(ProjArgs a) {
     if (lane == 0) a.u[(size_t)row * a.rank + j] = sum * a.alpha[id];
 }
 
+// Sequences long enough for row tiles of their own.
+static bool adapter_own_tiles(int n_q) { return n_q >= 64; }
+
 static hipError_t launch_adapter_down(const ProjArgs &a, int batch, hipStream_t stream) {
     if (a.rows <= kSplitMaxRows) {
         adapter_down_kernel<<<dim3(a.rows * (a.rank / 4)), dim3(256), 0, stream>>>(a);
         return hipGetLastError();
     }
     // 32 rows a workgroup where that still fills the chip
-    const bool two = (int64_t)batch * div_up(a.n_q, 32) >= 256 && a.n_q > 16, wide = a.rank > 16;
+    const bool two = (int64_t)batch * div_up(a.n_q, 32) >= 256 && a.n_q > 16;
     const int64_t tiles = (int64_t)batch * div_up(a.n_q, two ? 32 : 16);
     if (tiles > 0x7fffff) return hipErrorInvalidConfiguration;  // 2^32 threads a launch
-    const dim3 grid((unsigned)tiles, div_up(a.rank, wide ? 32 : 16)), wg(512);
-    if (two && wide) adapter_down_tile_kernel<2, 2><<<grid, wg, 0, stream>>>(a);
-    else if (two) adapter_down_tile_kernel<2, 1><<<grid, wg, 0, stream>>>(a);
-    else if (wide) adapter_down_tile_kernel<1, 2><<<grid, wg, 0, stream>>>(a);
-    else adapter_down_tile_kernel<1, 1><<<grid, wg, 0, stream>>>(a);
+    const bool all = tiles >= 256;  // all ranks in one workgroup
+    const dim3 grid((unsigned)tiles, all ? 1 : div_up(a.rank, 32)), wg(512);
+#define CLSA_DOWN(NT)                                                             \
+    if (two) adapter_down_tile_kernel<2, NT><<<grid, wg, 0, stream>>>(a);         \
+    else adapter_down_tile_kernel<1, NT><<<grid, wg, 0, stream>>>(a)
+    if (a.rank <= 16) { CLSA_DOWN(1); }
+    else if (a.rank <= 32 || !all) { CLSA_DOWN(2); }
+    else if (a.rank <= 64) { CLSA_DOWN(4); }
+    else { CLSA_DOWN(8); }
+#undef CLSA_DOWN
     return hipGetLastError();
 }
 
@@ -589,21 +651,28 @@ static hipError_t launch_project_args(const Geometry &g, int d_model, ProjArgs a
         }
         return hipGetLastError();
     }
-    a.rtiles = div_up(g.rows, kGemmM);
+    a.seq_tiles = div_up(g.n_q, kGemmM);
+    const bool own = ADAPTED && adapter_own_tiles(g.n_q);
+    const int64_t rtiles = own ? (int64_t)g.batch * a.seq_tiles : div_up(g.rows, kGemmM);
+    if (rtiles > 0xffffff) return hipErrorInvalidConfiguration;
+    a.rtiles = (int)rtiles;
     a.ftiles = n_feat / kGemmN;
     // bands of up to 8 row tiles, dealt to the 8 XCDs in turn (the last round
     // padded); fewer row tiles per band when that still leaves XCDs idle
     a.band = a.rtiles >= 64 ? 8 : div_up(a.rtiles, 8);
     const long bands = div_up(a.rtiles, a.band);
     const long blocks = div_up((int)bands, 8) * 8 * (long)a.band * a.ftiles;
-    if (blocks > 0x7fffffffL) return hipErrorInvalidConfiguration;
+    if (blocks > 0xffffffL) return hipErrorInvalidConfiguration;  // 2^32 threads a launch
     const dim3 grid((unsigned)blocks);
-    const void *fn = paged ? reinterpret_cast<const void *>(&project_gemm_kernel<true, ADAPTED>)
-                           : reinterpret_cast<const void *>(&project_gemm_kernel<false, ADAPTED>);
-    hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kGemmLds);
+    using Kernel = void (*)(ProjArgs);
+    Kernel fn = paged ? project_gemm_kernel<true, kPlain> : project_gemm_kernel<false, kPlain>;
+    if (ADAPTED)
+        fn = own ? (paged ? project_gemm_kernel<true, kOwnTiles> : project_gemm_kernel<false, kOwnTiles>)
+                 : (paged ? project_gemm_kernel<true, kMixed> : project_gemm_kernel<false, kMixed>);
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(fn),
+                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)kGemmLds);
     if (e != hipSuccess) return e;
-    if (paged) project_gemm_kernel<true, ADAPTED><<<grid, dim3(256), kGemmLds, stream>>>(a);
-    else project_gemm_kernel<false, ADAPTED><<<grid, dim3(256), kGemmLds, stream>>>(a);
+    fn<<<grid, dim3(256), kGemmLds, stream>>>(a);
     return hipGetLastError();
 }
 
