@@ -44,7 +44,17 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
     return make_uint4(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]), bf16_pair(f[4], f[5]), bf16_pair(f[6], f[7]));
 }
 
-__device__ __forceinline__ uint4 ld16(const uint16_t *p) { return *reinterpret_cast<const uint4 *>(p); }
+// NT: with the non-temporal hint, for rows that together are larger than the caches
+// (kNormStreamed).
+template <bool NT = false>
+__device__ __forceinline__ uint4 ld16(const uint16_t *p) {
+    return NT ? load16_nt(p) : *reinterpret_cast<const uint4 *>(p);
+}
+template <bool NT>
+__device__ __forceinline__ void st16(uint16_t *p, uint4 v) {
+    if (NT) __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4 *>(p));
+    else *reinterpret_cast<uint4 *>(p) = v;
+}
 
 // Sum (or largest) of a row's values: over the wave, then over the workgroup's waves
 // where they share the row.
@@ -61,14 +71,12 @@ __device__ __forceinline__ T row_reduce(T v, T *s, F f) {
     return v;
 }
 
-// A row's P pieces a thread; WAVE: a wave holds a row, else the workgroup does.
-template <int P, bool WAVE>
-__global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_kernel(NormArgs a) {
+// One workgroup = one row, P pieces a thread.
+template <int P, bool NT>
+__global__ __launch_bounds__(1024) void norm_kernel(NormArgs a) {
     __shared__ double s_sum[16];
     __shared__ uint32_t s_top[16];
-    const int t = WAVE ? threadIdx.x & 63 : threadIdx.x, width = WAVE ? 64 : blockDim.x;
-    const int row = WAVE ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
-    if (row >= a.rows) return;  // a whole wave or workgroup
+    const int t = threadIdx.x, width = blockDim.x, row = blockIdx.x;
     const size_t at = (size_t)row * a.d;
     uint4 v[P], r[P], w[P];
     bool live[P];
@@ -78,8 +86,8 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_kernel(NormArgs a) {
         live[i] = p < a.pieces;
         v[i] = r[i] = w[i] = make_uint4(0u, 0u, 0u, 0u);
         if (live[i]) {
-            v[i] = ld16(a.x + at + 8 * p);
-            if (a.residual) r[i] = ld16(a.residual + at + 8 * p);
+            v[i] = ld16<NT>(a.x + at + 8 * p);
+            if (a.residual) r[i] = ld16<NT>(a.residual + at + 8 * p);
             w[i] = ld16(a.weight + 8 * p);
         }
     }
@@ -99,13 +107,13 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_kernel(NormArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum = fma((double)f[e], (double)f[e], sum);
     }
-    sum = row_reduce<WAVE>(sum, s_sum, [](double x, double y) { return x + y; });
+    sum = row_reduce<false>(sum, s_sum, [](double x, double y) { return x + y; });
     const float rstd = (float)(1.0 / sqrt(sum / a.d + a.eps));
     if (a.rstd && t == 0) a.rstd[row] = rstd;
     if (a.sum) {
 #pragma unroll
         for (int i = 0; i < P; ++i)
-            if (live[i]) *reinterpret_cast<uint4 *>(a.sum + at + 8 * (t + i * width)) = v[i];
+            if (live[i]) st16<NT>(a.sum + at + 8 * (t + i * width), v[i]);
     }
     float whole = 0.0f;  // the row's scale, where the row is one group
     if (a.y8 && a.group_shift < 0) {
@@ -121,7 +129,7 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_kernel(NormArgs a) {
                 top = max(top, m < 0x7f800000u ? m : 0u);
             }
         }
-        top = row_reduce<WAVE>(top, s_top, [](uint32_t x, uint32_t y) { return max(x, y); });
+        top = row_reduce<false>(top, s_top, [](uint32_t x, uint32_t y) { return max(x, y); });
         whole = e4m3_scale(top);
         if (t == 0) a.y_scale[row] = whole;
     }
@@ -138,7 +146,7 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_kernel(NormArgs a) {
             const uint32_t m = __float_as_uint(f[e]) & 0x7fffffffu;
             top = max(top, m < 0x7f800000u ? m : 0u);
         }
-        if (a.y && live[i]) *reinterpret_cast<uint4 *>(a.y + at + 8 * p) = pack8(f);
+        if (a.y && live[i]) st16<NT>(a.y + at + 8 * p, pack8(f));
         if (a.y8) {
             float scale = whole;
             if (a.group_shift >= 0) {  // 4, 8 or 16 neighbouring lanes hold a group
@@ -171,7 +179,7 @@ struct NormGradArgs {
 // Rows in turn, each held by a wave (or the workgroup): the sum g xhat, then dx; dy xhat
 // stays in registers until the last row, so that each workgroup writes one row of sums.
 constexpr int kGradWaves = 8;  // of a workgroup whose waves hold a row each
-template <int P, bool WAVE>
+template <int P, bool WAVE, bool NT>
 __global__ __launch_bounds__(WAVE ? 64 * kGradWaves : 1024) void norm_grad_kernel(NormGradArgs a) {
     __shared__ float s_sum[2][16];
     extern __shared__ float s_dw[];  // WAVE: the waves' sums meet here, [d]
@@ -199,9 +207,9 @@ __global__ __launch_bounds__(WAVE ? 64 * kGradWaves : 1024) void norm_grad_kerne
             const int p = t + i * width;
             v[i] = y[i] = u[i] = make_uint4(0u, 0u, 0u, 0u);
             if (p < a.pieces) {
-                v[i] = ld16(a.s + at + 8 * p);
-                y[i] = ld16(a.dy + at + 8 * p);
-                if (a.dsum) u[i] = ld16(a.dsum + at + 8 * p);
+                v[i] = ld16<NT>(a.s + at + 8 * p);
+                y[i] = ld16<NT>(a.dy + at + 8 * p);
+                if (a.dsum) u[i] = ld16<NT>(a.dsum + at + 8 * p);
             }
         }
         const float rstd = a.rstd[row];
@@ -234,7 +242,7 @@ __global__ __launch_bounds__(WAVE ? 64 * kGradWaves : 1024) void norm_grad_kerne
                 const float z = (g[e] * h[e] - f[e] * rstd * c) * rstd;
                 f[e] = a.dsum ? z + o[e] : z;
             }
-            if (p < a.pieces) *reinterpret_cast<uint4 *>(a.dx + at + 8 * p) = pack8(f);
+            if (p < a.pieces) st16<NT>(a.dx + at + 8 * p, pack8(f));
         }
     }
     float *part = a.part + (size_t)blockIdx.x * a.d;
@@ -302,19 +310,27 @@ __global__ __launch_bounds__(256) void norm_grad_join_kernel(NormGradArgs a) {
     }
 }
 
-// Rows from which a wave holds a row (below, a workgroup).
-constexpr int kNormWaveRows = 1024;
-constexpr int kNormWavePieces = 512;  // pieces of a row that a wave can hold (8 a lane: d 4096)
+// Many rows: a workgroup's second piece a thread pays from 128 pieces a row on (8192 rows
+// both ways, 2 / 1 pieces: d 4096 57.0 / 58.5 us, 2560 38.8 / 40.4, 512 11.9 / 10.1); few rows
+// are bound by latency, where the widest workgroup is best (1 row of 2560: 3.9 / 3.5 us).
+constexpr int kNormManyRows = 1024;
+// Backward pass: rows of up to 256 pieces held by a wave each, whose sums of dy xhat need
+// four pieces' registers at most (32768 rows by wave / by workgroup: d 2560 136 / 122 us;
+// 8192 rows: 2048 32.8 / 33.6, 1024 19.6 / 28.5).
+constexpr int kGradWavePieces = 256;
+
+// Values from which rows are streamed past the caches: 16 MB a tensor, half of the second-level
+// caches, so that smaller results stay where the next call reads them (8192 x 4096 with and
+// without: 51.7 / 57.0 us; backward pass of 32768 x 2560 114.9 / 122.5).
+constexpr size_t kNormStreamed = (size_t)8 << 20;
 
 bool norm_supported(int d) { return d >= 8 && d <= kNormMaxDim && d % 8 == 0; }
 
-static bool norm_by_wave(int rows, int pieces) { return rows >= kNormWaveRows && pieces <= kNormWavePieces; }
+static bool streamed(int rows, int d) { return (size_t)rows * d >= kNormStreamed; }
 
-// Workgroup threads for a row, and pieces a thread.
-static int norm_threads(int pieces, int &per) {
-    per = pieces <= 1024 ? 1 : 2;
-    return div_up(pieces, 64 * per) * 64;
-}
+static int threads_of(int pieces, int per) { return div_up(pieces, 64 * per) * 64; }
+
+static bool grad_by_wave(int rows, int pieces) { return rows >= kNormManyRows && pieces <= kGradWavePieces; }
 
 hipError_t launch_norm(int rows, int d, double eps, const void *x, const void *residual,
                        const void *weight, void *sum, void *y, int group, void *y8, float *y_scale,
@@ -335,32 +351,41 @@ hipError_t launch_norm(int rows, int d, double eps, const void *x, const void *r
     a.pieces = d / 8;
     a.group_shift = !y8 || group == d ? -1 : __builtin_ctz((unsigned)group / 8);
     a.groups = !y8 ? 0 : div_up(d, group);
-    if (norm_by_wave(rows, a.pieces)) {
-        const dim3 grid(div_up(rows, 4)), wg(256);
-        switch (div_up(a.pieces, 64)) {
-            case 1: norm_kernel<1, true><<<grid, wg, 0, stream>>>(a); break;
-            case 2: norm_kernel<2, true><<<grid, wg, 0, stream>>>(a); break;
-            case 3: norm_kernel<3, true><<<grid, wg, 0, stream>>>(a); break;
-            case 4: norm_kernel<4, true><<<grid, wg, 0, stream>>>(a); break;
-            case 5: norm_kernel<5, true><<<grid, wg, 0, stream>>>(a); break;
-            case 6: norm_kernel<6, true><<<grid, wg, 0, stream>>>(a); break;
-            case 7: norm_kernel<7, true><<<grid, wg, 0, stream>>>(a); break;
-            default: norm_kernel<8, true><<<grid, wg, 0, stream>>>(a); break;
-        }
-        return hipGetLastError();
+    const int per = a.pieces > 1024 || (rows >= kNormManyRows && a.pieces >= 128) ? 2 : 1;
+    const dim3 grid(rows), wg(threads_of(a.pieces, per));
+    if (streamed(rows, d)) {
+        if (per == 1) norm_kernel<1, true><<<grid, wg, 0, stream>>>(a);
+        else norm_kernel<2, true><<<grid, wg, 0, stream>>>(a);
+    } else {
+        if (per == 1) norm_kernel<1, false><<<grid, wg, 0, stream>>>(a);
+        else norm_kernel<2, false><<<grid, wg, 0, stream>>>(a);
     }
-    int per;
-    const dim3 grid(rows), wg(norm_threads(a.pieces, per));
-    if (per == 1) norm_kernel<1, false><<<grid, wg, 0, stream>>>(a);
-    else norm_kernel<2, false><<<grid, wg, 0, stream>>>(a);
     return hipGetLastError();
 }
 
 // Workgroups of the backward pass: one a CU where waves hold rows, else one a row up to
 // two a CU.
 int norm_grad_parts(int rows, int d) {
-    if (norm_by_wave(rows, d / 8)) return rows < 256 * kGradWaves ? div_up(rows, kGradWaves) : 256;
+    if (grad_by_wave(rows, d / 8)) return rows < 256 * kGradWaves ? div_up(rows, kGradWaves) : 256;
     return rows < 512 ? rows : 512;
+}
+
+template <bool NT>
+static void launch_grad_rows(const NormGradArgs &a, hipStream_t stream) {
+    const dim3 grid(a.parts), wg(64 * kGradWaves);
+    const size_t lds = sizeof(float) * a.d;
+    if (!grad_by_wave(a.rows, a.pieces)) {
+        // 4096 rows of 8192, 1 / 2 pieces a thread: 62.4 / 58.1 us
+        if (a.pieces <= 512) norm_grad_kernel<1, false, NT><<<grid, dim3(threads_of(a.pieces, 1)), 0, stream>>>(a);
+        else norm_grad_kernel<2, false, NT><<<grid, dim3(threads_of(a.pieces, 2)), 0, stream>>>(a);
+        return;
+    }
+    switch (div_up(a.pieces, 64)) {
+        case 1: norm_grad_kernel<1, true, NT><<<grid, wg, lds, stream>>>(a); break;
+        case 2: norm_grad_kernel<2, true, NT><<<grid, wg, lds, stream>>>(a); break;
+        case 3: norm_grad_kernel<3, true, NT><<<grid, wg, lds, stream>>>(a); break;
+        default: norm_grad_kernel<4, true, NT><<<grid, wg, lds, stream>>>(a); break;
+    }
 }
 
 hipError_t launch_norm_grad(int rows, int d, const void *s, const float *rstd, const void *weight,
@@ -380,26 +405,8 @@ hipError_t launch_norm_grad(int rows, int d, const void *s, const float *rstd, c
     a.d = d;
     a.pieces = d / 8;
     a.parts = norm_grad_parts(rows, d);
-    const dim3 grid(a.parts);
-    if (norm_by_wave(rows, a.pieces)) {
-        const dim3 wg(64 * kGradWaves);
-        const size_t lds = sizeof(float) * d;
-        switch (div_up(a.pieces, 64)) {
-            case 1: norm_grad_kernel<1, true><<<grid, wg, lds, stream>>>(a); break;
-            case 2: norm_grad_kernel<2, true><<<grid, wg, lds, stream>>>(a); break;
-            case 3: norm_grad_kernel<3, true><<<grid, wg, lds, stream>>>(a); break;
-            case 4: norm_grad_kernel<4, true><<<grid, wg, lds, stream>>>(a); break;
-            case 5: norm_grad_kernel<5, true><<<grid, wg, lds, stream>>>(a); break;
-            case 6: norm_grad_kernel<6, true><<<grid, wg, lds, stream>>>(a); break;
-            case 7: norm_grad_kernel<7, true><<<grid, wg, lds, stream>>>(a); break;
-            default: norm_grad_kernel<8, true><<<grid, wg, lds, stream>>>(a); break;
-        }
-    } else {
-        int per;
-        const dim3 wg(norm_threads(a.pieces, per));
-        if (per == 1) norm_grad_kernel<1, false><<<grid, wg, 0, stream>>>(a);
-        else norm_grad_kernel<2, false><<<grid, wg, 0, stream>>>(a);
-    }
+    if (streamed(rows, d)) launch_grad_rows<true>(a, stream);
+    else launch_grad_rows<false>(a, stream);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     norm_grad_join_kernel<<<dim3(div_up(d, 64)), dim3(256), 0, stream>>>(a);

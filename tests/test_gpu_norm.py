@@ -15,7 +15,8 @@ pytestmark = pytest.mark.gpu
 U24 = 2.0 ** -24
 EPS = 1e-6
 FORMS = [(1, 8), (1, 2560), (3, 72), (5, 1000), (77, 8200), (2, 16384), (1500, 520), (1030, 2560), (1100, 4096),
-         (1029, 4104), (2050, 8), (1027, 3592)]
+         (1029, 4104), (2050, 8), (1027, 3592),
+         (1030, 1544), (4100, 2080), (1100, 8008), (17000, 512)]
 
 
 def f32(bits):
