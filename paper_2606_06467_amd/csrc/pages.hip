@@ -17,6 +17,8 @@ namespace clsa {
 constexpr int kPlanThreads = 1024;
 constexpr int kForkEntries = kMaxForkBatch;  // table entries of a fork's workgroup (64 KB of LDS)
 constexpr int kCopyBytes = 8192;       // a copying workgroup's piece of a page
+// Copies of this many bytes go past the caches.
+constexpr int64_t kCopyStreamed = (int64_t)64 << 20;
 
 struct PageArgs {
     int32_t *table, *refs;
@@ -47,20 +49,39 @@ __global__ __launch_bounds__(256) void pages_fork_kernel(ForkArgs a) {
         return;
     }
     const int c0 = blockIdx.x * a.cols, width = min(a.cols, a.max_pages - c0), n = a.batch * width;
-    for (int i = threadIdx.x; i < n; i += 256)
-        s_old[i] = a.table[(size_t)(i / width) * a.max_pages + c0 + i % width];
+    int32_t *table = a.table + c0;
+    for (int i0 = threadIdx.x; i0 < n; i0 += 1024) {  // four loads in flight
+        int v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = i0 + 256 * j, b = i / width;
+            if (i < n) v[j] = table[(size_t)b * a.max_pages + (i - b * width)];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (i0 + 256 * j < n) s_old[i0 + 256 * j] = v[j];
+    }
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += 256) {
-        const int b = i / width, c = i % width, up = a.parent[b];
-        if (up < -1 || up >= a.batch || up == b) continue;
-        const int old = s_old[i], from = up < 0 ? -1 : s_old[up * width + c];
-        const bool held = from >= 0 && from < a.pages;
-        if (from >= a.pages || old >= a.pages) note_device_error(kDevErrPages);
-        const int now = held ? from : -1;
-        if (now == old) continue;
-        a.table[(size_t)b * a.max_pages + c0 + c] = now;
-        if (held) atomicAdd(a.refs + now, 1);
-        if (old >= 0 && old < a.pages) atomicSub(a.refs + old, 1);
+    for (int i0 = threadIdx.x; i0 < n; i0 += 1024) {
+        int up[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = i0 + 256 * j;
+            up[j] = i < n ? a.parent[i / width] : -2;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = i0 + 256 * j, b = i / width, c = i - b * width;
+            if (up[j] < -1 || up[j] >= a.batch || up[j] == b) continue;
+            const int old = s_old[i], from = up[j] < 0 ? -1 : s_old[up[j] * width + c];
+            const bool held = from >= 0 && from < a.pages;
+            if (from >= a.pages || old >= a.pages) note_device_error(kDevErrPages);
+            const int now = held ? from : -1;
+            if (now == old) continue;
+            table[(size_t)b * a.max_pages + c] = now;
+            if (held) atomicAdd(a.refs + now, 1);
+            if (old >= 0 && old < a.pages) atomicSub(a.refs + old, 1);
+        }
     }
 }
 
@@ -84,80 +105,109 @@ struct CopyArgs {
     int64_t bytes[kMaxPaged];   // of a page
     int first[kMaxPaged + 1];   // piece numbers
     int tensors, pages;
+    int64_t page_bytes;         // of all tensors
     const int32_t *src, *dst, *count;  // count: null if n is known
     int n;
+    unsigned grid, step_pairs, step_pieces;  // copying workgroups, and their number in pairs and pieces
 };
 
-__device__ __forceinline__ void copy_pages(const CopyArgs &a, int n) {
+// One piece: N 16-byte loads a thread in flight.  NT: streamed past the caches.
+template <bool NT>
+__device__ __forceinline__ void copy_piece(const char *from, char *to, int len) {
+    constexpr int N = kCopyBytes / 16 / 256;
+    u32x4 v[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int o = (threadIdx.x + 256 * j) * 16;
+        const u32x4 *p = reinterpret_cast<const u32x4 *>(from + o);
+        if (o < len) v[j] = NT ? __builtin_nontemporal_load(p) : *p;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int o = (threadIdx.x + 256 * j) * 16;
+        u32x4 *p = reinterpret_cast<u32x4 *>(to + o);
+        if (o < len) {
+            if (NT) __builtin_nontemporal_store(v[j], p);
+            else *p = v[j];
+        }
+    }
+}
+
+// Work item i: piece i % per of pair i / per.  The pairs' lists have room for every item of
+// the launch, so that a pair is loaded along with their number.
+__device__ __forceinline__ void copy_pages(const CopyArgs &a) {
     const int per = a.first[a.tensors];
-    const int64_t all = (int64_t)n * per;
-    for (int64_t i = blockIdx.x; i < all; i += gridDim.x) {
-        const int k = (int)(i / per), piece = (int)(i % per);
-        const int src = a.src[k], dst = a.dst[k];
-        if (src == -1 || src == dst) continue;
-        if (src < 0 || src >= a.pages || dst < 0 || dst >= a.pages) {
-            if (piece == 0) note_device_error(kDevErrPages);
-            continue;
-        }
-        int t = 0;
-        while (piece >= a.first[t + 1]) ++t;
-        const int64_t bytes = a.bytes[t], at = (int64_t)(piece - a.first[t]) * kCopyBytes;
-        const int len = (int)min((int64_t)kCopyBytes, bytes - at);
-        const char *from = a.data[t] + src * bytes + at;
-        char *to = a.data[t] + dst * bytes + at;
-        if (((uintptr_t)a.data[t] | bytes) % 16 == 0) {
-            constexpr int N = kCopyBytes / 16 / 256;
-            u32x4 v[N];
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const int o = (threadIdx.x + 256 * j) * 16;
-                if (o < len) v[j] = *reinterpret_cast<const u32x4 *>(from + o);
+    uint32_t k = blockIdx.x / (uint32_t)per, piece = blockIdx.x - k * per;
+    int src = a.src[k], dst = a.dst[k];
+    const int n = a.count ? *a.count : a.n;
+    const bool stream = (int64_t)n * a.page_bytes >= kCopyStreamed;
+    while (k < (uint32_t)n) {
+        if (src != -1 && src != dst) {
+            if (src < 0 || src >= a.pages || dst < 0 || dst >= a.pages) {
+                if (piece == 0 && threadIdx.x == 0) note_device_error(kDevErrPages);
+            } else {
+                int t = 0;
+                while ((int)piece >= a.first[t + 1]) ++t;
+                const int64_t bytes = a.bytes[t], at = (int64_t)((int)piece - a.first[t]) * kCopyBytes;
+                const int len = (int)min((int64_t)kCopyBytes, bytes - at);
+                const char *from = a.data[t] + src * bytes + at;
+                char *to = a.data[t] + dst * bytes + at;
+                if (((uintptr_t)a.data[t] | bytes) % 16 != 0) {
+                    for (int o = threadIdx.x * 4; o < len; o += 1024)
+                        *reinterpret_cast<uint32_t *>(to + o) = *reinterpret_cast<const uint32_t *>(from + o);
+                } else if (stream) {
+                    copy_piece<true>(from, to, len);
+                } else {
+                    copy_piece<false>(from, to, len);
+                }
             }
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const int o = (threadIdx.x + 256 * j) * 16;
-                if (o < len) *reinterpret_cast<u32x4 *>(to + o) = v[j];
-            }
-        } else {
-            for (int o = threadIdx.x * 4; o < len; o += 1024)
-                *reinterpret_cast<uint32_t *>(to + o) = *reinterpret_cast<const uint32_t *>(from + o);
         }
+        k += a.step_pairs;
+        piece += a.step_pieces;
+        if (piece >= (uint32_t)per) {
+            piece -= per;
+            ++k;
+        }
+        if (k >= (uint32_t)n) break;
+        src = a.src[k];
+        dst = a.dst[k];
     }
 }
 
 __global__ __launch_bounds__(256) void pages_copy_kernel(CopyArgs a) {
-    copy_pages(a, a.count ? *a.count : a.n);
+    copy_pages(a);
 }
 
-static int copy_args(CopyArgs &a, int pages, int tensors, const PagedTensor *t) {
+// For at most n pairs, whose lists have that many places.
+static void copy_args(CopyArgs &a, int pages, int tensors, const PagedTensor *t, int64_t n) {
     a.pages = pages;
     a.tensors = tensors;
-    int at = 0;
+    int per = 0;
     for (int i = 0; i < tensors; ++i) {
         a.data[i] = static_cast<char *>(t[i].data);
         a.bytes[i] = t[i].page_bytes;
-        a.first[i] = at;
-        at += (int)((t[i].page_bytes + kCopyBytes - 1) / kCopyBytes);
+        a.page_bytes += t[i].page_bytes;
+        a.first[i] = per;
+        per += (int)((t[i].page_bytes + kCopyBytes - 1) / kCopyBytes);
     }
-    a.first[tensors] = at;
-    return at;
-}
-
-// Workgroups for at most n pairs of `per` pieces: eight a CU.
-static unsigned copy_grid(int64_t n, int per) {
-    const int64_t all = n * per;
-    return (unsigned)(all < 2048 ? (all < 1 ? 1 : all) : 2048);
+    a.first[tensors] = per;
+    // a workgroup for each piece, eight a CU at most: those that find no pair cost their launch
+    a.grid = (unsigned)(n * per < 2048 ? n * per : 2048);
+    if (per) {
+        a.step_pairs = a.grid / per;
+        a.step_pieces = a.grid % per;
+    }
 }
 
 hipError_t launch_pages_copy(int pages, int tensors, const PagedTensor *t, int n,
                              const int32_t *src, const int32_t *dst, hipStream_t stream) {
     if (n == 0 || tensors == 0) return hipSuccess;
     CopyArgs a{};
-    const int per = copy_args(a, pages, tensors, t);
+    copy_args(a, pages, tensors, t, n);
     a.src = src;
     a.dst = dst;
     a.n = n;
-    pages_copy_kernel<<<dim3(copy_grid(n, per)), dim3(256), 0, stream>>>(a);
+    pages_copy_kernel<<<dim3(a.grid), dim3(256), 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -438,11 +488,11 @@ hipError_t launch_pages_reserve(const Geometry &g, int pages, int tensors, const
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || tensors == 0) return e;
     CopyArgs c{};
-    const int per = copy_args(c, pages, tensors, t);
+    copy_args(c, pages, tensors, t, (int64_t)entries);
     c.src = a.src;
     c.dst = a.dst;
     c.count = a.n_pairs;
-    pages_copy_kernel<<<dim3(copy_grid((int64_t)entries, per)), dim3(256), 0, stream>>>(c);
+    pages_copy_kernel<<<dim3(c.grid), dim3(256), 0, stream>>>(c);
     return hipGetLastError();
 }
 
@@ -477,6 +527,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_compact_kernel(CompactArgs
     __shared__ int s_scan[kPlanThreads / 64];
     __shared__ int s_bound, s_odd;
     __shared__ int32_t s_held[COUNT ? kLdsPages : 1];
+    __shared__ uint16_t s_src[COUNT ? kLdsPages / 2 : 1], s_dst[COUNT ? kLdsPages : 1];
     const int tid = threadIdx.x;
     int r[N], mine = 0;
     if (COUNT)
@@ -531,8 +582,13 @@ __global__ __launch_bounds__(kPlanThreads) void pages_compact_kernel(CompactArgs
         int h = holes + (before & 0xffff), m = moves + (before >> 16);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            if (hole[j]) a.dst[h++] = first + j;
-            if (move[j]) a.src[m++] = first + j;
+            if (COUNT) {
+                if (hole[j]) s_dst[h++] = (uint16_t)(first + j);
+                if (move[j]) s_src[m++] = (uint16_t)(first + j);
+            } else {
+                if (hole[j]) a.dst[h++] = first + j;
+                if (move[j]) a.src[m++] = first + j;
+            }
         }
         holes += all & 0xffff;
         moves += all >> 16;
@@ -541,14 +597,18 @@ __global__ __launch_bounds__(kPlanThreads) void pages_compact_kernel(CompactArgs
     __threadfence_block();
     __syncthreads();
     for (int k = tid; k < moves; k += kPlanThreads) {
-        const int src = a.src[k], dst = a.dst[k];
+        const int src = COUNT ? s_src[k] : a.src[k], dst = COUNT ? s_dst[k] : a.dst[k];
+        if (COUNT) {
+            a.src[k] = src;
+            a.dst[k] = dst;
+        }
         a.to[src] = dst;
-        a.p.refs[dst] = a.p.refs[src];
+        a.p.refs[dst] = COUNT ? s_held[src] : a.held[src];  // all of its holders are entries
         a.p.refs[src] = 0;
     }
     if (tid == 0) {
         *a.n_pairs = moves;
-        *a.bound = max(s_bound, moves ? a.dst[moves - 1] + 1 : 0);
+        *a.bound = max(s_bound, moves ? (COUNT ? s_dst[moves - 1] : a.dst[moves - 1]) + 1 : 0);
         if (s_odd) note_device_error(kDevErrPages);
     }
 }
@@ -568,7 +628,7 @@ __global__ __launch_bounds__(256) void pages_move_kernel(MoveArgs m) {
             if (now != e) a.p.table[i] = now;
         }
     }
-    if (m.c.tensors) copy_pages(m.c, *m.c.count);
+    if (m.c.tensors && blockIdx.x < m.c.grid) copy_pages(m.c);
 }
 
 size_t compact_ws_ints(int pages) { return (size_t)pages * 4 + 64; }
@@ -595,12 +655,12 @@ hipError_t launch_pages_compact(const Geometry &g, int pages, int tensors, const
         pages_compact_kernel<false><<<dim3(1), dim3(kPlanThreads), 0, stream>>>(a);
     }
     MoveArgs m{a, {}};
-    const int per = tensors ? copy_args(m.c, pages, tensors, t) : 0;
+    // at most half of the pages move, and at least one pair has room
+    if (tensors) copy_args(m.c, pages, tensors, t, (pages + 1) / 2);
     m.c.src = a.src;
     m.c.dst = a.dst;
     m.c.count = a.n_pairs;
-    const unsigned copies = copy_grid(pages / 2, per);
-    pages_move_kernel<<<dim3(grid > copies ? grid : copies), dim3(256), 0, stream>>>(m);
+    pages_move_kernel<<<dim3(grid > m.c.grid ? grid : m.c.grid), dim3(256), 0, stream>>>(m);
     return hipGetLastError();
 }
 

@@ -274,6 +274,8 @@ inline uint32_t perm(uint32_t hi, uint32_t lo, uint32_t sel) {
 #define __builtin_amdgcn_ds_read_tr16_b64_v4i16(p) emu::read_tr16((const void *)(p))
 #define __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, x, y, z) emu::mfma_32x32x16(a, b, c)
 #define __builtin_amdgcn_sched_barrier(m) ((void)0)
+#define __builtin_nontemporal_load(p) (*(p))
+#define __builtin_nontemporal_store(v, p) ((void)(*(p) = (v)))
 #define __builtin_amdgcn_wave_barrier emu::converge
 #define __builtin_amdgcn_perm emu::perm
 #define __builtin_amdgcn_mbcnt_lo(m, a) (a)

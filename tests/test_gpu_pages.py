@@ -114,6 +114,26 @@ def test_compact(bits8, batch, cols, pages, pinned):
     assert np.array_equal(T.cpu().numpy(), t) and np.array_equal(R.cpu().numpy(), r) and _same(cache, want)
 
 
+def test_compact_past_the_caches():
+    """Enough pages that the copies are streamed."""
+    from paper_2606_06467_amd import binding as B
+    rng = np.random.default_rng(1)
+    pages, batch, cols = 3000, 20, 75
+    table = np.full((batch, cols), -1, np.int32)
+    table[:] = rng.permutation(pages)[:batch * cols].reshape(batch, cols)
+    refs = P.holders(table, pages)
+    t, r, moves, bound = P.compact(table, refs)
+    cache = _cache(rng, pages, False)
+    assert len(moves) * sum(c[0].nbytes for c in cache) > 64 << 20
+    want = _moved(cache, moves)
+    T, R = _dev(table, refs)
+    M, = _dev(np.zeros(1, np.int32))
+    sh = _shape(batch, cols)
+    B.clsa_pages_compact(sh, cache, T, R, M, B.workspace(sh, B.CLSA_OP_PAGES_COMPACT, pages))
+    assert np.array_equal(T.cpu().numpy(), t) and np.array_equal(R.cpu().numpy(), r) and int(M[0]) == bound
+    assert _same(cache, want)
+
+
 def test_copy():
     import torch
     from paper_2606_06467_amd import binding as B
