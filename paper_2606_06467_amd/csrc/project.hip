@@ -194,56 +194,59 @@ constexpr int kGemmM = 128, kGemmN = 128, kGemmK = 64;
 // the stores).
 constexpr int kGemmPitch = kGemmK;           // bf16 per staged row
 constexpr int kGemmOutPitch = kGemmN + 8;    // bf16 per staged output row
-constexpr size_t kGemmLds = sizeof(uint16_t) * 2 * 2 * kGemmM * kGemmPitch;
+constexpr size_t gemm_lds(int rows) { return sizeof(uint16_t) * 2 * (rows + kGemmN) * kGemmPitch; }
 
-// kMixed: adds the adapters' part to a wave's 64 x 64 tile of the tiled product (c[mt][nt]: rows
-// r0 + 16 mt, features f0 + 16 nt).  A 32-wide product step holds 16 ranks twice, the high and
+// kMixed: adds the adapters' part to a wave's 16 MT x 64 tile of the tiled product (c[mt][nt]:
+// rows r0 + 16 mt, features f0 + 16 nt).  A 32-wide product step holds 16 ranks twice, the high and
 // the low parts of u against the same B.  Rows of different sequences can share a 16-row
-// tile: the step is then made once for each adapter in it and added to that adapter's rows
-// only (a factor of zero would carry one adapter's infinities to another's rows).
-__device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, f32x4 (&c)[4][4]) {
+// tile: the step is then made once for each adapter in it, Q adapters' loads in flight
+// together, and added to that adapter's rows only (a factor of zero would carry one
+// adapter's infinities to another's rows).
+template <int MT, int Q>
+__device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, f32x4 (&c)[MT][4]) {
     const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
     const uint16_t *halves = reinterpret_cast<const uint16_t *>(a.u);
     const int pitch = div_up(a.rank, 16) * 32;
-    int mine[4];
+    int mine[MT];
 #pragma unroll
-    for (int mt = 0; mt < 4; ++mt) {
+    for (int mt = 0; mt < MT; ++mt) {
         const int r = r0 + 16 * mt + col;
         mine[mt] = r < a.rows ? adapter_of(a, r / a.n_q) : -1;
     }
 #pragma unroll 1
     for (int j = 0; j < a.rank; j += 16) {
-        bf16x8 av[4], bv[2][4];
+        bf16x8 av[MT], bv[Q][4];
 #pragma unroll
-        for (int mt = 0; mt < 4; ++mt) {
+        for (int mt = 0; mt < MT; ++mt) {
             av[mt] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
             if (mine[mt] >= 0) av[mt] = ld8(halves + (size_t)(r0 + 16 * mt + col) * pitch + 2 * j + grp * 8);
         }
         const int ro = j + (grp & 1) * 8;
-        auto load = [&](int id, bf16x8 (&b)[4]) {
+        int held = -1;  // the adapter that bv[0] holds
 #pragma unroll
-            for (int nt = 0; nt < 4; ++nt) {
-                b[nt] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
-                if (ro < a.rank) b[nt] = ld8(a.up + ((size_t)id * a.n_feat + f0 + 16 * nt + col) * a.rank + ro);
-            }
-        };
-#pragma unroll
-        for (int mt = 0; mt < 4; ++mt) {
+        for (int mt = 0; mt < MT; ++mt) {
             uint64_t todo = __ballot(mine[mt] >= 0) & 0xffffull;
-            while (todo) {  // two adapters at a time: their loads in flight together
-                uint64_t same[2];
+            while (todo) {
+                uint64_t same[Q];
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
+                for (int q = 0; q < Q; ++q) {
                     same[q] = 0;
                     if (todo) {
                         const int id = __builtin_amdgcn_readlane(mine[mt], __builtin_ctzll(todo));
                         same[q] = __ballot(mine[mt] == id) & 0xffffull;
                         todo &= ~same[q];
-                        load(id, bv[q]);
+                        if (q == 0 && id == held) continue;
+                        if (q == 0) held = id;
+#pragma unroll
+                        for (int nt = 0; nt < 4; ++nt) {
+                            bv[q][nt] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
+                            if (ro < a.rank)
+                                bv[q][nt] = ld8(a.up + ((size_t)id * a.n_feat + f0 + 16 * nt + col) * a.rank + ro);
+                        }
                     }
                 }
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
+                for (int q = 0; q < Q; ++q) {
                     if (!same[q]) break;
 #pragma unroll
                     for (int nt = 0; nt < 4; ++nt) {
@@ -263,16 +266,17 @@ __device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, 
 // the high and the low parts of u against the same B).  kMixed: adapter_tile above.
 enum GemmMode { kPlain, kOwnTiles, kMixed };
 
-template <bool PAGED, GemmMode MODE>
+template <bool PAGED, GemmMode MODE, int BM>
 __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
+    constexpr int MT = BM / 32, OPS = MT + 4;  // 16-row tiles of a wave; its operands of a half step
     // two stages of A (rows of h) and B (features of w), 128 x 64 bf16 each
     // (dynamic LDS, kGemmLds bytes); the output tile (128 x 128 bf16) reuses it
     extern __shared__ __align__(16) uint16_t s_lds[];
-    uint16_t(*s_ab)[2][kGemmM][kGemmPitch] =
-        reinterpret_cast<uint16_t(*)[2][kGemmM][kGemmPitch]>(s_lds);
+    // (BM rows of A, then the features, in each stage)
+    auto s_row = [&](int st, int r) { return s_lds + (size_t)(st * (BM + kGemmN) + r) * kGemmPitch; };
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int col = lane & 15, grp = lane >> 4;
-    const int wm = wave >> 1, wn = wave & 1;  // the wave's 64 x 64 quadrant
+    const int wm = wave >> 1, wn = wave & 1;  // the wave's BM / 2 x 64 quadrant
     // Tile order: workgroups are dealt to the 8 XCDs in turn (L mod 8); XCD x
     // takes bands of `band` row tiles (8, fewer when there are few rows) and
     // walks, for each band, the feature tiles with the band's row tiles next to
@@ -282,18 +286,27 @@ __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
     int rt, ft;
     {
         const int L = blockIdx.x, x = L & 7, q = L >> 3;
-        const int per_band = a.band * a.ftiles;          // workgroups of one band
-        const int band = 8 * (q / per_band) + x;         // bands dealt to the XCDs in turn
-        const int qi = q % per_band;
-        rt = a.band * band + qi % a.band;
-        ft = qi / a.band;
+        if (MODE != kPlain && a.band == 0) {
+            // few row tiles: every XCD takes an eighth of the tiles, feature after feature, so
+            // that none has more than its share (9 row tiles x 20 in bands: 50 us; so 39)
+            const int tile = x * div_up(a.rtiles * a.ftiles, 8) + q;
+            rt = q < div_up(a.rtiles * a.ftiles, 8) ? tile % a.rtiles : a.rtiles;
+            ft = tile / a.rtiles;
+            if (ft >= a.ftiles) return;  // uniform
+        } else {
+            const int per_band = a.band * a.ftiles;          // workgroups of one band
+            const int band = 8 * (q / per_band) + x;         // bands dealt to the XCDs in turn
+            const int qi = q % per_band;
+            rt = a.band * band + qi % a.band;
+            ft = qi / a.band;
+        }
     }
     if (rt >= a.rtiles) return;  // uniform: padding workgroups of the last bands
     const int f0 = ft * kGemmN;
-    int r0 = rt * kGemmM, row_end = a.rows, id = -1;
+    int r0 = rt * BM, row_end = a.rows, id = -1;
     if (MODE == kOwnTiles) {
         const int b = rt / a.seq_tiles;
-        r0 = b * a.n_q + (rt - b * a.seq_tiles) * kGemmM;
+        r0 = b * a.n_q + (rt - b * a.seq_tiles) * BM;
         row_end = (b + 1) * a.n_q;
         id = adapter_of(a, b);
     }
@@ -301,32 +314,32 @@ __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
     // tile: row (t >> 3) + 32 i, columns 8 (t & 7) .. + 8
     const int lrow = tid >> 3, lcol = (tid & 7) * 8;
     const int wcol = ((tid & 7) ^ ((lrow >> 1) & 7)) * 8, rswz = (col >> 1) & 7;
-    const uint16_t *hp[4], *wp[4];
+    const uint16_t *hp[MT], *wp[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        hp[i] = a.h + (size_t)min(r0 + lrow + 32 * i, row_end - 1) * a.d + lcol;  // tail rows: never stored
+        if (i < MT) hp[i] = a.h + (size_t)min(r0 + lrow + 32 * i, row_end - 1) * a.d + lcol;  // tail rows: never stored
         wp[i] = a.w + (size_t)(f0 + lrow + 32 * i) * a.d + lcol;
     }
     // two register sets: the loads for step k + 2 are issued while step k is
     // computed, and step k + 1 (loaded a step earlier) goes to LDS after it
-    u32x4 ra[2][4], rb[2][4];
+    u32x4 ra[2][MT], rb[2][4];
     auto gload = [&](int set, int k0) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            ra[set][i] = *reinterpret_cast<const u32x4 *>(hp[i] + k0);
+            if (i < MT) ra[set][i] = *reinterpret_cast<const u32x4 *>(hp[i] + k0);
             rb[set][i] = *reinterpret_cast<const u32x4 *>(wp[i] + k0);
         }
     };
     auto lstore = [&](int set, int st) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            *reinterpret_cast<u32x4 *>(&s_ab[st][0][lrow + 32 * i][wcol]) = ra[set][i];
-            *reinterpret_cast<u32x4 *>(&s_ab[st][1][lrow + 32 * i][wcol]) = rb[set][i];
+            if (i < MT) *reinterpret_cast<u32x4 *>(s_row(st, lrow + 32 * i) + wcol) = ra[set][i];
+            *reinterpret_cast<u32x4 *>(s_row(st, BM + lrow + 32 * i) + wcol) = rb[set][i];
         }
     };
-    f32x4 c[4][4];
+    f32x4 c[MT][4];
 #pragma unroll
-    for (int mt = 0; mt < 4; ++mt)
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int nt = 0; nt < 4; ++nt) c[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int nk = a.d / kGemmK;  // even (d_model is a multiple of 512)
@@ -337,8 +350,9 @@ __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
         const uint16_t *halves = reinterpret_cast<const uint16_t *>(a.u);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            ra[set][i] = rb[set][i] = u32x4{0u, 0u, 0u, 0u};
-            if (chunk * 16 < a.rank)
+            rb[set][i] = u32x4{0u, 0u, 0u, 0u};
+            if (i < MT) ra[set][i] = u32x4{0u, 0u, 0u, 0u};
+            if (i < MT && chunk * 16 < a.rank)
                 ra[set][i] = *reinterpret_cast<const u32x4 *>(
                     halves + (size_t)min(r0 + lrow + 32 * i, row_end - 1) * pitch + e * 64 + lcol);
             if (ro < a.rank)
@@ -354,38 +368,44 @@ __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
     // k + 2 were issued; step k + 1 goes to the other stage meanwhile.
     auto step = [&](int h) {
         const int st = h;
-        // operand o of 32-wide half ks: A rows (o < 4) and B features of the wave's quadrant
-        bf16x8 op[2][8];
+        // operand o of 32-wide half ks: the features of the wave's quadrant (o < 4), then its rows
+        bf16x8 op[2][OPS];
         auto read_op = [&](int ks, int o) {
-            const int r = (o < 4 ? wm * 64 + o * 16 : wn * 64 + (o - 4) * 16) + col;
+            const int r = (o < 4 ? BM + wn * 64 + o * 16 : wm * (BM / 2) + (o - 4) * 16) + col;
             op[ks][o] = __builtin_bit_cast(
-                bf16x8, *reinterpret_cast<const u32x4 *>(&s_ab[st][o >> 2][r][((ks * 4 + grp) ^ rswz) * 8]));
+                bf16x8, *reinterpret_cast<const u32x4 *>(s_row(st, r) + ((ks * 4 + grp) ^ rswz) * 8));
         };
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int o = 0; o < 8; ++o) read_op(0, o < 4 ? o + 4 : o - 4);
-        // 16 parts of two products whose order is pinned: the first eight each read
-        // an operand of the second half, the others each store a piece of the next
-        // step (the last step stores an old piece that is not read).  8192 rows x 2560
-        // features x 2560: 127.6 us with padded rows and the compiler's order, 124.0
-        // swizzled, 117.4 in this order; 32-wide steps (three workgroups per CU) 139.6.
+        for (int o = 0; o < OPS; ++o) read_op(0, o);
+        // Parts of two products whose order is pinned: those of the first half each read
+        // operands of the second half (one each with 128 rows), the others each store
+        // pieces of the next step (the last step stores old pieces that are not read).  8192
+        // rows x 2560 features x 2560: 127.6 us with padded rows and the compiler's order,
+        // 124.0 swizzled, 117.4 in this order; 32-wide steps (three workgroups per CU) 139.6.
         // What bounds it now: 1280 tiles on 512 resident workgroups are 2.5 rounds, and
         // the step's own chain of barrier, operand reads and products at two waves per
         // SIMD.
+        constexpr int H = 2 * MT;  // parts of a half step
 #pragma unroll
-        for (int p = 0; p < 16; ++p) {
-            const int ks = p >> 3;
-            if (ks == 0) read_op(1, p < 4 ? p + 4 : p - 4);
+        for (int p = 0; p < 2 * H; ++p) {
+            const int ks = p / H, q0 = (p % H) * OPS / H, q1 = (p % H + 1) * OPS / H;
+            if (ks == 0)
+#pragma unroll
+                for (int o = q0; o < q1; ++o) read_op(1, o);
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int m = 2 * (p & 7) + e, mt = m >> 2, nt = m & 3;
-                c[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op[ks][mt], op[ks][4 + nt], c[mt][nt], 0, 0, 0);
+                const int m = 2 * (p % H) + e, mt = m >> 2, nt = m & 3;
+                c[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op[ks][4 + mt], op[ks][nt], c[mt][nt], 0, 0, 0);
             }
-            if (ks == 1) {
-                const int i = (p & 7) >> 1;
-                if (p & 1) *reinterpret_cast<u32x4 *>(&s_ab[st ^ 1][1][lrow + 32 * i][wcol]) = rb[h ^ 1][i];
-                else *reinterpret_cast<u32x4 *>(&s_ab[st ^ 1][0][lrow + 32 * i][wcol]) = ra[h ^ 1][i];
-            }
+            if (ks == 1)
+#pragma unroll
+                for (int o = q0; o < q1; ++o) {  // rows and features in turn, then the other features
+                    const bool row = o < 2 * MT && !(o & 1);
+                    const int i = o < 2 * MT ? o >> 1 : o - MT;
+                    const u32x4 v = row ? ra[h ^ 1][i < MT ? i : 0] : rb[h ^ 1][i];
+                    *reinterpret_cast<u32x4 *>(s_row(st ^ 1, (row ? 0 : BM) + lrow + 32 * i) + wcol) = v;
+                }
             __builtin_amdgcn_sched_barrier(0);
         }
         __syncthreads();
@@ -407,17 +427,17 @@ __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
             step(h);
         }
     }
-    if (MODE == kMixed) adapter_tile(a, r0 + wm * 64, f0 + wn * 64, c);
+    if (MODE == kMixed) adapter_tile<MT, MT == 2 ? 4 : 2>(a, r0 + wm * (BM / 2), f0 + wn * 64, c);
     // bf16 results into LDS: C tile (mt, nt) row 4 grp + r, column col
-    uint16_t(*s_out)[kGemmOutPitch] = reinterpret_cast<uint16_t(*)[kGemmOutPitch]>(&s_ab[0][0][0][0]);
-    static_assert(kGemmLds >= sizeof(uint16_t) * kGemmM * kGemmOutPitch, "output tile fits");
+    uint16_t(*s_out)[kGemmOutPitch] = reinterpret_cast<uint16_t(*)[kGemmOutPitch]>(s_lds);
+    static_assert(gemm_lds(BM) >= sizeof(uint16_t) * BM * kGemmOutPitch, "output tile fits");
 #pragma unroll
-    for (int mt = 0; mt < 4; ++mt)
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int nt = 0; nt < 4; ++nt)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                s_out[wm * 64 + mt * 16 + 4 * grp + r][wn * 64 + nt * 16 + col] =
+                s_out[wm * (BM / 2) + mt * 16 + 4 * grp + r][wn * 64 + nt * 16 + col] =
                     (uint16_t)f32_to_bf16_bits(c[mt][nt][r]);
     __syncthreads();
     // whole rows out: 16 pieces of 16 bytes per row, 8 rows per pass of 128 threads
@@ -427,7 +447,7 @@ __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
     else if (f0 < 512) { dst_kind = 1; width = 256; fo = f0 - 256; }
     else if (f0 < 512 + a.kvw) { dst_kind = 2; width = a.kvw; fo = f0 - 512; }
     else { dst_kind = 3; width = a.kvw; fo = f0 - 512 - a.kvw; }
-    for (int rr = tid >> 4; rr < kGemmM; rr += 16) {
+    for (int rr = tid >> 4; rr < BM; rr += 16) {
         const int r = r0 + rr;
         if (r >= row_end) break;
         const u32x4 v = *reinterpret_cast<const u32x4 *>(&s_out[rr][piece * 8]);
@@ -560,9 +580,6 @@ __global__ __launch_bounds__(256) void adapter_down_kernel(ProjArgs a) {
     if (lane == 0) a.u[(size_t)row * a.rank + j] = sum * a.alpha[id];
 }
 
-// Sequences long enough for row tiles of their own.
-static bool adapter_own_tiles(int n_q) { return n_q >= 64; }
-
 static hipError_t launch_adapter_down(const ProjArgs &a, int batch, hipStream_t stream) {
     if (a.rows <= kSplitMaxRows) {
         adapter_down_kernel<<<dim3(a.rows * (a.rank / 4)), dim3(256), 0, stream>>>(a);
@@ -651,28 +668,44 @@ static hipError_t launch_project_args(const Geometry &g, int d_model, ProjArgs a
         }
         return hipGetLastError();
     }
-    a.seq_tiles = div_up(g.n_q, kGemmM);
-    const bool own = ADAPTED && adapter_own_tiles(g.n_q);
-    const int64_t rtiles = own ? (int64_t)g.batch * a.seq_tiles : div_up(g.rows, kGemmM);
+    a.ftiles = n_feat / kGemmN;
+    // Adapters: row tiles of one sequence each where that pads the rows by half at most (30
+    // sequences of 150 rows x 2560 features: 137 us, 98 shared), or where the tiles are no
+    // more than the CUs; else tiles that sequences share.
+    // Tiles of 64 rows where those are no more than the CUs (512 rows x 2560 features,
+    // d_model 2560: 30 us against 36 with 128; 1024 rows 41 against 38).
+    auto own_tiles = [&](int rows) { return (int64_t)g.batch * div_up(g.n_q, rows); };
+    const bool own = ADAPTED && (own_tiles(kGemmM) * kGemmM * 2 <= (int64_t)g.rows * 3 ||
+                                 own_tiles(kGemmM) * a.ftiles <= 256);
+    int bm = kGemmM;
+    if (ADAPTED && (own ? own_tiles(kGemmM / 2) : div_up(g.rows, kGemmM / 2)) * a.ftiles <= 256) bm = kGemmM / 2;
+    a.seq_tiles = div_up(g.n_q, bm);
+    const int64_t rtiles = own ? own_tiles(bm) : div_up(g.rows, bm);
     if (rtiles > 0xffffff) return hipErrorInvalidConfiguration;
     a.rtiles = (int)rtiles;
-    a.ftiles = n_feat / kGemmN;
     // bands of up to 8 row tiles, dealt to the 8 XCDs in turn (the last round
     // padded); fewer row tiles per band when that still leaves XCDs idle
     a.band = a.rtiles >= 64 ? 8 : div_up(a.rtiles, 8);
-    const long bands = div_up(a.rtiles, a.band);
-    const long blocks = div_up((int)bands, 8) * 8 * (long)a.band * a.ftiles;
+    if (ADAPTED && a.rtiles < 64 && a.rtiles * a.ftiles <= 512) a.band = 0;
+    const long bands = div_up(a.rtiles, a.band ? a.band : 1);
+    const long blocks = a.band ? div_up((int)bands, 8) * 8 * (long)a.band * a.ftiles
+                               : div_up(a.rtiles * a.ftiles, 8) * 8L;
     if (blocks > 0xffffffL) return hipErrorInvalidConfiguration;  // 2^32 threads a launch
     const dim3 grid((unsigned)blocks);
     using Kernel = void (*)(ProjArgs);
-    Kernel fn = paged ? project_gemm_kernel<true, kPlain> : project_gemm_kernel<false, kPlain>;
-    if (ADAPTED)
-        fn = own ? (paged ? project_gemm_kernel<true, kOwnTiles> : project_gemm_kernel<false, kOwnTiles>)
-                 : (paged ? project_gemm_kernel<true, kMixed> : project_gemm_kernel<false, kMixed>);
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(fn),
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)kGemmLds);
+    Kernel fn = paged ? project_gemm_kernel<true, kPlain, 128> : project_gemm_kernel<false, kPlain, 128>;
+    if (own && bm == 64)
+        fn = paged ? project_gemm_kernel<true, kOwnTiles, 64> : project_gemm_kernel<false, kOwnTiles, 64>;
+    else if (own)
+        fn = paged ? project_gemm_kernel<true, kOwnTiles, 128> : project_gemm_kernel<false, kOwnTiles, 128>;
+    else if (ADAPTED && bm == 64)
+        fn = paged ? project_gemm_kernel<true, kMixed, 64> : project_gemm_kernel<false, kMixed, 64>;
+    else if (ADAPTED)
+        fn = paged ? project_gemm_kernel<true, kMixed, 128> : project_gemm_kernel<false, kMixed, 128>;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(fn),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)gemm_lds(bm));
     if (e != hipSuccess) return e;
-    fn<<<grid, dim3(256), kGemmLds, stream>>>(a);
+    fn<<<grid, dim3(256), gemm_lds(bm), stream>>>(a);
     return hipGetLastError();
 }
 
