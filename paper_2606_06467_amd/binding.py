@@ -273,6 +273,7 @@ def _stream_object(device):
 # The current stream's raw handle: making a torch Stream object takes 3 us, as long as the
 # library's call.  It is no public name of torch, and a torch built without a GPU lacks it.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _stream_object)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _call(where, shape, block, names, tensors, ws, stream, sizes=(), device=-1):
@@ -285,7 +286,10 @@ def _call(where, shape, block, names, tensors, ws, stream, sizes=(), device=-1):
         if t is None:
             args.append(None)
             continue
-        at = t.get_device() if isinstance(t, _Tensor) else -1
+        try:
+            at = t.get_device()
+        except AttributeError:  # no tensor
+            _refuse(names[i], t)
         if at < 0 or not t.is_contiguous() or at != device:
             if device >= 0 or at < 0 or not t.is_contiguous():
                 _refuse(names[i], t)
@@ -297,7 +301,7 @@ def _call(where, shape, block, names, tensors, ws, stream, sizes=(), device=-1):
         args += ws.data_ptr(), ws.numel() * ws.element_size()
     elif ws is None:
         args += None, 0
-    if device >= 0 and device != torch.cuda.current_device():
+    if device >= 0 and device != _current_device():
         with torch.cuda.device(device):
             return _call(where, shape, block, names, tensors, ws, stream, sizes, given)
     raw = _raw_stream(max(device, 0)) if stream is None else stream.cuda_stream
