@@ -196,14 +196,14 @@ constexpr int kGemmPitch = kGemmK;           // bf16 per staged row
 constexpr int kGemmOutPitch = kGemmN + 8;    // bf16 per staged output row
 constexpr size_t gemm_lds(int rows) { return sizeof(uint16_t) * 2 * (rows + kGemmN) * kGemmPitch; }
 
-// kMixed: adds the adapters' part to a wave's 16 MT x 64 tile of the tiled product (c[mt][nt]:
+// kMixed: adds the adapters' part to a wave's 16 MT x 16 NT tile of the tiled product (c[mt][nt]:
 // rows r0 + 16 mt, features f0 + 16 nt).  A 32-wide product step holds 16 ranks twice, the high and
 // the low parts of u against the same B.  Rows of different sequences can share a 16-row
 // tile: the step is then made once for each adapter in it, Q adapters' loads in flight
 // together, and added to that adapter's rows only (a factor of zero would carry one
 // adapter's infinities to another's rows).
-template <int MT, int Q>
-__device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, f32x4 (&c)[MT][4]) {
+template <int MT, int NT, int Q>
+__device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, f32x4 (&c)[MT][NT]) {
     const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
     const uint16_t *halves = reinterpret_cast<const uint16_t *>(a.u);
     const int pitch = div_up(a.rank, 16) * 32;
@@ -215,7 +215,7 @@ __device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, 
     }
 #pragma unroll 1
     for (int j = 0; j < a.rank; j += 16) {
-        bf16x8 av[MT], bv[Q][4];
+        bf16x8 av[MT], bv[Q][NT];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             av[mt] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
@@ -238,7 +238,7 @@ __device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, 
                         if (q == 0 && id == held) continue;
                         if (q == 0) held = id;
 #pragma unroll
-                        for (int nt = 0; nt < 4; ++nt) {
+                        for (int nt = 0; nt < NT; ++nt) {
                             bv[q][nt] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
                             if (ro < a.rank)
                                 bv[q][nt] = ld8(a.up + ((size_t)id * a.n_feat + f0 + 16 * nt + col) * a.rank + ro);
@@ -249,7 +249,7 @@ __device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, 
                 for (int q = 0; q < Q; ++q) {
                     if (!same[q]) break;
 #pragma unroll
-                    for (int nt = 0; nt < 4; ++nt) {
+                    for (int nt = 0; nt < NT; ++nt) {
                         const f32x4 t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[mt], bv[q][nt], c[mt][nt], 0, 0, 0);
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
@@ -266,9 +266,12 @@ __device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, 
 // the high and the low parts of u against the same B).  kMixed: adapter_tile above.
 enum GemmMode { kPlain, kOwnTiles, kMixed };
 
-template <bool PAGED, GemmMode MODE, int BM>
-__global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
-    constexpr int MT = BM / 32, OPS = MT + 4;  // 16-row tiles of a wave; its operands of a half step
+// BM rows x 128 features by W waves, two of them side by side in the rows.  Eight waves where
+// there is one workgroup a CU: two waves a SIMD then hide each other's waits.
+template <bool PAGED, GemmMode MODE, int BM, int W>
+__global__ __launch_bounds__(64 * W, 2) void project_gemm_kernel(ProjArgs a) {
+    constexpr int MT = BM / 32, NT = 16 / W, OPS = MT + NT;  // 16-wide tiles of a wave; its operands of a half step
+    constexpr int RS = 8 * W, AP = BM / RS, BP = kGemmN / RS;  // staging: rows a pass, pieces a thread
     // two stages of A (rows of h) and B (features of w), 128 x 64 bf16 each
     // (dynamic LDS, kGemmLds bytes); the output tile (128 x 128 bf16) reuses it
     extern __shared__ __align__(16) uint16_t s_lds[];
@@ -276,7 +279,7 @@ __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
     auto s_row = [&](int st, int r) { return s_lds + (size_t)(st * (BM + kGemmN) + r) * kGemmPitch; };
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int col = lane & 15, grp = lane >> 4;
-    const int wm = wave >> 1, wn = wave & 1;  // the wave's BM / 2 x 64 quadrant
+    const int wm = wave / (W / 2), wn = wave % (W / 2);  // the wave's BM / 2 x 16 NT part
     // Tile order: workgroups are dealt to the 8 XCDs in turn (L mod 8); XCD x
     // takes bands of `band` row tiles (8, fewer when there are few rows) and
     // walks, for each band, the feature tiles with the band's row tiles next to
@@ -310,38 +313,38 @@ __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
         row_end = (b + 1) * a.n_q;
         id = adapter_of(a, b);
     }
-    // staging: thread t moves 16-byte pieces t + 256 i (i < 4) of each 128 x 64
-    // tile: row (t >> 3) + 32 i, columns 8 (t & 7) .. + 8
+    // staging: thread t moves 16-byte pieces t + 64 W i of each tile of 64-wide rows: row
+    // (t >> 3) + RS i, columns 8 (t & 7) .. + 8
     const int lrow = tid >> 3, lcol = (tid & 7) * 8;
     const int wcol = ((tid & 7) ^ ((lrow >> 1) & 7)) * 8, rswz = (col >> 1) & 7;
-    const uint16_t *hp[MT], *wp[4];
+    const uint16_t *hp[AP], *wp[BP];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (i < MT) hp[i] = a.h + (size_t)min(r0 + lrow + 32 * i, row_end - 1) * a.d + lcol;  // tail rows: never stored
-        wp[i] = a.w + (size_t)(f0 + lrow + 32 * i) * a.d + lcol;
+    for (int i = 0; i < BP; ++i) {
+        if (i < AP) hp[i] = a.h + (size_t)min(r0 + lrow + RS * i, row_end - 1) * a.d + lcol;  // tail rows: never stored
+        wp[i] = a.w + (size_t)(f0 + lrow + RS * i) * a.d + lcol;
     }
     // two register sets: the loads for step k + 2 are issued while step k is
     // computed, and step k + 1 (loaded a step earlier) goes to LDS after it
-    u32x4 ra[2][MT], rb[2][4];
+    u32x4 ra[2][AP], rb[2][BP];
     auto gload = [&](int set, int k0) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i < MT) ra[set][i] = *reinterpret_cast<const u32x4 *>(hp[i] + k0);
+        for (int i = 0; i < BP; ++i) {
+            if (i < AP) ra[set][i] = *reinterpret_cast<const u32x4 *>(hp[i] + k0);
             rb[set][i] = *reinterpret_cast<const u32x4 *>(wp[i] + k0);
         }
     };
     auto lstore = [&](int set, int st) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i < MT) *reinterpret_cast<u32x4 *>(s_row(st, lrow + 32 * i) + wcol) = ra[set][i];
-            *reinterpret_cast<u32x4 *>(s_row(st, BM + lrow + 32 * i) + wcol) = rb[set][i];
+        for (int i = 0; i < BP; ++i) {
+            if (i < AP) *reinterpret_cast<u32x4 *>(s_row(st, lrow + RS * i) + wcol) = ra[set][i];
+            *reinterpret_cast<u32x4 *>(s_row(st, BM + lrow + RS * i) + wcol) = rb[set][i];
         }
     };
-    f32x4 c[MT][4];
+    f32x4 c[MT][NT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int nt = 0; nt < 4; ++nt) c[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int nt = 0; nt < NT; ++nt) c[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int nk = a.d / kGemmK;  // even (d_model is a multiple of 512)
     const int steps = nk + (MODE == kOwnTiles && id >= 0 ? div_up(a.rank, 32) : 0);
     // step e of the adapter's ranks: this thread's pieces of u and of B
@@ -349,15 +352,15 @@ __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
         const int chunk = 2 * e + (lcol >> 5), ro = chunk * 16 + (lcol & 8), pitch = div_up(a.rank, 16) * 32;
         const uint16_t *halves = reinterpret_cast<const uint16_t *>(a.u);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < BP; ++i) {
             rb[set][i] = u32x4{0u, 0u, 0u, 0u};
-            if (i < MT) ra[set][i] = u32x4{0u, 0u, 0u, 0u};
-            if (i < MT && chunk * 16 < a.rank)
+            if (i < AP) ra[set][i] = u32x4{0u, 0u, 0u, 0u};
+            if (i < AP && chunk * 16 < a.rank)
                 ra[set][i] = *reinterpret_cast<const u32x4 *>(
-                    halves + (size_t)min(r0 + lrow + 32 * i, row_end - 1) * pitch + e * 64 + lcol);
+                    halves + (size_t)min(r0 + lrow + RS * i, row_end - 1) * pitch + e * 64 + lcol);
             if (ro < a.rank)
                 rb[set][i] = *reinterpret_cast<const u32x4 *>(
-                    a.up + ((size_t)id * a.n_feat + f0 + lrow + 32 * i) * a.rank + ro);
+                    a.up + ((size_t)id * a.n_feat + f0 + lrow + RS * i) * a.rank + ro);
         }
     };
     gload(0, 0);
@@ -368,10 +371,10 @@ __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
     // k + 2 were issued; step k + 1 goes to the other stage meanwhile.
     auto step = [&](int h) {
         const int st = h;
-        // operand o of 32-wide half ks: the features of the wave's quadrant (o < 4), then its rows
+        // operand o of 32-wide half ks: the features of the wave's part (o < NT), then its rows
         bf16x8 op[2][OPS];
         auto read_op = [&](int ks, int o) {
-            const int r = (o < 4 ? BM + wn * 64 + o * 16 : wm * (BM / 2) + (o - 4) * 16) + col;
+            const int r = (o < NT ? BM + (wn * NT + o) * 16 : wm * (BM / 2) + (o - NT) * 16) + col;
             op[ks][o] = __builtin_bit_cast(
                 bf16x8, *reinterpret_cast<const u32x4 *>(s_row(st, r) + ((ks * 4 + grp) ^ rswz) * 8));
         };
@@ -379,32 +382,32 @@ __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
 #pragma unroll
         for (int o = 0; o < OPS; ++o) read_op(0, o);
         // Parts of two products whose order is pinned: those of the first half each read
-        // operands of the second half (one each with 128 rows), the others each store
+        // operands of the second half (one each with 128 rows and four waves), the others each store
         // pieces of the next step (the last step stores old pieces that are not read).  8192
         // rows x 2560 features x 2560: 127.6 us with padded rows and the compiler's order,
         // 124.0 swizzled, 117.4 in this order; 32-wide steps (three workgroups per CU) 139.6.
         // What bounds it now: 1280 tiles on 512 resident workgroups are 2.5 rounds, and
         // the step's own chain of barrier, operand reads and products at two waves per
         // SIMD.
-        constexpr int H = 2 * MT;  // parts of a half step
+        constexpr int H = MT * NT / 2, ST = AP + BP;  // parts of a half step; pieces to store
 #pragma unroll
         for (int p = 0; p < 2 * H; ++p) {
-            const int ks = p / H, q0 = (p % H) * OPS / H, q1 = (p % H + 1) * OPS / H;
+            const int ks = p / H, part = p % H;
             if (ks == 0)
 #pragma unroll
-                for (int o = q0; o < q1; ++o) read_op(1, o);
+                for (int o = part * OPS / H; o < (part + 1) * OPS / H; ++o) read_op(1, o);
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int m = 2 * (p % H) + e, mt = m >> 2, nt = m & 3;
-                c[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op[ks][4 + mt], op[ks][nt], c[mt][nt], 0, 0, 0);
+                const int m = 2 * part + e, mt = m / NT, nt = m % NT;
+                c[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(op[ks][NT + mt], op[ks][nt], c[mt][nt], 0, 0, 0);
             }
             if (ks == 1)
 #pragma unroll
-                for (int o = q0; o < q1; ++o) {  // rows and features in turn, then the other features
-                    const bool row = o < 2 * MT && !(o & 1);
-                    const int i = o < 2 * MT ? o >> 1 : o - MT;
-                    const u32x4 v = row ? ra[h ^ 1][i < MT ? i : 0] : rb[h ^ 1][i];
-                    *reinterpret_cast<u32x4 *>(s_row(st ^ 1, (row ? 0 : BM) + lrow + 32 * i) + wcol) = v;
+                for (int o = part * ST / H; o < (part + 1) * ST / H; ++o) {  // rows and features in turn, then the rest
+                    const bool row = o < 2 * AP && !(o & 1);
+                    const int i = o < 2 * AP ? o >> 1 : o - AP;
+                    const u32x4 v = row ? ra[h ^ 1][i < AP ? i : 0] : rb[h ^ 1][i];
+                    *reinterpret_cast<u32x4 *>(s_row(st ^ 1, (row ? 0 : BM) + lrow + RS * i) + wcol) = v;
                 }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -427,27 +430,27 @@ __global__ __launch_bounds__(256, 2) void project_gemm_kernel(ProjArgs a) {
             step(h);
         }
     }
-    if (MODE == kMixed) adapter_tile<MT, MT == 2 ? 4 : 2>(a, r0 + wm * (BM / 2), f0 + wn * 64, c);
+    if (MODE == kMixed) adapter_tile<MT, NT, (MT * NT > 8 ? 2 : 4)>(a, r0 + wm * (BM / 2), f0 + wn * 16 * NT, c);
     // bf16 results into LDS: C tile (mt, nt) row 4 grp + r, column col
     uint16_t(*s_out)[kGemmOutPitch] = reinterpret_cast<uint16_t(*)[kGemmOutPitch]>(s_lds);
     static_assert(gemm_lds(BM) >= sizeof(uint16_t) * BM * kGemmOutPitch, "output tile fits");
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int nt = 0; nt < 4; ++nt)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                s_out[wm * (BM / 2) + mt * 16 + 4 * grp + r][wn * 64 + nt * 16 + col] =
+                s_out[wm * (BM / 2) + mt * 16 + 4 * grp + r][(wn * NT + nt) * 16 + col] =
                     (uint16_t)f32_to_bf16_bits(c[mt][nt][r]);
     __syncthreads();
-    // whole rows out: 16 pieces of 16 bytes per row, 8 rows per pass of 128 threads
+    // whole rows out: 16 pieces of 16 bytes per row
     const int piece = tid & 15;
     int dst_kind, width, fo;  // 0: index query, 1: index key, 2: K, 3: V
     if (f0 < 256) { dst_kind = 0; width = 256; fo = f0; }
     else if (f0 < 512) { dst_kind = 1; width = 256; fo = f0 - 256; }
     else if (f0 < 512 + a.kvw) { dst_kind = 2; width = a.kvw; fo = f0 - 512; }
     else { dst_kind = 3; width = a.kvw; fo = f0 - 512 - a.kvw; }
-    for (int rr = tid >> 4; rr < BM; rr += 16) {
+    for (int rr = tid >> 4; rr < BM; rr += 4 * W) {
         const int r = r0 + rr;
         if (r >= row_end) break;
         const u32x4 v = *reinterpret_cast<const u32x4 *>(&s_out[rr][piece * 8]);
@@ -617,6 +620,11 @@ static void launch_splitk(const ProjArgs &a, bool paged, int n_feat, hipStream_t
     else project_splitk_kernel<KS, NB, 1, false, ADAPTED><<<grid, block, 0, stream>>>(a);
 }
 
+// Workgroups up to which the adapted product takes eight waves each, four beyond (with the
+// inner products, eight / four: 1024 rows x 2560 features, d_model 2560, 160 workgroups 34.1 /
+// 37.4 us; 2048 rows, 320 workgroups 58.6 / 52.4).
+constexpr long kWideGemmBlocks = 256;
+
 template <bool ADAPTED = false>
 static hipError_t launch_project_args(const Geometry &g, int d_model, ProjArgs a, const void *h,
                                       const void *w, const int32_t *page_table, void *q_idx,
@@ -690,22 +698,30 @@ static hipError_t launch_project_args(const Geometry &g, int d_model, ProjArgs a
     const long bands = div_up(a.rtiles, a.band ? a.band : 1);
     const long blocks = a.band ? div_up((int)bands, 8) * 8 * (long)a.band * a.ftiles
                                : div_up(a.rtiles * a.ftiles, 8) * 8L;
-    if (blocks > 0xffffffL) return hipErrorInvalidConfiguration;  // 2^32 threads a launch
+    if (blocks > 0x7fffffL) return hipErrorInvalidConfiguration;  // 2^32 threads a launch
     const dim3 grid((unsigned)blocks);
+    const int waves = ADAPTED && blocks <= kWideGemmBlocks ? 8 : 4;
     using Kernel = void (*)(ProjArgs);
-    Kernel fn = paged ? project_gemm_kernel<true, kPlain, 128> : project_gemm_kernel<false, kPlain, 128>;
-    if (own && bm == 64)
-        fn = paged ? project_gemm_kernel<true, kOwnTiles, 64> : project_gemm_kernel<false, kOwnTiles, 64>;
-    else if (own)
-        fn = paged ? project_gemm_kernel<true, kOwnTiles, 128> : project_gemm_kernel<false, kOwnTiles, 128>;
-    else if (ADAPTED && bm == 64)
-        fn = paged ? project_gemm_kernel<true, kMixed, 64> : project_gemm_kernel<false, kMixed, 64>;
-    else if (ADAPTED)
-        fn = paged ? project_gemm_kernel<true, kMixed, 128> : project_gemm_kernel<false, kMixed, 128>;
+    Kernel fn;
+#define CLSA_GEMM(MODE, BM, W) fn = paged ? project_gemm_kernel<true, MODE, BM, W> : project_gemm_kernel<false, MODE, BM, W>
+    if constexpr (!ADAPTED) {
+        CLSA_GEMM(kPlain, 128, 4);
+    } else if (own) {
+        if (bm == 64 && waves == 8) CLSA_GEMM(kOwnTiles, 64, 8);
+        else if (bm == 64) CLSA_GEMM(kOwnTiles, 64, 4);
+        else if (waves == 8) CLSA_GEMM(kOwnTiles, 128, 8);
+        else CLSA_GEMM(kOwnTiles, 128, 4);
+    } else {
+        if (bm == 64 && waves == 8) CLSA_GEMM(kMixed, 64, 8);
+        else if (bm == 64) CLSA_GEMM(kMixed, 64, 4);
+        else if (waves == 8) CLSA_GEMM(kMixed, 128, 8);
+        else CLSA_GEMM(kMixed, 128, 4);
+    }
+#undef CLSA_GEMM
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(fn),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)gemm_lds(bm));
     if (e != hipSuccess) return e;
-    fn<<<grid, dim3(256), gemm_lds(bm), stream>>>(a);
+    fn<<<grid, dim3(64 * waves), gemm_lds(bm), stream>>>(a);
     return hipGetLastError();
 }
 
