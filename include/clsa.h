@@ -430,8 +430,8 @@ clsa_status clsa_project_append8_adapted(const clsa_shape *shape, int32_t block,
 
 /* ---- The norm in front of the projections ----
  *
- * For every row r of the batch * n_q rows (up to 2^22) of d_model values (a multiple of 8
- * up to 16384; nothing else of the shape is read):
+ * For every row r of the batch * n_q rows (fewer than 2^22) of d_model values (a multiple of
+ * 8 up to 16384; nothing else of the shape is read):
  *   s = bf16(x + residual) (x itself if residual is NULL),
  *   rstd = 1 / sqrt(mean(s^2) + eps),   y = s * rstd * weight.
  * x, residual, sum, y: bf16 [batch, n_q, d_model]; weight: bf16 [d_model].  sum receives s

@@ -304,7 +304,7 @@ hipError_t take_device_error_project(uint32_t *bits);
 
 // ---- norm.hip ----
 constexpr int kNormMaxDim = 16384;
-constexpr int kNormMaxRows = 1 << 22;
+constexpr int kNormMaxRows = (1 << 22) - 1;  // 2^32 threads a launch
 bool norm_supported(int d);
 // group: 32, 64, 128 or d (a whole row); residual, sum, y, y8 (with y_scale) and rstd may be null.
 hipError_t launch_norm(int rows, int d, double eps, const void *x, const void *residual,

@@ -700,20 +700,19 @@ static hipError_t launch_project_args(const Geometry &g, int d_model, ProjArgs a
                                : div_up(a.rtiles * a.ftiles, 8) * 8L;
     if (blocks > 0x7fffffL) return hipErrorInvalidConfiguration;  // 2^32 threads a launch
     const dim3 grid((unsigned)blocks);
-    const int waves = ADAPTED && blocks <= kWideGemmBlocks ? 8 : 4;
+    // (tiles of 64 rows are no more than the CUs, so that their workgroups are not either)
+    const int waves = ADAPTED && (bm == 64 || blocks <= kWideGemmBlocks) ? 8 : 4;
     using Kernel = void (*)(ProjArgs);
     Kernel fn;
 #define CLSA_GEMM(MODE, BM, W) fn = paged ? project_gemm_kernel<true, MODE, BM, W> : project_gemm_kernel<false, MODE, BM, W>
     if constexpr (!ADAPTED) {
         CLSA_GEMM(kPlain, 128, 4);
     } else if (own) {
-        if (bm == 64 && waves == 8) CLSA_GEMM(kOwnTiles, 64, 8);
-        else if (bm == 64) CLSA_GEMM(kOwnTiles, 64, 4);
+        if (bm == 64) CLSA_GEMM(kOwnTiles, 64, 8);
         else if (waves == 8) CLSA_GEMM(kOwnTiles, 128, 8);
         else CLSA_GEMM(kOwnTiles, 128, 4);
     } else {
-        if (bm == 64 && waves == 8) CLSA_GEMM(kMixed, 64, 8);
-        else if (bm == 64) CLSA_GEMM(kMixed, 64, 4);
+        if (bm == 64) CLSA_GEMM(kMixed, 64, 8);
         else if (waves == 8) CLSA_GEMM(kMixed, 128, 8);
         else CLSA_GEMM(kMixed, 128, 4);
     }

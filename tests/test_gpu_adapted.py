@@ -97,8 +97,8 @@ class Case:
         ref, tol = self.reference()
         rows, kvw = self.rows(), self.kvw
         keep = np.ones(len(ref), bool) if only is None else np.repeat(only, self.n_q)
-        err = np.abs(f64(got[0]) - ref[:, :256])
-        assert np.all(err[keep] <= tol[keep, :256]), float((err[keep] / tol[keep, :256]).max())
+        err = np.abs(f64(got[0][keep]) - ref[keep, :256])
+        assert np.all(err <= tol[keep, :256]), float((err / tol[keep, :256]).max())
         for x, c0, c1 in ((got[1], 256, 512), (got[2], 512, 512 + kvw), (got[3], 512 + kvw, 512 + 2 * kvw)):
             live = (rows >= 0) & keep
             err = np.abs(f64(x[rows[live]]) - ref[live, c0:c1])
@@ -111,7 +111,10 @@ class Case:
 CASES = [  # batch, n_q, d_model, rank, adapters, page
     (1, 1, 512, 8, 1, 0), (5, 1, 2560, 16, 3, 16), (32, 1, 2560, 16, 40, 16), (33, 1, 1024, 64, 5, 0), (70, 1, 4096, 8, 9, 16),
     (128, 1, 512, 128, 130, 0), (200, 1, 512, 16, 11, 16), (3, 5, 1536, 24, 2, 0), (300, 2, 512, 40, 250, 0),
-    (7, 37, 512, 16, 3, 16), (1, 300, 2560, 16, 2, 0), (9, 33, 1024, 128, 9, 16), (2, 100, 512, 8, 2, 0), (4, 64, 3584, 56, 3, 0)]
+    (7, 37, 512, 16, 3, 16), (1, 300, 2560, 16, 2, 0), (9, 33, 1024, 128, 9, 16), (2, 100, 512, 8, 2, 0), (4, 64, 3584, 56, 3, 0),
+    # each form of the tiled product: 128-row tiles of one sequence and shared ones, by four and eight waves
+    (1, 2100, 512, 24, 2, 16), (1, 4200, 512, 16, 2, 0), (1, 8300, 512, 40, 1, 16), (2100, 1, 512, 8, 7, 0),
+    (700, 6, 512, 24, 60, 16), (30, 150, 512, 72, 4, 16)]
 
 
 @pytest.mark.parametrize("batch,n_q,d,rank,n,page", CASES)
@@ -126,6 +129,25 @@ def test_adapted(batch, n_q, d, rank, n, page):
     c.check(got)
     for a, b in zip(got, c.run()):
         assert np.array_equal(a, b)
+
+
+@pytest.mark.parametrize("batch,n_q", [(3, 1), (9, 40)])
+def test_adapters_past_32_bits(batch, n_q):
+    """The last of adapters that together are larger than 4 GiB."""
+    import torch
+    rank, n = 128, 18000
+    c = Case(batch, n_q, 1024, rank, 3, np.full(batch, 2), max_len=96, seed=11)  # 256 KiB each of A and B
+    d = c.dev()
+    for k in ("a", "b"):
+        t = d[k]
+        big = torch.zeros((n, *t.shape[1:]), dtype=t.dtype, device="cuda")
+        assert big.nbytes > 1 << 32
+        big[-1] = t[2]
+        d[k] = big
+    d["alpha"] = torch.zeros(n, device="cuda")
+    d["alpha"][-1] = float(c.alpha[2])
+    d["ids"] = torch.full((batch,), n - 1, dtype=torch.int32, device="cuda")
+    c.check(c.run(d))
 
 
 @pytest.mark.parametrize("batch,n_q", [(6, 1), (150, 1), (3, 70)])
@@ -159,10 +181,11 @@ def test_infinities_stay_with_their_adapter(batch, n_q):
     c.check(got, others)
     q = f64(got[0]).reshape(batch, n_q, 256)
     bad = q[~others]
-    want = np.sign(f64(c.b[0, :256, 2])) * np.sign(c.alpha[0]) * np.inf
+    with np.errstate(invalid="ignore"):
+        want = np.sign(f64(c.b[0, :256, 2])) * np.sign(c.alpha[0]) * np.inf
     assert np.isnan(bad[..., 7]).all()
-    fine = np.arange(256) != 7
-    fine &= np.isfinite(want) | np.isinf(want)
+    fine = (np.arange(256) != 7) & np.isinf(want)
+    assert fine.sum() > 200
     assert np.array_equal(bad[..., fine], np.broadcast_to(want[fine], bad[..., fine].shape))
 
 

@@ -187,7 +187,7 @@ def _check_grad(got, s, rstd, w, dy, ds):
     assert np.all(np.abs(got[1] - dw) <= (rows + 4) * U24 * mag + 1e-40)
 
 
-@pytest.mark.parametrize("rows,d", FORMS)
+@pytest.mark.parametrize("rows,d", FORMS + [(1100, 1200), (8200, 1024), (5600, 1504), (4200, 2048)])
 def test_norm_grad(rows, d):
     s, rstd, w, dy, ds = _grad_inputs(rows, d, 70 + rows + d)
     got = _grad(s, rstd, w, dy, ds, rows, d)
@@ -220,6 +220,32 @@ def test_norm_grad_against_differences():
         e = np.zeros_like(wt)
         e[j] = h
         assert abs(dw[j] - (loss(v, wt + e) - loss(v, wt - e)) / (2 * h)) <= 1e-7
+
+
+def test_norm_of_offsets_past_32_bits():
+    """2^22 - 1 rows of 1032 values: the last rows like the same rows alone."""
+    import torch
+    from paper_2606_06467_amd import binding as B
+    rows, d, n = (1 << 22) - 1, 1032, 5
+    x = torch.full((rows, d), 0.5, dtype=torch.bfloat16, device="cuda")
+    end = B.bf16_from_bits(inputs.normal_bf16(1, (n, d), 1.0))
+    x[-n:] = end
+    w = B.bf16_from_bits(inputs.normal_bf16(2, (d,), 1.0))
+    y, few = torch.empty_like(x), torch.empty_like(end)
+    rstd, dw, dw1 = torch.empty(rows, device="cuda"), torch.empty(d, device="cuda"), torch.empty(d, device="cuda")
+    sh, one = B.make_shape(rows, 1, 1, 1), B.make_shape(n, 1, 1, 1)
+    B.clsa_residual_norm(sh, d, EPS, x, None, w, y=y, rstd=rstd)
+    B.clsa_residual_norm(one, d, EPS, end, None, w, y=few)
+    assert torch.equal(y[-n:].view(torch.int16), few.view(torch.int16))
+    # the gradient in place of y, from dy = x
+    B.clsa_residual_norm_grad(sh, d, x, rstd, w, x, None, y, dw, B.workspace(sh, B.CLSA_OP_NORM_GRAD, d))
+    B.clsa_residual_norm_grad(one, d, end, rstd[-n:].contiguous(), w, end, None, few, dw1,
+                              B.workspace(one, B.CLSA_OP_NORM_GRAD, d))
+    assert torch.allclose(y[-n:].float(), few.float(), rtol=2 ** -7, atol=1e-6)  # sums of d in another order
+    # dw = sum of x^2 rstd: rows - n equal terms of 0.25 / sqrt(0.25 + EPS), summed in fp32 by few
+    # chains of rows / 2048 at most: that many roundings
+    want = (rows - n) * 0.25 / (0.25 + EPS) ** 0.5
+    assert torch.all((dw - want).abs() <= want * (rows / 512 + 300) * U24 + dw1.abs())
 
 
 def test_norm_on_a_stream_and_replayed():

@@ -151,6 +151,18 @@ def test_copy():
         B.clsa_pages_copy(cache, *_dev(src[:3], dst[:2]))
 
 
+def test_copy_of_offsets_past_32_bits():
+    import torch
+    from paper_2606_06467_amd import binding as B
+    pages, width = 70000, 1 << 16
+    x = torch.zeros((pages, width), dtype=torch.uint8, device="cuda")  # 4.6 GB
+    x[69999], x[2] = 7, 9
+    src, dst = _dev(np.array([69999, 2], np.int32), np.array([1, 69998], np.int32))
+    B.clsa_pages_copy([x], src, dst)
+    assert bool((x[1] == 7).all()) and bool((x[69998] == 9).all()) and bool((x[69999] == 7).all())
+    assert int(x.view(pages, -1)[:, 0].ne(0).sum()) == 4
+
+
 def test_captured_twice_with_one_workspace_each():
     """Two captured steps of fork and reserve, replayed in turn, against the same steps run eagerly."""
     import torch

@@ -106,3 +106,72 @@ def test_forked_requests_like_requests_of_their_own():
     for a, b in zip(*got):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
     assert torch.equal(shared.lens, alone.lens) and B.clsa_get_device_error() == 0
+
+
+@pytest.mark.parametrize("block", [16, 64])
+def test_forks_of_the_8bit_cache(block):
+    """The same over the 8-bit cache, with its scales and block keys among a page's tensors: dense
+    and block-routed attention of forked requests, bit for bit as of requests of their own."""
+    import torch
+    from paper_2606_06467_amd import binding as B
+    gen = torch.Generator().manual_seed(3)
+    ids = torch.tensor([0, 0, 0, 0, 2, 2], dtype=torch.int32, device="cuda")
+    n = PAGE // block
+
+    def server():
+        s = Server(90, 60)
+        s.adapter = ids
+        u8 = lambda *d: torch.zeros(d, dtype=torch.uint8, device="cuda")  # noqa: E731
+        s.k8, s.v8 = u8(90, PAGE, 8, 128), u8(90, PAGE, 8, 128)
+        s.ks, s.vs = (torch.ones((90, n, 8), device="cuda") for _ in "kv")
+        s.means = torch.zeros((90, n, 256), dtype=torch.bfloat16, device="cuda")
+        s.cache = [s.cache[0], s.k8, s.v8, s.ks, s.vs, s.means]
+        return s
+
+    def append(s, h, count):
+        n_q = h.shape[1]
+        sh = s.shape(n_q)
+        c = torch.tensor(count, dtype=torch.int32, device="cuda")
+        B.clsa_pages_reserve(sh, s.cache, s.lens, c, s.table, s.refs, s.missing, B.workspace(sh, B.CLSA_OP_PAGES_RESERVE))
+        q = torch.empty((SLOTS, n_q, 4, 64), dtype=torch.bfloat16, device="cuda")
+        B.clsa_project_append8_adapted(sh, block, D, h, s.w, s.a, s.b, s.alpha, s.adapter, s.lens, c, s.table, q,
+                                       s.cache[0], s.k8, s.v8, s.ks, s.vs, B.workspace(sh, B.CLSA_OP_ADAPTED8, RANK))
+        B.clsa_block_means(sh, block, s.cache[0], s.lens, c, s.table, s.means)
+        s.lens += c
+        assert int(s.missing[0]) == 0
+        return q
+
+    def attend(s, q_idx, q):
+        sh = s.shape(1)
+        dense, sparse = torch.zeros_like(q), torch.zeros_like(q)
+        cache = s.k8, s.v8, s.ks, s.vs, s.table
+        B.clsa_dense_attn8(sh, block, q, *cache, s.lens, None, dense, ws=B.workspace(sh, B.CLSA_OP_DENSE8))
+        idx = torch.zeros((SLOTS, 1, K), dtype=torch.int32, device="cuda")
+        ns = torch.zeros((SLOTS, 1), dtype=torch.int32, device="cuda")
+        B.clsa_block_topk(sh, block, q_idx, s.means, s.table, s.lens, None, idx, ns,
+                          B.workspace(sh, B.CLSA_OP_BLOCK_TOPK, block))
+        B.clsa_sparse_attn8(sh, block, q, *cache, idx, ns, sparse, ws=B.workspace(sh, B.CLSA_OP_ATTN8))
+        return dense, sparse, idx, ns
+
+    shared, alone = server(), server()
+    prompt = torch.randn((SLOTS, 150, D), generator=gen).cuda().to(torch.bfloat16)
+    same = prompt.clone()
+    same[1:4], same[4:] = same[:1], same[4:5]
+    append(shared, prompt, [150, 0, 0, 0, 75, 0])
+    shared.fork([0, 0, 0, 0, 4, 4])
+    append(alone, same, [150, 150, 150, 150, 75, 75])
+    for t in range(4):
+        h = torch.randn((SLOTS, 9, D), generator=gen).cuda().to(torch.bfloat16)
+        q = torch.randn((SLOTS, 1, 32, 128), generator=gen).cuda().to(torch.bfloat16)
+        count = [9, 8, 7, 1, 0, 9]
+        got = []
+        for s in (shared, alone):
+            qi = append(s, h, count)
+            got.append(attend(s, qi[:, :1].contiguous(), q))
+        for a, b in zip(*got):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), t
+        if t == 2:
+            bound = torch.zeros(1, dtype=torch.int32, device="cuda")
+            B.clsa_pages_compact(shared.shape(1), shared.cache, shared.table, shared.refs, bound,
+                                 B.workspace(shared.shape(1), B.CLSA_OP_PAGES_COMPACT, shared.pages))
+            assert int(bound[0]) == int((shared.refs > 0).sum())

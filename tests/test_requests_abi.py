@@ -72,7 +72,7 @@ def test_norm_refusals():
     assert B.lib().clsa_residual_norm(None, 512, 1e-6, 128, A, A, A, A, A, A, A, A, None) == -1
     for d, code in ((0, -1), (-8, -1), (12, -2), (16392, -2)):
         assert _norm(sh, d=d) == code and _grad(sh, d=d) == code, d
-    assert _norm(_shape(batch=1 << 15, n_q=1 << 8)) == -2   # 2^23 rows
+    assert _norm(_shape(batch=1 << 12, n_q=1 << 10)) == -2   # 2^22 rows
     for eps in (0.0, -1e-6, float("nan"), float("inf"), 1e-39):
         assert _norm(sh, eps=eps) == -1, eps
     for group, code in ((0, -1), (-128, -1), (16, -2), (96, -2), (256, -2)):
