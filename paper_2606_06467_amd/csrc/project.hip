@@ -113,25 +113,53 @@ __device__ __forceinline__ void store_feature(const ProjArgs &a, int r, int f, f
     else a.v_cache[row * a.kvw + (f - 512 - a.kvw)] = bits;
 }
 
-// (alpha A h) . B of row r and output feature f: fp32 products and sums.
-__device__ __forceinline__ float adapter_dot(const ProjArgs &a, int id, int r, int f) {
-    const uint16_t *bp = a.up + ((size_t)id * a.n_feat + f) * a.rank;
-    const float4 *up = reinterpret_cast<const float4 *>(a.u + (size_t)r * a.rank);
-    float sum = 0.0f;
-    for (int j = 0; j < a.rank / 8; ++j) {
-        const uint4 b = *reinterpret_cast<const uint4 *>(bp + 8 * j);
-        const float4 x = up[2 * j], y = up[2 * j + 1];
-        sum = fmaf(x.x, bf16_lo(b.x), sum);
-        sum = fmaf(x.y, bf16_hi(b.x), sum);
-        sum = fmaf(x.z, bf16_lo(b.y), sum);
-        sum = fmaf(x.w, bf16_hi(b.y), sum);
-        sum = fmaf(y.x, bf16_lo(b.z), sum);
-        sum = fmaf(y.y, bf16_hi(b.z), sum);
-        sum = fmaf(y.z, bf16_lo(b.w), sum);
-        sum = fmaf(y.w, bf16_hi(b.w), sum);
+// (alpha A h) . B of a row and output feature, fp32 products and sums.  What the first 32
+// ranks need is asked for before the parts of the product with w meet in LDS.
+struct AdapterDot {
+    static constexpr int N = 4;  // pieces of 8 ranks in flight
+    const uint16_t *bp;
+    const float4 *up;
+    uint4 b[N];
+    float4 x[2 * N];
+    int n;  // pieces, none without an adapter
+
+    __device__ __forceinline__ void load(int j0) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (j0 + j < n) {
+                b[j] = *reinterpret_cast<const uint4 *>(bp + 8 * (j0 + j));
+                x[2 * j] = up[2 * (j0 + j)];
+                x[2 * j + 1] = up[2 * (j0 + j) + 1];
+            }
     }
-    return sum;
-}
+    __device__ __forceinline__ void start(const ProjArgs &a, int r, int f) {
+        const int id = r < a.rows ? adapter_of(a, r / a.n_q) : -1;
+        n = id < 0 ? 0 : a.rank / 8;
+        bp = a.up + ((size_t)max(id, 0) * a.n_feat + f) * a.rank;
+        up = reinterpret_cast<const float4 *>(a.u + (size_t)r * a.rank);
+        load(0);
+    }
+    __device__ __forceinline__ float finish() {
+        float sum = 0.0f;
+        for (int j0 = 0;;) {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (j0 + j < n) {
+                    sum = fmaf(x[2 * j].x, bf16_lo(b[j].x), sum);
+                    sum = fmaf(x[2 * j].y, bf16_hi(b[j].x), sum);
+                    sum = fmaf(x[2 * j].z, bf16_lo(b[j].y), sum);
+                    sum = fmaf(x[2 * j].w, bf16_hi(b[j].y), sum);
+                    sum = fmaf(x[2 * j + 1].x, bf16_lo(b[j].z), sum);
+                    sum = fmaf(x[2 * j + 1].y, bf16_hi(b[j].z), sum);
+                    sum = fmaf(x[2 * j + 1].z, bf16_lo(b[j].w), sum);
+                    sum = fmaf(x[2 * j + 1].w, bf16_hi(b[j].w), sum);
+                }
+            j0 += N;
+            if (j0 >= n) return sum;
+            load(j0);
+        }
+    }
+};
 
 // Few rows: one 16 RT-row x 16-feature tile per workgroup, d_model split over 8
 // waves of NB * KS 32-dim steps each (d_model = 256 * NB * KS), KS at a time.
@@ -167,6 +195,9 @@ __global__ __launch_bounds__(512) void project_splitk_kernel(ProjArgs a) {
             for (int t = 0; t < RT; ++t)
                 c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[t][s], bv[s], c[t], 0, 0, 0);
     }
+    AdapterDot dot;
+    if (ADAPTED && threadIdx.x < 256 * RT)
+        dot.start(a, rt * 16 * RT + (threadIdx.x >> 4), ft * 16 + (threadIdx.x & 15));
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
@@ -178,10 +209,7 @@ __global__ __launch_bounds__(512) void project_splitk_kernel(ProjArgs a) {
 #pragma unroll
         for (int w = 0; w < kSplitWaves; ++w) sum += part[w][rr][f];
         const int r = rt * 16 * RT + rr;
-        if (ADAPTED && r < a.rows) {
-            const int id = adapter_of(a, r / a.n_q);
-            if (id >= 0) sum += adapter_dot(a, id, r, ft * 16 + f);
-        }
+        if (ADAPTED && dot.n) sum += dot.finish();
         store_feature<PAGED>(a, r, ft * 16 + f, sum);
     }
 }
@@ -568,16 +596,31 @@ __global__ __launch_bounds__(512) void adapter_down_tile_kernel(ProjArgs a) {
     }
 }
 
-// u = alpha A h of few rows: a wave makes one rank of one row.
+// u = alpha A h of few rows: a wave makes one rank of one row.  Latency bounds it: h is
+// asked for before the adapter is known, and 4096 dimensions at a time (32 rows, d_model 2560,
+// rank 16: 3.4 us, 4.4 with 512 at a time; 1 row, d_model 8192 3.6, 6.4).
 __global__ __launch_bounds__(256) void adapter_down_kernel(ProjArgs a) {
+    constexpr int N = 8;
     const int per_row = a.rank / 4, row = blockIdx.x / per_row;
     const int j = (blockIdx.x % per_row) * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int id = adapter_of(a, row / a.n_q);
-    if (id < 0) return;
-    const uint16_t *hp = a.h + (size_t)row * a.d, *ap = a.down + ((size_t)id * a.rank + j) * a.d;
+    const uint16_t *hp = a.h + (size_t)row * a.d + lane * 8;
+    uint4 hv[N], av[N];
     float sum = 0.0f;
-    for (int i = lane * 8; i < a.d; i += 512)
-        sum = dot8_bf16(*reinterpret_cast<const uint4 *>(hp + i), *reinterpret_cast<const uint4 *>(ap + i), sum);
+    int id = -1;
+    for (int i0 = 0; i0 < a.d; i0 += 512 * N) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i0 + 512 * i < a.d) hv[i] = *reinterpret_cast<const uint4 *>(hp + i0 + 512 * i);
+        if (i0 == 0) id = adapter_of(a, row / a.n_q);
+        if (id < 0) return;
+        const uint16_t *ap = a.down + ((size_t)id * a.rank + j) * a.d + lane * 8;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i0 + 512 * i < a.d) av[i] = *reinterpret_cast<const uint4 *>(ap + i0 + 512 * i);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i0 + 512 * i < a.d) sum = dot8_bf16(hv[i], av[i], sum);
+    }
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) sum += __shfl_xor(sum, m);
     if (lane == 0) a.u[(size_t)row * a.rank + j] = sum * a.alpha[id];
@@ -612,7 +655,9 @@ static void launch_splitk(const ProjArgs &a, bool paged, int n_feat, hipStream_t
     // 16.5), and from 65 rows on; 32 rows x 1536 features fit with 16 (9.3 against 12.8
     // at 4096), 48 x 2560 fit with neither (11.3 against 13.9)
     const int tiles = n_feat / 16;
-    const bool two = tiles * div_up(a.rows, 16) > 256 && (tiles * div_up(a.rows, 32) <= 256 || a.rows > 64);
+    // (adapted: from 49 on, 64 rows, d_model 2560, rank 16 20.7 us against 23.7)
+    const bool two = tiles * div_up(a.rows, 16) > 256 &&
+                     (tiles * div_up(a.rows, 32) <= 256 || a.rows > (ADAPTED ? 48 : 64));
     const dim3 grid(tiles, div_up(a.rows, two ? 32 : 16)), block(512);
     if (two && paged) project_splitk_kernel<KS, NB, 2, true, ADAPTED><<<grid, block, 0, stream>>>(a);
     else if (two) project_splitk_kernel<KS, NB, 2, false, ADAPTED><<<grid, block, 0, stream>>>(a);
