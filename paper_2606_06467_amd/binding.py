@@ -8,6 +8,7 @@ there is no fallback: if ``libclsa.so`` is missing the first call raises.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import math
 import os
@@ -389,9 +390,9 @@ def clsa_residual_norm_grad(shape, d_model, s, rstd, weight, dy, dsum, dx, dweig
 
 
 def _paged(tensors, pages):
-    """The host array of a paged cache's tensors, their number and their device."""
-    n, device = len(tensors), -1
-    arr = (ClsaPaged * max(1, n))()
+    """The host array of a paged cache's tensors (held by the caller while it is in use), its length
+    and address as arguments, and the tensors' device."""
+    fields, device = array.array("q"), -1  # data and page_bytes of each
     for i, t in enumerate(tensors):
         if not isinstance(t, _Tensor):
             raise TypeError(f"tensors[{i}] must be a torch.Tensor")
@@ -401,9 +402,9 @@ def _paged(tensors, pages):
         if t.dim() < 1 or t.shape[0] != pages:
             raise ValueError(f"tensors[{i}] must have one row for each of the {pages} pages of refs")
         device = at
-        arr[i].data = t.data_ptr()
-        arr[i].page_bytes = t.nbytes // pages
-    return n, arr, device
+        fields.append(t.data_ptr())
+        fields.append(t.nbytes // pages)
+    return fields, (len(tensors), fields.buffer_info()[0]), device
 
 
 def clsa_pages_fork(shape, parent, page_table, seq_lens, refs, stream=None):
@@ -414,25 +415,25 @@ def clsa_pages_fork(shape, parent, page_table, seq_lens, refs, stream=None):
 def clsa_pages_reserve(shape, tensors, start, count, page_table, refs, missing, ws=None, stream=None):
     """tensors: the cache's tensors, each with a leading dimension of refs.numel() pages."""
     pages = refs.numel()
-    n, arr, device = _paged(tensors, pages)
+    held, sizes, device = _paged(tensors, pages)
     _call("clsa_pages_reserve", shape, pages, ("start", "count", "page_table", "refs", "missing"),
-          (start, count, page_table, refs, missing), ws, stream, (n, arr), device)
+          (start, count, page_table, refs, missing), ws, stream, sizes, device)
 
 
 def clsa_pages_compact(shape, tensors, page_table, refs, bound, ws=None, stream=None):
     pages = refs.numel()
-    n, arr, device = _paged(tensors, pages)
+    held, sizes, device = _paged(tensors, pages)
     _call("clsa_pages_compact", shape, pages, ("page_table", "refs", "bound"), (page_table, refs, bound), ws,
-          stream, (n, arr), device)
+          stream, sizes, device)
 
 
 def clsa_pages_copy(tensors, src, dst, stream=None):
     """Pages src[i] to dst[i] of every tensor (they have the same number of pages)."""
     pages = tensors[0].shape[0] if tensors else 1
-    n, arr, device = _paged(tensors, pages)
+    held, sizes, device = _paged(tensors, pages)
     if src.numel() != dst.numel():
         raise ValueError("src and dst must have one length")
-    _call("clsa_pages_copy", None, pages, ("src", "dst"), (src, dst), False, stream, (n, arr, src.numel()),
+    _call("clsa_pages_copy", None, pages, ("src", "dst"), (src, dst), False, stream, (*sizes, src.numel()),
           device)
 
 

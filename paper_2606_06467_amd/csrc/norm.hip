@@ -176,6 +176,88 @@ struct NormGradArgs {
     int rows, d, pieces, parts;
 };
 
+// dx of a thread's piece: s, dy, weight and dsum there, rstd, and c = mean(g xhat).
+__device__ __forceinline__ uint4 grad_piece(uint4 v, uint4 y, uint4 w, uint4 u, bool add, float rstd, float c) {
+    float f[8], g[8], h[8], o[8];
+    unpack8(v, f);
+    unpack8(y, g);
+    unpack8(w, h);
+    unpack8(u, o);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float z = (g[e] * h[e] - f[e] * rstd * c) * rstd;
+        f[e] = add ? z + o[e] : z;
+    }
+    return pack8(f);
+}
+
+// Few rows in one launch: a workgroup for each row's dx, and behind those one for every 64
+// columns of dw, which reads its columns of dy and s again (from the caches) instead of waiting
+// for sums from the others.
+template <int P>
+__global__ __launch_bounds__(1024) void norm_grad_few_kernel(NormGradArgs a) {
+    __shared__ float s_sum[16];
+    __shared__ float s_col[128][64 + 1];
+    const int t = threadIdx.x, width = blockDim.x;
+    if ((int)blockIdx.x >= a.rows) {
+        const int col = ((int)blockIdx.x - a.rows) * 64 + (t & 7) * 8, groups = width >> 3;
+        float dw[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (col < a.d) {
+#pragma unroll 4
+            for (int row = t >> 3; row < a.rows; row += groups) {
+                float f[8], g[8];
+                unpack8(ld16(a.s + (size_t)row * a.d + col), f);
+                unpack8(ld16(a.dy + (size_t)row * a.d + col), g);
+                const float rstd = a.rstd[row];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) dw[e] += g[e] * (f[e] * rstd);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s_col[t >> 3][(t & 7) * 8 + e] = dw[e];
+        __syncthreads();
+        const int c = ((int)blockIdx.x - a.rows) * 64 + t;
+        if (t < 64 && c < a.d) {
+            float sum = s_col[0][t];
+            for (int k = 1; k < groups; ++k) sum += s_col[k][t];
+            a.dweight[c] = sum;
+        }
+        return;
+    }
+    const size_t at = (size_t)blockIdx.x * a.d;
+    uint4 v[P], y[P], u[P], w[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        const int p = t + i * width;
+        v[i] = y[i] = u[i] = w[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (p < a.pieces) {
+            v[i] = ld16(a.s + at + 8 * p);
+            y[i] = ld16(a.dy + at + 8 * p);
+            w[i] = ld16(a.weight + 8 * p);
+            if (a.dsum) u[i] = ld16(a.dsum + at + 8 * p);
+        }
+    }
+    const float rstd = a.rstd[blockIdx.x];
+    float dot = 0.0f;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        float f[8], g[8], h[8];
+        unpack8(v[i], f);
+        unpack8(y[i], g);
+        unpack8(w[i], h);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dot = fmaf(g[e] * (f[e] * rstd), h[e], dot);
+    }
+    dot = row_reduce<false>(dot, s_sum, [](float x, float y) { return x + y; });
+    const float c = dot * (1.0f / a.d);
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        const int p = t + i * width;
+        if (p < a.pieces)
+            *reinterpret_cast<uint4 *>(a.dx + at + 8 * p) = grad_piece(v[i], y[i], w[i], u[i], a.dsum != nullptr, rstd, c);
+    }
+}
+
 // Rows in turn, each held by a wave (or the workgroup): the sum g xhat, then dx; dy xhat
 // stays in registers until the last row, so that each workgroup writes one row of sums.
 constexpr int kGradWaves = 8;  // of a workgroup whose waves hold a row each
@@ -232,17 +314,8 @@ __global__ __launch_bounds__(WAVE ? 64 * kGradWaves : 1024) void norm_grad_kerne
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             const int p = t + i * width;
-            float f[8], g[8], h[8], o[8];
-            unpack8(v[i], f);
-            unpack8(y[i], g);
-            unpack8(w[i], h);
-            unpack8(u[i], o);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float z = (g[e] * h[e] - f[e] * rstd * c) * rstd;
-                f[e] = a.dsum ? z + o[e] : z;
-            }
-            if (p < a.pieces) st16<NT>(a.dx + at + 8 * p, pack8(f));
+            if (p < a.pieces)
+                st16<NT>(a.dx + at + 8 * p, grad_piece(v[i], y[i], w[i], u[i], a.dsum != nullptr, rstd, c));
         }
     }
     float *part = a.part + (size_t)blockIdx.x * a.d;
@@ -370,6 +443,14 @@ int norm_grad_parts(int rows, int d) {
     return rows < 512 ? rows : 512;
 }
 
+// Whether two [rows, d] bf16 tensors share memory: the columns of dw must not be read after
+// their rows' dx was written.
+static bool overlaps(const void *x, const void *y, int rows, int d) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y);
+    const uintptr_t n = (uintptr_t)rows * d * sizeof(uint16_t);
+    return a < b + n && b < a + n;
+}
+
 template <bool NT>
 static void launch_grad_rows(const NormGradArgs &a, hipStream_t stream) {
     const dim3 grid(a.parts), wg(64 * kGradWaves);
@@ -405,6 +486,16 @@ hipError_t launch_norm_grad(int rows, int d, const void *s, const float *rstd, c
     a.d = d;
     a.pieces = d / 8;
     a.parts = norm_grad_parts(rows, d);
+    // One launch where a column's threads have at most eight rows each (256 rows of 2560: 6.9 us
+    // against 7.4 with two; 512 rows 13.6 / 11.0, of 5120 8.1 / 14.7; 77 rows of 1000 2.8 / 6.0)
+    const int per = a.pieces <= 512 ? 1 : 2, row_threads = threads_of(a.pieces, per);
+    const int threads = row_threads < 256 ? 256 : row_threads;
+    if (rows <= threads && !overlaps(dx, dy, rows, d) && !overlaps(dx, s, rows, d)) {
+        const dim3 grid(rows + div_up(d, 64)), wg(threads);
+        if (per == 1) norm_grad_few_kernel<1><<<grid, wg, 0, stream>>>(a);
+        else norm_grad_few_kernel<2><<<grid, wg, 0, stream>>>(a);
+        return hipGetLastError();
+    }
     if (streamed(rows, d)) launch_grad_rows<true>(a, stream);
     else launch_grad_rows<false>(a, stream);
     hipError_t e = hipGetLastError();

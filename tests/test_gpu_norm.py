@@ -14,7 +14,7 @@ from tests import gpu_util as U
 pytestmark = pytest.mark.gpu
 U24 = 2.0 ** -24
 EPS = 1e-6
-FORMS = [(1, 8), (1, 2560), (3, 72), (5, 1000), (77, 8200), (2, 16384), (1500, 520), (1030, 2560), (1100, 4096),
+FORMS = [(1, 8), (1, 2560), (3, 72), (5, 1000), (77, 8200), (2, 16384), (256, 16), (257, 16), (320, 2560), (321, 2560), (1500, 520), (1030, 2560), (1100, 4096),
          (1029, 4104), (2050, 8), (1027, 3592),
          (1030, 1544), (4100, 2080), (1100, 8008), (17000, 512)]
 
@@ -193,6 +193,7 @@ def test_norm_grad(rows, d):
     got = _grad(s, rstd, w, dy, ds, rows, d)
     _check_grad(got, s, rstd, w, dy, ds)
     _check_grad(_grad(s, rstd, w, dy, None, rows, d), s, rstd, w, dy, None)
+    _check_grad(_grad(s, rstd, w, dy, None, rows, d, alias=True), s, rstd, w, dy, None)  # in dy's place
     # the same bits again, whatever the workspace holds, and in place
     for again in (_grad(s, rstd, w, dy, ds, rows, d, poison=0xFF), _grad(s, rstd, w, dy, ds, rows, d, alias=True)):
         assert np.array_equal(again[0], got[0]) and np.array_equal(again[1], got[1])
