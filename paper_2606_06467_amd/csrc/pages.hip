@@ -376,9 +376,24 @@ __global__ __launch_bounds__(T) void pages_reserve_few_kernel(ReserveArgs a) {
     __shared__ uint32_t s_odd;
     const int tid = threadIdx.x;
     int32_t *refs = a.p.refs;
+    // the entry's chain of loads first (range, table, holders), the first pages' refs beside it
+    uint32_t odd = 0u;
+    size_t at = 0;
+    const bool reached = tid < a.p.batch * a.slots && reserve_entry(a, tid, at);
     bool free[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) free[j] = N * tid + j < a.p.pages && refs[N * tid + j] == 0;
+    int src = -1, held = 0, h = 0;
+    if (reached) {
+        src = a.p.table[at];
+        if (src < -1 || src >= a.p.pages) odd |= kDevErrPages;
+        if (src < 0 || src >= a.p.pages) src = -1;
+        else held = refs[src];
+    }
+    for (int b = tid; b < a.p.batch; b += T) {
+        const int first = a.start[b], n = a.count[b];
+        if (first < 0 || first > a.max_len || n < 0 || n > a.n_q || n > a.max_len - first) odd |= kDevErrAppend;
+    }
     if (tid == 0) s_odd = 0u;
     for (int h = tid; h < H; h += T) {
         s_key[h] = -1;
@@ -386,19 +401,7 @@ __global__ __launch_bounds__(T) void pages_reserve_few_kernel(ReserveArgs a) {
         s_last[h] = -1;
     }
     __syncthreads();
-    uint32_t odd = 0u;
-    for (int b = tid; b < a.p.batch; b += T) {
-        const int first = a.start[b], n = a.count[b];
-        if (first < 0 || first > a.max_len || n < 0 || n > a.n_q || n > a.max_len - first) odd |= kDevErrAppend;
-    }
-    size_t at = 0;
-    const bool reached = tid < a.p.batch * a.slots && reserve_entry(a, tid, at);
-    int src = -1, held = 0, h = 0;
     if (reached) {
-        src = a.p.table[at];
-        if (src < -1 || src >= a.p.pages) odd |= kDevErrPages;
-        if (src < 0 || src >= a.p.pages) src = -1;
-        else held = refs[src];
         if (src >= 0 && held != 1) {
             h = (int)(((uint32_t)src * 2654435761u) >> 16) & (H - 1);
             for (;;) {  // at most T keys in 2 T slots
