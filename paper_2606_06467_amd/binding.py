@@ -358,13 +358,24 @@ def clsa_block_topk(shape, block, q_idx, means, page_table, seq_lens, q_pos, idx
           (q_idx, means, page_table, seq_lens, q_pos, idx, n_sel), ws, stream)
 
 
+def _adapter_sizes(a, b):
+    """Number and rank of the adapters a [adapters, rank, d_model], b [adapters, features, rank]."""
+    for name, t in (("a", a), ("b", b)):
+        if not isinstance(t, _Tensor) or t.dim() != 3:
+            raise ValueError(f"{name} must be a tensor of three dimensions")
+    n, rank, _ = a.shape
+    if b.shape[0] != n or b.shape[2] != rank:
+        raise ValueError("a and b must hold the same adapters, of one rank")
+    return n, rank
+
+
 def clsa_project_append_adapted(shape, d_model, h, w, a, b, alpha, adapter, pos, page_table, q_idx, k_idx,
                                 k_cache, v_cache, ws=None, stream=None):
     """a: [adapters, rank, d_model], b: [adapters, features, rank]."""
     _call("clsa_project_append_adapted", shape, d_model,
           ("h", "w", "a", "b", "alpha", "adapter", "pos", "page_table", "q_idx", "k_idx", "k_cache", "v_cache"),
           (h, w, a, b, alpha, adapter, pos, page_table, q_idx, k_idx, k_cache, v_cache), ws, stream,
-          a.shape[:2])
+          _adapter_sizes(a, b))
 
 
 def clsa_project_append8_adapted(shape, block, d_model, h, w, a, b, alpha, adapter, start, count, page_table,
@@ -373,7 +384,7 @@ def clsa_project_append8_adapted(shape, block, d_model, h, w, a, b, alpha, adapt
           ("h", "w", "a", "b", "alpha", "adapter", "start", "count", "page_table", "q_idx", "k_idx", "k8", "v8",
            "k_scale", "v_scale"),
           (h, w, a, b, alpha, adapter, start, count, page_table, q_idx, k_idx, k8, v8, k_scale, v_scale), ws,
-          stream, (d_model, *a.shape[:2]))
+          stream, (d_model, *_adapter_sizes(a, b)))
 
 
 def clsa_residual_norm(shape, d_model, eps, x, residual, weight, sum=None, y=None, y8=None, y_scale=None,

@@ -75,7 +75,7 @@ __global__ __launch_bounds__(256) void pages_fork_kernel(ForkArgs a) {
             if (up[j] < -1 || up[j] >= a.batch || up[j] == b) continue;
             const int old = s_old[i], from = up[j] < 0 ? -1 : s_old[up[j] * width + c];
             const bool held = from >= 0 && from < a.pages;
-            if (from >= a.pages || old >= a.pages) note_device_error(kDevErrPages);
+            if (from < -1 || from >= a.pages || old < -1 || old >= a.pages) note_device_error(kDevErrPages);
             const int now = held ? from : -1;
             if (now == old) continue;
             table[(size_t)b * a.max_pages + c] = now;

@@ -21,7 +21,7 @@ def fork(parent, table, lens, refs):
             l[b] = 0 if up < 0 else lens[up]
             for c in range(table.shape[1]):
                 old, new = int(table[b, c]), -1 if up < 0 else int(table[up, c])
-                bad |= old >= pages or new >= pages
+                bad |= not (-1 <= old < pages and -1 <= new < pages)
                 new = new if 0 <= new < pages else -1
                 if new == old:
                     continue

@@ -111,6 +111,18 @@ def test_fork(emu, batch, cols, bad, order):
     assert emu.emu_bits() == (PAGES if want[3] else 0)
 
 
+def test_fork_of_entries_below_none(emu):
+    """A negative entry other than -1 is no page, and is reported when its slot changes hands."""
+    table = np.array([[3, -5], [1, -1]], np.int32)
+    refs = P.holders(table, 6)
+    for parent, bits in (([0, 1], 0), ([0, 0], PAGES), ([-1, 1], PAGES)):
+        parent = np.array(parent, np.int32)
+        want = P.fork(parent, table, np.array([20, 5], np.int32), refs)
+        g = [Guarded(x) for x in (table, np.array([20, 5], np.int32), refs)]
+        assert emu.emu_fork(2, 2, 6, Guarded(parent).p, *(x.p for x in g), 0) == 0
+        assert all(np.array_equal(x.x, w) for x, w in zip(g, want)) and emu.emu_bits() == bits
+
+
 def _reserve(emu, rng, table, refs, start, count, n_q, page, order, tensors=True, max_len=None):
     batch, cols = table.shape
     max_len = cols * page if max_len is None else max_len

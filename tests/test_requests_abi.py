@@ -181,5 +181,10 @@ def test_binding_takes_gpu_tensors_only():
         B.clsa_pages_fork(_paged(), i, i, i, i)
     with pytest.raises(ValueError, match=r"tensors\[0\] must be a GPU tensor"):
         B.clsa_pages_reserve(_paged(), [x], i, i, i, i, i)
+    for a, b in ((x, x), (x[None], None), (x[None], x[None, :1]), (x[None], torch.zeros(2, 8, 2))):
+        with pytest.raises(ValueError, match="three dimensions|one rank"):
+            B.clsa_project_append_adapted(_shape(), 512, x, x, a, b, x, i, i, None, x, x, x, x)
+        with pytest.raises(ValueError, match="three dimensions|one rank"):
+            B.clsa_project_append8_adapted(_shape(), 64, 512, x, x, a, b, x, i, i, i, None, x, x, x, x, x, x)
     with pytest.raises(TypeError, match=r"tensors\[0\]"):
         B.clsa_pages_compact(_paged(), [None], i, i, i)
