@@ -225,66 +225,94 @@ constexpr int kGemmOutPitch = kGemmN + 8;    // bf16 per staged output row
 constexpr size_t gemm_lds(int rows) { return sizeof(uint16_t) * 2 * (rows + kGemmN) * kGemmPitch; }
 
 // kMixed: adds the adapters' part to a wave's 16 MT x 16 NT tile of the tiled product (c[mt][nt]:
-// rows r0 + 16 mt, features f0 + 16 nt).  A 32-wide product step holds 16 ranks twice, the high and
-// the low parts of u against the same B.  Rows of different sequences can share a 16-row
-// tile: the step is then made once for each adapter in it, Q adapters' loads in flight
-// together, and added to that adapter's rows only (a factor of zero would carry one
-// adapter's infinities to another's rows).
-template <int MT, int NT, int Q>
+// rows r0 + 16 mt, features f0 + 16 nt), 32 ranks a step, the high and then the low parts of
+// u against the same B.  Rows of different sequences can share a tile: its products are
+// then made once for each adapter in it and added to that adapter's rows only (a factor of
+// zero would carry one adapter's infinities to another's rows).  Q adapters' loads, J steps
+// of each, are in flight together.  What bounds it is the number of those loads, 16 lines each
+// (16 ranks twice in a step, as in the tiles of one sequence: twice as many of B, 200 tokens
+// of rank 128 with 64 adapters 161 us, XX).
+template <int MT, int NT, int Q, int J>
 __device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, f32x4 (&c)[MT][NT]) {
     const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
+    const bf16x8 none = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
     const uint16_t *halves = reinterpret_cast<const uint16_t *>(a.u);
     const int pitch = div_up(a.rank, 16) * 32;
     int mine[MT];
+    uint32_t left[MT], any = 0;  // rows whose adapter is still to come
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
         const int r = r0 + 16 * mt + col;
         mine[mt] = r < a.rows ? adapter_of(a, r / a.n_q) : -1;
+        left[mt] = (uint32_t)__ballot(mine[mt] >= 0) & 0xffffu;
+        any |= left[mt];
     }
-#pragma unroll 1
-    for (int j = 0; j < a.rank; j += 16) {
-        bf16x8 av[MT], bv[Q][NT];
+    while (any) {
+        int id[Q];
+        uint32_t same[Q][MT];  // rows of adapter q
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            av[mt] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
-            if (mine[mt] >= 0) av[mt] = ld8(halves + (size_t)(r0 + 16 * mt + col) * pitch + 2 * j + grp * 8);
+        for (int q = 0; q < Q; ++q) {
+            id[q] = -1;
+#pragma unroll
+            for (int mt = MT - 1; mt >= 0; --mt)
+                if (left[mt]) id[q] = __builtin_amdgcn_readlane(mine[mt], __builtin_ctz(left[mt]));
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                same[q][mt] = id[q] < 0 ? 0u : (uint32_t)__ballot(mine[mt] == id[q]) & 0xffffu;
+                left[mt] &= ~same[q][mt];
+            }
         }
-        const int ro = j + (grp & 1) * 8;
-        int held = -1;  // the adapter that bv[0] holds
+        any = 0;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            uint64_t todo = __ballot(mine[mt] >= 0) & 0xffffull;
-            while (todo) {
-                uint64_t same[Q];
+        for (int mt = 0; mt < MT; ++mt) any |= left[mt];
+#pragma unroll 1
+        for (int j0 = 0; j0 < a.rank; j0 += 32 * J) {
+            bf16x8 av[MT][J][2], bv[Q][J][NT];
 #pragma unroll
-                for (int q = 0; q < Q; ++q) {
-                    same[q] = 0;
-                    if (todo) {
-                        const int id = __builtin_amdgcn_readlane(mine[mt], __builtin_ctzll(todo));
-                        same[q] = __ballot(mine[mt] == id) & 0xffffull;
-                        todo &= ~same[q];
-                        if (q == 0 && id == held) continue;
-                        if (q == 0) held = id;
+            for (int q = 0; q < Q; ++q) {
+                if (id[q] < 0) break;
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            bv[q][nt] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
-                            if (ro < a.rank)
-                                bv[q][nt] = ld8(a.up + ((size_t)id * a.n_feat + f0 + 16 * nt + col) * a.rank + ro);
-                        }
-                    }
-                }
+                for (int nt = 0; nt < NT; ++nt) {
+                    const uint16_t *up = a.up + ((size_t)id[q] * a.n_feat + f0 + 16 * nt + col) * a.rank;
 #pragma unroll
-                for (int q = 0; q < Q; ++q) {
-                    if (!same[q]) break;
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        const f32x4 t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[mt], bv[q][nt], c[mt][nt], 0, 0, 0);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            c[mt][nt][e] = (same[q] >> (4 * grp + e)) & 1 ? t[e] : c[mt][nt][e];
+                    for (int j = 0; j < J; ++j) {
+                        const int ro = j0 + 32 * j + grp * 8;
+                        bv[q][j][nt] = none;
+                        if (ro < a.rank) bv[q][j][nt] = ld8(up + ro);
                     }
                 }
             }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    const int ro = j0 + 32 * j + grp * 8;
+                    const uint16_t *p = halves + (size_t)(r0 + 16 * mt + col) * pitch + 2 * (ro & ~15) + (ro & 8);
+                    av[mt][j][0] = av[mt][j][1] = none;
+                    if (mine[mt] >= 0 && ro < a.rank) {
+                        av[mt][j][0] = ld8(p);
+                        av[mt][j][1] = ld8(p + 16);
+                    }
+                }
+#pragma unroll
+            for (int q = 0; q < Q; ++q)
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    if (!same[q][mt]) continue;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        f32x4 t = c[mt][nt];
+#pragma unroll
+                        for (int j = 0; j < J; ++j)
+                            if (j0 + 32 * j < a.rank) {
+                                t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[mt][j][0], bv[q][j][nt], t, 0, 0, 0);
+                                t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[mt][j][1], bv[q][j][nt], t, 0, 0, 0);
+                            }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            c[mt][nt][e] = (same[q][mt] >> (4 * grp + e)) & 1 ? t[e] : c[mt][nt][e];
+                    }
+                }
         }
     }
 }
@@ -458,7 +486,8 @@ __global__ __launch_bounds__(64 * W, 2) void project_gemm_kernel(ProjArgs a) {
             step(h);
         }
     }
-    if (MODE == kMixed) adapter_tile<MT, NT, (MT * NT > 8 ? 2 : 4)>(a, r0 + wm * (BM / 2), f0 + wn * 16 * NT, c);
+    constexpr int QA = MT * NT > 4 ? 2 : 4, JA = NT > 2 ? 1 : 2;
+    if (MODE == kMixed) adapter_tile<MT, NT, QA, JA>(a, r0 + wm * (BM / 2), f0 + wn * 16 * NT, c);
     // bf16 results into LDS: C tile (mt, nt) row 4 grp + r, column col
     uint16_t(*s_out)[kGemmOutPitch] = reinterpret_cast<uint16_t(*)[kGemmOutPitch]>(s_lds);
     static_assert(gemm_lds(BM) >= sizeof(uint16_t) * BM * kGemmOutPitch, "output tile fits");
