@@ -231,7 +231,7 @@ constexpr size_t gemm_lds(int rows) { return sizeof(uint16_t) * 2 * (rows + kGem
 // zero would carry one adapter's infinities to another's rows).  Q adapters' loads, J steps
 // of each, are in flight together.  What bounds it is the number of those loads, 16 lines each
 // (16 ranks twice in a step, as in the tiles of one sequence: twice as many of B, 200 tokens
-// of rank 128 with 64 adapters 161 us, XX).
+// of rank 128 with 64 adapters 161 us against 115; 80 with tiles of 32 rows).
 template <int MT, int NT, int Q, int J>
 __device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, f32x4 (&c)[MT][NT]) {
     const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
@@ -753,14 +753,16 @@ static hipError_t launch_project_args(const Geometry &g, int d_model, ProjArgs a
     a.ftiles = n_feat / kGemmN;
     // Adapters: row tiles of one sequence each where that pads the rows by half at most (30
     // sequences of 150 rows x 2560 features: 137 us, 98 shared), or where the tiles are no
-    // more than the CUs; else tiles that sequences share.
-    // Tiles of 64 rows where those are no more than the CUs (512 rows x 2560 features,
-    // d_model 2560: 30 us against 36 with 128; 1024 rows 41 against 38).
+    // more than the CUs; else tiles that sequences share.  Tiles of 32 or 64 rows where
+    // those are no more than the CUs (512 rows x 2560 features, d_model 2560: 30 us with 64, 36
+    // with 128; 1024 rows 41 and 38; 200 rows 23.5 with 32, 24.5 with 64).
     auto own_tiles = [&](int rows) { return (int64_t)g.batch * div_up(g.n_q, rows); };
     const bool own = ADAPTED && (own_tiles(kGemmM) * kGemmM * 2 <= (int64_t)g.rows * 3 ||
                                  own_tiles(kGemmM) * a.ftiles <= 256);
     int bm = kGemmM;
-    if (ADAPTED && (own ? own_tiles(kGemmM / 2) : div_up(g.rows, kGemmM / 2)) * a.ftiles <= 256) bm = kGemmM / 2;
+    if (ADAPTED)
+        for (int rows : {64, 32})
+            if ((own ? own_tiles(rows) : div_up(g.rows, rows)) * a.ftiles <= 256) bm = rows;
     a.seq_tiles = div_up(g.n_q, bm);
     const int64_t rtiles = own ? own_tiles(bm) : div_up(g.rows, bm);
     if (rtiles > 0xffffff) return hipErrorInvalidConfiguration;
@@ -774,19 +776,22 @@ static hipError_t launch_project_args(const Geometry &g, int d_model, ProjArgs a
                                : div_up(a.rtiles * a.ftiles, 8) * 8L;
     if (blocks > 0x7fffffL) return hipErrorInvalidConfiguration;  // 2^32 threads a launch
     const dim3 grid((unsigned)blocks);
-    // (tiles of 64 rows are no more than the CUs, so that their workgroups are not either)
-    const int waves = ADAPTED && (bm == 64 || blocks <= kWideGemmBlocks) ? 8 : 4;
+    // (tiles of 64 rows are no more than the CUs, so that their workgroups are not either; 32 rows
+    // have too little work for eight waves)
+    const int waves = ADAPTED && bm > 32 && (bm == 64 || blocks <= kWideGemmBlocks) ? 8 : 4;
     using Kernel = void (*)(ProjArgs);
     Kernel fn;
 #define CLSA_GEMM(MODE, BM, W) fn = paged ? project_gemm_kernel<true, MODE, BM, W> : project_gemm_kernel<false, MODE, BM, W>
     if constexpr (!ADAPTED) {
         CLSA_GEMM(kPlain, 128, 4);
     } else if (own) {
-        if (bm == 64) CLSA_GEMM(kOwnTiles, 64, 8);
+        if (bm == 32) CLSA_GEMM(kOwnTiles, 32, 4);
+        else if (bm == 64) CLSA_GEMM(kOwnTiles, 64, 8);
         else if (waves == 8) CLSA_GEMM(kOwnTiles, 128, 8);
         else CLSA_GEMM(kOwnTiles, 128, 4);
     } else {
-        if (bm == 64) CLSA_GEMM(kMixed, 64, 8);
+        if (bm == 32) CLSA_GEMM(kMixed, 32, 4);
+        else if (bm == 64) CLSA_GEMM(kMixed, 64, 8);
         else if (waves == 8) CLSA_GEMM(kMixed, 128, 8);
         else CLSA_GEMM(kMixed, 128, 4);
     }

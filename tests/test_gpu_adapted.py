@@ -112,8 +112,8 @@ CASES = [  # batch, n_q, d_model, rank, adapters, page
     (1, 1, 512, 8, 1, 0), (5, 1, 2560, 16, 3, 16), (32, 1, 2560, 16, 40, 16), (33, 1, 1024, 64, 5, 0), (70, 1, 4096, 8, 9, 16),
     (128, 1, 512, 128, 130, 0), (200, 1, 512, 16, 11, 16), (3, 5, 1536, 24, 2, 0), (300, 2, 512, 40, 250, 0),
     (7, 37, 512, 16, 3, 16), (1, 300, 2560, 16, 2, 0), (9, 33, 1024, 128, 9, 16), (2, 100, 512, 8, 2, 0), (4, 64, 3584, 56, 3, 0),
-    # each form of the tiled product: 128-row tiles of one sequence and shared ones, by four and eight waves
-    (1, 2100, 512, 24, 2, 16), (1, 4200, 512, 16, 2, 0), (1, 8300, 512, 40, 1, 16), (2100, 1, 512, 8, 7, 0),
+    # each form of the tiled product: 64- and 128-row tiles of one sequence and shared ones, by four and eight waves
+    (1, 1500, 512, 24, 2, 16), (1500, 1, 512, 40, 50, 0), (250, 5, 512, 128, 9, 16), (1, 2100, 512, 24, 2, 16), (1, 4200, 512, 16, 2, 0), (1, 8300, 512, 40, 1, 16), (2100, 1, 512, 8, 7, 0),
     (700, 6, 512, 24, 60, 16), (30, 150, 512, 72, 4, 16)]
 
 
