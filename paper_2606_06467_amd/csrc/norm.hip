@@ -56,19 +56,57 @@ __device__ __forceinline__ void st16(uint16_t *p, uint4 v) {
     else *reinterpret_cast<uint4 *>(p) = v;
 }
 
-// Sum (or largest) of a row's values: over the wave, then over the workgroup's waves
-// where they share the row.
+// Exchanges of 4- or 8-byte values without the LDS crossbar: inside a row of 16 lanes by DPP
+// (device_common.h), across rows by the permlane swaps, which leave both lanes of a pair with
+// the pair's two values, the lower lane's first.
+template <int CTRL, class T>
+__device__ __forceinline__ T dpp_of(T v) {
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, false));
+    } else {
+        const uint2 w = __builtin_bit_cast(uint2, v);
+        return __builtin_bit_cast(T, make_uint2((uint32_t)__builtin_amdgcn_mov_dpp((int)w.x, CTRL, 0xf, 0xf, false),
+                                                (uint32_t)__builtin_amdgcn_mov_dpp((int)w.y, CTRL, 0xf, 0xf, false)));
+    }
+}
+template <bool HALVES, class T, class F>
+__device__ __forceinline__ T across_rows(T v, F f) {
+    auto swap = [](uint32_t x) {
+        if constexpr (HALVES) return __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        else return __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    };
+    if constexpr (sizeof(T) == 4) {
+        const auto r = swap(__builtin_bit_cast(uint32_t, v));
+        const uint32_t x = r[0], y = r[1];
+        return f(__builtin_bit_cast(T, x), __builtin_bit_cast(T, y));
+    } else {
+        const uint2 w = __builtin_bit_cast(uint2, v);
+        const auto lo = swap(w.x), hi = swap(w.y);
+        return f(__builtin_bit_cast(T, make_uint2(lo[0], hi[0])), __builtin_bit_cast(T, make_uint2(lo[1], hi[1])));
+    }
+}
+// Over the 16 lanes of a row: mirrored, mirrored in halves, then by quads.
+template <class T, class F>
+__device__ __forceinline__ T over_row(T v, F f) {
+    v = f(v, dpp_of<0x140>(v));
+    v = f(v, dpp_of<0x141>(v));
+    v = f(v, dpp_of<0x4E>(v));
+    return f(v, dpp_of<0xB1>(v));
+}
+
+// Sum (or largest; zero changes neither) of a row's values: over the wave, then over the
+// workgroup's waves where they share the row (a lane of 16 takes each wave's).
 template <bool WAVE, class T, class F>
 __device__ __forceinline__ T row_reduce(T v, T *s, F f) {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) v = f(v, __shfl_xor(v, m));
+    v = over_row(v, f);
+    v = across_rows<false>(v, f);
+    v = across_rows<true>(v, f);
     if (WAVE) return v;
-    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 15;
     if ((threadIdx.x & 63) == 0) s[wave] = v;
     __syncthreads();
-    v = s[0];
-    for (int w = 1; w < waves; ++w) v = f(v, s[w]);
-    return v;
+    v = lane < (int)(blockDim.x >> 6) ? s[lane] : T(0);
+    return over_row(v, f);
 }
 
 // One workgroup = one row, P pieces a thread.
