@@ -229,32 +229,48 @@ __device__ __forceinline__ uint4 grad_piece(uint4 v, uint4 y, uint4 w, uint4 u, 
     return pack8(f);
 }
 
-// Few rows in one launch: a workgroup for each row's dx, and behind those one for every 64
-// columns of dw, which reads its columns of dy and s again (from the caches) instead of waiting
-// for sums from the others.
+// Few rows in one launch: a workgroup for every 64 columns of dw, which reads its columns of dy
+// and s with four rows in flight, and behind those, as they are shorter, one for each row's dx.
+// The inputs are read twice, from the caches, so that no workgroup waits for another's sums.
 template <int P>
 __global__ __launch_bounds__(1024) void norm_grad_few_kernel(NormGradArgs a) {
     __shared__ float s_sum[16];
     __shared__ float s_col[128][64 + 1];
     const int t = threadIdx.x, width = blockDim.x;
-    if ((int)blockIdx.x >= a.rows) {
-        const int col = ((int)blockIdx.x - a.rows) * 64 + (t & 7) * 8, groups = width >> 3;
+    const int row = (int)blockIdx.x - (a.d + 63) / 64;
+    if (row < 0) {
+        const int col = (int)blockIdx.x * 64 + (t & 7) * 8, groups = width >> 3;
         float dw[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (col < a.d) {
-#pragma unroll 4
-            for (int row = t >> 3; row < a.rows; row += groups) {
-                float f[8], g[8];
-                unpack8(ld16(a.s + (size_t)row * a.d + col), f);
-                unpack8(ld16(a.dy + (size_t)row * a.d + col), g);
-                const float rstd = a.rstd[row];
+            constexpr int N = 4;  // rows in flight
+            for (int first = t >> 3; first < a.rows; first += N * groups) {
+                uint4 v[N], y[N];
+                float r[N];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) dw[e] += g[e] * (f[e] * rstd);
+                for (int j = 0; j < N; ++j) {
+                    const int k = first + j * groups;
+                    v[j] = y[j] = make_uint4(0u, 0u, 0u, 0u);
+                    r[j] = 0.0f;
+                    if (k < a.rows) {
+                        v[j] = ld16(a.s + (size_t)k * a.d + col);
+                        y[j] = ld16(a.dy + (size_t)k * a.d + col);
+                        r[j] = a.rstd[k];
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    float f[8], g[8];
+                    unpack8(v[j], f);
+                    unpack8(y[j], g);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) dw[e] += g[e] * (f[e] * r[j]);
+                }
             }
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) s_col[t >> 3][(t & 7) * 8 + e] = dw[e];
         __syncthreads();
-        const int c = ((int)blockIdx.x - a.rows) * 64 + t;
+        const int c = (int)blockIdx.x * 64 + t;
         if (t < 64 && c < a.d) {
             float sum = s_col[0][t];
             for (int k = 1; k < groups; ++k) sum += s_col[k][t];
@@ -262,7 +278,7 @@ __global__ __launch_bounds__(1024) void norm_grad_few_kernel(NormGradArgs a) {
         }
         return;
     }
-    const size_t at = (size_t)blockIdx.x * a.d;
+    const size_t at = (size_t)row * a.d;
     uint4 v[P], y[P], u[P], w[P];
 #pragma unroll
     for (int i = 0; i < P; ++i) {
@@ -275,7 +291,7 @@ __global__ __launch_bounds__(1024) void norm_grad_few_kernel(NormGradArgs a) {
             if (a.dsum) u[i] = ld16(a.dsum + at + 8 * p);
         }
     }
-    const float rstd = a.rstd[blockIdx.x];
+    const float rstd = a.rstd[row];
     float dot = 0.0f;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
@@ -439,6 +455,11 @@ bool norm_supported(int d) { return d >= 8 && d <= kNormMaxDim && d % 8 == 0; }
 
 static bool streamed(int rows, int d) { return (size_t)rows * d >= kNormStreamed; }
 
+// Below it (and with dx apart from dy and s) the backward pass is one launch; one / two launches:
+// 77 rows of 2560 2.7 / 6.3 us, 768 rows of 512 5.4 / 7.2, 2560 8.4 / 11.2, 8192 14.5 / 18.0;
+// 1024 rows of 512 7.5 / 5.8, 2560 12.6 / 11.9, 8192 18.5 / 24.6.
+constexpr int kGradFewRows = 768;
+
 static int threads_of(int pieces, int per) { return div_up(pieces, 64 * per) * 64; }
 
 static bool grad_by_wave(int rows, int pieces) { return rows >= kNormManyRows && pieces <= kGradWavePieces; }
@@ -524,12 +545,12 @@ hipError_t launch_norm_grad(int rows, int d, const void *s, const float *rstd, c
     a.d = d;
     a.pieces = d / 8;
     a.parts = norm_grad_parts(rows, d);
-    // One launch where a column's threads have at most eight rows each (256 rows of 2560: 6.9 us
-    // against 7.4 with two; 512 rows 13.6 / 11.0, of 5120 8.1 / 14.7; 77 rows of 1000 2.8 / 6.0)
+    // One launch up to kGradFewRows; above 256 rows 512 threads at least, for the columns' sake
+    // (64 rows of 2560: 2.7 us with 320 threads, 2.9 with 512; 512 rows 7.1 / 6.5)
     const int per = a.pieces <= 512 ? 1 : 2, row_threads = threads_of(a.pieces, per);
-    const int threads = row_threads < 256 ? 256 : row_threads;
-    if (rows <= threads && !overlaps(dx, dy, rows, d) && !overlaps(dx, s, rows, d)) {
-        const dim3 grid(rows + div_up(d, 64)), wg(threads);
+    const int least = rows <= 256 ? 256 : 512, threads = row_threads < least ? least : row_threads;
+    if (rows <= kGradFewRows && !overlaps(dx, dy, rows, d) && !overlaps(dx, s, rows, d)) {
+        const dim3 grid(div_up(d, 64) + rows), wg(threads);
         if (per == 1) norm_grad_few_kernel<1><<<grid, wg, 0, stream>>>(a);
         else norm_grad_few_kernel<2><<<grid, wg, 0, stream>>>(a);
         return hipGetLastError();

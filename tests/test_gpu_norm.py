@@ -16,7 +16,7 @@ U24 = 2.0 ** -24
 EPS = 1e-6
 FORMS = [(1, 8), (1, 2560), (3, 72), (5, 1000), (77, 8200), (2, 16384), (256, 16), (257, 16), (320, 2560), (321, 2560), (1500, 520), (1030, 2560), (1100, 4096),
          (1029, 4104), (2050, 8), (1027, 3592),
-         (1030, 1544), (4100, 2080), (1100, 8008), (17000, 512)]
+         (768, 5120), (769, 1000), (600, 8), (1030, 1544), (4100, 2080), (1100, 8008), (17000, 512)]
 
 
 def f32(bits):
