@@ -18,7 +18,7 @@
 //     partial tiles are added in LDS: the weights (13 MB at d_model 2560, the
 //     bytes that bound this case) are then read by 160 workgroups at once.
 //     Models wider than 3072 had gone to the tiled product, 20 workgroups that
-//     walk d_model alone: 16 rows, d_model 4096 37 us, now 10; 8192 70, now 17;
+//     walk d_model alone: 16 rows, d_model 4096 37 us, now 5.9; 8192 70, now 9.9;
 //   * many rows (prefill): a tiled product, 128 rows x 128 features per
 //     workgroup of 4 waves (64 x 64 each, 4 x 4 tiles of 16 x 16), d_model in
 //     steps of 64 staged through LDS (double-buffered: the next step's global
@@ -35,8 +35,9 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kSplitWaves = 8;     // d_model split of the few-rows kernel
 // Rows up to which the weights' bytes bound the product.  Against the tiled
-// product (2560 features): 96 rows, d_model 2560 15.8 us against 28.4; 128 rows 22.2
-// against 30.1, d_model 4096 33.9 against 42.6; 192 rows, 4096 44.7 against 41.5.
+// product (2560 features): 128 rows, d_model 2560 10.0 us against 28.4, d_model 4096 15.5 against
+// 41.3.  It would be ahead for some more (192 rows, 4096: 18.8 / 40.7; 384 rows 33.9 / 41.6);
+// those keep the tiled product and with it the order of their sums.
 constexpr int kSplitMaxRows = 128;
 
 struct ProjArgs {
@@ -75,6 +76,12 @@ __device__ __forceinline__ int adapter_of(const ProjArgs &a, int b) {
 
 __device__ __forceinline__ bf16x8 ld8(const uint16_t *p) {
     return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(p));
+}
+
+__device__ __forceinline__ u32x4 ld_piece(const uint16_t *p) { return *reinterpret_cast<const u32x4 *>(p); }
+
+__device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
 // Position of row r of sequence b, negative for a row that has none.
@@ -161,39 +168,75 @@ struct AdapterDot {
     }
 };
 
+// Operand tiles of a matrix product (16 rows x 32 values) loaded straight from memory.  The
+// product wants row lane & 15 in each lane, so that 16 neighbouring lanes would ask for 16
+// lines.  Loaded are four neighbouring lanes a row (lane >> 2) instead, and a wave hands the
+// pieces over through its own LDS, where its accesses stay in order: no workgroup barrier.
+// Piece p of a row r lies at p ^ (r >> 2), so that reads fall on all banks once.
+struct OperandTurn {
+    static constexpr int kTiles = 3;  // at a time
+    u32x4 *put;
+    const u32x4 *get;
+    __device__ __forceinline__ OperandTurn(u32x4 (&own)[kTiles][64], int lane)
+        : put(own[0] + lane), get(own[0] + (lane & 15) * 4 + ((lane >> 4) ^ ((lane >> 2) & 3))) {}
+    static __device__ __forceinline__ int row(int lane) { return lane >> 2; }
+    static __device__ __forceinline__ int piece(int lane) { return (lane & 3) ^ (lane >> 4); }
+    static __device__ __forceinline__ void fence() {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+    template <int N>
+    __device__ __forceinline__ void operator()(u32x4 (&v)[N]) const {
+#pragma unroll
+        for (int i0 = 0; i0 < N; i0 += kTiles) {
+#pragma unroll
+            for (int i = i0; i < N && i < i0 + kTiles; ++i) put[64 * (i - i0)] = v[i];
+            fence();
+#pragma unroll
+            for (int i = i0; i < N && i < i0 + kTiles; ++i) v[i] = get[64 * (i - i0)];
+            fence();
+        }
+    }
+};
+
 // Few rows: one 16 RT-row x 16-feature tile per workgroup, d_model split over 8
 // waves of NB * KS 32-dim steps each (d_model = 256 * NB * KS), KS at a time.
 // RT = 2: a weight is read once for 32 rows (launch_splitk: when).
 template <int KS, int NB, int RT, bool PAGED, bool ADAPTED>
 __global__ __launch_bounds__(512) void project_splitk_kernel(ProjArgs a) {
     __shared__ float part[kSplitWaves][16 * RT][16 + 1];
+    __shared__ u32x4 s_turn[kSplitWaves][OperandTurn::kTiles][64];
     const int ft = blockIdx.x, rt = blockIdx.y;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int col = lane & 15, grp = lane >> 4;
-    const int k0 = wave * NB * KS * 32 + grp * 8;
+    const OperandTurn turn(s_turn[wave], lane);
+    const int k0 = wave * NB * KS * 32 + turn.piece(lane) * 8;
     const uint16_t *hp[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t)
-        hp[t] = a.h + (size_t)min((rt * RT + t) * 16 + col, a.rows - 1) * a.d + k0;
-    const uint16_t *wp = a.w + (size_t)(ft * 16 + col) * a.d + k0;
+        hp[t] = a.h + (size_t)min((rt * RT + t) * 16 + turn.row(lane), a.rows - 1) * a.d + k0;
+    const uint16_t *wp = a.w + (size_t)(ft * 16 + turn.row(lane)) * a.d + k0;
     f32x4 c[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) c[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-        bf16x8 av[RT][KS], bv[KS];
+        u32x4 v[KS][RT + 1];  // rows of h, then features
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-            bv[s] = ld8(wp + (nb * KS + s) * 32);
+            v[s][RT] = ld_piece(wp + (nb * KS + s) * 32);
 #pragma unroll
-            for (int t = 0; t < RT; ++t) av[t][s] = ld8(hp[t] + (nb * KS + s) * 32);
+            for (int t = 0; t < RT; ++t) v[s][t] = ld_piece(hp[t] + (nb * KS + s) * 32);
         }
         __builtin_amdgcn_sched_barrier(0);  // every load in flight before the first product
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
+        for (int s = 0; s <= KS; ++s) {
+            if (s < KS) turn(v[s]);
+            if (s == 0) continue;
 #pragma unroll
-            for (int t = 0; t < RT; ++t)
-                c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[t][s], bv[s], c[t], 0, 0, 0);
+            for (int t = 0; t < RT; ++t)  // one step behind, while the next one's pieces are handed over
+                c[t] = mfma(v[s - 1][t], v[s - 1][RT], c[t]);
+        }
     }
     AdapterDot dot;
     if (ADAPTED && threadIdx.x < 256 * RT)
@@ -551,53 +594,51 @@ __device__ __forceinline__ void adapter_halves(float u, uint16_t *p) {
 // ranks, d_model split over 8 waves whose parts meet in LDS, 32 ranks at a time.  Where there
 // are rows enough, all ranks: h is then read once, which bounds it, and A comes from the
 // caches (8192 rows, d_model 2560, rank 128: 30 us; 41 with a workgroup for each 32 ranks).
-// Few rows take 32 ranks a workgroup (1505 rows, d_model 4096, rank 64: 14 us, 21 with all).
+// Few rows take 32 ranks a workgroup (1505 rows, d_model 4096, rank 64: 10.6 us).
 template <int RT, int NT>
 __global__ __launch_bounds__(512) void adapter_down_tile_kernel(ProjArgs a) {
     constexpr int S = NT > 4 ? 2 : RT + NT > 3 ? 4 : 8;  // 32-wide steps whose loads are in flight together
     constexpr int J = NT > 2 ? 2 : NT;     // rank tiles that meet in LDS at a time
     __shared__ float part[kSplitWaves][16 * RT][16 * J + 1];
+    __shared__ u32x4 s_turn[kSplitWaves][OperandTurn::kTiles][64];
     const int tiles = div_up(a.n_q, 16 * RT), b = blockIdx.x / tiles, t0 = (blockIdx.x % tiles) * 16 * RT;
     const int id = adapter_of(a, b);
     if (id < 0) return;  // uniform
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int col = lane & 15, grp = lane >> 4, steps = a.d / 256;
     const int ranks = div_up(a.rank, 16) * 16, j0 = blockIdx.y * 16 * NT;
-    const uint16_t *hp[RT], *ap[NT];
+    const OperandTurn turn(s_turn[wave], lane);
+    const int k0 = wave * steps * 32 + turn.piece(lane) * 8;
+    const uint16_t *p[RT + NT];  // rows of h, then ranks
 #pragma unroll
     for (int m = 0; m < RT; ++m)
-        hp[m] = a.h + ((size_t)b * a.n_q + min(t0 + 16 * m + col, a.n_q - 1)) * a.d + wave * steps * 32 + grp * 8;
+        p[m] = a.h + ((size_t)b * a.n_q + min(t0 + 16 * m + turn.row(lane), a.n_q - 1)) * a.d + k0;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
-        ap[n] = a.down + ((size_t)id * a.rank + min(j0 + 16 * n + col, a.rank - 1)) * a.d + wave * steps * 32 + grp * 8;
+        p[RT + n] = a.down + ((size_t)id * a.rank + min(j0 + 16 * n + turn.row(lane), a.rank - 1)) * a.d + k0;
     f32x4 c[RT][NT];
 #pragma unroll
     for (int m = 0; m < RT; ++m)
 #pragma unroll
         for (int n = 0; n < NT; ++n) c[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int s0 = 0; s0 < steps; s0 += S) {
-        bf16x8 av[S][RT], bv[S][NT];
-#pragma unroll
-        for (int s = 0; s < S; ++s) {
-            const bool in = s0 + s < steps;  // uniform
-#pragma unroll
-            for (int m = 0; m < RT; ++m) {
-                av[s][m] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
-                if (in) av[s][m] = ld8(hp[m] + (s0 + s) * 32);
-            }
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                bv[s][n] = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
-                if (in) bv[s][n] = ld8(ap[n] + (s0 + s) * 32);
-            }
-        }
+        u32x4 v[S][RT + NT];
 #pragma unroll
         for (int s = 0; s < S; ++s)
 #pragma unroll
+            for (int i = 0; i < RT + NT; ++i) {
+                v[s][i] = u32x4{0u, 0u, 0u, 0u};
+                if (s0 + s < steps) v[s][i] = ld_piece(p[i] + (s0 + s) * 32);  // uniform
+            }
+#pragma unroll
+        for (int s = 0; s <= S; ++s) {
+            if (s < S) turn(v[s]);
+            if (s == 0) continue;
+#pragma unroll
             for (int m = 0; m < RT; ++m)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-                    c[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[s][m], bv[s][n], c[m][n], 0, 0, 0);
+                for (int n = 0; n < NT; ++n) c[m][n] = mfma(v[s - 1][m], v[s - 1][RT + n], c[m][n]);
+        }
     }
     uint16_t *halves = reinterpret_cast<uint16_t *>(a.u);
     const float alpha = a.alpha[id];
@@ -680,11 +721,11 @@ static hipError_t launch_adapter_down(const ProjArgs &a, int batch, hipStream_t 
 template <int KS, int NB = 1, bool ADAPTED = false>
 static void launch_splitk(const ProjArgs &a, bool paged, int n_feat, hipStream_t stream) {
     // 32 rows a workgroup where 16 would not fit the chip in one round but 32 do
-    // (32 rows x 2560 features, d_model 2560: 9.1 us against 11.3; 4096: 13.2 against
-    // 16.5), and from 65 rows on; 32 rows x 1536 features fit with 16 (9.3 against 12.8
-    // at 4096), 48 x 2560 fit with neither (11.3 against 13.9)
+    // (32 rows x 2560 features, d_model 2560: 5.3 us against 5.6; 4096: 7.5 against
+    // 8.3; 8192 12.4 against 15.7), and from 65 rows on; 32 rows x 1024 features fit with 16
+    // (5.2 against 6.7 at 4096), 48 x 2560 fit with neither (9.1 against 10.7)
     const int tiles = n_feat / 16;
-    // (adapted: from 49 on, 64 rows, d_model 2560, rank 16 20.7 us against 23.7)
+    // (adapted: from 49 on, 64 rows, d_model 2560, rank 16 10.9 us against 11.8)
     const bool two = tiles * div_up(a.rows, 16) > 256 &&
                      (tiles * div_up(a.rows, 32) <= 256 || a.rows > (ADAPTED ? 48 : 64));
     const dim3 grid(tiles, div_up(a.rows, two ? 32 : 16)), block(512);
