@@ -272,13 +272,19 @@ constexpr size_t gemm_lds(int rows) { return sizeof(uint16_t) * 2 * (rows + kGem
 // u against the same B.  Rows of different sequences can share a tile: its products are
 // then made once for each adapter in it and added to that adapter's rows only (a factor of
 // zero would carry one adapter's infinities to another's rows).  Q adapters' loads, J steps
-// of each, are in flight together.  What bounds it is the number of those loads, 16 lines each
-// (16 ranks twice in a step, as in the tiles of one sequence: twice as many of B, 200 tokens
-// of rank 128 with 64 adapters 161 us against 115; 80 with tiles of 32 rows).
+// of each, are in flight together.  What bounds it is the number of those loads (16
+// ranks twice in a step, as in the tiles of one sequence, and so twice as many of B: 200 tokens
+// of rank 128 with 64 adapters 161 us against 115; 73 with tiles of 32 rows).  From 64 ranks on
+// neighbouring rows lie in different lines and the pieces are turned (1200 rows of 64 ranks, 64
+// adapters 71.5 / 58.5 us; of 48 ranks 54.0 / 57.1, of 16 45.4 / 49.1).
 template <int MT, int NT, int Q, int J>
-__device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, f32x4 (&c)[MT][NT]) {
+__device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, f32x4 (&c)[MT][NT],
+                                             u32x4 (&own)[OperandTurn::kTiles][64]) {
     const int lane = threadIdx.x & 63, col = lane & 15, grp = lane >> 4;
-    const bf16x8 none = __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u});
+    const OperandTurn turn(own, lane);
+    const bool turned = a.rank >= 64;  // uniform
+    const int row = turned ? turn.row(lane) : col, piece = turned ? turn.piece(lane) : grp;
+    const u32x4 none{0u, 0u, 0u, 0u};
     const uint16_t *halves = reinterpret_cast<const uint16_t *>(a.u);
     const int pitch = div_up(a.rank, 16) * 32;
     int mine[MT];
@@ -310,18 +316,18 @@ __device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, 
         for (int mt = 0; mt < MT; ++mt) any |= left[mt];
 #pragma unroll 1
         for (int j0 = 0; j0 < a.rank; j0 += 32 * J) {
-            bf16x8 av[MT][J][2], bv[Q][J][NT];
+            u32x4 av[MT][J][2], bv[Q][J][NT];
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
                 if (id[q] < 0) break;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    const uint16_t *up = a.up + ((size_t)id[q] * a.n_feat + f0 + 16 * nt + col) * a.rank;
+                    const uint16_t *up = a.up + ((size_t)id[q] * a.n_feat + f0 + 16 * nt + row) * a.rank;
 #pragma unroll
                     for (int j = 0; j < J; ++j) {
-                        const int ro = j0 + 32 * j + grp * 8;
+                        const int ro = j0 + 32 * j + piece * 8;
                         bv[q][j][nt] = none;
-                        if (ro < a.rank) bv[q][j][nt] = ld8(up + ro);
+                        if (ro < a.rank) bv[q][j][nt] = ld_piece(up + ro);
                     }
                 }
             }
@@ -329,14 +335,27 @@ __device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, 
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
-                    const int ro = j0 + 32 * j + grp * 8;
-                    const uint16_t *p = halves + (size_t)(r0 + 16 * mt + col) * pitch + 2 * (ro & ~15) + (ro & 8);
+                    const int ro = j0 + 32 * j + piece * 8;
+                    const int r = r0 + 16 * mt + row;
+                    const uint16_t *p = halves + (size_t)r * pitch + 2 * (ro & ~15) + (ro & 8);
                     av[mt][j][0] = av[mt][j][1] = none;
-                    if (mine[mt] >= 0 && ro < a.rank) {
-                        av[mt][j][0] = ld8(p);
-                        av[mt][j][1] = ld8(p + 16);
+                    if (r < a.rows && ro < a.rank) {  // (rows without an adapter: as the workspace was)
+                        av[mt][j][0] = ld_piece(p);
+                        av[mt][j][1] = ld_piece(p + 16);
                     }
                 }
+            if (turned) {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int j = 0; j < J; ++j) turn(av[mt][j]);
+#pragma unroll
+                for (int q = 0; q < Q; ++q) {
+                    if (id[q] < 0) break;
+#pragma unroll
+                    for (int j = 0; j < J; ++j) turn(bv[q][j]);
+                }
+            }
 #pragma unroll
             for (int q = 0; q < Q; ++q)
 #pragma unroll
@@ -348,8 +367,8 @@ __device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, 
 #pragma unroll
                         for (int j = 0; j < J; ++j)
                             if (j0 + 32 * j < a.rank) {
-                                t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[mt][j][0], bv[q][j][nt], t, 0, 0, 0);
-                                t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[mt][j][1], bv[q][j][nt], t, 0, 0, 0);
+                                t = mfma(av[mt][j][0], bv[q][j][nt], t);
+                                t = mfma(av[mt][j][1], bv[q][j][nt], t);
                             }
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
@@ -530,7 +549,12 @@ __global__ __launch_bounds__(64 * W, 2) void project_gemm_kernel(ProjArgs a) {
         }
     }
     constexpr int QA = MT * NT > 4 ? 2 : 4, JA = NT > 2 ? 1 : 2;
-    if (MODE == kMixed) adapter_tile<MT, NT, QA, JA>(a, r0 + wm * (BM / 2), f0 + wn * 16 * NT, c);
+    if (MODE == kMixed) {
+        u32x4(*turn)[OperandTurn::kTiles][64] = reinterpret_cast<u32x4(*)[OperandTurn::kTiles][64]>(s_lds);
+        static_assert(gemm_lds(BM) >= sizeof(*turn) * W, "a wave's pieces fit");
+        adapter_tile<MT, NT, QA, JA>(a, r0 + wm * (BM / 2), f0 + wn * 16 * NT, c, turn[wave]);
+        __syncthreads();
+    }
     // bf16 results into LDS: C tile (mt, nt) row 4 grp + r, column col
     uint16_t(*s_out)[kGemmOutPitch] = reinterpret_cast<uint16_t(*)[kGemmOutPitch]>(s_lds);
     static_assert(gemm_lds(BM) >= sizeof(uint16_t) * BM * kGemmOutPitch, "output tile fits");
