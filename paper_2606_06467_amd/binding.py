@@ -277,29 +277,35 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _stream_object)
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
+# As functions: a call of a method is a third slower, and these three are most of a call's time here.
+_get_device, _is_contiguous, _data_ptr = _Tensor.get_device, _Tensor.is_contiguous, _Tensor.data_ptr
+
+
 def _call(where, shape, block, names, tensors, ws, stream, sizes=(), device=-1):
     """An entry point of the 8-bit cache or of what came after it: numbers after the block (or
     d_model, or the pool's pages), its tensors and their names, and its workspace (False: it takes
     none).  The call runs on the tensors' device (that of tensors among the numbers: device); their
     stream is the current one of that device unless one is given."""
     args, given = [*sizes], device
-    for i, t in enumerate(tensors):
-        if t is None:
-            args.append(None)
-            continue
-        try:
-            at = t.get_device()
-        except AttributeError:  # no tensor
-            _refuse(names[i], t)
-        if at < 0 or not t.is_contiguous() or at != device:
-            if device >= 0 or at < 0 or not t.is_contiguous():
-                _refuse(names[i], t)
-            device = at
-        args.append(t.data_ptr())
+    append = args.append
+    try:
+        for t in tensors:
+            if t is None:
+                append(None)
+            elif _get_device(t) == device >= 0 and _is_contiguous(t):
+                append(_data_ptr(t))
+            else:
+                at = _get_device(t)
+                if device >= 0 or at < 0 or not _is_contiguous(t):
+                    _refuse(names[len(args) - len(sizes)], t)
+                device = at
+                append(_data_ptr(t))
+    except TypeError:  # no tensor
+        _refuse(names[len(args) - len(sizes)], t)
     if isinstance(ws, _Tensor):
         if ws.get_device() != device or device < 0 or not ws.is_contiguous():
             _refuse("ws", ws)
-        args += ws.data_ptr(), ws.numel() * ws.element_size()
+        args += ws.data_ptr(), ws.nbytes
     elif ws is None:
         args += None, 0
     if device >= 0 and device != _current_device():
@@ -407,13 +413,13 @@ def _paged(tensors, pages):
     for i, t in enumerate(tensors):
         if not isinstance(t, _Tensor):
             raise TypeError(f"tensors[{i}] must be a torch.Tensor")
-        at = t.get_device()
-        if at < 0 or not t.is_contiguous() or (at != device and device >= 0):
+        at = _get_device(t)
+        if at < 0 or not _is_contiguous(t) or (at != device and device >= 0):
             _refuse(f"tensors[{i}]", t)
-        if t.dim() < 1 or t.shape[0] != pages:
+        if t.dim() < 1 or t.size(0) != pages:
             raise ValueError(f"tensors[{i}] must have one row for each of the {pages} pages of refs")
         device = at
-        fields.append(t.data_ptr())
+        fields.append(_data_ptr(t))
         fields.append(t.nbytes // pages)
     return fields, (len(tensors), fields.buffer_info()[0]), device
 
