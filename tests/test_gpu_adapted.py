@@ -189,6 +189,20 @@ def test_infinities_stay_with_their_adapter(batch, n_q):
     assert np.array_equal(bad[..., fine], np.broadcast_to(want[fine], bad[..., fine].shape))
 
 
+@pytest.mark.parametrize("batch,n_q,rank", [(6, 1, 72), (128, 1, 64), (150, 1, 72), (150, 1, 128), (40, 7, 64)])
+def test_infinities_among_many_ranks(batch, n_q, rank):
+    """Ranks of a feature in lines of their own, and the last of them at an odd place."""
+    c = Case(batch, n_q, 512, rank, 3, np.arange(batch) % 3 - 1, max_len=96, seed=8)
+    c.b[0, 9, rank - 1] = 0x7F80      # an infinity against one feature
+    c.b[0, 14, rank - 8] = 0x7FC0     # a NaN
+    got = c.run()
+    others = c.ids != 0
+    c.check(got, others)
+    q = f64(got[0]).reshape(batch, n_q, 256)[~others]
+    assert not np.isfinite(q[..., [9, 14]]).any() and np.isnan(q[..., 14]).all()
+    assert np.isfinite(np.delete(q, [9, 14], -1)).all()
+
+
 @pytest.mark.parametrize("batch,n_q", [(6, 1), (150, 1), (5, 70)])
 def test_adapter_numbers_out_of_range(batch, n_q):
     from paper_2606_06467_amd import binding as B
