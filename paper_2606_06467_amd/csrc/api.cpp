@@ -267,9 +267,9 @@ clsa_status check_adapters(int32_t n, int32_t rank, const void *a, const void *b
 
 bool rank_supported(int32_t rank) { return rank >= 8 && rank <= clsa::kMaxRank && rank % 8 == 0; }
 
-// alpha A h of every row (its ranks filled up to a multiple of 16).
+// alpha A h of every row, in fp32 or in three bf16 (its ranks filled up to a multiple of 16).
 size_t adapted_bytes(const Geometry &g, int32_t rank) {
-    return align_up(sizeof(float) * (size_t)g.rows * ((rank + 15) / 16 * 16));
+    return align_up(3 * sizeof(uint16_t) * (size_t)g.rows * ((rank + 15) / 16 * 16));
 }
 
 // A shape whose rows alone matter, and the width of a row.

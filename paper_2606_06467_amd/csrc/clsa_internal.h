@@ -282,7 +282,7 @@ hipError_t launch_project_rows(const Geometry &g, int d_model, const void *h, co
 
 // Low-rank adapters beside the projections: sequence b adds alpha B (A h) of adapter
 // adapter[b] (-1: none) to its rows.  a: [n, rank, d_model], b: [n, features, rank];
-// u: [rows, rank] scratch for alpha A h.
+// u: scratch for alpha A h, 6 bytes for each row and rank, the ranks filled up to a multiple of 16.
 struct Adapters {
     const void *a, *b;
     const float *alpha;

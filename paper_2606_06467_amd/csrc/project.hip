@@ -57,12 +57,16 @@ struct ProjArgs {
     const uint16_t *up;        // [n_adapters, features, rank]
     const float *alpha;
     const int32_t *adapter;    // [batch]
-    // alpha A h of the rows that have an adapter: fp32 [rows, rank] for the few-rows kernel, two
-    // bf16 [rows, rank / 16, 2, 16] (adapter_halves) for the tiled one
+    // alpha A h of the rows that have an adapter: fp32 [rows, rank] for the few-rows kernel, three
+    // bf16 [rows, rank / 16, 3, 16] (adapter_parts) for the tiled one
     float *u;
     int n_adapters, rank, n_feat;
     int seq_tiles;             // kOwnTiles: 128-row tiles of a sequence
 };
+
+// bf16 parts of an inner sum (adapter_parts), and the elements of a row's.
+constexpr int kParts = 3;
+__host__ __device__ __forceinline__ constexpr int parts_pitch(int rank) { return (rank + 15) / 16 * 16 * kParts; }
 
 // Adapter of sequence b, -1 for none.
 __device__ __forceinline__ int adapter_of(const ProjArgs &a, int b) {
@@ -276,15 +280,16 @@ constexpr int kGemmOutPitch = kGemmN + 8;    // bf16 per staged output row
 constexpr size_t gemm_lds(int rows) { return sizeof(uint16_t) * 2 * (rows + kGemmN) * kGemmPitch; }
 
 // kMixed: adds the adapters' part to a wave's 16 MT x 16 NT tile of the tiled product (c[mt][nt]:
-// rows r0 + 16 mt, features f0 + 16 nt), 32 ranks a step, the high and then the low parts of
-// u against the same B.  Rows of different sequences can share a tile: its products are
+// rows r0 + 16 mt, features f0 + 16 nt), 32 ranks a step, the three parts of u (adapter_parts)
+// against the same B.  Rows of different sequences can share a tile: its products are
 // then made once for each adapter in it and added to that adapter's rows only (a factor of
 // zero would carry one adapter's infinities to another's rows).  Q adapters' loads, J steps
 // of each, are in flight together.  What bounds it is the number of those loads (16
 // ranks twice in a step, as in the tiles of one sequence, and so twice as many of B: 200 tokens
-// of rank 128 with 64 adapters 161 us against 115; 73 with tiles of 32 rows).  From 64 ranks on
-// neighbouring rows lie in different lines and the pieces are turned (1200 rows of 64 ranks, 64
-// adapters 71.5 / 58.5 us; of 48 ranks 54.0 / 57.1, of 16 45.4 / 49.1).
+// of rank 128 with 64 adapters 161 us against 115; 78 with tiles of 32 rows).  From 64 ranks on
+// neighbouring rows lie in different lines and the pieces are turned (1200 tokens x 2560 features,
+// 64 adapters, direct / turned: 64 ranks 220 / 147 us, 128 ranks 415 / 269; 48 ranks 133 / 136, 16
+// ranks 87 / 106).
 template <int MT, int NT, int Q, int J>
 __device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, f32x4 (&c)[MT][NT],
                                              u32x4 (&own)[OperandTurn::kTiles][64]) {
@@ -293,8 +298,8 @@ __device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, 
     const bool turned = a.rank >= 64;  // uniform
     const int row = turned ? turn.row(lane) : col, piece = turned ? turn.piece(lane) : grp;
     const u32x4 none{0u, 0u, 0u, 0u};
-    const uint16_t *halves = reinterpret_cast<const uint16_t *>(a.u);
-    const int pitch = div_up(a.rank, 16) * 32;
+    const uint16_t *parts = reinterpret_cast<const uint16_t *>(a.u);
+    const int pitch = parts_pitch(a.rank);
     int mine[MT];
     uint32_t left[MT], any = 0;  // rows whose adapter is still to come
 #pragma unroll
@@ -324,7 +329,7 @@ __device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, 
         for (int mt = 0; mt < MT; ++mt) any |= left[mt];
 #pragma unroll 1
         for (int j0 = 0; j0 < a.rank; j0 += 32 * J) {
-            u32x4 av[MT][J][2], bv[Q][J][NT];
+            u32x4 av[MT][J][kParts], bv[Q][J][NT];
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
                 if (id[q] < 0) break;
@@ -345,11 +350,11 @@ __device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, 
                 for (int j = 0; j < J; ++j) {
                     const int ro = j0 + 32 * j + piece * 8;
                     const int r = r0 + 16 * mt + row;
-                    const uint16_t *p = halves + (size_t)r * pitch + 2 * (ro & ~15) + (ro & 8);
-                    av[mt][j][0] = av[mt][j][1] = none;
-                    if (r < a.rows && ro < a.rank) {  // (rows without an adapter: as the workspace was)
-                        av[mt][j][0] = ld_piece(p);
-                        av[mt][j][1] = ld_piece(p + 16);
+                    const uint16_t *p = parts + (size_t)r * pitch + kParts * (ro & ~15) + (ro & 8);
+#pragma unroll
+                    for (int k = 0; k < kParts; ++k) {
+                        av[mt][j][k] = none;  // (rows without an adapter: as the workspace was)
+                        if (r < a.rows && ro < a.rank) av[mt][j][k] = ld_piece(p + 16 * k);
                     }
                 }
             if (turned) {
@@ -374,10 +379,9 @@ __device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, 
                         f32x4 t = c[mt][nt];
 #pragma unroll
                         for (int j = 0; j < J; ++j)
-                            if (j0 + 32 * j < a.rank) {
-                                t = mfma(av[mt][j][0], bv[q][j][nt], t);
-                                t = mfma(av[mt][j][1], bv[q][j][nt], t);
-                            }
+                            if (j0 + 32 * j < a.rank)
+#pragma unroll
+                                for (int k = 0; k < kParts; ++k) t = mfma(av[mt][j][k], bv[q][j][nt], t);
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             c[mt][nt][e] = (same[q][mt] >> (4 * grp + e)) & 1 ? t[e] : c[mt][nt][e];
@@ -388,8 +392,8 @@ __device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, 
 }
 
 // The tiled product's adapters.  kOwnTiles: no row tile holds two sequences; the ranks of its
-// adapter are more of the sum's dimensions, a 64-wide step for every 32 (16 ranks twice,
-// the high and the low parts of u against the same B).  kMixed: adapter_tile above.
+// adapter are more of the sum's dimensions, 48 for every 16 (the three parts of u against the same
+// B).  kMixed: adapter_tile above.
 enum GemmMode { kPlain, kOwnTiles, kMixed };
 
 // BM rows x 128 features by W waves, two of them side by side in the rows.  Eight waves where
@@ -472,18 +476,19 @@ __global__ __launch_bounds__(64 * W, 2) void project_gemm_kernel(ProjArgs a) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) c[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int nk = a.d / kGemmK;  // even (d_model is a multiple of 512)
-    const int steps = nk + (MODE == kOwnTiles && id >= 0 ? div_up(a.rank, 32) : 0);
+    const int pitch = MODE == kOwnTiles ? parts_pitch(a.rank) : 0;
+    const int steps = nk + (MODE == kOwnTiles && id >= 0 ? div_up(pitch, kGemmK) : 0);
     // step e of the adapter's ranks: this thread's pieces of u and of B
     auto xload = [&](int set, int e) {
-        const int chunk = 2 * e + (lcol >> 5), ro = chunk * 16 + (lcol & 8), pitch = div_up(a.rank, 16) * 32;
-        const uint16_t *halves = reinterpret_cast<const uint16_t *>(a.u);
+        const int at = e * kGemmK + lcol, ro = at / (16 * kParts) * 16 + (at & 8);
+        const uint16_t *parts = reinterpret_cast<const uint16_t *>(a.u);
 #pragma unroll
         for (int i = 0; i < BP; ++i) {
             rb[set][i] = u32x4{0u, 0u, 0u, 0u};
             if (i < AP) ra[set][i] = u32x4{0u, 0u, 0u, 0u};
-            if (i < AP && chunk * 16 < a.rank)
+            if (i < AP && at < pitch)
                 ra[set][i] = *reinterpret_cast<const u32x4 *>(
-                    halves + (size_t)min(r0 + lrow + RS * i, row_end - 1) * pitch + e * 64 + lcol);
+                    parts + (size_t)min(r0 + lrow + RS * i, row_end - 1) * pitch + at);
             if (ro < a.rank)
                 rb[set][i] = *reinterpret_cast<const u32x4 *>(
                     a.up + ((size_t)id * a.n_feat + f0 + lrow + RS * i) * a.rank + ro);
@@ -612,14 +617,17 @@ bool project_supported(int d_model) {
     return d_model >= 512 && d_model <= 8192 && d_model % 512 == 0;
 }
 
-// alpha A h in two bf16: the high one cut off, the low one the rest rounded, together 16
-// bits (so that an infinity stays one; its rest is none).
-__device__ __forceinline__ void adapter_halves(float u, uint16_t *p) {
-    const uint32_t hi = __float_as_uint(u) & 0xffff0000u;
-    const float rest = u - __uint_as_float(hi);
-    const __bf16 lo = rest == rest ? (__bf16)rest : (__bf16)0.0f;
-    p[0] = (uint16_t)(hi >> 16);
-    p[16] = __builtin_bit_cast(uint16_t, lo);
+// alpha A h in three bf16, eight bits each, cut off one after the other: their sum is the fp32
+// value (above 2^-110; below, what a bf16 cannot hold is lost).  An infinity stays one; its
+// rests are none.
+__device__ __forceinline__ void adapter_parts(float u, uint16_t *p) {
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+        const uint32_t cut = __float_as_uint(u) & 0xffff0000u;
+        p[16 * k] = (uint16_t)(cut >> 16);
+        u -= __uint_as_float(cut);
+        u = u == u ? u : 0.0f;
+    }
 }
 
 // u = alpha A h of many rows: one workgroup = up to 16 RT rows of one sequence and 16 NT
@@ -672,7 +680,7 @@ __global__ __launch_bounds__(512) void adapter_down_tile_kernel(ProjArgs a) {
                 for (int n = 0; n < NT; ++n) c[m][n] = mfma(v[s - 1][m], v[s - 1][RT + n], c[m][n]);
         }
     }
-    uint16_t *halves = reinterpret_cast<uint16_t *>(a.u);
+    uint16_t *parts = reinterpret_cast<uint16_t *>(a.u);
     const float alpha = a.alpha[id];
 #pragma unroll
     for (int n0 = 0; n0 < NT; n0 += J) {
@@ -692,8 +700,8 @@ __global__ __launch_bounds__(512) void adapter_down_tile_kernel(ProjArgs a) {
 #pragma unroll
             for (int w = 0; w < kSplitWaves; ++w) sum += part[w][m][n];
             // ranks past the last fill up a step with zeros
-            adapter_halves(j < a.rank ? sum * alpha : 0.0f,
-                           halves + ((size_t)b * a.n_q + t0 + m) * (2 * ranks) + (j >> 4) * 32 + (j & 15));
+            adapter_parts(j < a.rank ? sum * alpha : 0.0f,
+                          parts + ((size_t)b * a.n_q + t0 + m) * (kParts * ranks) + (j >> 4) * (16 * kParts) + (j & 15));
         }
     }
 }

@@ -281,3 +281,36 @@ def test_adapted_replayed(batch, n_q):
         assert all(np.array_equal(B.bits_from_bf16(t), w) for t, w in zip(out, want))
         step()
         torch.cuda.synchronize()
+
+
+def _exact_case(batch, n_q, rank):
+    """h = 1, 1, 1, 0 ... and weights -1, -2^-8 in every feature's first two dimensions."""
+    c = Case(batch, n_q, 512, rank, 3, np.arange(batch) % 4 - 1, max_len=-(-max(n_q + 8, 48) // 16) * 16, seed=12)
+    c.h[:] = 0
+    c.h[:, :3] = 0x3F80
+    c.w[:] = 0
+    c.w[:, 0], c.w[:, 1] = 0xBF80, 0xBB80
+    c.a[:], c.b[:] = 0, 0
+    c.alpha[:] = 1
+    if batch == 1:
+        c.ids[:] = 2
+    return c
+
+
+@pytest.mark.parametrize("batch,n_q", [(6, 1), (128, 1), (150, 1), (1500, 1), (2100, 1), (700, 6), (1, 200), (3, 90), (1, 1500), (1, 4200)])
+@pytest.mark.parametrize("rank", [8, 24, 64, 72, 128])
+def test_inner_sums_keep_24_bits(batch, n_q, rank):
+    """u_j = 1 + 2^-8 + 2^-(17 + j mod 7), every product and sum a multiple of 2^-23 below 2: exact in
+    fp32 in any order.  Feature f takes rank f mod rank alone, and the weights take 1 + 2^-8 away."""
+    c = _exact_case(batch, n_q, rank)
+    j = np.arange(rank)
+    c.a[:, :, 0], c.a[:, :, 1] = 0x3F80, 0x3B80
+    c.a[:, :, 2] = (127 - 17 - j % 7) << 7
+    f = np.arange(c.feats)
+    c.b[:, f, f % rank] = 0x3F80
+    got = c.run()
+    want = ((127 - 17 - f % rank % 7) << 7).astype(np.uint16)
+    rows, has = c.rows(), np.repeat(c.ids >= 0, n_q)
+    for x, c0, at in ((got[0], 0, np.arange(len(rows))), (got[1], 256, rows), (got[2], 512, rows), (got[3], 512 + c.kvw, rows)):
+        assert np.array_equal(x[at[(at >= 0) & has]], np.broadcast_to(want[c0:c0 + x.shape[1]], (((at >= 0) & has).sum(), x.shape[1])))
+        assert np.all(x[at[(at >= 0) & ~has]] == 0xBF80)   # -(1 + 2^-8): a tie, to the even -1
