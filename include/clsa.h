@@ -405,7 +405,8 @@ clsa_status clsa_block_topk(const clsa_shape *shape, int32_t block, const void *
  *            [-1, n_adapters) counts as -1 and raises CLSA_DEVERR_ADAPTER.
  * rank: a multiple of 8 up to 128, the same for all adapters (fill up smaller ones with
  * zeros).  bf16 inputs; fp32 products and sums, one rounding at the end; with many rows
- * the inner sum enters its product with B as three bf16, with all of its 24 bits.  One adapter's
+ * the inner sum enters its product with B as three bf16, with all of its 24 bits (fewer, and NaN
+ * for an infinite B, below 2^-109).  One adapter's
  * infinities and NaN stay with the sequences that use it.  Everything else as in
  * clsa_project_append.  Workspace: CLSA_OP_ADAPTED, whose size asks for the rank in
  * n_layers. */

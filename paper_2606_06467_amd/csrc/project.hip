@@ -618,15 +618,19 @@ bool project_supported(int d_model) {
 }
 
 // alpha A h in three bf16, eight bits each, cut off one after the other: their sum is the fp32
-// value (above 2^-110; below, what a bf16 cannot hold is lost).  An infinity stays one; its
-// rests are none.
+// value.  An infinite B meets all three, so that none may be zero unless u is: a cut that leaves
+// nothing takes the next smaller bf16 and leaves the difference.  (Below 2^-109, where the parts
+// reach the least bf16, their last bits are lost and some are zero.)  Infinities and NaN are all
+// three parts.
 __device__ __forceinline__ void adapter_parts(float u, uint16_t *p) {
+    const bool finite = u - u == 0.0f;
 #pragma unroll
     for (int k = 0; k < kParts; ++k) {
-        const uint32_t cut = __float_as_uint(u) & 0xffff0000u;
+        const uint32_t v = __float_as_uint(u);
+        uint32_t cut = v & 0xffff0000u;
+        if (k < kParts - 1 && finite && cut == v && u != 0.0f) cut -= 0x10000u;
         p[16 * k] = (uint16_t)(cut >> 16);
-        u -= __uint_as_float(cut);
-        u = u == u ? u : 0.0f;
+        if (finite) u -= __uint_as_float(cut);
     }
 }
 

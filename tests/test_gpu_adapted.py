@@ -314,3 +314,35 @@ def test_inner_sums_keep_24_bits(batch, n_q, rank):
     for x, c0, at in ((got[0], 0, np.arange(len(rows))), (got[1], 256, rows), (got[2], 512, rows), (got[3], 512 + c.kvw, rows)):
         assert np.array_equal(x[at[(at >= 0) & has]], np.broadcast_to(want[c0:c0 + x.shape[1]], (((at >= 0) & has).sum(), x.shape[1])))
         assert np.all(x[at[(at >= 0) & ~has]] == 0xBF80)   # -(1 + 2^-8): a tie, to the even -1
+
+
+@pytest.mark.parametrize("batch,n_q", [(6, 1), (150, 1), (1500, 1), (700, 6), (1, 200), (3, 90), (1, 4200)])
+@pytest.mark.parametrize("rank", [8, 40, 72, 128])
+def test_infinite_upper_factors_keep_their_sign(batch, n_q, rank):
+    """u B of a u that is a power of two, any other bf16, an infinity or zero, and an infinite B: the
+    product's sign, or NaN for zero."""
+    c = _exact_case(batch, n_q, rank)
+    c.a[:, :, 0] = np.resize(np.array([0x3F80, 0xBF80, 0x3FC1, 0x0D80, 0x7F7F, 0x7F80, 0xFF80, 0], np.uint16), rank)
+    f = np.arange(c.feats)
+    j = f % rank
+    c.b[:, f, j] = np.where(f // rank % 2, 0xFF80, 0x7F80)
+    # the other ranks of a feature are zeros: against an infinite u they would be NaN
+    wild = np.flatnonzero(~np.isfinite(f64(c.a[0, :, 0])))
+    c.a[:, wild, 0] = 0
+    q = f64(c.run()[0])
+    u = f64(c.a[0, :, 0])[j[:256]]
+    with np.errstate(invalid="ignore"):
+        want = u * f64(c.b[0, f, j])[:256]
+    has = np.repeat(c.ids >= 0, n_q)
+    assert np.array_equal(q[has], np.broadcast_to(want, (has.sum(), 256)), equal_nan=True)
+    assert np.all(q[~has] == -1)
+    # an infinite u in one rank alone: infinities of both signs of B, and NaN against zeros
+    for k in wild[:2]:
+        c.a[:, :, 0] = 0
+        c.a[:, k, 0] = 0x7F80 if k % 2 else 0xFF80
+        c.b[:] = 0
+        c.b[:, f, k] = np.resize(np.array([0x3F80, 0xC000, 0x7F80, 0xFF80, 0, 0x0080], np.uint16), c.feats)
+        q = f64(c.run()[0])
+        with np.errstate(invalid="ignore"):
+            want = f64(c.a[0, k:k + 1, 0]) * f64(c.b[0, :256, k])
+        assert np.array_equal(q[has], np.broadcast_to(want, (has.sum(), 256)), equal_nan=True)
