@@ -96,11 +96,13 @@ __device__ __forceinline__ int row_position(const ProjArgs &a, int b, int r) {
 }
 
 // Writes output feature f of row r (rows past the end are dropped; cache rows
-// only for positions inside [0, max_len)).
-template <bool PAGED>
+// only for positions inside [0, max_len)).  ADAPTED: alpha is fp32, and a NaN of it can carry low
+// bits that the rounding of finite values would take into the sign; the conversion keeps it NaN.
+// (Every other NaN here comes from a bf16, whose low half is zero.)
+template <bool PAGED, bool ADAPTED>
 __device__ __forceinline__ void store_feature(const ProjArgs &a, int r, int f, float v) {
     if (r >= a.rows) return;
-    const uint16_t bits = (uint16_t)f32_to_bf16_bits(v);
+    const uint16_t bits = ADAPTED ? __builtin_bit_cast(uint16_t, (__bf16)v) : (uint16_t)f32_to_bf16_bits(v);
     if (f < 256) {
         a.q_idx[(size_t)r * 256 + f] = bits;
         return;
@@ -265,7 +267,7 @@ __global__ __launch_bounds__(512) void project_splitk_kernel(ProjArgs a) {
         for (int w = 0; w < kSplitWaves; ++w) sum += part[w][rr][f];
         const int r = rt * 16 * RT + rr;
         if (ADAPTED && dot.n) sum += dot.finish();
-        store_feature<PAGED>(a, r, ft * 16 + f, sum);
+        store_feature<PAGED, ADAPTED>(a, r, ft * 16 + f, sum);
     }
 }
 

@@ -346,3 +346,20 @@ def test_infinite_upper_factors_keep_their_sign(batch, n_q, rank):
         with np.errstate(invalid="ignore"):
             want = f64(c.a[0, k:k + 1, 0]) * f64(c.b[0, :256, k])
         assert np.array_equal(q[has], np.broadcast_to(want, (has.sum(), 256)), equal_nan=True)
+
+
+@pytest.mark.parametrize("batch,n_q", [(6, 1), (128, 1), (150, 1), (1500, 1), (700, 6), (1, 200), (5, 70), (1, 4200)])
+@pytest.mark.parametrize("bits", [0x7FFFFFFF, 0xFFFFFFFF, 0x7FFF8000, 0x7F800001, 0x7FC00000])
+def test_a_factor_that_is_no_number(batch, n_q, bits):
+    """NaN of every payload in alpha: NaN in its sequences' features, and there alone."""
+    c = Case(batch, n_q, 512, 16, 3, np.arange(batch) % 4 - 1, max_len=-(-max(n_q + 8, 48) // 16) * 16, seed=13)
+    if batch == 1:
+        c.ids[:] = 1
+    c.alpha[1] = np.array([bits], np.uint32).view(np.float32)[0]
+    got = c.run()
+    others = c.ids != 1
+    c.check(got, others)
+    rows, bad = c.rows(), np.repeat(~others, n_q)
+    assert np.isnan(f64(got[0][bad])).all()
+    for x in got[1:]:
+        assert np.isnan(f64(x[rows[bad & (rows >= 0)]])).all()
