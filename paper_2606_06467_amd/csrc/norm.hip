@@ -212,6 +212,7 @@ struct NormGradArgs {
     uint16_t *dx;
     float *dweight, *part;  // part: [workgroups, d] sums of dy xhat
     int rows, d, pieces, parts;
+    int first;  // norm_grad_few_kernel: the launch's first workgroup
 };
 
 // dx of a thread's piece: s, dy, weight and dsum there, rstd, and c = mean(g xhat).
@@ -232,14 +233,17 @@ __device__ __forceinline__ uint4 grad_piece(uint4 v, uint4 y, uint4 w, uint4 u, 
 // Few rows in one launch: a workgroup for every 64 columns of dw, which reads its columns of dy
 // and s with four rows in flight, and behind those, as they are shorter, one for each row's dx.
 // The inputs are read twice, from the caches, so that no workgroup waits for another's sums.
+// Where dx takes the place of an input, the columns' workgroups are a launch before the rows'
+// (one launch / two: 77 rows of 2560 3.0 / 5.4 us, 768 rows 5.5 / 10.8): the same sums, so the same
+// bits.
 template <int P>
 __global__ __launch_bounds__(1024) void norm_grad_few_kernel(NormGradArgs a) {
     __shared__ float s_sum[16];
     __shared__ float s_col[128][64 + 1];
     const int t = threadIdx.x, width = blockDim.x;
-    const int row = (int)blockIdx.x - (a.d + 63) / 64;
+    const int block = a.first + (int)blockIdx.x, row = block - (a.d + 63) / 64;
     if (row < 0) {
-        const int col = (int)blockIdx.x * 64 + (t & 7) * 8, groups = width >> 3;
+        const int col = block * 64 + (t & 7) * 8, groups = width >> 3;
         float dw[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (col < a.d) {
             constexpr int N = 4;  // rows in flight
@@ -270,7 +274,7 @@ __global__ __launch_bounds__(1024) void norm_grad_few_kernel(NormGradArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) s_col[t >> 3][(t & 7) * 8 + e] = dw[e];
         __syncthreads();
-        const int c = (int)blockIdx.x * 64 + t;
+        const int c = block * 64 + t;
         if (t < 64 && c < a.d) {
             float sum = s_col[0][t];
             for (int k = 1; k < groups; ++k) sum += s_col[k][t];
@@ -455,9 +459,9 @@ bool norm_supported(int d) { return d >= 8 && d <= kNormMaxDim && d % 8 == 0; }
 
 static bool streamed(int rows, int d) { return (size_t)rows * d >= kNormStreamed; }
 
-// Below it (and with dx apart from dy and s) the backward pass is one launch; one / two launches:
-// 77 rows of 2560 2.7 / 6.3 us, 768 rows of 512 5.4 / 7.2, 2560 8.4 / 11.2, 8192 14.5 / 18.0;
-// 1024 rows of 512 7.5 / 5.8, 2560 12.6 / 11.9, 8192 18.5 / 24.6.
+// Up to it columns and rows are workgroups of one launch, beyond it rows are summed by workgroup
+// and joined; the one / the other: 77 rows of 2560 2.7 / 6.3 us, 768 rows of 512 5.4 / 7.2, 2560
+// 8.4 / 11.2, 8192 14.5 / 18.0; 1024 rows of 512 7.5 / 5.8, 2560 12.6 / 11.9, 8192 18.5 / 24.6.
 constexpr int kGradFewRows = 768;
 
 static int threads_of(int pieces, int per) { return div_up(pieces, 64 * per) * 64; }
@@ -545,15 +549,21 @@ hipError_t launch_norm_grad(int rows, int d, const void *s, const float *rstd, c
     a.d = d;
     a.pieces = d / 8;
     a.parts = norm_grad_parts(rows, d);
-    // One launch up to kGradFewRows; above 256 rows 512 threads at least, for the columns' sake
+    // Above 256 rows 512 threads at least, for the columns' sake
     // (64 rows of 2560: 2.7 us with 320 threads, 2.9 with 512; 512 rows 7.1 / 6.5)
     const int per = a.pieces <= 512 ? 1 : 2, row_threads = threads_of(a.pieces, per);
     const int least = rows <= 256 ? 256 : 512, threads = row_threads < least ? least : row_threads;
-    if (rows <= kGradFewRows && !overlaps(dx, dy, rows, d) && !overlaps(dx, s, rows, d)) {
-        const dim3 grid(div_up(d, 64) + rows), wg(threads);
-        if (per == 1) norm_grad_few_kernel<1><<<grid, wg, 0, stream>>>(a);
-        else norm_grad_few_kernel<2><<<grid, wg, 0, stream>>>(a);
-        return hipGetLastError();
+    if (rows <= kGradFewRows) {
+        const int columns = div_up(d, 64), all = columns + rows;
+        const bool apart = !overlaps(dx, dy, rows, d) && !overlaps(dx, s, rows, d);
+        for (int end = apart ? all : columns;; end = all) {
+            const dim3 grid(end - a.first), wg(threads);
+            if (per == 1) norm_grad_few_kernel<1><<<grid, wg, 0, stream>>>(a);
+            else norm_grad_few_kernel<2><<<grid, wg, 0, stream>>>(a);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess || end == all) return e;
+            a.first = end;
+        }
     }
     if (streamed(rows, d)) launch_grad_rows<true>(a, stream);
     else launch_grad_rows<false>(a, stream);

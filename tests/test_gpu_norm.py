@@ -289,3 +289,22 @@ def test_norm_on_a_stream_and_replayed():
         assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(outs, ref))
         step()
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("rows,d", [(1, 8), (3, 72), (77, 1000), (256, 2560), (300, 512), (768, 520), (2, 16384), (769, 520), (1500, 520), (1030, 4104)])
+@pytest.mark.parametrize("place", ["dy", "s"])
+def test_norm_grad_in_place_has_the_same_bits(rows, d, place):
+    """dx in the place of dy or of s: the bits of dx and dweight on their own, with and without dsum."""
+    import torch
+    from paper_2606_06467_amd import binding as B
+    s, rstd, w, dy, ds = _grad_inputs(rows, d, 40 + rows + d)
+    sh, R, W = B.make_shape(rows, 1, 1, 1), torch.from_numpy(rstd).cuda(), B.bf16_from_bits(w)
+    ws = B.workspace(sh, B.CLSA_OP_NORM_GRAD, d)
+    for more in (None, B.bf16_from_bits(ds)):
+        want = _grad(s, rstd, w, dy, None if more is None else ds, rows, d)
+        t = dict(s=B.bf16_from_bits(s), dy=B.bf16_from_bits(dy))
+        dw = torch.full((d,), 7.0, device="cuda")
+        B.clsa_residual_norm_grad(sh, d, t["s"], R, W, t["dy"], more, t[place], dw, ws)
+        torch.cuda.synchronize()
+        assert np.array_equal(B.bits_from_bf16(t[place]), want[0])
+        assert np.array_equal(dw.cpu().numpy().view(np.uint32), want[1].view(np.uint32))
