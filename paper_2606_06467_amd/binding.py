@@ -364,14 +364,24 @@ def clsa_block_topk(shape, block, q_idx, means, page_table, seq_lens, q_pos, idx
           (q_idx, means, page_table, seq_lens, q_pos, idx, n_sel), ws, stream)
 
 
-def _adapter_sizes(a, b):
-    """Number and rank of the adapters a [adapters, rank, d_model], b [adapters, features, rank]."""
+def _adapter_sizes(shape, d_model, a, b, alpha, adapter):
+    """Number and rank of the adapters a [adapters, rank, d_model], b [adapters, features, rank], whose
+    other sizes, and those of alpha and adapter, the library takes from the shape."""
     for name, t in (("a", a), ("b", b)):
         if not isinstance(t, _Tensor) or t.dim() != 3:
             raise ValueError(f"{name} must be a tensor of three dimensions")
-    n, rank, _ = a.shape
-    if b.shape[0] != n or b.shape[2] != rank:
+    n, rank, width = a.shape
+    held, features, held_rank = b.shape
+    if held != n or held_rank != rank:
         raise ValueError("a and b must hold the same adapters, of one rank")
+    if width != d_model:
+        raise ValueError(f"a must hold vectors of d_model {d_model} values, not {width}")
+    if features != 512 + 2 * shape.kv_heads * shape.head_dim:
+        raise ValueError(f"b must hold the shape's {512 + 2 * shape.kv_heads * shape.head_dim} features, not {features}")
+    if isinstance(alpha, _Tensor) and alpha.numel() < n:
+        raise ValueError(f"alpha must hold a factor for each of the {n} adapters")
+    if isinstance(adapter, _Tensor) and adapter.numel() < shape.batch:
+        raise ValueError(f"adapter must hold a number for each of the {shape.batch} sequences")
     return n, rank
 
 
@@ -381,7 +391,7 @@ def clsa_project_append_adapted(shape, d_model, h, w, a, b, alpha, adapter, pos,
     _call("clsa_project_append_adapted", shape, d_model,
           ("h", "w", "a", "b", "alpha", "adapter", "pos", "page_table", "q_idx", "k_idx", "k_cache", "v_cache"),
           (h, w, a, b, alpha, adapter, pos, page_table, q_idx, k_idx, k_cache, v_cache), ws, stream,
-          _adapter_sizes(a, b))
+          _adapter_sizes(shape, d_model, a, b, alpha, adapter))
 
 
 def clsa_project_append8_adapted(shape, block, d_model, h, w, a, b, alpha, adapter, start, count, page_table,
@@ -390,7 +400,7 @@ def clsa_project_append8_adapted(shape, block, d_model, h, w, a, b, alpha, adapt
           ("h", "w", "a", "b", "alpha", "adapter", "start", "count", "page_table", "q_idx", "k_idx", "k8", "v8",
            "k_scale", "v_scale"),
           (h, w, a, b, alpha, adapter, start, count, page_table, q_idx, k_idx, k8, v8, k_scale, v_scale), ws,
-          stream, (d_model, *_adapter_sizes(a, b)))
+          stream, (d_model, *_adapter_sizes(shape, d_model, a, b, alpha, adapter)))
 
 
 def clsa_residual_norm(shape, d_model, eps, x, residual, weight, sum=None, y=None, y8=None, y_scale=None,

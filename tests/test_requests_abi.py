@@ -188,3 +188,29 @@ def test_binding_takes_gpu_tensors_only():
             B.clsa_project_append8_adapted(_shape(), 64, 512, x, x, a, b, x, i, i, i, None, x, x, x, x, x, x)
     with pytest.raises(TypeError, match=r"tensors\[0\]"):
         B.clsa_pages_compact(_paged(), [None], i, i, i)
+
+
+def test_binding_compares_adapters_with_the_shape():
+    """Sizes that the library takes from the shape: refused before any device address is asked for."""
+    sh = _shape(kv_heads=2, q_heads=2)     # 1024 features, 2 sequences
+    x, i = torch.zeros((2, 512), dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
+    ok = dict(a=(3, 8, 512), b=(3, 1024, 8), alpha=(3,), adapter=(2,))
+
+    def call(which, **kw):
+        t = {k: torch.zeros(v, dtype=torch.int32 if k == "adapter" else torch.float32 if k == "alpha" else torch.bfloat16)
+             for k, v in {**ok, **kw}.items()}
+        if which == 8:
+            B.clsa_project_append8_adapted(sh, 64, 512, x, x, *t.values(), i, i, None, x, x, x, x, x, x)
+        else:
+            B.clsa_project_append_adapted(sh, 512, x, x, *t.values(), i, None, x, x, x, x)
+
+    for which in (16, 8):
+        for bad, what in ((dict(a=(3, 8, 1024)), "a must hold vectors of d_model 512"),
+                          (dict(a=(3, 8, 256)), "a must hold vectors of d_model 512"),
+                          (dict(b=(3, 768, 8)), "b must hold the shape's 1024 features"),
+                          (dict(b=(3, 2560, 8)), "b must hold the shape's 1024 features"),
+                          (dict(alpha=(2,)), "alpha must hold a factor for each of the 3"),
+                          (dict(adapter=(1,)), "adapter must hold a number for each of the 2"),
+                          ({}, "h must be a GPU tensor"), (dict(adapter=(9,)), "h must be a GPU tensor")):
+            with pytest.raises(ValueError, match=what):
+                call(which, **bad)
