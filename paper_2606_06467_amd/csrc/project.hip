@@ -861,11 +861,11 @@ static hipError_t launch_project_args(const Geometry &g, int d_model, ProjArgs a
     const long bands = div_up(a.rtiles, a.band ? a.band : 1);
     const long blocks = a.band ? div_up((int)bands, 8) * 8 * (long)a.band * a.ftiles
                                : div_up(a.rtiles * a.ftiles, 8) * 8L;
-    if (blocks > 0x7fffffL) return hipErrorInvalidConfiguration;  // 2^32 threads a launch
     const dim3 grid((unsigned)blocks);
     // (tiles of 64 rows are no more than the CUs, so that their workgroups are not either; 32 rows
     // have too little work for eight waves)
     const int waves = ADAPTED && bm > 32 && (bm == 64 || blocks <= kWideGemmBlocks) ? 8 : 4;
+    if (blocks * 64 * waves >= 1L << 32) return hipErrorInvalidConfiguration;  // threads a launch
     using Kernel = void (*)(ProjArgs);
     Kernel fn;
 #define CLSA_GEMM(MODE, BM, W) fn = paged ? project_gemm_kernel<true, MODE, BM, W> : project_gemm_kernel<false, MODE, BM, W>

@@ -118,3 +118,29 @@ def test_few_rows_split_depth(rows, d_model, kvh, page):
     pos = [[(7 * r) % 400 for r in range(rows)]]
     pos[0][rows // 2] = -1
     _case(w, d_model, pos, 16, f"{rows} rows d={d_model} Hkv={kvh} page={page}")
+
+
+def test_more_tiles_than_2_to_the_23():
+    """8.2 million rows of 16896 features are 8456448 workgroups of 256 threads: inside the 2^32
+    threads of a launch.  The last rows like the same rows of a call of their own."""
+    import torch
+    from paper_2606_06467_amd import binding as B
+    rows, d, heads, n = 8_200_000, 512, 64, 300
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    h = torch.full((rows, d), 0.25, dtype=torch.bfloat16, device="cuda")
+    h[-n:] = torch.randn((n, d), generator=gen, device="cuda").to(torch.bfloat16)
+    w = (torch.randn((512 + 2 * heads * 128, d), generator=gen, device="cuda") * 0.05).to(torch.bfloat16)
+    pos = torch.full((rows,), -1, dtype=torch.int32, device="cuda")
+    pos[-n:] = torch.arange(n, dtype=torch.int32, device="cuda")
+
+    def run(h, pos):
+        out = [torch.zeros((len(h) if k == 0 else n, 256 if k < 2 else heads * 128), dtype=torch.bfloat16, device="cuda")
+               for k in range(4)]
+        sh = B.make_shape(1, len(h), n, 1, q_heads=heads, kv_heads=heads)
+        B.clsa_project_append(sh, d, h, w, pos, None, *out)
+        torch.cuda.synchronize()
+        return out
+
+    got, want = run(h, pos), run(h[-n:].contiguous(), pos[-n:].contiguous())
+    assert torch.equal(got[0][-n:], want[0]) and all(torch.equal(a, b) for a, b in zip(got[1:], want[1:]))
+    assert torch.equal(got[0][:-n], got[0][:1].expand(rows - n, -1)) and got[0][0].any()
