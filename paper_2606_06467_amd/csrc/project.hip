@@ -809,12 +809,12 @@ static hipError_t launch_project_args(const Geometry &g, int d_model, ProjArgs a
     if (g.rows == 0) return hipSuccess;
     const int n_feat = 512 + 2 * a.kvw;  // a multiple of 256 (kv_heads * 128 per K and V)
     const bool paged = g.page_shift >= 0;
-    if (ADAPTED) {
-        a.n_feat = n_feat;
-        const hipError_t e = launch_adapter_down(a, g.batch, stream);
-        if (e != hipSuccess) return e;
-    }
+    a.n_feat = n_feat;
     if (g.rows <= kSplitMaxRows) {
+        if (ADAPTED) {
+            const hipError_t e = launch_adapter_down(a, g.batch, stream);
+            if (e != hipSuccess) return e;
+        }
         switch (d_model / 512) {
             case 1: launch_splitk<2, 1, ADAPTED>(a, paged, n_feat, stream); break;
             case 2: launch_splitk<4, 1, ADAPTED>(a, paged, n_feat, stream); break;
@@ -883,8 +883,9 @@ static hipError_t launch_project_args(const Geometry &g, int d_model, ProjArgs a
         else CLSA_GEMM(kMixed, 128, 4);
     }
 #undef CLSA_GEMM
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(fn),
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)gemm_lds(bm));
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(fn),
+                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)gemm_lds(bm));
+    if (e == hipSuccess && ADAPTED) e = launch_adapter_down(a, g.batch, stream);  // (nothing where the product is refused)
     if (e != hipSuccess) return e;
     fn<<<grid, dim3(64 * waves), gemm_lds(bm), stream>>>(a);
     return hipGetLastError();

@@ -363,3 +363,22 @@ def test_a_factor_that_is_no_number(batch, n_q, bits):
     assert np.isnan(f64(got[0][bad])).all()
     for x in got[1:]:
         assert np.isnan(f64(x[rows[bad & (rows >= 0)]])).all()
+
+
+def test_too_many_tiles_enqueue_nothing():
+    """17 million rows of 16896 features are more workgroups than a launch has: refused, and the
+    inner sums' place in the workspace is as it was."""
+    import torch
+    from paper_2606_06467_amd import binding as B
+    rows, d, heads = 17_000_000, 512, 64
+    sh = B.make_shape(1, rows, 16, 1, q_heads=heads, kv_heads=heads)
+    h = torch.ones((rows, d), dtype=torch.bfloat16, device="cuda")
+    w, a, b = (torch.ones(s, dtype=torch.bfloat16, device="cuda") for s in ((16896, d), (1, 8, d), (1, 16896, 8)))
+    pos, out = torch.full((rows,), -1, dtype=torch.int32, device="cuda"), torch.zeros((rows, 256), dtype=torch.bfloat16, device="cuda")
+    ws = B.workspace(sh, B.CLSA_OP_ADAPTED, 8).fill_(0xFF)
+    with pytest.raises(B.ClsaError):
+        B.clsa_project_append_adapted(sh, d, h, w, a, b, torch.ones(1, device="cuda"),
+                                      torch.zeros(1, dtype=torch.int32, device="cuda"), pos, None, out, out, out, out, ws)
+    torch.cuda.synchronize()
+    kept = bool((ws == 0xFF).all())   # (not in the assertion, which would take the tensor apart)
+    assert kept
