@@ -881,7 +881,7 @@ clsa_status clsa_residual_norm(const clsa_shape *shape, int32_t d_model, double 
                                const void *x, const void *residual, const void *weight, void *sum,
                                void *y, void *y8, float *y_scale, float *rstd, void *stream) {
     CLSA_TRY(check_norm(shape, d_model));
-    if (!(eps >= FLT_MIN) || !isfinite(eps)) return CLSA_ERR_INVALID_ARG;
+    if (!(eps >= FLT_MIN && eps <= FLT_MAX)) return CLSA_ERR_INVALID_ARG;
     CLSA_TRY(check_ptr(x, 16));
     CLSA_TRY(check_ptr(weight, 16));
     if (residual) CLSA_TRY(check_ptr(residual, 16));

@@ -214,3 +214,10 @@ def test_binding_compares_adapters_with_the_shape():
                           ({}, "h must be a GPU tensor"), (dict(adapter=(9,)), "h must be a GPU tensor")):
             with pytest.raises(ValueError, match=what):
                 call(which, **bad)
+
+
+@pytest.mark.parametrize("eps", [3.5e38, 1e60, 1e300])
+def test_norm_refuses_an_eps_past_fp32(eps):
+    """As an invalid argument, before it looks at a group that it does not have."""
+    assert _norm(_shape(), group=16) == -2
+    assert _norm(_shape(), eps=eps, group=16) == -1
