@@ -405,11 +405,10 @@ clsa_status clsa_block_topk(const clsa_shape *shape, int32_t block, const void *
  *            [-1, n_adapters) counts as -1 and raises CLSA_DEVERR_ADAPTER.
  * rank: a multiple of 8 up to 128, the same for all adapters (fill up smaller ones with
  * zeros).  bf16 inputs; fp32 products and sums, one rounding at the end; with many rows
- * the inner sum enters its product with B as three bf16, with all of its 24 bits (fewer, and NaN
- * for an infinite B, below 2^-109).  One adapter's
- * infinities and NaN stay with the sequences that use it.  Everything else as in
- * clsa_project_append.  Workspace: CLSA_OP_ADAPTED, whose size asks for the rank in
- * n_layers. */
+ * the inner sum enters its product with B as three bf16, with all of its 24 bits (below 2^-109
+ * with fewer, and against an infinite B as NaN).  One adapter's infinities and NaN stay with
+ * the sequences that use it.  Everything else as in clsa_project_append.  Workspace:
+ * CLSA_OP_ADAPTED, whose size asks for the rank in n_layers. */
 clsa_status clsa_project_append_adapted(const clsa_shape *shape, int32_t d_model,
                                         int32_t n_adapters, int32_t rank, const void *h,
                                         const void *w, const void *a, const void *b,
@@ -451,7 +450,7 @@ clsa_status clsa_residual_norm(const clsa_shape *shape, int32_t d_model, double 
 /* Its backward pass, from s and rstd as above: with g = dy * weight and xhat = s * rstd,
  *   dx = dsum + rstd * (g - xhat * mean(g * xhat)),   dweight = sum over rows of dy * xhat.
  * dy: bf16, the gradient of y; dsum: bf16, that of s from what follows it, or NULL; dx: bf16,
- * the gradient of s, i.e. of x and of residual alike (may be dy or dsum).  dweight: fp32
+ * the gradient of s, i.e. of x and of residual alike (may be s, dy or dsum).  dweight: fp32
  * [d_model], added up in an order that the sizes alone decide.  fp32 products and sums.
  * Workspace: CLSA_OP_NORM_GRAD, whose size asks for d_model in n_layers. */
 clsa_status clsa_residual_norm_grad(const clsa_shape *shape, int32_t d_model, const void *s,

@@ -51,7 +51,7 @@ struct ProjArgs {
     uint16_t *k_cache, *v_cache;
     bool kv_rows;              // K and V stay in the rows' own order: [rows, kvw]
     int rows, d, n_q, max_len, page_shift, max_pages, kvw;  // kvw = kv_heads * 128
-    int rtiles, ftiles, band;  // tiled kernel: 128-row and 128-feature tiles, row tiles per band
+    int rtiles, ftiles, band;  // tiled kernel: row tiles and 128-feature tiles, row tiles per band
     // adapters (adapted kernels only)
     const uint16_t *down;      // [n_adapters, rank, d]
     const uint16_t *up;        // [n_adapters, features, rank]
@@ -61,7 +61,7 @@ struct ProjArgs {
     // bf16 [rows, rank / 16, 3, 16] (adapter_parts) for the tiled one
     float *u;
     int n_adapters, rank, n_feat;
-    int seq_tiles;             // kOwnTiles: 128-row tiles of a sequence
+    int seq_tiles;             // kOwnTiles: row tiles of a sequence
 };
 
 // bf16 parts of an inner sum (adapter_parts), and the elements of a row's.
@@ -286,9 +286,9 @@ constexpr size_t gemm_lds(int rows) { return sizeof(uint16_t) * 2 * (rows + kGem
 // against the same B.  Rows of different sequences can share a tile: its products are
 // then made once for each adapter in it and added to that adapter's rows only (a factor of
 // zero would carry one adapter's infinities to another's rows).  Q adapters' loads, J steps
-// of each, are in flight together.  What bounds it is the number of those loads (16
-// ranks twice in a step, as in the tiles of one sequence, and so twice as many of B: 200 tokens
-// of rank 128 with 64 adapters 161 us against 115; 78 with tiles of 32 rows).  From 64 ranks on
+// of each, are in flight together.  What bounds it is the number of those loads (with
+// fewer ranks a step, as in the tiles of one sequence, and so twice as many of B, 200 tokens of
+// rank 128 with 64 adapters took 161 us against 115; with tiles of 32 rows they take 78).  From 64 ranks on
 // neighbouring rows lie in different lines and the pieces are turned (1200 tokens x 2560 features,
 // 64 adapters, direct / turned: 64 ranks 220 / 147 us, 128 ranks 415 / 269; 48 ranks 133 / 136, 16
 // ranks 87 / 106).
@@ -404,8 +404,8 @@ template <bool PAGED, GemmMode MODE, int BM, int W>
 __global__ __launch_bounds__(64 * W, 2) void project_gemm_kernel(ProjArgs a) {
     constexpr int MT = BM / 32, NT = 16 / W, OPS = MT + NT;  // 16-wide tiles of a wave; its operands of a half step
     constexpr int RS = 8 * W, AP = BM / RS, BP = kGemmN / RS;  // staging: rows a pass, pieces a thread
-    // two stages of A (rows of h) and B (features of w), 128 x 64 bf16 each
-    // (dynamic LDS, kGemmLds bytes); the output tile (128 x 128 bf16) reuses it
+    // two stages of A (BM rows of h) and B (128 features of w), 64 bf16 a row (dynamic LDS,
+    // gemm_lds(BM) bytes); the output tile (BM x 128 bf16) reuses it
     extern __shared__ __align__(16) uint16_t s_lds[];
     // (BM rows of A, then the features, in each stage)
     auto s_row = [&](int st, int r) { return s_lds + (size_t)(st * (BM + kGemmN) + r) * kGemmPitch; };
@@ -639,7 +639,7 @@ __device__ __forceinline__ void adapter_parts(float u, uint16_t *p) {
 // u = alpha A h of many rows: one workgroup = up to 16 RT rows of one sequence and 16 NT
 // ranks, d_model split over 8 waves whose parts meet in LDS, 32 ranks at a time.  Where there
 // are rows enough, all ranks: h is then read once, which bounds it, and A comes from the
-// caches (8192 rows, d_model 2560, rank 128: 30 us; 41 with a workgroup for each 32 ranks).
+// caches (8192 rows, d_model 2560, rank 128: 27 us; 41 with a workgroup for each 32 ranks).
 // Few rows take 32 ranks a workgroup (1505 rows, d_model 4096, rank 64: 10.6 us).
 template <int RT, int NT>
 __global__ __launch_bounds__(512) void adapter_down_tile_kernel(ProjArgs a) {
