@@ -286,12 +286,12 @@ constexpr size_t gemm_lds(int rows) { return sizeof(uint16_t) * 2 * (rows + kGem
 // against the same B.  Rows of different sequences can share a tile: its products are
 // then made once for each adapter in it and added to that adapter's rows only (a factor of
 // zero would carry one adapter's infinities to another's rows).  Q adapters' loads, J steps
-// of each, are in flight together.  What bounds it is the number of those loads (with
-// fewer ranks a step, as in the tiles of one sequence, and so twice as many of B, 200 tokens of
-// rank 128 with 64 adapters took 161 us against 115; with tiles of 32 rows they take 78).  From 64 ranks on
-// neighbouring rows lie in different lines and the pieces are turned (1200 tokens x 2560 features,
-// 64 adapters, direct / turned: 64 ranks 220 / 147 us, 128 ranks 415 / 269; 48 ranks 133 / 136, 16
-// ranks 87 / 106).
+// of each, are in flight together.  What bounds it is the number of those loads (with fewer ranks
+// a step, as in the tiles of one sequence, and so twice as many of B, 200 tokens of rank 128 with
+// 64 adapters took 161 us against 115; with tiles of 32 rows they take 78).  From 64 ranks on
+// neighbouring rows lie in different lines and the pieces are turned (1200 tokens x 2560
+// features, 64 adapters, direct / turned: 64 ranks 220 / 147 us, 128 ranks 415 / 269; 48 ranks
+// 133 / 136, 16 ranks 87 / 106).
 template <int MT, int NT, int Q, int J>
 __device__ __forceinline__ void adapter_tile(const ProjArgs &a, int r0, int f0, f32x4 (&c)[MT][NT],
                                              u32x4 (&own)[OperandTurn::kTiles][64]) {
